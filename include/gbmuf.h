@@ -350,6 +350,174 @@ int gbmuf_state_copy(const gbmuf_plan_t *plan, const gbmuf_state_t *dst, const g
 int gbmuf_probe_copy(float *dst_dev, const float *src_dev, int64_t n_floats, int32_t flags,
                      void *stream);
 
+/* =====================================================================================
+ * The local half of Algorithm 1: what every worker does between two syncs, on replicas that are
+ * resident.  Products with a model's matrices and their gradients, for all workers in one call,
+ * straight from their rows; the norm of each worker's gradients, and clipping; the local update.
+ * Conventions as above; the arithmetic is floating point with 32-bit sums (64-bit for norms) in a fixed
+ * order: equal calls give equal bits.
+ * ===================================================================================== */
+
+/* Number formats of matrices and gradients. */
+enum { GBMUF_F32 = 0, GBMUF_BF16 = 1, GBMUF_F16 = 2 };
+
+/* act(z).  GELU is z/2 (1 + erf(z / sqrt 2)), SILU z / (1 + exp(-z)). */
+enum {
+    GBMUF_ACT_NONE = 0, GBMUF_ACT_RELU = 1, GBMUF_ACT_GELU = 2, GBMUF_ACT_SILU = 3, GBMUF_ACT_SIGMOID = 4,
+    GBMUF_ACT_TANH = 5
+};
+
+/* Where the residual r is added: z = x w' + b + r (a recurrent layer's gates: r is the input's share), or
+   y = act(z) + r. */
+enum { GBMUF_RESIDUAL_NONE = 0, GBMUF_RESIDUAL_BEFORE = 1, GBMUF_RESIDUAL_AFTER = 2 };
+
+/*
+ * One product for each of `batch` workers g:
+ *     z[g,i,n] = sum_k x[g,i,k] w[g,n,k] + bias[g,n]  (+ r[g,i,n])
+ *     y[g,i,n] = act(z[g,i,n])                        (+ r[g,i,n])
+ * with i < rows, n < out_features, k < in_features; any of the sizes may be 0.  Zero the struct, set struct_size, fill in
+ * what is needed.
+ */
+typedef struct gbmuf_linear_desc {
+    uint32_t struct_size;    /* sizeof(gbmuf_linear_desc_t) of the caller's header                */
+    int32_t dtype;           /* GBMUF_F32, _BF16, _F16: x, w, bias, r, y, pre, dy, dx, dresidual   */
+    int32_t batch;           /* workers, 0 .. 65535                                               */
+    int32_t activation;      /* GBMUF_ACT_*                                                       */
+    int32_t residual;        /* GBMUF_RESIDUAL_*                                                  */
+    int32_t weight_grad_f32; /* backward: 1 = dw and dbias are f32 whatever dtype is              */
+    int32_t accumulate;      /* backward: 1 = dw and dbias are added to what is there             */
+    int32_t reserved0;
+    int64_t rows;            /* tokens per worker                                                 */
+    int64_t out_features;
+    int64_t in_features;
+} gbmuf_linear_desc_t;
+
+/* Element (g, i, j) of a matrix is data[g * batch_stride + i * ld + j], strides in elements, not negative.  An input may
+   have strides of 0 (one matrix for all workers); the elements of an output must all be apart.  data: device
+   memory, aligned to its elements; NULL: absent. */
+typedef struct gbmuf_matrix {
+    void *data;
+    int64_t ld;
+    int64_t batch_stride;
+} gbmuf_matrix_t;
+
+typedef struct gbmuf_linear_io {
+    gbmuf_matrix_t x;        /* in,  rows x in_features                                              */
+    gbmuf_matrix_t w;        /* in,  out_features x in_features, as the models' tensors lie in theta */
+    gbmuf_matrix_t bias;     /* in,  out_features (ld unused), or NULL                               */
+    gbmuf_matrix_t residual; /* in,  rows x out_features, if desc.residual asks for one              */
+    gbmuf_matrix_t y;        /* out, rows x out_features; may be the residual itself                 */
+    gbmuf_matrix_t pre;      /* out, rows x out_features: z, which the backward takes; or NULL       */
+} gbmuf_linear_io_t;
+
+/*
+ * gbmuf_linear -- the product, its bias, activation and residual: y, and z where asked for.
+ *   Sums of products are held in f32, rounded once to dtype.  GBMUF_F32: each row of x and w is scaled by a power of
+ *   two and its values are taken apart into two f16 numbers, of whose four products the matrix cores form three: a value keeps 22 bits or
+ *   more, or 2^-40 of its row's largest where that is more, so results are as near as those of f32 products whose
+ *   values lie within 2^16 of their row's largest.  An infinity or NaN in x or w makes NaN of the results that it reaches
+ *   (in f32; in bf16 and f16 infinities stay what IEEE says).  Few rows: plain f32 products.
+ *   workspace  device memory of gbmuf_linear_workspace bytes, 256-byte aligned, that nothing else uses until the call's work
+ *              is done; NULL if that is 0.  Calls that share one must be in order.
+ * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,
+ * pointers that are not aligned to their type, outputs that overlap inputs or each other, a workspace that is too small),
+ * EUNSUPPORTED (a size above 2^31 - 1, batch above 65535), EDEVICE.
+ */
+int gbmuf_linear_workspace(const gbmuf_linear_desc_t *desc, int32_t backward, int64_t *bytes);
+int gbmuf_linear(const gbmuf_linear_desc_t *desc, const gbmuf_linear_io_t *io, void *workspace, int64_t workspace_bytes,
+                 void *stream);
+
+typedef struct gbmuf_linear_grad_io {
+    gbmuf_matrix_t x;         /* in,  as in the forward; needed for dw                                    */
+    gbmuf_matrix_t w;         /* in,  as in the forward; needed for dx                                    */
+    gbmuf_matrix_t pre;       /* in,  z as the forward wrote it; unused with GBMUF_ACT_NONE               */
+    gbmuf_matrix_t dy;        /* in,  rows x out_features                                                 */
+    gbmuf_matrix_t dx;        /* out, rows x in_features, or NULL                                         */
+    gbmuf_matrix_t dw;        /* out, out_features x in_features, or NULL                                 */
+    gbmuf_matrix_t dbias;     /* out, out_features (ld unused), or NULL                                   */
+    gbmuf_matrix_t dresidual; /* out, rows x out_features, or NULL; dz with GBMUF_RESIDUAL_BEFORE.  (For a residual
+                                 that is added after the activation the gradient is dy: no output is taken.) */
+} gbmuf_linear_grad_io_t;
+
+/*
+ * gbmuf_linear_backward -- with dz = dy * act'(z):
+ *     dx = dz w,   dw = dz' x,   dbias[n] = sum_i dz[i,n],   dresidual = dz
+ * for each worker by itself (the gradient of an input that workers share is the sum of theirs).  relu'(0) = 0.  With bf16
+ * and f16, dz is rounded to dtype before the products (the matrix cores take 16 bits, and dy has no more); dbias sums what
+ * was not rounded.  Workspace and errors as above.
+ */
+int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_grad_io_t *io, void *workspace,
+                          int64_t workspace_bytes, void *stream);
+
+/* One gradient tensor of one worker: rows x cols values, row r at data + r * row_stride (a vector: rows = 1). */
+typedef struct gbmuf_grad_tensor {
+    void *data;              /* device                                                                   */
+    int64_t rows, cols;
+    int64_t row_stride;      /* elements, >= cols (unused if rows <= 1)                                   */
+    int64_t offset;          /* its first value's place among the worker's P parameters; -1: right behind the
+                                tensor of this worker that comes before it in the list (0 for the first)  */
+    int32_t worker;          /* 0 .. workers - 1                                                         */
+    int32_t dtype;           /* GBMUF_F32, _BF16, _F16                                                    */
+} gbmuf_grad_tensor_t;
+
+typedef struct gbmuf_grads_desc {
+    uint32_t struct_size;    /* sizeof(gbmuf_grads_desc_t) */
+    int32_t workers;         /* 1 .. GBMUF_MAX_K           */
+    int64_t n_tensors;       /* >= 0                       */
+    const gbmuf_grad_tensor_t *tensors;   /* host; copied  */
+} gbmuf_grads_desc_t;
+
+typedef struct gbmuf_grads_s gbmuf_grads_t;   /* opaque */
+
+/*
+ * The gradients of K workers, tensor by tensor, where they lie.  Immutable once made, like a plan: made once for gradients
+ * that stay where they are.  It owns small device tables and the scratch of its sums: calls with one handle must
+ * not be in flight at the same time on different streams.
+ * gbmuf_grads_create  EINVAL (NULLs, struct_size, workers, an unknown dtype, a worker out of range, negative sizes, a row_stride
+ *                     below cols, data not aligned to its type or NULL for a tensor that holds values, tensors of one
+ *                     worker whose places overlap), EUNSUPPORTED (workers > GBMUF_MAX_K; above 2^31 work items), ENOMEM, EDEVICE.
+ * gbmuf_grads_destroy synchronises the device first; NULL is OK.
+ */
+int gbmuf_grads_create(gbmuf_grads_t **out, const gbmuf_grads_desc_t *desc);
+int gbmuf_grads_destroy(gbmuf_grads_t *grads);
+
+/* norms[w] = sqrt of the sum of squares over all tensors of worker w, summed in 64 bits.  norms: device, `workers` floats. */
+int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream);
+
+/*
+ * gbmuf_grad_clip -- the norms, and dst = c_w * src with c_w = 1 where norms[w] <= max_norm and max_norm / norms[w] elsewhere
+ * (a norm that is NaN makes NaN of the worker's gradients).  dst has the tensors of src, in the same order and with the same
+ * rows, cols and worker; it may be src, or lie elsewhere and have other dtypes.  Tensors of dst must not share values with each
+ * other or, unless dst is src, with src.
+ * EINVAL also for max_norm < 0 or NaN (INFINITY: copies) and for a dst whose tensors differ.
+ */
+int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream);
+
+typedef struct gbmuf_step_desc {
+    uint32_t struct_size;    /* sizeof(gbmuf_step_desc_t)                                                 */
+    int32_t skip_nonfinite;  /* 1: a worker whose norm is infinite or NaN is left as it is                 */
+    int64_t P;               /* parameters per worker                                                     */
+    float rate;              /* alpha_t                                                                   */
+    float eps;               /* Adagrad only                                                              */
+    float max_norm;          /* gradients are clipped at this norm; INFINITY: not                         */
+    float reserved0;
+} gbmuf_step_desc_t;
+
+/*
+ * gbmuf_local_step -- Algorithm 1's local update, with g = c_w * gradient as gbmuf_grad_clip forms it:
+ *     sums  = sums + g * g;   theta = theta - rate * g / (sqrt(sums) + eps)     (Adagrad; sums not NULL)
+ *     theta = theta - rate * g                                                   (SGD; sums NULL)
+ *   theta, sums   the theta of these states, in rows or blocked, each by its own strides (omega and delta are not used).
+ *                 A blocked state takes any power of two of at least 4 floats as its block.
+ *   norms         device, `workers` floats, out: the norms before clipping (infinite max_norm and no skip_nonfinite: may be NULL, no
+ *                 norm is formed then).
+ * Parameters that no tensor covers stay as they are.
+ * EINVAL (NULLs, struct_size, rate, eps or max_norm NaN, max_norm or eps < 0, a tensor that reaches beyond P, strides as in
+ * gbmuf_state_t, theta and sums overlapping), EDEVICE.
+ */
+int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, const gbmuf_state_t *theta,
+                     const gbmuf_state_t *sums, float *norms, void *stream);
+
 /* Static description of a status code. */
 const char *gbmuf_strerror(int code);
 

@@ -24,6 +24,10 @@ SWEEP_AUTO, SWEEP_FORWARD = 0, 1
 LAYOUT_ROWS, LAYOUT_BLOCKED = 0, 1
 MAX_K = 1024
 STATIC_TABLE_ENTRIES = 1 << 19
+F32, BF16, F16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, ACT_SIGMOID, ACT_TANH = range(6)
+RESIDUAL_NONE, RESIDUAL_BEFORE, RESIDUAL_AFTER = 0, 1, 2
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
 class GbmufError(RuntimeError):
@@ -60,6 +64,40 @@ class State(ctypes.Structure):
 class Layout(ctypes.Structure):
     _fields_ = [("worker_stride", ctypes.c_int64), ("block_floats", ctypes.c_int64), ("block_stride", ctypes.c_int64),
                 ("omega_offset", ctypes.c_int64), ("delta_offset", ctypes.c_int64), ("arena_floats", ctypes.c_int64)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("residual", ctypes.c_int32), ("weight_grad_f32", ctypes.c_int32),
+                ("accumulate", ctypes.c_int32), ("reserved0", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("out_features", ctypes.c_int64), ("in_features", ctypes.c_int64)]
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("batch_stride", ctypes.c_int64)]
+
+
+class LinearIo(ctypes.Structure):
+    _fields_ = [(n, Matrix) for n in ("x", "w", "bias", "residual", "y", "pre")]
+
+
+class LinearGradIo(ctypes.Structure):
+    _fields_ = [(n, Matrix) for n in ("x", "w", "pre", "dy", "dx", "dw", "dbias", "dresidual")]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("offset", ctypes.c_int64), ("worker", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class GradsDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("workers", ctypes.c_int32), ("n_tensors", ctypes.c_int64),
+                ("tensors", ctypes.c_void_p)]
+
+
+class StepDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("skip_nonfinite", ctypes.c_int32), ("P", ctypes.c_int64),
+                ("rate", ctypes.c_float), ("eps", ctypes.c_float), ("max_norm", ctypes.c_float), ("reserved0", ctypes.c_float)]
 
 
 def _load() -> ctypes.CDLL:
@@ -100,6 +138,15 @@ def _load() -> ctypes.CDLL:
         getattr(L, name).restype = ctypes.c_int
     L.gbmuf_probe_copy.argtypes = [vp, vp, i64, i32, vp]
     L.gbmuf_probe_copy.restype = ctypes.c_int
+    ld, gp = ctypes.POINTER(LinearDesc), ctypes.POINTER(vp)
+    for name, args in (("gbmuf_linear_workspace", [ld, i32, ctypes.POINTER(i64)]),
+                       ("gbmuf_linear", [ld, ctypes.POINTER(LinearIo), vp, i64, vp]),
+                       ("gbmuf_linear_backward", [ld, ctypes.POINTER(LinearGradIo), vp, i64, vp]),
+                       ("gbmuf_grads_create", [gp, ctypes.POINTER(GradsDesc)]), ("gbmuf_grads_destroy", [vp]),
+                       ("gbmuf_grad_norm", [vp, vp, vp]), ("gbmuf_grad_clip", [vp, vp, f32, vp, vp]),
+                       ("gbmuf_local_step", [vp, ctypes.POINTER(StepDesc), sp, sp, vp, vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_int
     L.gbmuf_strerror.argtypes = [ctypes.c_int]
     L.gbmuf_strerror.restype = ctypes.c_char_p
     L.gbmuf_last_error_detail.argtypes = []
@@ -294,3 +341,138 @@ class Plan:
         rc = _lib.gbmuf_state_copy(self._h, ctypes.byref(dst), ctypes.byref(src), which, _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_state_copy")
+
+
+def _matrix(t, batch: int, rows: int, cols: int, dtype, what: str) -> Matrix:
+    """A [batch, rows, cols] tensor (or [rows, cols] where batch is 1) whose last axis is contiguous, as gbmuf_matrix_t."""
+    if t is None:
+        return Matrix()
+    if t.dim() == 2 and batch == 1:
+        t = t.unsqueeze(0)
+    if tuple(t.shape) != (batch, rows, cols) or t.dtype != dtype or (cols > 1 and t.stride(2) != 1):
+        raise GbmufError(GBMUF_EINVAL, what)
+    return Matrix(t.data_ptr(), t.stride(1), t.stride(0))
+
+
+def _vector(t, batch: int, cols: int, dtype, what: str) -> Matrix:
+    if t is None:
+        return Matrix()
+    if t.dim() == 1 and batch == 1:
+        t = t.unsqueeze(0)
+    if tuple(t.shape) != (batch, cols) or t.dtype != dtype or (cols > 1 and t.stride(1) != 1):
+        raise GbmufError(GBMUF_EINVAL, what)
+    return Matrix(t.data_ptr(), 0, t.stride(0))
+
+
+class Linear:
+    """gbmuf_linear_desc_t: one product y = act(x w' + bias ...) for each of ``batch`` workers.  Tensors are [batch, rows, columns] (or
+    [rows, columns] where batch is 1), views with strides among them; ``forward_io`` / ``backward_io`` check them and
+    return what ``forward`` / ``backward`` take, as often as the tensors stay where they are."""
+
+    def __init__(self, rows: int, out_features: int, in_features: int, batch: int = 1, dtype=torch.float32,
+                 activation: int = ACT_NONE, residual: int = RESIDUAL_NONE, weight_grad_f32: bool = False, accumulate: bool = False):
+        if dtype not in _TYPES:
+            raise GbmufError(GBMUF_EINVAL, "gbmuf_linear_desc_t")
+        self.dtype, self.grad_dtype = dtype, torch.float32 if weight_grad_f32 else dtype
+        self.desc = LinearDesc(ctypes.sizeof(LinearDesc), _TYPES[dtype], batch, activation, residual, int(weight_grad_f32),
+                               int(accumulate), 0, rows, out_features, in_features)
+        self._at = ctypes.byref(self.desc)
+        self.workspace_bytes()                               # the description's own checks
+
+    def workspace_bytes(self, backward: bool = False) -> int:
+        n = ctypes.c_int64()
+        rc = _lib.gbmuf_linear_workspace(self._at, int(backward), ctypes.byref(n))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_linear_workspace")
+        return n.value
+
+    def forward_io(self, x, w, y, bias=None, residual=None, pre=None) -> LinearIo:
+        d, t = self.desc, self.dtype
+        G, M, N, K = d.batch, d.rows, d.out_features, d.in_features
+        return LinearIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _vector(bias, G, N, t, "bias"),
+                        _matrix(residual, G, M, N, t, "residual"), _matrix(y, G, M, N, t, "y"), _matrix(pre, G, M, N, t, "pre"))
+
+    def backward_io(self, dy, x=None, w=None, pre=None, dx=None, dw=None, dbias=None, dresidual=None) -> LinearGradIo:
+        d, t, gt = self.desc, self.dtype, self.grad_dtype
+        G, M, N, K = d.batch, d.rows, d.out_features, d.in_features
+        return LinearGradIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _matrix(pre, G, M, N, t, "pre"),
+                            _matrix(dy, G, M, N, t, "dy"), _matrix(dx, G, M, K, t, "dx"), _matrix(dw, G, N, K, gt, "dw"),
+                            _vector(dbias, G, N, gt, "dbias"), _matrix(dresidual, G, M, N, t, "dresidual"))
+
+    @staticmethod
+    def _space(workspace):
+        return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+    def forward(self, io: LinearIo, workspace=None, stream=None) -> None:
+        p, n = self._space(workspace)
+        rc = _lib.gbmuf_linear(self._at, ctypes.byref(io), p, n, _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_linear")
+
+    def backward(self, io: LinearGradIo, workspace=None, stream=None) -> None:
+        p, n = self._space(workspace)
+        rc = _lib.gbmuf_linear_backward(self._at, ctypes.byref(io), p, n, _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_linear_backward")
+
+
+class Grads:
+    """Owns one ``gbmuf_grads_t``: the gradients of K workers where they lie.  ``tensors[w]`` lists worker w's tensors in the order of its
+    flat parameter vector (vectors, matrices whose last axis is contiguous, or contiguous tensors of any shape); ``offsets[w]``,
+    if given, says where each begins among the worker's parameters.  Keeps the tensors alive."""
+
+    def __init__(self, tensors: Sequence[Sequence], offsets: Optional[Sequence[Sequence[int]]] = None):
+        rows = []
+        for w, ts in enumerate(tensors):
+            for i, t in enumerate(ts):
+                if t.dtype not in _TYPES:
+                    raise GbmufError(GBMUF_EINVAL, "gbmuf_grads_create")
+                if t.is_contiguous():
+                    shape = (1, t.numel(), t.numel())
+                elif t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1):
+                    shape = (t.shape[0], t.shape[1], t.stride(0))
+                elif t.dim() == 1:
+                    shape = (t.shape[0], 1, t.stride(0))
+                else:
+                    raise GbmufError(GBMUF_EINVAL, "gbmuf_grads_create")
+                rows.append(GradTensor(t.data_ptr(), *shape, -1 if offsets is None else int(offsets[w][i]), w, _TYPES[t.dtype]))
+        table = (GradTensor * max(len(rows), 1))(*rows)
+        d = GradsDesc(ctypes.sizeof(GradsDesc), len(tensors), len(rows), ctypes.addressof(table))
+        self._h = ctypes.c_void_p()
+        rc = _lib.gbmuf_grads_create(ctypes.byref(self._h), ctypes.byref(d))
+        if rc != GBMUF_OK:
+            self._h = ctypes.c_void_p()
+            raise GbmufError(rc, "gbmuf_grads_create")
+        self._keep = [list(ts) for ts in tensors]
+        self.workers = len(tensors)
+
+    def destroy(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h:
+            _lib.gbmuf_grads_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def norm(self, norms, stream=None) -> None:
+        rc = _lib.gbmuf_grad_norm(self._h, _dev(norms), _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_grad_norm")
+
+    def clip(self, max_norm: float, norms, out: "Optional[Grads]" = None, stream=None) -> None:
+        """In place, or into the tensors of ``out``."""
+        rc = _lib.gbmuf_grad_clip(self._h, (out or self)._h, max_norm, _dev(norms), _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_grad_clip")
+
+    def local_step(self, theta: State, sums: Optional[State], P: int, rate: float, eps: float = 0.0,
+                   max_norm: float = float("inf"), norms=None, skip_nonfinite: bool = False, stream=None) -> None:
+        """Adagrad with ``sums`` (a state whose theta holds them), SGD with None."""
+        d = StepDesc(ctypes.sizeof(StepDesc), int(skip_nonfinite), P, rate, eps, max_norm, 0.0)
+        rc = _lib.gbmuf_local_step(self._h, ctypes.byref(d), ctypes.byref(theta), ctypes.byref(sums) if sums is not None else None,
+                                   _dev(norms), _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_local_step")

@@ -1,0 +1,454 @@
+// gbmuf_grads.hip -- the gradients of K workers: norms, clipping, and the local update of Algorithm 1.
+#include "gbmuf_device.h"
+#include "gbmuf_values.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+namespace gbmuf {
+namespace {
+
+struct GradTensor {              // on the device
+    char *p;
+    int64_t cols, ld;            // ld == cols where rows follow each other
+    int64_t offset;              // of the first value among the worker's parameters
+    int32_t worker, type;
+    int64_t rows;
+};
+
+struct GradTile {                // one workgroup's share: values [start, start + n) of a tensor, counted row by row
+    int64_t start;
+    int32_t tensor, n;
+};
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
+{
+    if (t.ld == t.cols) return i;
+    const int64_t r = i / t.cols;
+    return i + r * (t.ld - t.cols);
+}
+
+// do4(i) for four values of the tile from value i on that lie side by side in the tensor, do1(i) for single ones.
+template <class Do4, class Do1>
+__device__ __forceinline__ void each(const GradTensor &t, const GradTile &tile, Do4 do4, Do1 do1)
+{
+    for (int32_t k = static_cast<int32_t>(threadIdx.x) * 4; k < tile.n; k += kThreads * 4) {
+        const int64_t i = tile.start + k;
+        const int left = min(4, tile.n - k);
+        if (left == 4 && (t.ld == t.cols || i % t.cols + 4 <= t.cols)) do4(i);
+        else
+            for (int c = 0; c < left; ++c) do1(i + c);
+    }
+}
+
+__device__ __forceinline__ double block_sum(double s, double *lds)
+{
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+template <int T>
+__device__ __forceinline__ double tile_squares(const GradTensor &t, const GradTile &tile)
+{
+    double s = 0.0;
+    each(t, tile,
+         [&](int64_t i) {
+             const v4f v = read4<T>(t.p, grad_at(t, i));
+             for (int c = 0; c < 4; ++c) s = fma(static_cast<double>(v[c]), static_cast<double>(v[c]), s);
+         },
+         [&](int64_t i) {
+             const double v = static_cast<double>(load_one(t.p, grad_at(t, i), T));
+             s = fma(v, v, s);
+         });
+    return s;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(const GradTensor *tensors, const GradTile *tiles, double *partial)
+{
+    __shared__ double lds[4];
+    const GradTile tile = tiles[blockIdx.x];
+    const GradTensor t = tensors[tile.tensor];
+    double s = t.type == kF32 ? tile_squares<kF32>(t, tile) : t.type == kBf16 ? tile_squares<kBf16>(t, tile) : tile_squares<kF16>(t, tile);
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(const double *partial, const int32_t *first, float *norms)
+{
+    __shared__ double lds[4];
+    double s = 0.0;
+    for (int32_t i = first[blockIdx.x] + static_cast<int32_t>(threadIdx.x); i < first[blockIdx.x + 1]; i += kThreads) s += partial[i];
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) norms[blockIdx.x] = static_cast<float>(sqrt(s));
+}
+
+__device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most ? 1.0f : most / norm; }
+
+template <int T, int D>
+__device__ __forceinline__ void clip_tile(const GradTensor &t, const GradTensor &d, const GradTile &tile, float f)
+{
+    each(t, tile,
+         [&](int64_t i) {
+             const v4f v = read4<T>(t.p, grad_at(t, i)) * f;
+             if (d.ld == d.cols || i % d.cols + 4 <= d.cols) write4<D>(d.p, grad_at(d, i), v);
+             else
+                 for (int c = 0; c < 4; ++c) store_one(d.p, grad_at(d, i + c), D, v[c]);
+         },
+         [&](int64_t i) { store_one(d.p, grad_at(d, i), D, load_one(t.p, grad_at(t, i), T) * f); });
+}
+
+template <int T>
+__device__ __forceinline__ void clip_to(const GradTensor &t, const GradTensor &d, const GradTile &tile, float f)
+{
+    if (d.type == kF32) clip_tile<T, kF32>(t, d, tile, f);
+    else if (d.type == kBf16) clip_tile<T, kBf16>(t, d, tile, f);
+    else clip_tile<T, kF16>(t, d, tile, f);
+}
+
+__global__ __launch_bounds__(kThreads) void clip_kernel(const GradTensor *tensors, const GradTensor *to, const GradTile *tiles, const float *norms,
+                                                        float most)
+{
+    const GradTile tile = tiles[blockIdx.x];
+    const GradTensor t = tensors[tile.tensor];
+    const float f = clip_factor(norms[t.worker], most);
+    if (tensors == to && f == 1.0f) return;                // in place: nothing changes
+    const GradTensor d = to[tile.tensor];
+    if (t.type == kF32) clip_to<kF32>(t, d, tile, f);
+    else if (t.type == kBf16) clip_to<kBf16>(t, d, tile, f);
+    else clip_to<kF16>(t, d, tile, f);
+}
+
+struct StepArgs {
+    const GradTensor *tensors;
+    const GradTile *tiles;
+    const float *norms;          // nullptr: no clipping
+    float *theta, *sums;         // sums nullptr: SGD
+    Placement at, sums_at;
+    float rate, eps, most;
+    int32_t skip_nonfinite;
+};
+
+// The update rounds every multiply and add by itself, like the rest of the method.
+__device__ __forceinline__ void update(float &theta, float &h, float g, const StepArgs &a)
+{
+    if (a.sums) {
+        h = h + g * g;
+        theta = theta - a.rate * g / (sqrtf(h) + a.eps);
+    } else {
+        theta = theta - a.rate * g;
+    }
+}
+
+template <int T>
+__device__ __forceinline__ void step_tile(const GradTensor &t, const GradTile &tile, float f, const StepArgs &a)
+{
+    float *theta = a.theta + t.worker * a.at.stride;
+    float *sums = a.sums ? a.sums + t.worker * a.sums_at.stride : nullptr;
+    const auto one = [&](int64_t i) {
+        const float g = load_one(t.p, grad_at(t, i), T) * f;
+        const int64_t e = t.offset + i;
+        float *p = theta + placed(a.at, e), *q = sums ? sums + placed(a.sums_at, e) : nullptr;
+        float h = q ? *q : 0.0f, v = *p;
+        update(v, h, g, a);
+        *p = v;
+        if (q) *q = h;
+    };
+    each(t, tile,
+         [&](int64_t i) {
+             const int64_t e = t.offset + i;
+             if (((e ^ (e + 3)) >> a.at.logB) != 0 || (sums && ((e ^ (e + 3)) >> a.sums_at.logB) != 0)) {
+                 for (int c = 0; c < 4; ++c) one(i + c);
+                 return;
+             }
+             const v4f g = read4<T>(t.p, grad_at(t, i)) * f;
+             float *p = theta + placed(a.at, e), *q = sums ? sums + placed(a.sums_at, e) : nullptr;
+             v4f v = load4<kPlain>(p), h = q ? load4<kPlain>(q) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+             for (int c = 0; c < 4; ++c) {
+                 float x = v[c], y = h[c];
+                 update(x, y, g[c], a);
+                 v[c] = x;
+                 h[c] = y;
+             }
+             store4<kPlain>(p, v);
+             if (q) store4<kPlain>(q, h);
+         },
+         one);
+}
+
+__global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a)
+{
+    const GradTile tile = a.tiles[blockIdx.x];
+    const GradTensor t = a.tensors[tile.tensor];
+    float f = 1.0f;
+    if (a.norms) {
+        const float norm = a.norms[t.worker];
+        if (a.skip_nonfinite && !(norm < INFINITY)) return;
+        f = clip_factor(norm, a.most);
+    }
+    if (t.type == kF32) step_tile<kF32>(t, tile, f, a);
+    else if (t.type == kBf16) step_tile<kBf16>(t, tile, f, a);
+    else step_tile<kF16>(t, tile, f, a);
+}
+
+}  // namespace
+}  // namespace gbmuf
+
+using namespace gbmuf;
+
+struct gbmuf_grads_s {
+    int32_t workers = 0;
+    int device = -1;
+    int64_t n_tiles = 0, reach = 0;              // reach: end of the last tensor among a worker's parameters
+    std::vector<GradTensor> tensors;             // by worker, in the order of the list
+    GradTensor *d_tensors = nullptr;
+    GradTile *d_tiles = nullptr;
+    int32_t *d_first = nullptr;                  // [workers + 1]: first tile of every worker
+    double *d_partial = nullptr;
+};
+
+namespace {
+
+void free_grads(gbmuf_grads_s &g)
+{
+    for (void *p : {static_cast<void *>(g.d_tensors), static_cast<void *>(g.d_tiles), static_cast<void *>(g.d_first), static_cast<void *>(g.d_partial)})
+        if (p) (void)hipFree(p);
+}
+
+template <class T>
+int to_device(T **dst, const T *src, size_t n)
+{
+    if (n == 0) return GBMUF_OK;
+    hipError_t err = hipMalloc(reinterpret_cast<void **>(dst), n * sizeof(T));
+    if (err != hipSuccess) return hip_failed("hipMalloc(gradient tables)", err, err == hipErrorOutOfMemory ? GBMUF_ENOMEM : GBMUF_EDEVICE);
+    if (!src) return GBMUF_OK;
+    err = hipMemcpy(*dst, src, n * sizeof(T), hipMemcpyHostToDevice);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipMemcpy(gradient tables)", err, GBMUF_EDEVICE);
+}
+
+int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
+{
+    const size_t n = static_cast<size_t>(d.n_tensors);
+    h.workers = d.workers;
+    std::vector<int64_t> next(static_cast<size_t>(d.workers), 0);
+    std::vector<GradTensor> list(n);
+    int64_t values = 0;
+    for (size_t i = 0; i < n; ++i) {
+        const gbmuf_grad_tensor_t &t = d.tensors[i];
+        if (t.worker < 0 || t.worker >= d.workers || t.dtype < GBMUF_F32 || t.dtype > GBMUF_F16 || t.rows < 0 || t.cols < 0 || t.offset < -1)
+            return GBMUF_EINVAL;
+        if (t.rows > 1 && t.row_stride < t.cols) return GBMUF_EINVAL;
+        if (t.rows > 0 && t.cols > (static_cast<int64_t>(1) << 48) / t.rows) return GBMUF_EUNSUPPORTED;
+        const int64_t count = t.rows * t.cols;
+        if (count > 0 && (!t.data || reinterpret_cast<uintptr_t>(t.data) % type_bytes(t.dtype) != 0)) return GBMUF_EINVAL;
+        int64_t &at = next[static_cast<size_t>(t.worker)];
+        const int64_t offset = t.offset < 0 ? at : t.offset;
+        if (offset > (static_cast<int64_t>(1) << 48)) return GBMUF_EUNSUPPORTED;
+        at = offset + count;
+        list[i] = GradTensor{static_cast<char *>(t.data), t.cols, t.rows > 1 ? t.row_stride : t.cols, offset, t.worker, t.dtype, t.rows};
+        if (count > 0) h.reach = std::max(h.reach, at);
+        values += count;
+    }
+    std::stable_sort(list.begin(), list.end(), [](const GradTensor &a, const GradTensor &b) { return a.worker < b.worker; });
+    h.tensors = list;
+    std::sort(list.begin(), list.end(), [](const GradTensor &a, const GradTensor &b) { return a.worker != b.worker ? a.worker < b.worker : a.offset < b.offset; });
+    const GradTensor *before = nullptr;                    // places of one worker's tensors are apart
+    for (const GradTensor &t : list) {
+        if (t.rows * t.cols == 0) continue;
+        if (before && before->worker == t.worker && before->offset + before->rows * before->cols > t.offset) return GBMUF_EINVAL;
+        before = &t;
+    }
+    // some 4096 tiles, of 2 K to 32 K values
+    int64_t size = 2048;
+    while (size < 32768 && values / size > 4096) size *= 2;
+    std::vector<GradTile> tiles;
+    std::vector<int32_t> first(static_cast<size_t>(d.workers) + 1, 0);
+    int64_t count = 0;
+    for (const GradTensor &t : h.tensors) count += (t.rows * t.cols + size - 1) / size;
+    if (count > 0x7fffffffLL / kThreads) return GBMUF_EUNSUPPORTED;
+    tiles.reserve(static_cast<size_t>(count));
+    for (size_t i = 0; i < h.tensors.size(); ++i) {
+        const int64_t all = h.tensors[i].rows * h.tensors[i].cols;
+        for (int64_t s = 0; s < all; s += size) tiles.push_back(GradTile{s, static_cast<int32_t>(i), static_cast<int32_t>(std::min(size, all - s))});
+        first[static_cast<size_t>(h.tensors[i].worker) + 1] = static_cast<int32_t>(tiles.size());
+    }
+    for (size_t w = 1; w < first.size(); ++w) first[w] = std::max(first[w], first[w - 1]);
+    h.n_tiles = count;
+    int devices = 0;
+    hipError_t err = hipGetDeviceCount(&devices);
+    if (err != hipSuccess || devices < 1) return GBMUF_OK;  // host-side checks work without a GPU; the calls say EDEVICE
+    if ((err = hipGetDevice(&h.device)) != hipSuccess) return hip_failed("hipGetDevice", err, GBMUF_EDEVICE);
+    int rc = to_device(&h.d_tensors, h.tensors.data(), h.tensors.size());
+    if (rc == GBMUF_OK) rc = to_device(&h.d_tiles, tiles.data(), tiles.size());
+    if (rc == GBMUF_OK) rc = to_device(&h.d_first, first.data(), first.size());
+    if (rc == GBMUF_OK) rc = to_device<double>(&h.d_partial, nullptr, tiles.size());
+    return rc;
+}
+
+int check_grads_device(const gbmuf_grads_s *g)
+{
+    if (g->device < 0) return hip_failed("no GPU when the handle was made", hipErrorNoDevice, GBMUF_EDEVICE);
+    int now = -1;
+    const hipError_t err = hipGetDevice(&now);
+    if (err != hipSuccess) return hip_failed("hipGetDevice", err, GBMUF_EDEVICE);
+    return now == g->device ? GBMUF_OK : hip_failed("another GPU than the handle's is current", hipErrorInvalidDevice, GBMUF_EDEVICE);
+}
+
+int launch(const void *fn, int64_t blocks, void **argv, const char *what, hipStream_t stream)
+{
+    if (blocks <= 0) return GBMUF_OK;
+    const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
+}
+
+int enqueue_norm(const gbmuf_grads_s *g, float *norms, hipStream_t stream)
+{
+    const GradTensor *tensors = g->d_tensors;
+    const GradTile *tiles = g->d_tiles;
+    double *partial = g->d_partial;
+    const int32_t *first = g->d_first;
+    void *a1[] = {&tensors, &tiles, &partial}, *a2[] = {&partial, &first, &norms};
+    const int rc = launch(reinterpret_cast<const void *>(norm_kernel), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
+    return rc != GBMUF_OK ? rc : launch(reinterpret_cast<const void *>(norm_join_kernel), g->workers, a2, "hipLaunchKernel(norm join)", stream);
+}
+
+// Where the arrays of a step lie.
+int place(const gbmuf_state_t &s, int64_t K, int64_t P, Placement *at, int64_t *extent)
+{
+    if (reinterpret_cast<uintptr_t>(s.theta) % 4 != 0) return GBMUF_EINVAL;
+    const int64_t B = s.block_floats;
+    if (B == 0) {
+        if (s.worker_stride < P) return GBMUF_EINVAL;
+        *at = Placement{s.worker_stride, 0, 62, 0};
+        *extent = (K - 1) * s.worker_stride + P;
+        return GBMUF_OK;
+    }
+    if (B < 4 || (B & (B - 1)) != 0 || B > (static_cast<int64_t>(1) << 30) || s.worker_stride < B) return GBMUF_EINVAL;
+    if (s.block_stride < (K - 1) * s.worker_stride + B) return GBMUF_EINVAL;
+    int32_t lg = 0;
+    while ((static_cast<int64_t>(1) << lg) < B) ++lg;
+    *at = Placement{s.worker_stride, s.block_stride - B, lg, 0};
+    const int64_t blocks = (P + B - 1) / B;
+    *extent = blocks > 0 ? (blocks - 1) * s.block_stride + (K - 1) * s.worker_stride + B : 0;
+    return GBMUF_OK;
+}
+
+// Whether rows (blocks) of two placements of the same kind lie side by side, or their ranges apart.
+bool apart(const gbmuf_state_t &a, int64_t extent_a, const gbmuf_state_t &b, int64_t extent_b, int64_t K, int64_t P)
+{
+    const float *x = a.theta, *y = b.theta;
+    if (x + extent_a <= y || y + extent_b <= x) return true;
+    if (a.block_floats != b.block_floats || a.worker_stride != b.worker_stride || a.block_stride != b.block_stride) return false;
+    const int64_t d = x < y ? y - x : x - y;               // equal strides: pieces repeat alike
+    const int64_t piece = a.block_floats ? a.block_floats : P;
+    const auto inside = [&](int64_t len, int64_t step) { return step > 0 && d % step >= len && d % step + len <= step; };
+    if (a.block_floats) return inside((K - 1) * a.worker_stride + piece, a.block_stride) ||
+                               (inside(piece, a.worker_stride) && a.block_stride % a.worker_stride == 0);
+    return inside(piece, a.worker_stride);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gbmuf_grads_create(gbmuf_grads_t **out, const gbmuf_grads_desc_t *desc)
+{
+    if (!out) return GBMUF_EINVAL;
+    *out = nullptr;
+    if (!desc || desc->struct_size < sizeof(gbmuf_grads_desc_t) || desc->workers < 1 || desc->n_tensors < 0) return GBMUF_EINVAL;
+    if (desc->n_tensors > 0 && !desc->tensors) return GBMUF_EINVAL;
+    if (desc->workers > GBMUF_MAX_K || desc->n_tensors > 0x7fffffffLL) return GBMUF_EUNSUPPORTED;
+    gbmuf_grads_s *h = new (std::nothrow) gbmuf_grads_s;
+    if (!h) return GBMUF_ENOMEM;
+    int rc = GBMUF_OK;
+    try {
+        rc = make_grads(*h, *desc);
+    } catch (const std::bad_alloc &) {
+        rc = GBMUF_ENOMEM;
+    } catch (const std::length_error &) {
+        rc = GBMUF_ENOMEM;
+    }
+    if (rc != GBMUF_OK) {
+        free_grads(*h);
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return GBMUF_OK;
+}
+
+int gbmuf_grads_destroy(gbmuf_grads_t *grads)
+{
+    if (!grads) return GBMUF_OK;
+    int rc = GBMUF_OK;
+    if (grads->device >= 0) {
+        if (hipDeviceSynchronize() != hipSuccess) rc = GBMUF_EDEVICE;
+        free_grads(*grads);
+    }
+    delete grads;
+    return rc;
+}
+
+int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream)
+{
+    if (!grads || !norms) return GBMUF_EINVAL;
+    const int rc = check_grads_device(grads);
+    return rc != GBMUF_OK ? rc : enqueue_norm(grads, norms, static_cast<hipStream_t>(stream));
+}
+
+int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream)
+{
+    if (!src || !dst || !norms || !(max_norm >= 0.0f)) return GBMUF_EINVAL;
+    if (src != dst) {
+        if (src->workers != dst->workers || src->tensors.size() != dst->tensors.size()) return GBMUF_EINVAL;
+        for (size_t i = 0; i < src->tensors.size(); ++i) {
+            const GradTensor &a = src->tensors[i], &b = dst->tensors[i];
+            if (a.worker != b.worker || a.rows != b.rows || a.cols != b.cols) return GBMUF_EINVAL;
+        }
+    }
+    int rc = check_grads_device(src);
+    if (rc != GBMUF_OK || (rc = check_grads_device(dst)) != GBMUF_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if ((rc = enqueue_norm(src, norms, s)) != GBMUF_OK) return rc;
+    const GradTensor *from = src->d_tensors, *to = dst->d_tensors;
+    const GradTile *tiles = src->d_tiles;
+    const float *n = norms;
+    void *argv[] = {&from, &to, &tiles, &n, &max_norm};
+    return launch(reinterpret_cast<const void *>(clip_kernel), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
+}
+
+int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, const gbmuf_state_t *theta, const gbmuf_state_t *sums, float *norms,
+                     void *stream)
+{
+    if (!grads || !desc || desc->struct_size < sizeof(gbmuf_step_desc_t) || !theta || !theta->theta) return GBMUF_EINVAL;
+    if (desc->P < 0 || grads->reach > desc->P) return GBMUF_EINVAL;
+    if (desc->rate != desc->rate || !(desc->eps >= 0.0f) || !(desc->max_norm >= 0.0f)) return GBMUF_EINVAL;
+    const bool clip = desc->max_norm < INFINITY || desc->skip_nonfinite != 0;
+    if (clip && !norms) return GBMUF_EINVAL;
+    StepArgs a{};
+    int64_t extent = 0, extent_sums = 0;
+    int rc = place(*theta, grads->workers, desc->P, &a.at, &extent);
+    if (rc != GBMUF_OK) return rc;
+    if (sums) {
+        if (!sums->theta) return GBMUF_EINVAL;
+        if ((rc = place(*sums, grads->workers, desc->P, &a.sums_at, &extent_sums)) != GBMUF_OK) return rc;
+        if (!apart(*theta, extent, *sums, extent_sums, grads->workers, desc->P)) return GBMUF_EINVAL;
+        a.sums = sums->theta;
+    }
+    if ((rc = check_grads_device(grads)) != GBMUF_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (norms && (rc = enqueue_norm(grads, norms, s)) != GBMUF_OK) return rc;
+    a.tensors = grads->d_tensors; a.tiles = grads->d_tiles;
+    a.norms = clip ? norms : nullptr;
+    a.theta = theta->theta;
+    a.rate = desc->rate; a.eps = desc->eps; a.most = desc->max_norm; a.skip_nonfinite = desc->skip_nonfinite;
+    void *argv[] = {&a};
+    return launch(reinterpret_cast<const void *>(step_kernel), grads->n_tiles, argv, "hipLaunchKernel(local step)", s);
+}
+
+}  // extern "C"

@@ -1,0 +1,390 @@
+// gbmuf_linear.hip -- entry points of the products with a model's matrices: checks, workspace, and which kernels run.
+#include "gbmuf_local.h"
+
+#include "../../include/gbmuf.h"
+
+#include <algorithm>
+#include <numeric>
+
+namespace gbmuf {
+namespace {
+
+constexpr int64_t kLargest = 0x7fffffff;
+constexpr int64_t kStepWords = 64;
+
+// ---------------------------------------------------------------------------------------
+// Checks
+// ---------------------------------------------------------------------------------------
+struct Extent {                  // bytes that a matrix covers
+    uintptr_t at = 0;
+    int64_t rows = 0, row = 0, ld = 0;           // rows of `row` bytes, ld apart
+    int64_t batch = 0, stride = 0;               // matrices, stride apart
+    int64_t matrix() const { return (rows - 1) * ld + row; }
+    int64_t all() const { return (batch - 1) * stride + matrix(); }
+    bool none() const { return at == 0 || rows <= 0 || row <= 0 || batch <= 0; }
+};
+
+Extent extent(const gbmuf_matrix_t &m, int64_t rows, int64_t cols, int64_t batch, int32_t type)
+{
+    const int64_t b = static_cast<int64_t>(type_bytes(type));
+    Extent e;
+    e.at = reinterpret_cast<uintptr_t>(m.data);
+    e.rows = rows; e.row = cols * b; e.ld = rows > 1 ? m.ld * b : 0;
+    e.batch = batch; e.stride = batch > 1 ? m.batch_stride * b : 0;
+    return e;
+}
+
+// Pieces of `len` bytes, `step` apart, from a and from b, of which none of a meets one of b: so it is where the pieces of both lie side by
+// side in every step.
+bool side_by_side(uintptr_t a, int64_t len_a, uintptr_t b, int64_t len_b, int64_t step)
+{
+    if (step <= 0) return false;
+    const int64_t d = b >= a ? static_cast<int64_t>((b - a) % static_cast<uintptr_t>(step))
+                             : (step - static_cast<int64_t>((a - b) % static_cast<uintptr_t>(step))) % step;
+    return d >= len_a && d + len_b <= step;
+}
+
+// Whether two matrices may share bytes.  Apart are: ranges that do not meet; matrices, or else rows, that lie side by side in every
+// stretch of a length that divides all steps between them.
+bool overlap(const Extent &a, const Extent &b)
+{
+    if (a.none() || b.none()) return false;
+    if (a.at + a.all() <= b.at || b.at + b.all() <= a.at) return false;
+    const int64_t matrices = std::gcd(a.stride, b.stride), rows = std::gcd(matrices, std::gcd(a.ld, b.ld));
+    return !side_by_side(a.at, a.matrix(), b.at, b.matrix(), matrices) && !side_by_side(a.at, a.row, b.at, b.row, rows);
+}
+
+bool valid_input(const gbmuf_matrix_t &m, const Extent &e, int32_t type)
+{
+    if (m.ld < 0 || m.batch_stride < 0) return false;
+    if (e.rows <= 0 || e.row <= 0 || e.batch <= 0) return true;
+    return m.data && reinterpret_cast<uintptr_t>(m.data) % type_bytes(type) == 0;
+}
+
+// an output's elements are all apart: row after row and matrix after matrix, or the workers' rows inside each row's step
+bool valid_output(const gbmuf_matrix_t &m, const Extent &e, int32_t type)
+{
+    if (!valid_input(m, e, type)) return false;
+    if (e.none()) return true;
+    const bool rows_apart = e.rows <= 1 || e.ld >= e.row, matrices_apart = e.batch <= 1 || e.stride >= e.matrix();
+    const bool inside = e.stride >= e.row && (e.rows <= 1 || e.ld >= (e.batch - 1) * e.stride + e.row);
+    return rows_apart && (matrices_apart || inside);
+}
+
+int check_desc(const gbmuf_linear_desc_t *d)
+{
+    if (!d || d->struct_size < sizeof(gbmuf_linear_desc_t)) return GBMUF_EINVAL;
+    if (d->dtype < GBMUF_F32 || d->dtype > GBMUF_F16 || d->activation < GBMUF_ACT_NONE || d->activation > GBMUF_ACT_TANH) return GBMUF_EINVAL;
+    if (d->residual < GBMUF_RESIDUAL_NONE || d->residual > GBMUF_RESIDUAL_AFTER) return GBMUF_EINVAL;
+    if (d->batch < 0 || d->rows < 0 || d->out_features < 0 || d->in_features < 0) return GBMUF_EINVAL;
+    if (d->batch > 65535 || d->rows > kLargest || d->out_features > kLargest || d->in_features > kLargest / 2 - 64) return GBMUF_EUNSUPPORTED;
+    return GBMUF_OK;
+}
+
+int check_device()
+{
+    int n = 0;
+    const hipError_t err = hipGetDeviceCount(&n);
+    if (err != hipSuccess || n < 1) return hip_failed("hipGetDeviceCount", err == hipSuccess ? hipErrorNoDevice : err, GBMUF_EDEVICE);
+    return GBMUF_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// Workspace: the same calls count it and hand it out.
+// ---------------------------------------------------------------------------------------
+struct Space {
+    char *base;
+    int64_t used = 0;
+    template <class T>
+    T *take(int64_t n)
+    {
+        T *p = reinterpret_cast<T *>(base + used);
+        used += (n * static_cast<int64_t>(sizeof(T)) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// One operand of a product: rows of 16-bit words along the axis that is summed over.
+struct Operand {
+    const uint16_t *p = nullptr;
+    int64_t ld = 0, batch = 0;
+    uint32_t *max = nullptr;     // split
+    int64_t max_batch = 0;
+    bool whole = false;          // zeros follow up to the end of the last step
+};
+
+bool lies_well(const gbmuf_matrix_t &m)
+{
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && m.ld % 8 == 0 && m.batch_stride % 8 == 0;
+}
+
+// What one product needs besides its operands.
+struct Shape {
+    int32_t tiles_m, tiles_n, splits, steps;
+    int64_t partial;             // floats
+};
+
+Shape shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
+{
+    Shape s{};
+    s.tiles_m = static_cast<int32_t>((M + 127) / 128);
+    s.tiles_n = static_cast<int32_t>((N + 127) / 128);
+    const int64_t all = packed_words(K, split_type) / kStepWords, tiles = static_cast<int64_t>(s.tiles_m) * s.tiles_n * batch;
+    // few tiles: the sum over k is cut so that two workgroups a CU have work, in parts of 8 steps at least
+    int64_t splits = tiles > 0 && tiles < 256 ? std::min<int64_t>(512 / tiles, all / 8) : 1;
+    splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
+    s.steps = static_cast<int32_t>(std::max<int64_t>(1, (all + splits - 1) / splits));
+    s.splits = static_cast<int32_t>(std::max<int64_t>(1, (all + s.steps - 1) / s.steps));
+    s.partial = s.splits > 1 ? static_cast<int64_t>(s.splits) * batch * M * N : 0;
+    return s;
+}
+
+int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t type, const Epilogue &e,
+                const Shape &s, float *partial, hipStream_t stream)
+{
+    ProductArgs p{};
+    p.a = a.p; p.b = b.p; p.lda = a.ld; p.ldb = b.ld; p.a_batch = a.batch; p.b_batch = b.batch;
+    p.a_max = a.max; p.b_max = b.max; p.a_max_batch = a.max_batch; p.b_max_batch = b.max_batch;
+    p.M = static_cast<int32_t>(M); p.N = static_cast<int32_t>(N);
+    p.K = static_cast<int32_t>(a.whole && b.whole ? packed_words(K, type == kF32) : K);
+    p.batch = batch; p.tiles_m = s.tiles_m; p.tiles_n = s.tiles_n; p.splits = s.splits; p.steps = s.steps;
+    p.partial = partial; p.e = e;
+    int rc = launch_product(p, type, stream);
+    if (rc != GBMUF_OK || s.splits <= 1) return rc;
+    JoinArgs j{};
+    j.partial = partial; j.M = M; j.N = N; j.batch = batch; j.splits = s.splits; j.e = e;
+    return launch_join(j, stream);
+}
+
+LayArgs source(const gbmuf_matrix_t &m, int64_t R, int64_t C, int32_t batch, int32_t type)
+{
+    LayArgs l{};
+    l.src = m.data; l.ld = m.ld; l.batch_stride = m.batch_stride;
+    l.R = static_cast<int32_t>(R); l.C = static_cast<int32_t>(C);
+    l.batch = m.batch_stride == 0 ? std::min(batch, 1) : batch;        // what workers share is laid out once
+    l.type = type;
+    return l;
+}
+
+// Places of a packed copy of R rows of C values for `batch` workers (l.batch of them are written).
+Operand packed(Space &space, int64_t R, int64_t C, int32_t batch, int32_t written, bool split, uint32_t *max)
+{
+    Operand o;
+    o.ld = packed_words(C, split);
+    o.p = space.take<uint16_t>(static_cast<int64_t>(batch) * R * o.ld);
+    o.batch = written < batch ? 0 : R * o.ld;
+    o.max = max;
+    o.max_batch = written < batch ? 0 : R;
+    o.whole = true;
+    return o;
+}
+
+Epilogue into(const gbmuf_matrix_t &m, int32_t type)
+{
+    Epilogue e{};
+    e.y = m.data; e.ldy = m.ld; e.y_batch = m.batch_stride; e.type = type;
+    return e;
+}
+
+// ---------------------------------------------------------------------------------------
+// Forward.  io nullptr: only count the workspace, for matrices that lie as badly as can be.
+// ---------------------------------------------------------------------------------------
+int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &space, hipStream_t stream)
+{
+    const int64_t M = d.rows, N = d.out_features, K = d.in_features;
+    const int32_t G = d.batch, type = d.dtype;
+    const bool split = type == kF32;
+    const Shape s = shape_of(M, N, K, G, split);
+    float *partial = space.take<float>(s.partial);
+    uint32_t *max = space.take<uint32_t>(split ? G * (M + N) : 0);
+    const gbmuf_matrix_t none{};
+    const gbmuf_matrix_t &xm = io ? io->x : none, &wm = io ? io->w : none;
+    const LayArgs lx = source(xm, M, K, G, type), lw = source(wm, N, K, G, type);
+    Operand x{static_cast<const uint16_t *>(xm.data), xm.ld, xm.batch_stride, nullptr, 0, false};
+    Operand w{static_cast<const uint16_t *>(wm.data), wm.ld, wm.batch_stride, nullptr, 0, false};
+    const bool lay_x = split || !io || !lies_well(xm), lay_w = split || !io || !lies_well(wm);
+    if (lay_x) x = packed(space, M, K, G, lx.batch, split, max);
+    if (lay_w) w = packed(space, N, K, G, lw.batch, split, max + G * M);
+    if (!io) return GBMUF_OK;
+    int rc = GBMUF_OK;
+    if (split && (rc = launch_zero(max, G * (M + N), stream)) != GBMUF_OK) return rc;
+    for (int i = 0; i < 2; ++i) {
+        if (!(i == 0 ? lay_x : lay_w)) continue;
+        LayArgs l = i == 0 ? lx : lw;
+        const Operand &o = i == 0 ? x : w;
+        l.row_max = o.max;
+        if (split && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
+        l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
+        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+    }
+    Epilogue e = into(io->y, type);
+    e.pre = io->pre.data; e.ldp = io->pre.ld; e.p_batch = io->pre.batch_stride;
+    e.bias = io->bias.data; e.bias_batch = io->bias.batch_stride;
+    e.res = io->residual.data; e.ldr = io->residual.ld; e.r_batch = io->residual.batch_stride;
+    e.act = d.activation; e.place = d.residual;
+    return run_product(x, w, M, N, K, G, type, e, s, partial, stream);
+}
+
+// ---------------------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------------------
+int backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+{
+    const int64_t M = d.rows, N = d.out_features, K = d.in_features;
+    const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
+    const bool split = type == kF32;
+    const bool dx = !io || io->dx.data, dw = !io || io->dw.data, db = !io || io->dbias.data, dr = io && io->dresidual.data;
+    const Shape sx = shape_of(M, K, N, G, split), sw = shape_of(N, K, M, G, split);
+    const int64_t row_tiles = (M + kLayTile - 1) / kLayTile;
+    float *partial = space.take<float>(std::max(dx ? sx.partial : 0, dw ? sw.partial : 0));     // one product after the other
+    float *sums = space.take<float>(db ? G * row_tiles * N : 0);
+    // largest magnitudes: rows and columns of dz, columns of w and of x
+    const int64_t n_max = split ? G * (M + N + 2 * K) : 0;
+    uint32_t *max = space.take<uint32_t>(n_max);
+    const gbmuf_matrix_t none{};
+    const gbmuf_matrix_t &dym = io ? io->dy : none, &wm = io ? io->w : none, &xm = io ? io->x : none;
+
+    // dz is a matrix for each worker even where dy is shared, since z may not be
+    LayArgs lz = source(dym, M, N, G, type);
+    if (d.activation) {
+        lz.batch = G;
+        if (io) { lz.pre = io->pre.data; lz.ldp = io->pre.ld; lz.p_batch = io->pre.batch_stride; }
+        lz.act = d.activation;
+    }
+    lz.batch = dr || db ? G : lz.batch;
+    const LayArgs lw = source(wm, N, K, G, type), lx = source(xm, M, K, G, type);
+    const bool plain = dx && (split || d.activation || !io || !lies_well(dym));
+    Operand z{static_cast<const uint16_t *>(dym.data), dym.ld, dym.batch_stride, nullptr, 0, false}, zt, wt, xt;
+    if (plain) z = packed(space, M, N, G, lz.batch, split, max);
+    if (dw) zt = packed(space, N, M, G, lz.batch, split, max + G * M);
+    if (dx) wt = packed(space, K, N, G, lw.batch, split, max + G * (M + N));
+    if (dw) xt = packed(space, K, M, G, lx.batch, split, max + G * (M + N + K));
+    if (!io) return GBMUF_OK;
+
+    int rc = GBMUF_OK;
+    if (split && (rc = launch_zero(max, n_max, stream)) != GBMUF_OK) return rc;
+    if (split || db) {
+        LayArgs l = lz;
+        l.row_max = split && dx ? z.max : nullptr;
+        l.col_max = split && dw ? zt.max : nullptr;
+        l.col_sums = db ? sums : nullptr;
+        if ((l.row_max || l.col_max || l.col_sums) && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
+    }
+    if (db) {
+        SumArgs a{};
+        a.sums = sums; a.out = io->dbias.data; a.out_batch = io->dbias.batch_stride;
+        a.C = static_cast<int32_t>(N); a.tiles = static_cast<int32_t>(row_tiles); a.batch = G; a.type = grad_type; a.accumulate = d.accumulate;
+        if ((rc = launch_column_sums(a, stream)) != GBMUF_OK) return rc;
+    }
+    if (plain || dw || dr) {
+        LayArgs l = lz;
+        if (plain) { l.plain = const_cast<uint16_t *>(z.p); l.plain_ld = z.ld; l.plain_batch = z.batch; l.row_max = z.max; }
+        if (dw) { l.trans = const_cast<uint16_t *>(zt.p); l.trans_ld = zt.ld; l.trans_batch = zt.batch; l.col_max = zt.max; }
+        if (dr) { l.dz = io->dresidual.data; l.dz_ld = io->dresidual.ld; l.dz_batch = io->dresidual.batch_stride; }
+        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (!(i == 0 ? dx : dw)) continue;
+        LayArgs l = i == 0 ? lw : lx;
+        const Operand &o = i == 0 ? wt : xt;
+        l.col_max = o.max;
+        if (split && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
+        l.trans = const_cast<uint16_t *>(o.p); l.trans_ld = o.ld; l.trans_batch = o.batch;
+        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+    }
+    if (dx && (rc = run_product(z, wt, M, K, N, G, type, into(io->dx, type), sx, partial, stream)) != GBMUF_OK) return rc;
+    if (dw) {
+        Epilogue e = into(io->dw, grad_type);
+        if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = io->dw.data; e.ldr = io->dw.ld; e.r_batch = io->dw.batch_stride; }
+        rc = run_product(zt, xt, N, K, M, G, type, e, sw, partial, stream);
+    }
+    return rc;
+}
+
+int check_workspace(const void *workspace, int64_t have, int64_t need)
+{
+    if (need == 0) return GBMUF_OK;
+    return workspace && have >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0 ? GBMUF_OK : GBMUF_EINVAL;
+}
+
+}  // namespace
+}  // namespace gbmuf
+
+using namespace gbmuf;
+
+extern "C" {
+
+int gbmuf_linear_workspace(const gbmuf_linear_desc_t *desc, int32_t backward_pass, int64_t *bytes)
+{
+    if (!bytes) return GBMUF_EINVAL;
+    *bytes = 0;
+    const int rc = check_desc(desc);
+    if (rc != GBMUF_OK) return rc;
+    Space space{nullptr};
+    if (backward_pass) backward(*desc, nullptr, space, nullptr);
+    else forward(*desc, nullptr, space, nullptr);
+    *bytes = space.used;
+    return GBMUF_OK;
+}
+
+int gbmuf_linear(const gbmuf_linear_desc_t *desc, const gbmuf_linear_io_t *io, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    int rc = check_desc(desc);
+    if (rc != GBMUF_OK) return rc;
+    if (!io) return GBMUF_EINVAL;
+    const int64_t M = desc->rows, N = desc->out_features, K = desc->in_features, G = desc->batch;
+    const int32_t t = desc->dtype;
+    const Extent x = extent(io->x, M, K, G, t), w = extent(io->w, N, K, G, t), b = extent(io->bias, 1, N, G, t),
+                 r = extent(io->residual, M, N, G, t), y = extent(io->y, M, N, G, t), p = extent(io->pre, M, N, G, t);
+    if (!valid_input(io->x, x, t) || !valid_input(io->w, w, t) || !valid_output(io->y, y, t)) return GBMUF_EINVAL;
+    if (io->bias.data && !valid_input(io->bias, b, t)) return GBMUF_EINVAL;
+    if (desc->residual != GBMUF_RESIDUAL_NONE && !valid_input(io->residual, r, t)) return GBMUF_EINVAL;
+    if (io->pre.data && !valid_output(io->pre, p, t)) return GBMUF_EINVAL;
+    for (const Extent *o : {&y, &p}) {
+        if (overlap(*o, x) || overlap(*o, w) || overlap(*o, b)) return GBMUF_EINVAL;
+        const bool in_place = o == &y && r.at == y.at && r.ld == y.ld && r.stride == y.stride;
+        if (desc->residual != GBMUF_RESIDUAL_NONE && !in_place && overlap(*o, r)) return GBMUF_EINVAL;
+    }
+    if (overlap(y, p)) return GBMUF_EINVAL;
+    int64_t need = 0;
+    if ((rc = gbmuf_linear_workspace(desc, 0, &need)) != GBMUF_OK) return rc;
+    if (M == 0 || N == 0 || G == 0) return GBMUF_OK;
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != GBMUF_OK) return rc;
+    if ((rc = check_device()) != GBMUF_OK) return rc;
+    Space space{static_cast<char *>(workspace)};
+    return forward(*desc, io, space, static_cast<hipStream_t>(stream));
+}
+
+int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_grad_io_t *io, void *workspace, int64_t workspace_bytes,
+                          void *stream)
+{
+    int rc = check_desc(desc);
+    if (rc != GBMUF_OK) return rc;
+    if (!io) return GBMUF_EINVAL;
+    const int64_t M = desc->rows, N = desc->out_features, K = desc->in_features, G = desc->batch;
+    const int32_t t = desc->dtype, gt = desc->weight_grad_f32 ? kF32 : t;
+    const Extent x = extent(io->x, M, K, G, t), w = extent(io->w, N, K, G, t), z = extent(io->pre, M, N, G, t), dy = extent(io->dy, M, N, G, t);
+    const Extent dx = extent(io->dx, M, K, G, t), dw = extent(io->dw, N, K, G, gt), db = extent(io->dbias, 1, N, G, gt),
+                 dr = extent(io->dresidual, M, N, G, t);
+    if (!valid_input(io->dy, dy, t) || (desc->activation && !valid_input(io->pre, z, t))) return GBMUF_EINVAL;
+    if (io->dx.data && (!valid_input(io->w, w, t) || !valid_output(io->dx, dx, t))) return GBMUF_EINVAL;
+    if (io->dw.data && (!valid_input(io->x, x, t) || !valid_output(io->dw, dw, gt))) return GBMUF_EINVAL;
+    if (io->dbias.data && !valid_output(io->dbias, db, gt)) return GBMUF_EINVAL;
+    if (io->dresidual.data && (desc->residual != GBMUF_RESIDUAL_BEFORE || !valid_output(io->dresidual, dr, t))) return GBMUF_EINVAL;
+    const Extent *outs[] = {&dx, &dw, &db, &dr};
+    for (int i = 0; i < 4; ++i) {
+        if (overlap(*outs[i], dy) || (desc->activation && overlap(*outs[i], z))) return GBMUF_EINVAL;
+        if ((io->dw.data && overlap(*outs[i], x)) || (io->dx.data && overlap(*outs[i], w))) return GBMUF_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (overlap(*outs[i], *outs[j])) return GBMUF_EINVAL;
+    }
+    int64_t need = 0;
+    if ((rc = gbmuf_linear_workspace(desc, 1, &need)) != GBMUF_OK) return rc;
+    if (G == 0) return GBMUF_OK;
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != GBMUF_OK) return rc;
+    if ((rc = check_device()) != GBMUF_OK) return rc;
+    Space space{static_cast<char *>(workspace)};
+    return backward(*desc, io, space, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

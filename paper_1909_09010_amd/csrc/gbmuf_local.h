@@ -1,0 +1,80 @@
+// gbmuf_local.h -- types shared by the local half's sources: products (gbmuf_product.hip), what is laid out for them
+// (gbmuf_layout.hip), their entry points (gbmuf_linear.hip) and the gradients of workers (gbmuf_grads.hip).
+#pragma once
+
+#include "gbmuf_internal.h"
+
+namespace gbmuf {
+
+enum : int32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };          // = GBMUF_F32 ..
+constexpr size_t type_bytes(int32_t t) { return t == kF32 ? 4 : 2; }
+
+// What is done with a sum s of products: z = s + bias (+ r), y = act(z) (+ r).
+struct Epilogue {
+    void *y, *pre;           // pre nullptr: not wanted
+    const void *bias, *res;
+    int64_t ldy, y_batch, ldp, p_batch, bias_batch, ldr, r_batch;
+    int32_t act, place;      // GBMUF_ACT_*, GBMUF_RESIDUAL_*
+    int32_t type;            // of all of them
+    int32_t reserved;
+};
+
+// out[g][m][n] = sum over k of a[g][m][k] * b[g][n][k], in 16-bit numbers whose k are contiguous.  Split: a row holds, for every 32
+// k, their 32 leading parts and then their 32 trailing parts, and `k` counts both; a_max and b_max hold the bits of the largest magnitude of
+// every row before the row was scaled.
+struct ProductArgs {
+    const uint16_t *a, *b;
+    int64_t lda, ldb, a_batch, b_batch;
+    const uint32_t *a_max, *b_max;
+    int64_t a_max_batch, b_max_batch;
+    int32_t M, N, K, batch;
+    int32_t tiles_m, tiles_n;
+    int32_t splits, steps;   // the sum over k goes to `splits` workgroups of `steps` steps of 64 each
+    int32_t reserved;
+    float *partial;          // splits > 1: [split][g][m][n]
+    Epilogue e;
+};
+
+// The sums of `splits` partial products, and what is done with them.
+struct JoinArgs {
+    const float *partial;
+    int64_t M, N;
+    int32_t batch, splits;
+    Epilogue e;
+};
+
+// A source matrix R x C of `type`, with the slope of the activation at `pre` as a factor where there is one, and what is written of it.
+struct LayArgs {
+    const void *src, *pre;
+    int64_t ld, batch_stride, ldp, p_batch;
+    int32_t R, C, batch;
+    int32_t type, act;       // act: GBMUF_ACT_NONE = no factor
+    // statistics (launch_stats): any of them nullptr
+    uint32_t *row_max, *col_max;          // [batch][R], [batch][C]: bits of the largest magnitude, zeroed before
+    float *col_sums;                      // [batch][row tiles][C]
+    // copies (launch_lay): any of them nullptr
+    uint16_t *plain, *trans;              // rows of R (C) values along C (R), 16-bit or split
+    int64_t plain_ld, plain_batch, trans_ld, trans_batch;
+    void *dz;                             // the product with the slope itself, of `type`
+    int64_t dz_ld, dz_batch;
+};
+constexpr int kLayTile = 64;
+
+struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
+    const float *sums;
+    void *out;
+    int64_t out_batch;
+    int32_t C, tiles, batch, type, accumulate;
+};
+
+// values of a packed row of n numbers, in 16-bit words: whole steps of 64
+constexpr int64_t packed_words(int64_t n, bool split) { return split ? (n + 31) / 32 * 64 : (n + 63) / 64 * 64; }
+
+int launch_product(const ProductArgs &a, int32_t type, hipStream_t stream);
+int launch_join(const JoinArgs &a, hipStream_t stream);
+int launch_stats(const LayArgs &a, hipStream_t stream);
+int launch_lay(const LayArgs &a, hipStream_t stream);
+int launch_column_sums(const SumArgs &a, hipStream_t stream);
+int launch_zero(uint32_t *p, int64_t words, hipStream_t stream);
+
+}  // namespace gbmuf

@@ -1,0 +1,363 @@
+"""Norms of workers' gradients, clipping and the local update, against 64 bits and, where the method fixes every rounding, bit for bit.
+
+A norm is summed in 64 bits and rounded once: within 2^-23 of the exact one.  The clip factor is one f32 division of the norm and the
+product one f32 multiply, then one rounding to the type of the output; the update rounds every operation by itself, so numpy's
+f32 arithmetic gives the same bits.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1909_09010_amd import binding as B
+from paper_1909_09010_amd import workloads as W
+
+DEV = "cuda:0"
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+gpu = pytest.mark.gpu
+
+SHAPES = [
+    [(7,), (3, 5), (1,)],
+    [(1000, 64), (256, 64), (256,)],
+    [(129, 33)],
+    [(0,), (4, 0), (70001,), (2, 2)],
+    [],
+]
+
+
+def tensors(dtype, seed=0, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return [[(torch.randn(s, generator=g) * scale).to(dtype).to(DEV) for s in ss] for ss in SHAPES]
+
+
+def norm64(ts):
+    return math.sqrt(sum(float(t.cpu().double().square().sum()) for t in ts))
+
+
+def factor(norm, most):
+    n, m = np.float32(norm), np.float32(most)
+    return np.float32(1.0) if n <= m else m / n
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_norms(dtype):
+    ts = tensors(dtype)
+    h, n = B.Grads(ts), torch.full((len(ts),), -1.0, device=DEV)
+    h.norm(n, torch.cuda.current_stream())
+    want = np.array([norm64(t) for t in ts])
+    assert np.all(np.abs(n.cpu().double().numpy() - want) <= 2.0 ** -23 * want)
+    again = torch.empty_like(n)
+    h.norm(again)
+    torch.cuda.synchronize()
+    assert torch.equal(n, again)
+
+
+@gpu
+def test_norms_of_very_large_and_very_small_values():
+    ts = [[torch.full((1000,), 1e30, device=DEV)], [torch.full((999,), 1e-35, device=DEV)], [torch.zeros(5, device=DEV)],
+          [torch.tensor([float("inf"), 1.0], device=DEV)], [torch.tensor([float("nan"), 1.0], device=DEV)], [torch.full((4,), 3e38, device=DEV)]]
+    h, n = B.Grads(ts), torch.empty(6, device=DEV)
+    h.norm(n, torch.cuda.current_stream())
+    n = n.cpu().numpy()
+    assert abs(n[0] / (1e30 * math.sqrt(1000)) - 1) < 1e-6 and abs(n[1] / (float(np.float32(1e-35)) * math.sqrt(999)) - 1) < 1e-6
+    assert n[2] == 0 and n[3] == np.inf and np.isnan(n[4]) and n[5] == np.inf
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("out_dtype", DTYPES)
+@pytest.mark.parametrize("most", [0.0, 1.5, 1e9, math.inf])
+def test_clip_into_other_tensors(dtype, out_dtype, most):
+    ts = tensors(dtype)
+    out = [[torch.full(t.shape, 9.0, dtype=out_dtype, device=DEV) for t in w] for w in ts]
+    before = [[t.clone() for t in w] for w in ts]
+    n = torch.empty(len(ts), device=DEV)
+    B.Grads(ts).clip(most, n, out=B.Grads(out), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for w, (a, b, c) in enumerate(zip(ts, out, before)):
+        f = torch.tensor(factor(n[w].item(), most))
+        for s, d, o in zip(a, b, c):
+            assert torch.equal(s, o)
+            assert torch.equal(d.cpu(), (s.cpu().float() * f).to(out_dtype))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_clip_in_place(dtype):
+    ts = tensors(dtype, scale=0.01)
+    before = [[t.cpu() for t in w] for w in ts]
+    n = torch.empty(len(ts), device=DEV)
+    h = B.Grads(ts)
+    h.clip(1.0, n, stream=torch.cuda.current_stream())
+    first = n.cpu()
+    clipped = 0
+    for w, (a, b) in enumerate(zip(ts, before)):
+        f = factor(first[w].item(), 1.0)
+        clipped += f < 1
+        for s, o in zip(a, b):
+            assert torch.equal(s.cpu(), (o.float() * torch.tensor(f)).to(dtype))
+    assert 0 < clipped < len(ts)
+    h.norm(n)
+    torch.cuda.synchronize()
+    assert (n.cpu() <= 1.0 + 2.0 ** -8).all()
+
+
+@gpu
+def test_clip_with_infinite_and_nan_gradients():
+    ts = [[torch.tensor([1.0, float("inf"), -2.0], device=DEV)], [torch.tensor([1.0, float("nan")], device=DEV)], [torch.ones(4, device=DEV)]]
+    n = torch.empty(3, device=DEV)
+    B.Grads(ts).clip(0.5, n, stream=torch.cuda.current_stream())
+    a, b, c = (t[0].cpu().numpy() for t in ts)
+    assert a[0] == 0 and np.isnan(a[1]) and a[2] == 0 and np.isnan(b).all() and (c == 0.25).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_strided_and_unaligned_tensors(dtype, shift):
+    g = torch.Generator().manual_seed(4)
+    flat = (torch.randn(50000, generator=g)).to(dtype).to(DEV)
+    wide = (torch.randn(300, 41, generator=g)).to(dtype).to(DEV)
+    ts = [[flat[shift: shift + 20003], flat[20010 + shift: 40000].view(-1)], [wide[:, 2: 39], wide[:, 40], flat[40001:49999:3]]]
+    keep_flat, keep_wide = flat.clone(), wide.clone()
+    n = torch.empty(2, device=DEV)
+    out = [[torch.empty(t.shape, dtype=torch.float32, device=DEV) for t in w] for w in ts]
+    out[1][0] = torch.full((300, 50), 5.0, device=DEV)[:, 7:44]
+    # the vector with gaps is a matrix of one column: its output is given the same form
+    out[1][1], out[1][2] = torch.full((300, 3), 5.0, device=DEV)[:, 1], torch.full((3333, 2), 5.0, device=DEV)[:, 0]
+    assert out[1][2].shape == ts[1][2].shape
+    B.Grads(ts).clip(2.0, n, out=B.Grads(out), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert torch.equal(flat, keep_flat) and torch.equal(wide, keep_wide)
+    want = np.array([norm64(t) for t in ts])
+    assert np.all(np.abs(n.cpu().double().numpy() - want) <= 2.0 ** -23 * want)
+    for w in range(2):
+        f = torch.tensor(factor(n[w].item(), 2.0))
+        for s, d in zip(ts[w], out[w]):
+            assert torch.equal(d.cpu(), s.cpu().float() * f)
+    assert (out[1][0]._base[:, :7] == 5.0).all() and (out[1][0]._base[:, 44:] == 5.0).all()
+    B.Grads(ts).clip(2.0, n, stream=torch.cuda.current_stream())          # and in place, beside values that stay
+    torch.cuda.synchronize()
+    assert torch.equal(flat[20003 + shift: 20010 + shift], keep_flat[20003 + shift: 20010 + shift])
+    assert torch.equal(wide[:, :2], keep_wide[:, :2]) and torch.equal(wide[:, 39], keep_wide[:, 39])
+    assert torch.equal(flat[40002:49999:3], keep_flat[40002:49999:3])
+
+
+# -- local update ---------------------------------------------------------------------------------
+class Placed:
+    """K x P values in rows, in blocks of B floats, or in blocks of an arena of three arrays."""
+
+    def __init__(self, values, layout, block=8192):
+        K, P = values.shape
+        self.K, self.P, self.layout = K, P, layout
+        if layout == "rows":
+            self.buf = torch.full((K, P + 5), 42.0, device=DEV)
+            self.view = self.buf[:, 3: P + 3]
+            self.view.copy_(values)
+            self.state = B.make_state(self.view, None, None, P + 5)
+        else:
+            nb, arrays = max(-(-P // block), 1), 3 if layout == "arena" else 1
+            self.buf = torch.full((nb, arrays, K, block), 42.0, device=DEV)
+            self.view = self.buf[:, arrays - 1]
+            pad = torch.full((K, nb * block), 42.0, device=DEV)
+            pad[:, :P] = values
+            self.view.copy_(pad.view(K, nb, block).transpose(0, 1))
+            self.state = B.make_state(self.view, None, None, block, block, arrays * K * block)
+
+    def get(self):
+        if self.layout == "rows":
+            return self.view.cpu().numpy()
+        return self.view.transpose(0, 1).reshape(self.K, -1)[:, : self.P].cpu().numpy()
+
+    def rest(self):
+        n = self.buf.numel() - self.K * self.P
+        return int((self.buf == 42.0).sum().item()) >= n
+
+
+def step_numpy(theta, sums, g, f, rate, eps):
+    g = (g.astype(np.float32) * np.float32(f)).astype(np.float32)
+    if sums is None:
+        return theta - np.float32(rate) * g, None
+    sums = sums + g * g
+    return theta - (np.float32(rate) * g) / (np.sqrt(sums) + np.float32(eps)), sums
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("layout,block", [("rows", 0), ("blocked", 8192), ("blocked", 4), ("arena", 64)])
+@pytest.mark.parametrize("adagrad", [True, False])
+@pytest.mark.parametrize("most", [2.0, math.inf])
+def test_local_step(dtype, layout, block, adagrad, most):
+    K, shapes = 3, [(50, 13), (7,), (0,), (2500,), (1,), (33, 64)]
+    P = sum(math.prod(s) for s in shapes) + 3            # the last 3 parameters have no gradient
+    rng = np.random.default_rng(5)
+    theta, sums = rng.standard_normal((K, P)).astype(np.float32), (rng.random((K, P)) + 0.1).astype(np.float32)
+    grads = [[torch.tensor(rng.standard_normal(s) * (0.001 if w == 1 else 1.0)).to(dtype).to(DEV) for s in shapes] for w in range(K)]
+    t, s = Placed(torch.tensor(theta), layout, block), Placed(torch.tensor(sums), "rows" if block == 4 else layout, block)
+    h, n = B.Grads(grads), torch.empty(K, device=DEV)
+    for _ in range(2):
+        h.local_step(t.state, s.state if adagrad else None, P, 0.1, 1e-7, most, n, stream=torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        norms = n.cpu().numpy()
+        for w in range(K):
+            assert abs(norms[w] - norm64(grads[w])) <= 2.0 ** -23 * norm64(grads[w])
+            g = np.concatenate([x.float().cpu().numpy().ravel() for x in grads[w]])
+            a, b = step_numpy(theta[w, :-3], sums[w, :-3] if adagrad else None, g, factor(norms[w], most), 0.1, 1e-7)
+            theta[w, :-3] = a
+            if adagrad:
+                sums[w, :-3] = b
+        assert np.array_equal(t.get(), theta) and np.array_equal(s.get(), sums)
+        assert t.rest() and s.rest()
+    assert (norms > 2.0).any() and (norms < 2.0).any()
+
+
+@gpu
+def test_local_step_by_offsets_and_without_norms():
+    rng = np.random.default_rng(6)
+    theta = rng.standard_normal((2, 100)).astype(np.float32)
+    grads = [[torch.tensor(rng.standard_normal(n).astype(np.float32)).to(DEV) for n in (10, 20)] for _ in range(2)]
+    t = Placed(torch.tensor(theta), "rows")
+    B.Grads(grads, offsets=[[70, 5], [0, 51]]).local_step(t.state, None, 100, 0.5, stream=torch.cuda.current_stream())
+    for w, offs in enumerate(((70, 5), (0, 51))):
+        for g, o in zip(grads[w], offs):
+            g = g.cpu().numpy()
+            theta[w, o: o + len(g)] -= np.float32(0.5) * g
+    assert np.array_equal(t.get(), theta)
+
+
+@gpu
+def test_a_worker_whose_gradients_are_not_finite_is_skipped_on_request():
+    theta = np.ones((3, 8), dtype=np.float32)
+    for skip in (True, False):
+        grads = [[torch.ones(8, device=DEV)], [torch.tensor([float("inf")] + [1.0] * 7, device=DEV)], [torch.tensor([float("nan")] + [1.0] * 7, device=DEV)]]
+        t, n = Placed(torch.tensor(theta), "rows"), torch.empty(3, device=DEV)
+        B.Grads(grads).local_step(t.state, None, 8, 0.5, max_norm=math.inf if skip else 1.0, norms=n, skip_nonfinite=skip, stream=torch.cuda.current_stream())
+        got = t.get()
+        assert (got[0] < 1).all()
+        if skip:
+            assert (got[1:] == 1).all()
+        else:
+            assert np.isnan(got[1, 0]) and (got[1, 1:] == 1).all() and np.isnan(got[2]).all()
+
+
+@gpu
+def test_step_on_a_state_of_the_library_and_a_sync_after_it():
+    """theta in the recommended arena, Adagrad's sums in their own; the sync that follows sees what the step wrote."""
+    w = W.get("tiny")
+    off = W.component_offsets(w)
+    P = int(off[-1])
+    pl = B.Plan(off, w.K, w.q, w.p, seed=w.seed)
+    st = W.init_state(w, DEV, layout="blocked", plan=pl)
+    rows = W.init_state(w, DEV, layout="rows", plan=pl)
+    sums = [W.DeviceState(w.K, P, DEV, layout, plan=pl) for layout in ("blocked", "rows")]
+    g = torch.Generator(device=DEV).manual_seed(1)
+    grads = [[torch.randn(r, c, device=DEV, generator=g) for _, r, c in W.tensors(w)] for _ in range(w.K)]
+    h, n, s = B.Grads(grads), torch.empty(w.K, device=DEV), torch.cuda.current_stream()
+    for a, b in zip((st, rows), sums):
+        b.zero_()
+        for rnd in range(2):
+            h.local_step(a.desc(), b.desc(), P, 0.1, 1e-7, 10.0, n, stream=s)
+            pl.sync_state(a.desc(), w.eta, w.zeta, w.mode, rnd, s)
+    torch.cuda.synchronize()
+    for i in range(3):
+        assert np.array_equal(st.to_host(i), rows.to_host(i))
+    assert np.array_equal(sums[0].to_host(0), sums[1].to_host(0)) and float(np.abs(sums[0].to_host(0)).max()) > 0
+    pl.destroy()
+
+
+@gpu
+def test_graph_replays_equal_eager_calls():
+    K, P = 4, 30000
+    g = torch.Generator(device=DEV).manual_seed(2)
+    grads = [[torch.randn(100, 200, device=DEV, generator=g), torch.randn(10000, device=DEV, generator=g)] for _ in range(K)]
+    theta = torch.randn(K, P, device=DEV, generator=g)
+    other, sums, sums2 = theta.clone(), torch.zeros(K, P, device=DEV), torch.zeros(K, P, device=DEV)
+    h, n = B.Grads(grads), torch.empty(K, device=DEV)
+    a, b = B.make_state(theta, None, None, P), B.make_state(other, None, None, P)
+    sa, sb = B.make_state(sums, None, None, P), B.make_state(sums2, None, None, P)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        h.local_step(a, sa, P, 0.1, 1e-7, 5.0, n, stream=torch.cuda.current_stream())
+    for replay in range(3):
+        for ts in grads:
+            for t in ts:
+                t.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        h.local_step(b, sb, P, 0.1, 1e-7, 5.0, n)
+        torch.cuda.synchronize()
+        assert torch.equal(theta, other) and torch.equal(sums, sums2), replay
+        assert torch.randn(1 << 18, device=DEV).sum().item() != 0.5
+
+
+# -- refusals ---------------------------------------------------------------------------------------
+def raw(entries, workers=1):
+    import ctypes
+    table = (B.GradTensor * max(len(entries), 1))(*[B.GradTensor(*e) for e in entries])
+    d = B.GradsDesc(ctypes.sizeof(B.GradsDesc), workers, len(entries), ctypes.addressof(table))
+    h = ctypes.c_void_p()
+    rc = B.lib().gbmuf_grads_create(ctypes.byref(h), ctypes.byref(d))
+    if rc == B.GBMUF_OK:
+        B.lib().gbmuf_grads_destroy(h)
+    else:
+        assert not h
+    return rc
+
+
+def test_handles_that_are_refused():
+    p = 4096                                              # only looked at, never followed
+    assert raw([(p, 1, 8, 8, -1, 0, 0)]) == B.GBMUF_OK
+    assert raw([]) == B.GBMUF_OK
+    assert raw([(0, 1, 0, 0, -1, 0, 0)]) == B.GBMUF_OK    # an empty tensor has no data
+    for e in ((p, 1, 8, 8, -1, 1, 0), (p, 1, 8, 8, -1, -1, 0), (p, 1, 8, 8, -1, 0, 3), (p, 1, 8, 8, -1, 0, -1), (p, -1, 8, 8, -1, 0, 0),
+              (p, 1, -8, 8, -1, 0, 0), (p, 2, 8, 7, -1, 0, 0), (p, 1, 8, 8, -2, 0, 0), (0, 1, 8, 8, -1, 0, 0), (p + 2, 1, 8, 8, -1, 0, 0),
+              (p + 1, 1, 8, 8, -1, 0, 1)):
+        assert raw([e]) == B.GBMUF_EINVAL, e
+    assert raw([(p, 1, 8, 8, 0, 0, 0), (p, 1, 8, 8, 7, 0, 0)]) == B.GBMUF_EINVAL          # places overlap
+    assert raw([(p, 1, 8, 8, 10, 0, 0), (p, 1, 8, 8, 0, 0, 0), (p, 1, 3, 3, 8, 0, 0)]) == B.GBMUF_EINVAL
+    assert raw([(p, 1, 8, 8, 0, 0, 0), (p, 1, 8, 8, 7, 1, 0)], workers=2) == B.GBMUF_OK   # of different workers
+    assert raw([], workers=0) == B.GBMUF_EINVAL
+    assert raw([], workers=1025) == B.GBMUF_EUNSUPPORTED
+    assert raw([(p, 1 << 40, 1 << 40, 1 << 40, -1, 0, 0)]) == B.GBMUF_EUNSUPPORTED
+    assert B.lib().gbmuf_grads_create(None, None) == B.GBMUF_EINVAL
+    assert B.lib().gbmuf_grads_destroy(None) == B.GBMUF_OK
+    with pytest.raises(B.GbmufError):
+        B.Grads([[torch.zeros(4, dtype=torch.float64)]])
+    with pytest.raises(B.GbmufError):
+        B.Grads([[torch.zeros(4, 5, 6)[:, :, 1:]]])
+
+
+def test_calls_that_are_refused():
+    ts = [[torch.zeros(10), torch.zeros(4, 5)], [torch.zeros(30)]]
+    h, n, theta, sums = B.Grads(ts) if not torch.cuda.is_available() else None, torch.zeros(2), torch.zeros(2, 30), torch.zeros(2, 30)
+    if h is None:
+        pytest.skip("host memory")
+    st, su = B.make_state(theta, None, None, 30), B.make_state(sums, None, None, 30)
+
+    def code(fn):
+        with pytest.raises(B.GbmufError) as e:
+            fn()
+        return e.value.code
+    E = B.GBMUF_EINVAL
+    assert code(lambda: h.norm(None)) == E
+    assert code(lambda: h.clip(-1.0, n)) == E and code(lambda: h.clip(float("nan"), n)) == E and code(lambda: h.clip(1.0, None)) == E
+    for other in ([[torch.zeros(10), torch.zeros(4, 5)]], [[torch.zeros(10), torch.zeros(5, 4).t()], [torch.zeros(30)]],
+                  [[torch.zeros(10), torch.zeros(21)], [torch.zeros(30)]], [[torch.zeros(10)], [torch.zeros(30)]]):
+        assert code(lambda: h.clip(1.0, n, out=B.Grads(other))) == E
+    step = lambda a=st, b=su, P=30, rate=0.1, eps=0.0, most=1.0, norms=n: h.local_step(a, b, P, rate, eps, most, norms)
+    assert code(lambda: step(P=29)) == E and code(lambda: step(P=-1)) == E
+    assert code(lambda: step(rate=float("nan"))) == E and code(lambda: step(eps=-1.0)) == E and code(lambda: step(eps=float("nan"))) == E
+    assert code(lambda: step(most=-1.0)) == E and code(lambda: step(most=float("nan"))) == E and code(lambda: step(norms=None)) == E
+    assert code(lambda: step(a=B.make_state(None, None, None, 30))) == E and code(lambda: step(b=B.make_state(None, None, None, 30))) == E
+    assert code(lambda: step(a=B.make_state(theta, None, None, 29))) == E
+    assert code(lambda: step(b=st)) == E and code(lambda: step(b=B.make_state(theta.data_ptr() + 40, None, None, 30))) == E
+    assert code(lambda: step(a=B.make_state(theta.data_ptr() + 2, None, None, 30))) == E
+    for B_, ws, bs in ((6, 6, 12), (2, 2, 4), (8, 7, 16), (8, 8, 15), (-8, 8, 16)):
+        assert code(lambda: step(a=B.make_state(theta, None, None, ws, B_, bs))) == E
+    # side by side in one arena: the checks pass, and the device is what is missing
+    arena = torch.zeros(2, 2, 32)
+    assert code(lambda: step(a=B.make_state(arena[:, 0], None, None, 64), b=B.make_state(arena[:, 1], None, None, 64))) == B.GBMUF_EDEVICE
+    assert code(lambda: step()) == B.GBMUF_EDEVICE and code(lambda: h.norm(n)) == B.GBMUF_EDEVICE and code(lambda: h.clip(1.0, n)) == B.GBMUF_EDEVICE
