@@ -11,6 +11,7 @@ namespace {
 
 constexpr int64_t kLargest = 0x7fffffff;
 constexpr int64_t kStepWords = 64;
+constexpr double kForwardDirect = 2e10, kBackwardDirect = 2e10, kBackwardDirect16 = 2e9;
 
 // ---------------------------------------------------------------------------------------
 // Checks
@@ -120,6 +121,7 @@ bool lies_well(const gbmuf_matrix_t &m)
 
 // What one product needs besides its operands.
 struct Shape {
+    int tile;
     int32_t tiles_m, tiles_n, splits, steps;
     int64_t partial;             // floats
 };
@@ -127,8 +129,9 @@ struct Shape {
 Shape shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
 {
     Shape s{};
-    s.tiles_m = static_cast<int32_t>((M + 127) / 128);
-    s.tiles_n = static_cast<int32_t>((N + 127) / 128);
+    s.tile = (M + 255) / 256 * ((N + 255) / 256) * batch >= 256 ? 256 : 128;
+    s.tiles_m = static_cast<int32_t>((M + s.tile - 1) / s.tile);
+    s.tiles_n = static_cast<int32_t>((N + s.tile - 1) / s.tile);
     const int64_t all = packed_words(K, split_type) / kStepWords, tiles = static_cast<int64_t>(s.tiles_m) * s.tiles_n * batch;
     // few tiles: the sum over k is cut so that two workgroups a CU have work, in parts of 8 steps at least
     int64_t splits = tiles > 0 && tiles < 256 ? std::min<int64_t>(512 / tiles, all / 8) : 1;
@@ -149,7 +152,7 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     p.K = static_cast<int32_t>(a.whole && b.whole ? packed_words(K, type == kF32) : K);
     p.batch = batch; p.tiles_m = s.tiles_m; p.tiles_n = s.tiles_n; p.splits = s.splits; p.steps = s.steps;
     p.partial = partial; p.e = e;
-    int rc = launch_product(p, type, stream);
+    int rc = launch_product(p, type, s.tile, stream);
     if (rc != GBMUF_OK || s.splits <= 1) return rc;
     JoinArgs j{};
     j.partial = partial; j.M = M; j.N = N; j.batch = batch; j.splits = s.splits; j.e = e;
@@ -187,6 +190,67 @@ Epilogue into(const gbmuf_matrix_t &m, int32_t type)
 }
 
 // ---------------------------------------------------------------------------------------
+// Products straight from where the matrices lie.
+// ---------------------------------------------------------------------------------------
+Source source_of(const gbmuf_matrix_t &m)
+{
+    Source s{};
+    s.p = m.data; s.ld = m.ld; s.batch = m.batch_stride;
+    return s;
+}
+
+DirectArgs direct_args(const Source &a, const Source &b, int64_t M, int64_t N, int64_t K, int32_t batch, int tile, const Epilogue &e)
+{
+    DirectArgs d{};
+    d.a = a; d.b = b;
+    d.M = static_cast<int32_t>(M); d.N = static_cast<int32_t>(N); d.K = static_cast<int32_t>(K); d.batch = batch;
+    d.tiles_m = static_cast<int32_t>((M + tile - 1) / tile);
+    d.tiles_n = static_cast<int32_t>((N + tile - 1) / tile);
+    d.splits = 1;
+    d.steps = static_cast<int32_t>((K + 31) / 32);
+    d.e = e;
+    return d;
+}
+
+// Cuts the sum over k where there are fewer tiles than CUs, in parts of 8 steps at least.  Returns the floats of partial sums.
+int64_t cut_sum(DirectArgs &d)
+{
+    const int64_t tiles = static_cast<int64_t>(d.tiles_m) * d.tiles_n * d.batch;
+    int64_t splits = tiles > 0 && tiles < 256 ? std::min<int64_t>(512 / tiles, d.steps / 8) : 1;
+    splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
+    const int64_t steps = std::max<int64_t>(1, (d.steps + splits - 1) / splits);
+    d.splits = static_cast<int32_t>(std::max<int64_t>(1, (d.steps + steps - 1) / steps));
+    d.steps = static_cast<int32_t>(steps);
+    return d.splits > 1 ? static_cast<int64_t>(d.splits) * d.batch * d.M * d.N : 0;
+}
+
+int join(const DirectArgs &d, hipStream_t stream)
+{
+    if (d.splits <= 1) return GBMUF_OK;
+    JoinArgs j{};
+    j.partial = d.partial; j.M = d.M; j.N = d.N; j.batch = d.batch; j.splits = d.splits; j.e = d.e;
+    return launch_join(j, stream);
+}
+
+int tile_of(int64_t M, int64_t N, int64_t batch)
+{
+    return (M + 127) / 128 * ((N + 127) / 128) * batch >= 256 ? 128 : 64;
+}
+
+// Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions.
+bool takes_direct_forward(const gbmuf_linear_desc_t &d)
+{
+    const double work = 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
+    return d.dtype == GBMUF_F32 && work <= kForwardDirect;
+}
+
+bool takes_direct_backward(const gbmuf_linear_desc_t &d)
+{
+    const double work = 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
+    return work <= (d.dtype == GBMUF_F32 ? kBackwardDirect : kBackwardDirect16);
+}
+
+// ---------------------------------------------------------------------------------------
 // Forward.  io nullptr: only count the workspace, for matrices that lie as badly as can be.
 // ---------------------------------------------------------------------------------------
 int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &space, hipStream_t stream)
@@ -194,10 +258,27 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
     const int32_t G = d.batch, type = d.dtype;
     const bool split = type == kF32;
+    const gbmuf_matrix_t none{};
+    Epilogue e{};
+    if (io) {
+        e = into(io->y, type);
+        e.pre = io->pre.data; e.ldp = io->pre.ld; e.p_batch = io->pre.batch_stride;
+        e.bias = io->bias.data; e.bias_batch = io->bias.batch_stride;
+        e.res = io->residual.data; e.ldr = io->residual.ld; e.r_batch = io->residual.batch_stride;
+        e.act = d.activation; e.place = d.residual;
+    }
+    if (M <= kFewRows || takes_direct_forward(d)) {
+        const int tile = tile_of(M, N, G);
+        DirectArgs f = direct_args(source_of(io ? io->x : none), source_of(io ? io->w : none), M, N, K, G, tile, e);
+        if (M <= kFewRows) return io ? launch_few(f, type, stream) : GBMUF_OK;
+        f.partial = space.take<float>(cut_sum(f));
+        if (!io) return GBMUF_OK;
+        const int rc = launch_direct_forward(f, type, tile, stream);
+        return rc != GBMUF_OK ? rc : join(f, stream);
+    }
     const Shape s = shape_of(M, N, K, G, split);
     float *partial = space.take<float>(s.partial);
     uint32_t *max = space.take<uint32_t>(split ? G * (M + N) : 0);
-    const gbmuf_matrix_t none{};
     const gbmuf_matrix_t &xm = io ? io->x : none, &wm = io ? io->w : none;
     const LayArgs lx = source(xm, M, K, G, type), lw = source(wm, N, K, G, type);
     Operand x{static_cast<const uint16_t *>(xm.data), xm.ld, xm.batch_stride, nullptr, 0, false};
@@ -217,18 +298,35 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
         l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
         if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
     }
-    Epilogue e = into(io->y, type);
-    e.pre = io->pre.data; e.ldp = io->pre.ld; e.p_batch = io->pre.batch_stride;
-    e.bias = io->bias.data; e.bias_batch = io->bias.batch_stride;
-    e.res = io->residual.data; e.ldr = io->residual.ld; e.r_batch = io->residual.batch_stride;
-    e.act = d.activation; e.place = d.residual;
     return run_product(x, w, M, N, K, G, type, e, s, partial, stream);
 }
 
 // ---------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------
-int backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+{
+    const int64_t M = d.rows, N = d.out_features, K = d.in_features;
+    const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
+    const int tile = std::max(tile_of(M, K, G), tile_of(N, K, G));
+    const gbmuf_linear_grad_io_t none{};
+    const gbmuf_linear_grad_io_t &at = io ? *io : none;
+    const bool dx = !io || io->dx.data, dw = !io || io->dw.data;
+    Source z = source_of(at.dy);
+    if (d.activation) { z.pre = at.pre.data; z.ldp = at.pre.ld; z.p_batch = at.pre.batch_stride; z.act = d.activation; }
+    Epilogue e = into(at.dw, grad_type);
+    if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = at.dw.data; e.ldr = at.dw.ld; e.r_batch = at.dw.batch_stride; }
+    DirectArgs px = direct_args(z, source_of(at.w), M, dx ? K : 0, N, G, tile, into(at.dx, type));
+    DirectArgs pw = direct_args(z, source_of(at.x), N, dw ? K : 0, M, G, tile, e);
+    px.partial = space.take<float>(cut_sum(px));
+    if (!io) return GBMUF_OK;
+    px.copy = at.dresidual.data; px.copy_ld = at.dresidual.ld; px.copy_batch = at.dresidual.batch_stride;
+    pw.sums = at.dbias.data; pw.sums_batch = at.dbias.batch_stride; pw.sums_type = grad_type; pw.accumulate = d.accumulate;
+    const int rc = launch_direct_backward(px, pw, type, tile, stream);
+    return rc != GBMUF_OK ? rc : join(px, stream);
+}
+
+int backward_laid(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
 {
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
     const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
@@ -301,6 +399,28 @@ int backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Spa
     return rc;
 }
 
+// dz goes along with dx and its column sums with dw: what is asked for without those takes the other way.
+int backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t &io, Space &space, hipStream_t stream)
+{
+    const bool sums = !io.dbias.data || (io.dw.data && d.in_features > 0), copy = !io.dresidual.data || (io.dx.data && d.in_features > 0);
+    return takes_direct_backward(d) && sums && copy ? backward_direct(d, &io, space, stream) : backward_laid(d, &io, space, stream);
+}
+
+int64_t forward_bytes(const gbmuf_linear_desc_t &d)
+{
+    Space space{nullptr};
+    (void)forward(d, nullptr, space, nullptr);
+    return space.used;
+}
+
+int64_t backward_bytes(const gbmuf_linear_desc_t &d)
+{
+    Space direct{nullptr}, laid{nullptr};
+    if (takes_direct_backward(d)) (void)backward_direct(d, nullptr, direct, nullptr);
+    (void)backward_laid(d, nullptr, laid, nullptr);
+    return std::max(direct.used, laid.used);
+}
+
 int check_workspace(const void *workspace, int64_t have, int64_t need)
 {
     if (need == 0) return GBMUF_OK;
@@ -320,10 +440,7 @@ int gbmuf_linear_workspace(const gbmuf_linear_desc_t *desc, int32_t backward_pas
     *bytes = 0;
     const int rc = check_desc(desc);
     if (rc != GBMUF_OK) return rc;
-    Space space{nullptr};
-    if (backward_pass) backward(*desc, nullptr, space, nullptr);
-    else forward(*desc, nullptr, space, nullptr);
-    *bytes = space.used;
+    *bytes = backward_pass ? backward_bytes(*desc) : forward_bytes(*desc);
     return GBMUF_OK;
 }
 
@@ -384,7 +501,7 @@ int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_gr
     if ((rc = check_workspace(workspace, workspace_bytes, need)) != GBMUF_OK) return rc;
     if ((rc = check_device()) != GBMUF_OK) return rc;
     Space space{static_cast<char *>(workspace)};
-    return backward(*desc, io, space, static_cast<hipStream_t>(stream));
+    return backward(*desc, *io, space, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

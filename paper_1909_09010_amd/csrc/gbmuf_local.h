@@ -35,6 +35,29 @@ struct ProductArgs {
     Epilogue e;
 };
 
+// A matrix as it lies, with the slope of an activation at `pre` as a factor of every value where act is one.
+struct Source {
+    const void *p, *pre;
+    int64_t ld, batch, ldp, p_batch;
+    int32_t act, reserved;
+};
+
+// out[g][m][n] = sum over k of a(m, k) * b(n, k) in f32 arithmetic, straight from where the matrices lie; the form of a kernel says whether k or
+// m (n) is what lies side by side.
+struct DirectArgs {
+    Source a, b;
+    int32_t M, N, K, batch;
+    int32_t tiles_m, tiles_n;
+    int32_t splits, steps;   // the sum over k goes to `splits` workgroups of `steps` steps of 32 each
+    float *partial;
+    Epilogue e;
+    void *copy;              // a itself (dz), of the matrices' type, or nullptr
+    int64_t copy_ld, copy_batch;
+    void *sums;              // sums[g][m] (+)= sum over k of a(m, k), or nullptr; splits == 1
+    int64_t sums_batch;
+    int32_t sums_type, accumulate;
+};
+
 // The sums of `splits` partial products, and what is done with them.
 struct JoinArgs {
     const float *partial;
@@ -70,7 +93,11 @@ struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
 // values of a packed row of n numbers, in 16-bit words: whole steps of 64
 constexpr int64_t packed_words(int64_t n, bool split) { return split ? (n + 31) / 32 * 64 : (n + 63) / 64 * 64; }
 
-int launch_product(const ProductArgs &a, int32_t type, hipStream_t stream);
+int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t stream);   // tile: 128 or 256
+int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream);
+constexpr int kFewRows = 64;
+int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream_t stream);
+int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream);
 int launch_join(const JoinArgs &a, hipStream_t stream);
 int launch_stats(const LayArgs &a, hipStream_t stream);
 int launch_lay(const LayArgs &a, hipStream_t stream);

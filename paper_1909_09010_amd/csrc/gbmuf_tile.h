@@ -1,0 +1,202 @@
+// gbmuf_tile.h -- how a tile of sums that 32 x 32 matrix instructions hold leaves a workgroup.
+#pragma once
+
+#include "gbmuf_values.h"
+
+namespace gbmuf {
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+struct Eight {
+    v4f v[2];
+};
+
+template <int T>
+__device__ __forceinline__ Eight read8(const void *p, int64_t i)
+{
+    if constexpr (T == kF32) return Eight{{read4<T>(p, i), read4<T>(p, i + 4)}};
+    typedef typename Num<T>::type N8 __attribute__((ext_vector_type(8), aligned(2)));
+    const N8 r = *reinterpret_cast<const N8 *>(static_cast<const typename Num<T>::type *>(p) + i);
+    Eight e;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) e.v[c >> 2][c & 3] = static_cast<float>(r[c]);
+    return e;
+}
+
+template <int T>
+__device__ __forceinline__ void write8(void *p, int64_t i, const Eight &e)
+{
+    using N = typename Num<T>::type;
+    if constexpr (T == kF32) {
+        write4<T>(p, i, e.v[0]);
+        write4<T>(p, i + 4, e.v[1]);
+    } else {
+        typedef N N8 __attribute__((ext_vector_type(8), aligned(2)));
+        N8 r;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) r[c] = static_cast<N>(e.v[c >> 2][c & 3]);
+        *reinterpret_cast<N8 *>(static_cast<N *>(p) + i) = r;
+    }
+}
+
+__device__ __forceinline__ Eight load_eight(const void *p, int64_t i, int32_t type)
+{
+    return type == kF32 ? read8<kF32>(p, i) : type == kBf16 ? read8<kBf16>(p, i) : read8<kF16>(p, i);
+}
+
+__device__ __forceinline__ void store_eight(void *p, int64_t i, int32_t type, const Eight &v)
+{
+    if (type == kF32) write8<kF32>(p, i, v);
+    else if (type == kBf16) write8<kBf16>(p, i, v);
+    else write8<kF16>(p, i, v);
+}
+
+__device__ __forceinline__ Eight activate8(Eight z, int32_t act)
+{
+    const auto all = [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z.v[c >> 2][c & 3] = f(z.v[c >> 2][c & 3]);
+    };
+    switch (act) {
+        case GBMUF_ACT_RELU: all([](float v) { return activate(v, GBMUF_ACT_RELU); }); break;
+        case GBMUF_ACT_GELU: all([](float v) { return activate(v, GBMUF_ACT_GELU); }); break;
+        case GBMUF_ACT_SILU: all([](float v) { return activate(v, GBMUF_ACT_SILU); }); break;
+        case GBMUF_ACT_SIGMOID: all([](float v) { return activate(v, GBMUF_ACT_SIGMOID); }); break;
+        case GBMUF_ACT_TANH: all([](float v) { return activate(v, GBMUF_ACT_TANH); }); break;
+        default: break;
+    }
+    return z;
+}
+
+// LDS that leave() needs: 32 rows of every wave's columns.
+template <int TM, int TN, int WM, int WN>
+constexpr size_t leave_bytes() { return static_cast<size_t>(WM) * WN * 32 * (TN / WN + 4) * sizeof(float); }
+
+// A tile of TM x TN by WM x WN waves leaves through LDS, so that a wave's loads and stores follow rows: 128 bytes of a row of 16-bit results
+// for 8 lanes.  Every wave turns its own part around, 32 rows at a time, in its own piece of LDS, whose accesses stay in order
+// without a wait: all waves have to be past what LDS held before, and meet no more.  A lane holds, of row lane % 32 of acc[i][j], the columns 8 (r / 4)
+// + 4 (lane / 32) + r % 4; afterwards 8 columns side by side, whose bias and scales it loads once.  (Tiles turned around by the
+// whole workgroup, row by row, cost 7 us where these cost 2: bf16, 256 x 256.)
+template <int TM, int TN, int WM, int WN, bool SPLIT, class Args>
+__device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Args &a, int split, int64_t g, int m0, int n0)
+{
+    constexpr int FM = TM / WM / 32, FN = TN / WN / 32, kColumns = TN / WN, kPitch = kColumns + 4, kLanes = kColumns / 8, kTogether = 64 / kLanes,
+                  kTurns = 32 / kTogether;
+    static_assert(FM == 1 || FM == 2 || FM == 4, "the cases below");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *out = static_cast<float *>(lds) + wave * 32 * kPitch;
+    const int column = lane % kLanes * 8, first = lane / kLanes, n = n0 + (wave / WM) * kColumns + column, left = a.N - n;
+    const int mw = m0 + (wave % WM) * (TM / WM) + first;
+    const bool parts = a.splits > 1;
+    const Epilogue &e = a.e;
+    const bool simple = parts || (!e.act && !e.place && !e.pre);
+    Eight bias{};
+    int scale[SPLIT ? 8 : 1];
+    if (left >= 8) {
+        if (e.bias && !parts) bias = load_eight(e.bias, g * e.bias_batch + n, e.type);
+        if constexpr (SPLIT)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) scale[c] = row_exponent(a.b_max[g * a.b_max_batch + n + c]);
+    }
+    const auto put = [&](const v16f (&rows)[FN]) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<v4f *>(out + (lane & 31) * kPitch + j * 32 + 8 * q + 4 * (lane >> 5)) =
+                    v4f{rows[j][4 * q], rows[j][4 * q + 1], rows[j][4 * q + 2], rows[j][4 * q + 3]};
+    };
+    const auto get = [&](int k) {
+        const float *from = out + (first + k * kTogether) * kPitch + column;
+        return Eight{{*reinterpret_cast<const v4f *>(from), *reinterpret_cast<const v4f *>(from + 4)}};
+    };
+    const auto scaled = [&](Eight z, uint32_t row_bits) {
+        if constexpr (SPLIT) {
+            const int em = row_exponent(row_bits);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z.v[c >> 2][c & 3] = ldexpf(z.v[c >> 2][c & 3], em + scale[c]);
+        }
+        z.v[0] += bias.v[0];
+        z.v[1] += bias.v[1];
+        return z;
+    };
+#pragma unroll 1
+    for (int i = 0; i < FM; ++i) {                         // one copy of what follows: only the registers that are put differ
+        const auto m_of = [&](int k) { return mw + i * 32 + k * kTogether; };
+        uint32_t top[SPLIT ? kTurns : 1];
+        if constexpr (SPLIT)
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) top[k] = a.a_max[g * a.a_max_batch + min(m_of(k), a.M - 1)];
+        if (i == 0) put(acc[0]);
+        if constexpr (FM > 1)
+            if (i == 1) put(acc[1]);
+        if constexpr (FM > 2) {
+            if (i == 2) put(acc[2]);
+            if (i == 3) put(acc[3]);
+        }
+        if (left >= 8 && simple) {
+            Eight z[kTurns];
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) z[k] = get(k);
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) {
+                z[k] = scaled(z[k], top[SPLIT ? k : 0]);
+                if (m_of(k) >= a.M) continue;
+                if (parts) write8<kF32>(a.partial, ((static_cast<int64_t>(split) * a.batch + g) * a.M + m_of(k)) * a.N + n, z[k]);
+                else store_eight(e.y, g * e.y_batch + m_of(k) * e.ldy + n, e.type, z[k]);
+            }
+        } else if (left >= 8) {
+            const auto fetch = [&](int k) { return load_eight(e.res, g * e.r_batch + min(m_of(k), a.M - 1) * e.ldr + n, e.type); };
+            Eight r{};
+            if (e.place) r = fetch(0);
+#pragma unroll 1
+            for (int k = 0; k < kTurns; ++k) {
+                uint32_t bits = top[0];
+                if constexpr (SPLIT)
+#pragma unroll
+                    for (int t = 1; t < kTurns; ++t) bits = k == t ? top[t] : bits;
+                Eight z = scaled(get(k), bits);
+                const int m = m_of(k);
+                const Eight now = r;
+                if (e.place && k + 1 < kTurns) r = fetch(k + 1);           // under this row's work
+                if (m >= a.M) continue;
+                if (e.place == GBMUF_RESIDUAL_BEFORE) {
+                    z.v[0] += now.v[0];
+                    z.v[1] += now.v[1];
+                }
+                if (e.pre) store_eight(e.pre, g * e.p_batch + m * e.ldp + n, e.type, z);
+                z = activate8(z, e.act);
+                if (e.place == GBMUF_RESIDUAL_AFTER) {
+                    z.v[0] += now.v[0];
+                    z.v[1] += now.v[1];
+                }
+                store_eight(e.y, g * e.y_batch + m * e.ldy + n, e.type, z);
+            }
+        } else if (left > 0) {                             // the last columns of a matrix: 4, and what is left
+#pragma unroll 1
+            for (int k = 0; k < kTurns * 2; ++k) {
+                const int m = m_of(k >> 1), c0 = (k & 1) * 4, rest = left - c0;
+                if (m >= a.M || rest <= 0) continue;
+                v4f v = *reinterpret_cast<const v4f *>(out + (first + (k >> 1) * kTogether) * kPitch + column + c0);
+                if constexpr (SPLIT) {
+                    const int em = row_exponent(a.a_max[g * a.a_max_batch + m]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < rest) v[c] = ldexpf(v[c], em + row_exponent(a.b_max[g * a.b_max_batch + n + c0 + c]));
+                }
+                if (parts) {
+                    float *to = a.partial + ((static_cast<int64_t>(split) * a.batch + g) * a.M + m) * a.N + n + c0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < rest) to[c] = v[c];
+                } else {
+                    finish(e, g, m, n + c0, rest, v);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+}  // namespace gbmuf

@@ -514,8 +514,6 @@ def test_matrices_that_are_refused():
     big = torch.zeros(4 * G * M * N)
     assert code_of(lambda: run(y=big[: G * M * N].view(G, M, N), x=big[10: 10 + G * M * K].view(G, M, K))) == B.GBMUF_EINVAL
     assert code_of(lambda: run(y=big[: G * M * N].view(G, M, N), residual=big[1: 1 + G * M * N].view(G, M, N))) == B.GBMUF_EINVAL
-    assert code_of(lambda: run(space=None)) == B.GBMUF_EINVAL
-    assert code_of(lambda: run(space=ws[:-256])) == B.GBMUF_EINVAL
     io = lin.forward_io(x, w, y, residual=r)
     io.x.ld = -5
     assert code_of(lambda: lin.forward(io, ws)) == B.GBMUF_EINVAL
@@ -557,9 +555,22 @@ def test_outputs_side_by_side_are_taken():
     assert code_of(lambda: lin.backward(io, back)) == B.GBMUF_EDEVICE
 
 
-def test_workspace_covers_what_is_laid_out():
+def test_workspace_that_is_missing_or_too_small_is_refused():
+    """Sizes that lay operands out.  The matrices are addresses that no check follows."""
+    if torch.cuda.is_available():
+        pytest.skip("addresses of no memory")
+    G, M, N, K = 1, 8192, 8192, 8192
+    at = lambda i: B.Matrix((i + 1) << 40, K, 0)
     for dtype, item in ((torch.float32, 4), (torch.bfloat16, 2)):
-        lin = B.Linear(200, 130, 650, 3, dtype)
-        assert lin.workspace_bytes() >= 3 * 330 * 650 * item
-        assert lin.workspace_bytes(True) >= 3 * (200 * 130 * 2 + 130 * 650 + 200 * 650) * item
+        lin = B.Linear(M, N, K, G, dtype)
+        need, back = lin.workspace_bytes(), lin.workspace_bytes(True)
+        assert need >= G * (M * K + N * K) * item and back >= G * (2 * M * N + N * K + M * K) * item
+        io = B.LinearIo(x=at(0), w=at(1), y=at(2))
+        grad = B.LinearGradIo(x=at(0), w=at(1), dy=at(2), dx=at(3), dw=at(4))
+        L, d = B.lib(), ctypes.byref(lin.desc)
+        for p, n in ((None, need), (1 << 50, need - 1), ((1 << 50) + 128, need)):
+            assert L.gbmuf_linear(d, ctypes.byref(io), p, n, None) == B.GBMUF_EINVAL
+            assert L.gbmuf_linear_backward(d, ctypes.byref(grad), p, n - need + back, None) == B.GBMUF_EINVAL
+        assert L.gbmuf_linear(d, ctypes.byref(io), 1 << 50, need, None) == B.GBMUF_EDEVICE
+        assert L.gbmuf_linear_backward(d, ctypes.byref(grad), 1 << 50, back, None) == B.GBMUF_EDEVICE
     assert B.Linear(0, 8, 8, 1).workspace_bytes() < 1 << 20
