@@ -1,5 +1,5 @@
-// gbmuf_layout.hip -- what products need laid out first: rows of 16-bit numbers along the axis that is summed over, whole steps
-// long, taken apart into two f16 numbers where the source is f32; and, in the backward, dz = dy * act'(z) and its column sums.
+// gbmuf_layout.hip -- what products need laid out first: f32 values taken apart into two f16 numbers, in rows along the axis that is summed over;
+// 16-bit matrices whose rows do not lie on 16 bytes; and, in the backward, dz = dy * act'(z) and its column sums.
 #include "gbmuf_values.h"
 
 namespace gbmuf {
@@ -7,50 +7,68 @@ namespace {
 
 constexpr int kT = kLayTile;
 
-__device__ __forceinline__ float value_at(const LayArgs &a, int64_t g, int r, int c)
+// Up to 8 values (r, c) .. of a source, zeros behind the row's end.
+template <int T>
+__device__ __forceinline__ Eight row_read(const void *p, int64_t at, int left)
 {
-    float v = load_one(a.src, g * a.batch_stride + r * a.ld + c, a.type);
-    if (a.act) v *= slope(load_one(a.pre, g * a.p_batch + r * a.ldp + c, a.type), a.act);
-    return v;
+    if (left >= 8) return read8<T>(p, at);
+    Eight e{};
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        if (c < left) e.v[c >> 2][c & 3] = load_one(p, at + c, T);
+    return e;
 }
 
-// Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  Magnitudes compare as integers, and a maximum does not depend on
-// the order of the atomics.
-__global__ __launch_bounds__(256) void stats_kernel(LayArgs a)
+template <int T>
+__device__ __forceinline__ void row_write(void *p, int64_t at, int left, const Eight &e)
 {
-    __shared__ float sums[4][kT];
-    __shared__ uint32_t top[4][kT];
-    const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
+    if (left >= 8) return write8<T>(p, at, e);
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        if (c < left) store_one(p, at + c, T, e.v[c >> 2][c & 3]);
+}
+
+// ---------------------------------------------------------------------------------------
+// 16-bit sources: rows at aligned places with zeros behind them, dz on the way, and its column sums.  A workgroup takes kT rows of
+// 256 columns, a thread 8 columns of every eighth row.  Bound by HBM: one reading (two with an activation) and one writing.
+// ---------------------------------------------------------------------------------------
+template <int T>
+__global__ __launch_bounds__(256) void copy_kernel(LayArgs a)
+{
+    __shared__ float sums[8][256];
+    const int width = a.plain ? static_cast<int>(a.plain_ld) : a.C;        // zeros up to the end of the copy's rows
+    const int tiles_c = (width + 255) / 256, tiles_r = (a.R + kT - 1) / kT;
     int id = static_cast<int>(blockIdx.x);
     const int64_t g = id / (tiles_c * tiles_r);
     id -= static_cast<int>(g) * tiles_c * tiles_r;
-    const int tr = id / tiles_c, r0 = tr * kT, c = id % tiles_c * kT + static_cast<int>(threadIdx.x & 63), wave = threadIdx.x >> 6;
-    float s = 0.0f;
-    uint32_t most = 0;
-    for (int i = 0; i < kT / 4; ++i) {
-        const int r = r0 + i * 4 + wave;
-        const float v = r < a.R && c < a.C ? value_at(a, g, r, c) : 0.0f;
-        s += v;
-        const uint32_t bits = __float_as_uint(v) & 0x7fffffffu;
-        most = max(most, bits);
-        if (a.row_max) {
-            uint32_t m = bits;
-            for (int d = 32; d; d >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
-            if ((threadIdx.x & 63) == 0 && r < a.R && m) atomicMax(a.row_max + g * a.R + r, m);
+    const int tr = id / tiles_c, c0 = id % tiles_c * 256, c = c0 + static_cast<int>(threadIdx.x & 31) * 8, left = a.C - c;
+    const int end = min((tr + 1) * kT, a.R);
+    Eight total{};
+    if (c < width)
+        for (int r = tr * kT + static_cast<int>(threadIdx.x >> 5); r < end; r += 8) {
+            Eight v = row_read<T>(a.src, g * a.batch_stride + r * a.ld + c, left);
+            if (a.act) v = slope8(v, row_read<T>(a.pre, g * a.p_batch + r * a.ldp + c, left), a.act);
+            total.v[0] += v.v[0];
+            total.v[1] += v.v[1];
+            if (a.dz) row_write<T>(a.dz, g * a.dz_batch + r * a.dz_ld + c, left, v);
+            if (a.plain) write8<T>(a.plain, g * a.plain_batch + r * a.plain_ld + c, v);
         }
-    }
-    sums[wave][threadIdx.x & 63] = s;
-    top[wave][threadIdx.x & 63] = most;
+    if (!a.col_sums) return;
+    float *mine = &sums[threadIdx.x >> 5][(threadIdx.x & 31) * 8];
+    *reinterpret_cast<v4f *>(mine) = total.v[0];
+    *reinterpret_cast<v4f *>(mine + 4) = total.v[1];
     __syncthreads();
-    if (wave != 0 || c >= a.C) return;
     const int t = threadIdx.x;
-    if (a.col_max) {
-        const uint32_t m = max(max(top[0][t], top[1][t]), max(top[2][t], top[3][t]));
-        if (m) atomicMax(a.col_max + g * a.C + c, m);
-    }
-    if (a.col_sums) a.col_sums[(g * tiles_r + tr) * a.C + c] = (sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]);
+    if (c0 + t >= a.C) return;
+    float s = sums[0][t];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += sums[i][t];
+    a.col_sums[(g * tiles_r + tr) * a.C + c0 + t] = s;
 }
 
+// ---------------------------------------------------------------------------------------
+// f32 sources, taken apart.
+// ---------------------------------------------------------------------------------------
 // The two f16 numbers of a value that its row's exponent has scaled.
 __device__ __forceinline__ void take_apart(float v, uint16_t &lead, uint16_t &trail)
 {
@@ -61,30 +79,116 @@ __device__ __forceinline__ void take_apart(float v, uint16_t &lead, uint16_t &tr
     trail = __builtin_bit_cast(uint16_t, l);
 }
 
-__device__ __forceinline__ uint16_t word_of(float v, int32_t type)
-{
-    return type == kBf16 ? __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)) : __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
-}
-
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-// One row's 8 values from `at` on, at place k of the packed row.
-template <class At>
-__device__ __forceinline__ void write8(uint16_t *row, int k, int32_t type, uint32_t max_bits, At at)
+// Eight values at place k of a packed row.
+__device__ __forceinline__ void write_apart(uint16_t *row, int k, int exponent, const Eight &v)
 {
     uint16_t w[8], t[8];
-    if (type == kF32) {
-        const int e = -row_exponent(max_bits);
-        for (int i = 0; i < 8; ++i) take_apart(ldexpf(at(i), e), w[i], t[i]);
-        uint16_t *to = row + (k >> 5) * 64 + (k & 31);
-        *reinterpret_cast<v4u *>(to) = __builtin_bit_cast(v4u, w);
-        *reinterpret_cast<v4u *>(to + 32) = __builtin_bit_cast(v4u, t);
-    } else {
-        for (int i = 0; i < 8; ++i) w[i] = word_of(at(i), type);
-        *reinterpret_cast<v4u *>(row + k) = __builtin_bit_cast(v4u, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) take_apart(ldexpf(v.v[i >> 2][i & 3], -exponent), w[i], t[i]);
+    uint16_t *to = row + (k >> 5) * 64 + (k & 31);
+    *reinterpret_cast<v4u *>(to) = __builtin_bit_cast(v4u, w);
+    *reinterpret_cast<v4u *>(to + 32) = __builtin_bit_cast(v4u, t);
+}
+
+__device__ __forceinline__ uint32_t magnitude(const Eight &v)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) m = max(m, __float_as_uint(v.v[c >> 2][c & 3]) & 0x7fffffffu);
+    return m;
+}
+
+// Rows of up to 512 N values, a wave each, which holds its row in registers: read once, its largest magnitude found, taken apart and written
+// once.
+template <int N>
+__global__ __launch_bounds__(256) void rows_kernel(LayArgs a)
+{
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= static_cast<int64_t>(a.R) * a.batch) return;
+    const int64_t g = row / a.R, r = row - g * a.R;
+    const int lane = threadIdx.x & 63, width = static_cast<int>(a.plain_ld / 2);
+    const int64_t from = g * a.batch_stride + r * a.ld;
+    Eight v[N];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 64 + lane) * 8;
+        v[i] = row_read<kF32>(a.src, from + c, a.C - c);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = max(most, magnitude(v[i]));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), d)));
+    if (lane == 0) a.row_max[g * a.R + r] = most;
+    uint16_t *to = a.plain + g * a.plain_batch + r * a.plain_ld;
+    const int e = row_exponent(most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = (i * 64 + lane) * 8;
+        if (c < width) write_apart(to, c, e, v[i]);
     }
 }
 
+// A tile of kT x kT values in LDS, from a workgroup of 256: 8 columns a thread.
+__device__ __forceinline__ void read_tile(const LayArgs &a, int64_t g, int r0, int c0, float (*tile)[kT + 1], bool copy)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 32 + static_cast<int>(threadIdx.x >> 3), c = static_cast<int>(threadIdx.x & 7) * 8;
+        const int left = r0 + r < a.R ? a.C - c0 - c : 0;
+        Eight v = row_read<kF32>(a.src, g * a.batch_stride + (r0 + r) * a.ld + c0 + c, left);
+        if (a.act) v = slope8(v, row_read<kF32>(a.pre, g * a.p_batch + (r0 + r) * a.ldp + c0 + c, left), a.act);
+        if (copy && a.dz) row_write<kF32>(a.dz, g * a.dz_batch + (r0 + r) * a.dz_ld + c0 + c, left, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tile[r][c + k] = v.v[k >> 2][k & 3];
+    }
+    __syncthreads();
+}
+
+// Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  Magnitudes compare as integers, and a maximum does not depend on
+// the order of the atomics.
+__global__ __launch_bounds__(256) void stats_kernel(LayArgs a)
+{
+    __shared__ float tile[kT][kT + 1];
+    const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
+    int id = static_cast<int>(blockIdx.x);
+    const int64_t g = id / (tiles_c * tiles_r);
+    id -= static_cast<int>(g) * tiles_c * tiles_r;
+    const int tr = id / tiles_c, r0 = tr * kT, c0 = id % tiles_c * kT;
+    read_tile(a, g, r0, c0, tile, false);
+    // four threads for a row (column): 16 values each
+    const int line = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
+    if (a.row_max) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(tile[line][part + i]) & 0x7fffffffu);
+        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
+        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
+        if (part == 0 && r0 + line < a.R && m) atomicMax(a.row_max + g * a.R + r0 + line, m);
+    }
+    if (a.col_max || a.col_sums) {
+        uint32_t m = 0;
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float v = tile[part + i][line];
+            m = max(m, __float_as_uint(v) & 0x7fffffffu);
+            s += v;
+        }
+        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
+        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
+        s += __shfl_xor(s, 1);
+        s += __shfl_xor(s, 2);
+        if (part == 0 && c0 + line < a.C) {
+            if (a.col_max && m) atomicMax(a.col_max + g * a.C + c0 + line, m);
+            if (a.col_sums) a.col_sums[(g * tiles_r + tr) * a.C + c0 + line] = s;
+        }
+    }
+}
+
+// The copies along rows and along columns from one reading.
 __global__ __launch_bounds__(256) void lay_kernel(LayArgs a)
 {
     __shared__ float tile[kT][kT + 1];
@@ -93,30 +197,26 @@ __global__ __launch_bounds__(256) void lay_kernel(LayArgs a)
     const int64_t g = id / (tiles_c * tiles_r);
     id -= static_cast<int>(g) * tiles_c * tiles_r;
     const int r0 = id / tiles_c * kT, c0 = id % tiles_c * kT;
-    for (int i = 0; i < kT / 4; ++i) {
-        const int r = i * 4 + static_cast<int>(threadIdx.x >> 6), c = threadIdx.x & 63;
-        float v = 0.0f;
-        if (r0 + r < a.R && c0 + c < a.C) {
-            v = value_at(a, g, r0 + r, c0 + c);
-            if (a.dz) store_one(a.dz, g * a.dz_batch + (r0 + r) * a.dz_ld + c0 + c, a.type, v);
-        }
-        tile[r][c] = v;
-    }
-    __syncthreads();
-    const int room = a.type == kF32 ? 32 : 64;             // packed rows are whole multiples of this many values
+    read_tile(a, g, r0, c0, tile, true);
     if (a.plain)
+#pragma unroll
         for (int j = threadIdx.x; j < kT * 8; j += 256) {
             const int r = j >> 3, c = (j & 7) * 8;
-            if (r0 + r >= a.R || c0 + c >= (a.C + room - 1) / room * room) continue;
-            write8(a.plain + g * a.plain_batch + static_cast<int64_t>(r0 + r) * a.plain_ld, c0 + c, a.type,
-                   a.row_max ? a.row_max[g * a.R + r0 + r] : 0u, [&](int i) { return tile[r][c + i]; });
+            if (r0 + r >= a.R || c0 + c >= static_cast<int>(a.plain_ld / 2)) continue;
+            Eight v;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v.v[k >> 2][k & 3] = tile[r][c + k];
+            write_apart(a.plain + g * a.plain_batch + static_cast<int64_t>(r0 + r) * a.plain_ld, c0 + c, row_exponent(a.row_max[g * a.R + r0 + r]), v);
         }
     if (a.trans)
+#pragma unroll
         for (int j = threadIdx.x; j < kT * 8; j += 256) {
-            const int c = j & 63, r = (j >> 6) * 8;
-            if (c0 + c >= a.C || r0 + r >= (a.R + room - 1) / room * room) continue;
-            write8(a.trans + g * a.trans_batch + static_cast<int64_t>(c0 + c) * a.trans_ld, r0 + r, a.type,
-                   a.col_max ? a.col_max[g * a.C + c0 + c] : 0u, [&](int i) { return tile[r + i][c]; });
+            const int c = j >> 3, r = (j & 7) * 8;         // 8 threads follow a packed row
+            if (c0 + c >= a.C || r0 + r >= static_cast<int>(a.trans_ld / 2)) continue;
+            Eight v;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v.v[k >> 2][k & 3] = tile[r + k][c];
+            write_apart(a.trans + g * a.trans_batch + static_cast<int64_t>(c0 + c) * a.trans_ld, r0 + r, row_exponent(a.col_max[g * a.C + c0 + c]), v);
         }
 }
 
@@ -157,6 +257,19 @@ int64_t lay_blocks(const LayArgs &a)
 
 int launch_stats(const LayArgs &a, hipStream_t stream) { return launch_256(stats_kernel, a, lay_blocks(a), "hipLaunchKernel(stats)", stream); }
 int launch_lay(const LayArgs &a, hipStream_t stream) { return launch_256(lay_kernel, a, lay_blocks(a), "hipLaunchKernel(lay out)", stream); }
+
+int launch_rows(const LayArgs &a, hipStream_t stream)
+{
+    const int64_t blocks = (static_cast<int64_t>(a.R) * a.batch + 3) / 4;
+    const auto fn = a.C <= 1024 ? rows_kernel<2> : a.C <= 2048 ? rows_kernel<4> : rows_kernel<8>;
+    return launch_256(fn, a, blocks, "hipLaunchKernel(rows)", stream);
+}
+
+int launch_copy(const LayArgs &a, hipStream_t stream)
+{
+    const int64_t width = a.plain ? a.plain_ld : a.C, blocks = (width + 255) / 256 * ((a.R + kT - 1) / kT) * a.batch;
+    return launch_256(a.type == kBf16 ? copy_kernel<kBf16> : copy_kernel<kF16>, a, blocks, "hipLaunchKernel(copy)", stream);
+}
 
 int launch_column_sums(const SumArgs &a, hipStream_t stream)
 {

@@ -112,6 +112,7 @@ struct Operand {
     uint32_t *max = nullptr;     // split
     int64_t max_batch = 0;
     bool whole = false;          // zeros follow up to the end of the last step
+    bool across = false;         // [k][row]
 };
 
 bool lies_well(const gbmuf_matrix_t &m)
@@ -129,7 +130,11 @@ struct Shape {
 Shape shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
 {
     Shape s{};
-    s.tile = (M + 255) / 256 * ((N + 255) / 256) * batch >= 256 ? 256 : 128;
+    // One workgroup of 256 x 256 or two of 128 x 128 a CU, whichever are done first: in rounds of the whole chip, a round of the first being 4
+    // tiles of 128 x 128, one of the second 2, which take 1.23 times as long each (8192 x 8192 x 8192 bf16: 886 and 1088 us).  Where rounds
+    // are few they decide, us for 256 / 128: 4 x 5120 x 1024 over 8192, 609 / 480; 16 x 5120 x 512 over 2048, 192 / 211.
+    const int64_t wide = (M + 255) / 256 * ((N + 255) / 256) * batch, small = (M + 127) / 128 * ((N + 127) / 128) * batch;
+    s.tile = 4.0 * static_cast<double>((wide + 255) / 256) <= 2.46 * static_cast<double>((small + 511) / 512) ? 256 : 128;
     s.tiles_m = static_cast<int32_t>((M + s.tile - 1) / s.tile);
     s.tiles_n = static_cast<int32_t>((N + s.tile - 1) / s.tile);
     const int64_t all = packed_words(K, split_type) / kStepWords, tiles = static_cast<int64_t>(s.tiles_m) * s.tiles_n * batch;
@@ -149,7 +154,8 @@ int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_
     p.a = a.p; p.b = b.p; p.lda = a.ld; p.ldb = b.ld; p.a_batch = a.batch; p.b_batch = b.batch;
     p.a_max = a.max; p.b_max = b.max; p.a_max_batch = a.max_batch; p.b_max_batch = b.max_batch;
     p.M = static_cast<int32_t>(M); p.N = static_cast<int32_t>(N);
-    p.K = static_cast<int32_t>(a.whole && b.whole ? packed_words(K, type == kF32) : K);
+    p.across = (a.across ? 1 : 0) | (b.across ? 2 : 0);
+    p.K = static_cast<int32_t>(a.whole && b.whole && !p.across ? packed_words(K, type == kF32) : K);
     p.batch = batch; p.tiles_m = s.tiles_m; p.tiles_n = s.tiles_n; p.splits = s.splits; p.steps = s.steps;
     p.partial = partial; p.e = e;
     int rc = launch_product(p, type, s.tile, stream);
@@ -281,22 +287,24 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     uint32_t *max = space.take<uint32_t>(split ? G * (M + N) : 0);
     const gbmuf_matrix_t &xm = io ? io->x : none, &wm = io ? io->w : none;
     const LayArgs lx = source(xm, M, K, G, type), lw = source(wm, N, K, G, type);
-    Operand x{static_cast<const uint16_t *>(xm.data), xm.ld, xm.batch_stride, nullptr, 0, false};
-    Operand w{static_cast<const uint16_t *>(wm.data), wm.ld, wm.batch_stride, nullptr, 0, false};
+    Operand x{static_cast<const uint16_t *>(xm.data), xm.ld, xm.batch_stride, nullptr, 0, false, false};
+    Operand w{static_cast<const uint16_t *>(wm.data), wm.ld, wm.batch_stride, nullptr, 0, false, false};
     const bool lay_x = split || !io || !lies_well(xm), lay_w = split || !io || !lies_well(wm);
     if (lay_x) x = packed(space, M, K, G, lx.batch, split, max);
     if (lay_w) w = packed(space, N, K, G, lw.batch, split, max + G * M);
     if (!io) return GBMUF_OK;
     int rc = GBMUF_OK;
-    if (split && (rc = launch_zero(max, G * (M + N), stream)) != GBMUF_OK) return rc;
+    if (split && !(K > 0 && K <= kLongestRow) && (rc = launch_zero(max, G * (M + N), stream)) != GBMUF_OK) return rc;
     for (int i = 0; i < 2; ++i) {
         if (!(i == 0 ? lay_x : lay_w)) continue;
         LayArgs l = i == 0 ? lx : lw;
         const Operand &o = i == 0 ? x : w;
         l.row_max = o.max;
-        if (split && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
         l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
-        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+        if (!split) rc = launch_copy(l, stream);
+        else if (K > 0 && K <= kLongestRow) rc = launch_rows(l, stream);
+        else if ((rc = launch_stats(l, stream)) == GBMUF_OK) rc = launch_lay(l, stream);
+        if (rc != GBMUF_OK) return rc;
     }
     return run_product(x, w, M, N, K, G, type, e, s, partial, stream);
 }
@@ -326,77 +334,120 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
     return rc != GBMUF_OK ? rc : join(px, stream);
 }
 
-int backward_laid(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+// dw's epilogue
+Epilogue weight_grad(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &m, int32_t type)
+{
+    Epilogue e = into(m, type);
+    if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = m.data; e.ldr = m.ld; e.r_batch = m.batch_stride; }
+    return e;
+}
+
+int sum_columns(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &out, const float *sums, int32_t type, hipStream_t stream)
+{
+    SumArgs a{};
+    a.sums = sums; a.out = out.data; a.out_batch = out.batch_stride;
+    a.C = static_cast<int32_t>(d.out_features); a.tiles = static_cast<int32_t>((d.rows + kLayTile - 1) / kLayTile);
+    a.batch = d.batch; a.type = type; a.accumulate = d.accumulate;
+    return launch_column_sums(a, stream);
+}
+
+// f32: dz, w and x are taken apart, along the axis of each product.
+int backward_split(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
 {
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
-    const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
-    const bool split = type == kF32;
-    const bool dx = !io || io->dx.data, dw = !io || io->dw.data, db = !io || io->dbias.data, dr = io && io->dresidual.data;
-    const Shape sx = shape_of(M, K, N, G, split), sw = shape_of(N, K, M, G, split);
-    const int64_t row_tiles = (M + kLayTile - 1) / kLayTile;
+    const int32_t G = d.batch;
+    const gbmuf_linear_grad_io_t none{};
+    const gbmuf_linear_grad_io_t &at = io ? *io : none;
+    const bool dx = !io || at.dx.data, dw = !io || at.dw.data, db = !io || at.dbias.data, dr = at.dresidual.data;
+    const Shape sx = shape_of(M, K, N, G, true), sw = shape_of(N, K, M, G, true);
     float *partial = space.take<float>(std::max(dx ? sx.partial : 0, dw ? sw.partial : 0));     // one product after the other
-    float *sums = space.take<float>(db ? G * row_tiles * N : 0);
-    // largest magnitudes: rows and columns of dz, columns of w and of x
-    const int64_t n_max = split ? G * (M + N + 2 * K) : 0;
+    float *sums = space.take<float>(db ? G * ((M + kLayTile - 1) / kLayTile) * N : 0);
+    const int64_t n_max = G * (M + N + 2 * K);             // largest magnitudes: rows and columns of dz, columns of w and of x
     uint32_t *max = space.take<uint32_t>(n_max);
-    const gbmuf_matrix_t none{};
-    const gbmuf_matrix_t &dym = io ? io->dy : none, &wm = io ? io->w : none, &xm = io ? io->x : none;
 
     // dz is a matrix for each worker even where dy is shared, since z may not be
-    LayArgs lz = source(dym, M, N, G, type);
-    if (d.activation) {
-        lz.batch = G;
-        if (io) { lz.pre = io->pre.data; lz.ldp = io->pre.ld; lz.p_batch = io->pre.batch_stride; }
-        lz.act = d.activation;
-    }
-    lz.batch = dr || db ? G : lz.batch;
-    const LayArgs lw = source(wm, N, K, G, type), lx = source(xm, M, K, G, type);
-    const bool plain = dx && (split || d.activation || !io || !lies_well(dym));
-    Operand z{static_cast<const uint16_t *>(dym.data), dym.ld, dym.batch_stride, nullptr, 0, false}, zt, wt, xt;
-    if (plain) z = packed(space, M, N, G, lz.batch, split, max);
-    if (dw) zt = packed(space, N, M, G, lz.batch, split, max + G * M);
-    if (dx) wt = packed(space, K, N, G, lw.batch, split, max + G * (M + N));
-    if (dw) xt = packed(space, K, M, G, lx.batch, split, max + G * (M + N + K));
+    LayArgs lz = source(at.dy, M, N, G, kF32);
+    if (d.activation) { lz.pre = at.pre.data; lz.ldp = at.pre.ld; lz.p_batch = at.pre.batch_stride; lz.act = d.activation; }
+    if (d.activation || dr || db) lz.batch = G;
+    const LayArgs lw = source(at.w, N, K, G, kF32), lx = source(at.x, M, K, G, kF32);
+    Operand z, zt, wt, xt;
+    if (dx) z = packed(space, M, N, G, lz.batch, true, max);
+    if (dw) zt = packed(space, N, M, G, lz.batch, true, max + G * M);
+    if (dx) wt = packed(space, K, N, G, lw.batch, true, max + G * (M + N));
+    if (dw) xt = packed(space, K, M, G, lx.batch, true, max + G * (M + N + K));
     if (!io) return GBMUF_OK;
 
-    int rc = GBMUF_OK;
-    if (split && (rc = launch_zero(max, n_max, stream)) != GBMUF_OK) return rc;
-    if (split || db) {
-        LayArgs l = lz;
-        l.row_max = split && dx ? z.max : nullptr;
-        l.col_max = split && dw ? zt.max : nullptr;
-        l.col_sums = db ? sums : nullptr;
-        if ((l.row_max || l.col_max || l.col_sums) && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
-    }
-    if (db) {
-        SumArgs a{};
-        a.sums = sums; a.out = io->dbias.data; a.out_batch = io->dbias.batch_stride;
-        a.C = static_cast<int32_t>(N); a.tiles = static_cast<int32_t>(row_tiles); a.batch = G; a.type = grad_type; a.accumulate = d.accumulate;
-        if ((rc = launch_column_sums(a, stream)) != GBMUF_OK) return rc;
-    }
-    if (plain || dw || dr) {
-        LayArgs l = lz;
-        if (plain) { l.plain = const_cast<uint16_t *>(z.p); l.plain_ld = z.ld; l.plain_batch = z.batch; l.row_max = z.max; }
-        if (dw) { l.trans = const_cast<uint16_t *>(zt.p); l.trans_ld = zt.ld; l.trans_batch = zt.batch; l.col_max = zt.max; }
-        if (dr) { l.dz = io->dresidual.data; l.dz_ld = io->dresidual.ld; l.dz_batch = io->dresidual.batch_stride; }
-        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
-    }
+    int rc = launch_zero(max, n_max, stream);
+    if (rc != GBMUF_OK) return rc;
+    lz.row_max = dx ? z.max : nullptr;
+    lz.col_max = dw ? zt.max : nullptr;
+    lz.col_sums = db ? sums : nullptr;
+    if ((dx || dw || db) && (rc = launch_stats(lz, stream)) != GBMUF_OK) return rc;
+    if (db && (rc = sum_columns(d, at.dbias, sums, kF32, stream)) != GBMUF_OK) return rc;
+    if (dx) { lz.plain = const_cast<uint16_t *>(z.p); lz.plain_ld = z.ld; lz.plain_batch = z.batch; }
+    if (dw) { lz.trans = const_cast<uint16_t *>(zt.p); lz.trans_ld = zt.ld; lz.trans_batch = zt.batch; }
+    lz.dz = at.dresidual.data; lz.dz_ld = at.dresidual.ld; lz.dz_batch = at.dresidual.batch_stride;
+    if ((dx || dw || dr) && (rc = launch_lay(lz, stream)) != GBMUF_OK) return rc;
     for (int i = 0; i < 2; ++i) {
         if (!(i == 0 ? dx : dw)) continue;
         LayArgs l = i == 0 ? lw : lx;
         const Operand &o = i == 0 ? wt : xt;
         l.col_max = o.max;
-        if (split && (rc = launch_stats(l, stream)) != GBMUF_OK) return rc;
         l.trans = const_cast<uint16_t *>(o.p); l.trans_ld = o.ld; l.trans_batch = o.batch;
-        if ((rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+        if ((rc = launch_stats(l, stream)) != GBMUF_OK || (rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
     }
-    if (dx && (rc = run_product(z, wt, M, K, N, G, type, into(io->dx, type), sx, partial, stream)) != GBMUF_OK) return rc;
-    if (dw) {
-        Epilogue e = into(io->dw, grad_type);
-        if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = io->dw.data; e.ldr = io->dw.ld; e.r_batch = io->dw.batch_stride; }
-        rc = run_product(zt, xt, N, K, M, G, type, e, sw, partial, stream);
-    }
+    if (dx && (rc = run_product(z, wt, M, K, N, G, kF32, into(at.dx, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
+    return dw ? run_product(zt, xt, N, K, M, G, kF32, weight_grad(d, at.dw, kF32), sw, partial, stream) : rc;
+}
+
+// bf16, f16: the products read w, x and dz across their rows where they need to, so that matrices whose rows lie on 16 bytes are taken as
+// they are and the others copied to places that do.
+int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+{
+    const int64_t M = d.rows, N = d.out_features, K = d.in_features;
+    const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
+    const gbmuf_linear_grad_io_t none{};
+    const gbmuf_linear_grad_io_t &at = io ? *io : none;
+    const bool dx = !io || at.dx.data, dw = !io || at.dw.data, db = !io || at.dbias.data, dr = at.dresidual.data;
+    const Shape sx = shape_of(M, K, N, G, false), sw = shape_of(N, K, M, G, false);
+    float *partial = space.take<float>(std::max(dx ? sx.partial : 0, dw ? sw.partial : 0));
+    float *sums = space.take<float>(db ? G * ((M + kLayTile - 1) / kLayTile) * N : 0);
+
+    LayArgs lz = source(at.dy, M, N, G, type);
+    if (d.activation) { lz.pre = at.pre.data; lz.ldp = at.pre.ld; lz.p_batch = at.pre.batch_stride; lz.act = d.activation; }
+    if (d.activation || dr || db) lz.batch = G;            // a matrix for each worker even where dy is shared
+    const LayArgs lw = source(at.w, N, K, G, type), lx = source(at.x, M, K, G, type);
+    const auto as_it_lies = [&](const gbmuf_matrix_t &m, int64_t cols) { return io && lies_well(m) && cols % 8 == 0; };
+    const auto take = [&](const gbmuf_matrix_t &m, const LayArgs &l, bool copy) {
+        if (copy) return packed(space, l.R, l.C, G, l.batch, false, nullptr);
+        return Operand{static_cast<const uint16_t *>(m.data), m.ld, m.batch_stride, nullptr, 0, false, false};
+    };
+    const bool copy_z = (dx || dw) && (d.activation || !as_it_lies(at.dy, N)), copy_w = dx && !as_it_lies(at.w, K), copy_x = dw && !as_it_lies(at.x, K);
+    const Operand z = take(at.dy, lz, copy_z);
+    Operand w = take(at.w, lw, copy_w), x = take(at.x, lx, copy_x), zt = z;
+    zt.across = w.across = x.across = true;
+    if (!io) return GBMUF_OK;
+
+    const auto copy = [&](LayArgs l, const Operand &o) {
+        l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
+        return launch_copy(l, stream);
+    };
+    int rc = GBMUF_OK;
+    lz.col_sums = db ? sums : nullptr;
+    lz.dz = at.dresidual.data; lz.dz_ld = at.dresidual.ld; lz.dz_batch = at.dresidual.batch_stride;
+    if (copy_z) rc = copy(lz, z);
+    else if (db || dr) rc = launch_copy(lz, stream);
+    if (rc == GBMUF_OK && db) rc = sum_columns(d, at.dbias, sums, grad_type, stream);
+    if (rc == GBMUF_OK && copy_w) rc = copy(lw, w);
+    if (rc == GBMUF_OK && copy_x) rc = copy(lx, x);
+    if (rc == GBMUF_OK && dx) rc = run_product(z, w, M, K, N, G, type, into(at.dx, type), sx, partial, stream);
+    if (rc == GBMUF_OK && dw) rc = run_product(zt, x, N, K, M, G, type, weight_grad(d, at.dw, grad_type), sw, partial, stream);
     return rc;
+}
+
+int backward_laid(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
+{
+    return d.dtype == GBMUF_F32 ? backward_split(d, io, space, stream) : backward_16(d, io, space, stream);
 }
 
 // dz goes along with dx and its column sums with dw: what is asked for without those takes the other way.

@@ -30,7 +30,7 @@ struct ProductArgs {
     int32_t M, N, K, batch;
     int32_t tiles_m, tiles_n;
     int32_t splits, steps;   // the sum over k goes to `splits` workgroups of `steps` steps of 64 each
-    int32_t reserved;
+    int32_t across;          // 16-bit types: bit 0, 1: a (b) is [k][m] ([k][n]) with rows lda (ldb) apart, whole pieces of 8 columns
     float *partial;          // splits > 1: [split][g][m][n]
     Epilogue e;
 };
@@ -67,21 +67,22 @@ struct JoinArgs {
 };
 
 // A source matrix R x C of `type`, with the slope of the activation at `pre` as a factor where there is one, and what is written of it.
+// launch_copy: 16-bit types, plain, dz and col_sums.  launch_rows: f32 of up to kLongestRow columns, plain and row_max from one reading.
+// launch_stats and launch_lay: f32, row_max, col_max and col_sums from a first reading, plain, trans and dz from a second.
 struct LayArgs {
     const void *src, *pre;
     int64_t ld, batch_stride, ldp, p_batch;
     int32_t R, C, batch;
     int32_t type, act;       // act: GBMUF_ACT_NONE = no factor
-    // statistics (launch_stats): any of them nullptr
-    uint32_t *row_max, *col_max;          // [batch][R], [batch][C]: bits of the largest magnitude, zeroed before
+    // any of these nullptr
+    uint32_t *row_max, *col_max;          // [batch][R], [batch][C]: bits of the largest magnitude, zeroed before launch_stats
     float *col_sums;                      // [batch][row tiles][C]
-    // copies (launch_lay): any of them nullptr
-    uint16_t *plain, *trans;              // rows of R (C) values along C (R), 16-bit or split
+    uint16_t *plain, *trans;              // rows of R (C) values along C (R), in 16 bits or taken apart; their whole length is written
     int64_t plain_ld, plain_batch, trans_ld, trans_batch;
     void *dz;                             // the product with the slope itself, of `type`
     int64_t dz_ld, dz_batch;
 };
-constexpr int kLayTile = 64;
+constexpr int kLayTile = 64, kLongestRow = 4096;
 
 struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
     const float *sums;
@@ -99,6 +100,8 @@ constexpr int kFewRows = 64;
 int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream_t stream);
 int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream);
 int launch_join(const JoinArgs &a, hipStream_t stream);
+int launch_copy(const LayArgs &a, hipStream_t stream);
+int launch_rows(const LayArgs &a, hipStream_t stream);
 int launch_stats(const LayArgs &a, hipStream_t stream);
 int launch_lay(const LayArgs &a, hipStream_t stream);
 int launch_column_sums(const SumArgs &a, hipStream_t stream);

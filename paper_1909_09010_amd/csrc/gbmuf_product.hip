@@ -1,6 +1,8 @@
 // gbmuf_product.hip -- matrix products on gfx950's matrix cores for the local half: out = a b' over 16-bit numbers.
 #include "gbmuf_tile.h"
 
+#include <type_traits>
+
 namespace gbmuf {
 namespace {
 
@@ -71,23 +73,80 @@ __device__ __forceinline__ v4u chunk_of(const uint16_t *lds, int row, int chunk)
     return *reinterpret_cast<const v4u *>(lds + row * kStep + ((chunk ^ ((row >> 1) & 7)) * 8));
 }
 
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+// The same for an operand whose k lie across its rows: a step is 64 rows of R columns, the 16-byte chunk c of row k at place c ^ ((k & 3) << 2), so
+// that 4 rows of 32 columns lie in all banks.  The transposing load hands 16 lanes the 4 x 16 values that their addresses cover, a column of 4 k each.
+template <int R, int THREADS>
+struct StageAcross {
+    static constexpr int kChunks = R / 8, kPass = THREADS / kChunks, kPasses = kStep / kPass;
+    static_assert(kPass % 4 == 0, "every pass places its chunks alike");
+    const uint16_t *row[kPasses];
+    int64_t ld;
+
+    __device__ __forceinline__ static int row_of() { return static_cast<int>(threadIdx.x) / kChunks; }
+
+    // columns behind the last whole piece are read as that piece: their results are dropped
+    __device__ __forceinline__ void init(const uint16_t *base, int64_t stride, int first, int count)
+    {
+        ld = stride;
+        const int c = first + ((static_cast<int>(threadIdx.x) % kChunks) ^ ((row_of() & 3) << 2)) * 8;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) row[i] = base + static_cast<int64_t>(i * kPass + row_of()) * stride + min(c, (count - 1) / 8 * 8);
+    }
+
+    __device__ __forceinline__ void load(uint16_t *lds, int k0) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            uint16_t *to = lds + (i * THREADS + static_cast<int>(threadIdx.x >> 6) * 64) * 8;
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)(row[i] + k0 * ld),
+                                             (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+        }
+    }
+
+    __device__ __forceinline__ void load_rest(uint16_t *lds, int k0, int K) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            v4u v = {0u, 0u, 0u, 0u};
+            if (k0 + i * kPass + row_of() < K) v = *reinterpret_cast<const v4u *>(row[i] + k0 * ld);
+            *reinterpret_cast<v4u *>(lds + (i * THREADS + static_cast<int>(threadIdx.x)) * 8) = v;
+        }
+    }
+};
+
+// 8 k of column `first` + lane % 32, from k = 8 (2 turn + lane / 32) on
+template <int R>
+__device__ __forceinline__ v4u column_of(const uint16_t *lds, int first, int turn)
+{
+    const int lane = threadIdx.x & 63, p = lane & 15, k = turn * 16 + (lane >> 5) * 8 + (p >> 2), c = first + ((lane >> 4) & 1) * 16 + (p & 3) * 4;
+    const auto at = [&](int row) {
+        return __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(
+                                                lds + row * R + (((c >> 3) ^ ((row & 3) << 2)) << 3) + (c & 4))));
+    };
+    const uint64_t lo = at(k), hi = at(k + 4);
+    return v4u{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+}
+
 // What a wave needs of a step for one turn of matrix instructions: 16 of the 64 words of its rows (SPLIT: 16 leading and the 16
-// trailing parts).
-template <int T, bool SPLIT, int FM, int FN>
+// trailing parts).  m and n: the wave's first row of a and of b.
+template <int T, bool SPLIT, int TM, int TN, int FM, int FN, int ACROSS>
 struct Turn {
     static constexpr int kParts = SPLIT ? 2 : 1;
     v4u x[kParts][FM], w[kParts][FN];
 
-    __device__ __forceinline__ void load(const uint16_t *la, const uint16_t *lb, int turn)
+    __device__ __forceinline__ void load(const uint16_t *lds, int m, int n, int turn)
     {
         const int lane = threadIdx.x & 63;
+        const uint16_t *la = lds, *lb = lds + TM * kStep;
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
             const int c = p * 4 + turn * 2 + (lane >> 5);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) w[p][j] = chunk_of(lb, j * 32 + (lane & 31), c);
+            for (int j = 0; j < FN; ++j) w[p][j] = ACROSS & 2 ? column_of<TN>(lb, n + j * 32, turn) : chunk_of(lb, n + j * 32 + (lane & 31), c);
 #pragma unroll
-            for (int i = 0; i < FM; ++i) x[p][i] = chunk_of(la, i * 32 + (lane & 31), c);
+            for (int i = 0; i < FM; ++i) x[p][i] = ACROSS & 1 ? column_of<TM>(la, m + i * 32, turn) : chunk_of(la, m + i * 32 + (lane & 31), c);
         }
     }
 
@@ -102,6 +161,18 @@ struct Turn {
     }
 };
 
+// Spreads READS loads of LDS evenly between MFMAS matrix instructions.
+template <int READS, int MFMAS, int I = 0>
+__device__ __forceinline__ void interleave()
+{
+    if constexpr (I < MFMAS) {
+        constexpr int n = (I + 1) * READS / MFMAS - I * READS / MFMAS;
+        if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        interleave<READS, MFMAS, I + 1>();
+    }
+}
+
 __device__ __forceinline__ void wait_and_meet()
 {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -112,7 +183,7 @@ __device__ __forceinline__ void wait_and_meet()
 // One tile of TM x TN, WM x WN waves.  Two stages in LDS: while one is multiplied the next step arrives in the other.  A wave
 // loads a turn's operands while it multiplies the turn before, and the waves meet before the last turn of a step, whose operands they then
 // all hold: the next step's first turn is loaded, and the step after it sent for, under that last turn.
-template <int T, bool SPLIT, int TM, int TN, int WM, int WN>
+template <int T, bool SPLIT, int TM, int TN, int WM, int WN, int ACROSS>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 {
     constexpr int THREADS = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kTurns = SPLIT ? 2 : 4;
@@ -134,8 +205,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 
     const int all = (a.K + kStep - 1) / kStep, first = split * a.steps, last = min(first + a.steps, all);
     const int full = min(last, a.K / kStep);               // steps [first, full) are whole
-    Stage<TM, THREADS> sa;
-    Stage<TN, THREADS> sb;
+    std::conditional_t<(ACROSS & 1) != 0, StageAcross<TM, THREADS>, Stage<TM, THREADS>> sa;
+    std::conditional_t<(ACROSS & 2) != 0, StageAcross<TN, THREADS>, Stage<TN, THREADS>> sb;
     sa.init(a.a + g * a.a_batch, a.lda, m0, a.M);
     sb.init(a.b + g * a.b_batch, a.ldb, n0, a.N);
 
@@ -148,7 +219,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    Turn<T, SPLIT, FM, FN> turn[2];
+    constexpr int kReads = (SPLIT ? 2 : 1) * (FM * (ACROSS & 1 ? 2 : 1) + FN * (ACROSS & 2 ? 2 : 1)), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
+    Turn<T, SPLIT, TM, TN, FM, FN, ACROSS> turn[2];
     if (first < full) {
         sa.load(lds[0], first * kStep);
         sb.load(lds[0] + TM * kStep, first * kStep);
@@ -157,21 +229,25 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
             sa.load(lds[1], (first + 1) * kStep);
             sb.load(lds[1] + TM * kStep, (first + 1) * kStep);
         }
-        turn[0].load(lds[0] + wm * kStep, lds[0] + (TM + wn) * kStep, 0);
+        turn[0].load(lds[0], wm, wn, 0);
         for (int s = first; s < full; ++s) {
             uint16_t *now = lds[(s - first) & 1], *next = lds[(s - first + 1) & 1];
 #pragma unroll
             for (int t = 0; t + 1 < kTurns; ++t) {
-                turn[(t + 1) & 1].load(now + wm * kStep, now + (TM + wn) * kStep, t + 1);
+                turn[(t + 1) & 1].load(now, wm, wn, t + 1);
                 turn[t & 1].multiply(acc);
+                interleave<kReads, kMfmas>();
+                __builtin_amdgcn_sched_barrier(0);
             }
             wait_and_meet();
             if (s + 2 < full) {
                 sa.load(now, (s + 2) * kStep);
                 sb.load(now + TM * kStep, (s + 2) * kStep);
             }
-            if (s + 1 < full) turn[0].load(next + wm * kStep, next + (TM + wn) * kStep, 0);
+            if (s + 1 < full) turn[0].load(next, wm, wn, 0);
             turn[(kTurns - 1) & 1].multiply(acc);
+            interleave<kReads, kMfmas>();
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (full < last) {                                     // at most one step; nothing is in flight, the waves may be in the last turn
@@ -181,7 +257,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
-            turn[0].load(lds[0] + wm * kStep, lds[0] + (TM + wn) * kStep, t);
+            turn[0].load(lds[0], wm, wn, t);
             turn[0].multiply(acc);
         }
     }
@@ -218,10 +294,16 @@ int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t str
     ProductArgs args = a;
     void *argv[] = {&args};
     using Fn = void (*)(ProductArgs);
-    static constexpr Fn fns[3][2] = {{product_kernel<kF16, true, 128, 128, 2, 2>, product_kernel<kF16, true, 256, 256, 2, 4>},
-                                     {product_kernel<kBf16, false, 128, 128, 2, 2>, product_kernel<kBf16, false, 256, 256, 2, 4>},
-                                     {product_kernel<kF16, false, 128, 128, 2, 2>, product_kernel<kF16, false, 256, 256, 2, 4>}};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][tile == 256]), dim3(static_cast<unsigned>(blocks)),
+    static constexpr Fn split[2] = {product_kernel<kF16, true, 128, 128, 2, 2, 0>, product_kernel<kF16, true, 256, 256, 2, 4, 0>};
+    static constexpr Fn plain[2][3][2] = {
+        {{product_kernel<kBf16, false, 128, 128, 2, 2, 0>, product_kernel<kBf16, false, 256, 256, 2, 4, 0>},
+         {product_kernel<kBf16, false, 128, 128, 2, 2, 2>, product_kernel<kBf16, false, 256, 256, 2, 4, 2>},
+         {product_kernel<kBf16, false, 128, 128, 2, 2, 3>, product_kernel<kBf16, false, 256, 256, 2, 4, 3>}},
+        {{product_kernel<kF16, false, 128, 128, 2, 2, 0>, product_kernel<kF16, false, 256, 256, 2, 4, 0>},
+         {product_kernel<kF16, false, 128, 128, 2, 2, 2>, product_kernel<kF16, false, 256, 256, 2, 4, 2>},
+         {product_kernel<kF16, false, 128, 128, 2, 2, 3>, product_kernel<kF16, false, 256, 256, 2, 4, 3>}}};
+    const Fn fn = type == kF32 ? split[tile == 256] : plain[type == kF16][a.across == 0 ? 0 : a.across - 1][tile == 256];
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)),
                                            dim3(tile == 256 ? 512 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(product)", err, GBMUF_EDEVICE);
 }

@@ -125,6 +125,85 @@ __device__ __forceinline__ void finish(const Epilogue &e, int64_t g, int64_t m, 
     store(e.y, g * e.y_batch + m * e.ldy + n, z);
 }
 
+struct Eight {
+    v4f v[2];
+};
+
+template <int T>
+__device__ __forceinline__ Eight read8(const void *p, int64_t i)
+{
+    if constexpr (T == kF32) return Eight{{read4<T>(p, i), read4<T>(p, i + 4)}};
+    typedef typename Num<T>::type N8 __attribute__((ext_vector_type(8), aligned(2)));
+    const N8 r = *reinterpret_cast<const N8 *>(static_cast<const typename Num<T>::type *>(p) + i);
+    Eight e;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) e.v[c >> 2][c & 3] = static_cast<float>(r[c]);
+    return e;
+}
+
+template <int T>
+__device__ __forceinline__ void write8(void *p, int64_t i, const Eight &e)
+{
+    using N = typename Num<T>::type;
+    if constexpr (T == kF32) {
+        write4<T>(p, i, e.v[0]);
+        write4<T>(p, i + 4, e.v[1]);
+    } else {
+        typedef N N8 __attribute__((ext_vector_type(8), aligned(2)));
+        N8 r;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) r[c] = static_cast<N>(e.v[c >> 2][c & 3]);
+        *reinterpret_cast<N8 *>(static_cast<N *>(p) + i) = r;
+    }
+}
+
+__device__ __forceinline__ Eight load_eight(const void *p, int64_t i, int32_t type)
+{
+    return type == kF32 ? read8<kF32>(p, i) : type == kBf16 ? read8<kBf16>(p, i) : read8<kF16>(p, i);
+}
+
+__device__ __forceinline__ void store_eight(void *p, int64_t i, int32_t type, const Eight &v)
+{
+    if (type == kF32) write8<kF32>(p, i, v);
+    else if (type == kBf16) write8<kBf16>(p, i, v);
+    else write8<kF16>(p, i, v);
+}
+
+__device__ __forceinline__ Eight activate8(Eight z, int32_t act)
+{
+    const auto all = [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z.v[c >> 2][c & 3] = f(z.v[c >> 2][c & 3]);
+    };
+    switch (act) {
+        case GBMUF_ACT_RELU: all([](float v) { return activate(v, GBMUF_ACT_RELU); }); break;
+        case GBMUF_ACT_GELU: all([](float v) { return activate(v, GBMUF_ACT_GELU); }); break;
+        case GBMUF_ACT_SILU: all([](float v) { return activate(v, GBMUF_ACT_SILU); }); break;
+        case GBMUF_ACT_SIGMOID: all([](float v) { return activate(v, GBMUF_ACT_SIGMOID); }); break;
+        case GBMUF_ACT_TANH: all([](float v) { return activate(v, GBMUF_ACT_TANH); }); break;
+        default: break;
+    }
+    return z;
+}
+
+// v times the slope at z
+__device__ __forceinline__ Eight slope8(Eight v, const Eight &z, int32_t act)
+{
+    const auto all = [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v.v[c >> 2][c & 3] *= f(z.v[c >> 2][c & 3]);
+    };
+    switch (act) {
+        case GBMUF_ACT_RELU: all([](float t) { return slope(t, GBMUF_ACT_RELU); }); break;
+        case GBMUF_ACT_GELU: all([](float t) { return slope(t, GBMUF_ACT_GELU); }); break;
+        case GBMUF_ACT_SILU: all([](float t) { return slope(t, GBMUF_ACT_SILU); }); break;
+        case GBMUF_ACT_SIGMOID: all([](float t) { return slope(t, GBMUF_ACT_SIGMOID); }); break;
+        case GBMUF_ACT_TANH: all([](float t) { return slope(t, GBMUF_ACT_TANH); }); break;
+        default: break;
+    }
+    return v;
+}
+
 // The exponent of a scaled row of a split matrix: values are taken times 2^-row_exponent, the largest lies in [2^14, 2^15)
 // then.  bits: of the largest magnitude (infinity and NaN count as the largest finite exponent).
 __device__ __forceinline__ int row_exponent(uint32_t bits)

@@ -279,6 +279,10 @@ def test_f32_rows_of_very_different_sizes():
 
 
 # -- backward -------------------------------------------------------------------------------------
+def matmul64(a, b):
+    return torch.matmul(a, b)
+
+
 def backward_case(G, M, N, K, dtype, act, residual, f32_grads=False, accumulate=False, seed=0, place=None, want=("dx", "dw", "dbias")):
     g = torch.Generator().manual_seed(100 + seed)
     x, w = make((G, M, K), dtype, g), make((G, N, K), dtype, g, max(K, 1) ** -0.5)
@@ -308,15 +312,15 @@ def backward_case(G, M, N, K, dtype, act, residual, f32_grads=False, accumulate=
     r = bz + (h * dz.abs() + 2.0 ** -25 if dtype != torch.float32 else 0 * bz)       # as the products take it
     if "dx" in want:
         WT = W.transpose(1, 2)
-        want_v, S = torch.matmul(dz, W), torch.matmul(dz.abs(), W.abs())
-        b = sum_bound(N, S, dtype, spread(dz, WT)) + torch.matmul(r, W.abs())
-        rms = 2.0 ** -21 * S + torch.matmul(r.square(), W.square()).sqrt()
+        want_v, S = matmul64(dz, W), matmul64(dz.abs(), W.abs())
+        b = sum_bound(N, S, dtype, spread(dz, WT)) + matmul64(r, W.abs())
+        rms = 2.0 ** -21 * S + matmul64(r.square(), W.square()).sqrt()
         check(outs["dx"], want_v, b + h * (want_v.abs() + b) + 2.0 ** -25, rms + h * want_v.abs() + 2.0 ** -25, "dx")
     if "dw" in want:
         DT, XT = dz.transpose(1, 2), X.transpose(1, 2)
-        want_v, S = torch.matmul(DT, X), torch.matmul(DT.abs(), X.abs())
-        b = sum_bound(M, S, dtype, spread(DT, XT)) + torch.matmul(r.transpose(1, 2), X.abs())
-        rms = 2.0 ** -21 * S + torch.matmul(r.transpose(1, 2).square(), X.square()).sqrt()
+        want_v, S = matmul64(DT, X), matmul64(DT.abs(), X.abs())
+        b = sum_bound(M, S, dtype, spread(DT, XT)) + matmul64(r.transpose(1, 2), X.abs())
+        rms = 2.0 ** -21 * S + matmul64(r.transpose(1, 2).square(), X.square()).sqrt()
         if accumulate:
             want_v = want_v + old_w.double()
             b, rms = b + U * want_v.abs(), rms + U * want_v.abs()
@@ -431,6 +435,50 @@ def test_gradient_against_differences(act):
         move = (yu - yd).double().abs().max().item() / (2 * h)          # the largest |d y| along v
         tol = h * h / 6 * 3 * (c.double().abs().sum().item()) * max(move, 1.0) ** 3 * 0.05 + 2.0 ** -20 * (c.abs() * yu.abs()).double().sum().item() / h * 0.05
         assert abs(got - want) <= tol + 1e-3 * abs(want), (i, got, want, tol)
+
+
+# -- sizes that take the larger tiles, operands laid out, split sums ---------------------------------
+LARGE = [(16, 1030, 1031, 1029), (16, 1024, 1040, 1032), (2, 4100, 2056, 136), (1, 2049, 4104, 3001), (1, 200, 6000, 2500), (3, 300, 128, 9000),
+         (1, 70, 3000, 10240), (16, 1024, 776, 1016), (16, 1021, 775, 1013)]
+
+
+def product64(a, b):
+    """a b' for every worker, in 64 bits on the GPU."""
+    return torch.stack([(x.to(DEV) @ y.to(DEV).T.contiguous()).cpu() for x, y in zip(a, b)])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", LARGE)
+@pytest.mark.parametrize("kind", [(B.ACT_NONE, B.RESIDUAL_NONE), (B.ACT_GELU, B.RESIDUAL_AFTER)])
+def test_forward_large(size, dtype, kind, monkeypatch):
+    monkeypatch.setitem(globals(), "mm", product64)
+    forward_case(*size, dtype, kind[0], kind[1], True, kind[0] != 0, seed=7)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", LARGE)
+@pytest.mark.parametrize("act", [B.ACT_NONE, B.ACT_TANH])
+def test_backward_large(size, dtype, act, monkeypatch):
+    monkeypatch.setitem(globals(), "matmul64", lambda a, b: product64(a, b.transpose(1, 2)))
+    backward_case(*size, dtype, act, B.RESIDUAL_BEFORE, f32_grads=act == 0, accumulate=act == 0, seed=7,
+                  want=("dx", "dw", "dbias") + (("dresidual",) if act else ()))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_placements_and_each_output_alone(dtype, monkeypatch):
+    monkeypatch.setitem(globals(), "mm", product64)
+    monkeypatch.setitem(globals(), "matmul64", lambda a, b: product64(a, b.transpose(1, 2)))
+    G, M, N, K = 4, 1100, 1030, 520
+    aligned = {"x": columns_of(528, 8), "y": columns_of(1048, 0), "w": in_rows(8, N * K + 16), "dy": columns_of(1048, 16), "dx": columns_of(533, 1)}
+    odd = {"x": columns_of(531, 3), "y": columns_of(1037, 1), "w": in_rows(5, N * K + 7), "dy": tokens_first, "dx": tokens_first, "dw": in_rows(3, N * K + 9)}
+    for place in (aligned, odd):
+        forward_case(G, M, N, K, dtype, B.ACT_SILU, B.RESIDUAL_BEFORE, True, True, place=place)
+        backward_case(G, M, N, K, dtype, B.ACT_NONE, B.RESIDUAL_BEFORE, place=place, want=("dx", "dw", "dbias", "dresidual"))
+    for want in (("dx",), ("dw",), ("dbias",), ("dresidual",)):
+        backward_case(G, M, N, K, dtype, B.ACT_RELU, B.RESIDUAL_BEFORE, want=want)
 
 
 # -- streams, graphs, equal bits ------------------------------------------------------------------
