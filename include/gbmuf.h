@@ -421,7 +421,7 @@ typedef struct gbmuf_linear_io {
  *              is done; NULL if that is 0.  Calls that share one must be in order.
  * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,
  * pointers that are not aligned to their type, outputs that overlap inputs or each other, a workspace that is too small),
- * EUNSUPPORTED (a size above 2^31 - 1, batch above 65535), EDEVICE.
+ * EUNSUPPORTED (sizes near 2^30 and above, batch above 65535, a matrix of all workers with 2^21 tiles of 128 x 128 or more), EDEVICE.
  */
 int gbmuf_linear_workspace(const gbmuf_linear_desc_t *desc, int32_t backward, int64_t *bytes);
 int gbmuf_linear(const gbmuf_linear_desc_t *desc, const gbmuf_linear_io_t *io, void *workspace, int64_t workspace_bytes,

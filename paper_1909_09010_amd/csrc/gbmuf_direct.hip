@@ -114,13 +114,9 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
     constexpr int F = TILE / 64;
     using A = Stage<T, A_ALONG_K, TILE, SLOPE>;
     using B = Stage<T, B_ALONG_K, TILE>;
-    const int per = a.tiles_m * a.tiles_n;
-    const int split = id / (per * a.batch);
-    id -= split * per * a.batch;
-    const int64_t g = id / per;
-    id -= static_cast<int>(g) * per;
-    const int tm = id % a.tiles_m, tn = id / a.tiles_m, m0 = tm * TILE, n0 = tn * TILE;
-    const int all = (a.K + kDepth - 1) / kDepth, first = split * a.steps, last = min(first + a.steps, all);
+    const Share share = share_of<TILE, TILE>(a.t, id, (a.K + kDepth - 1) / kDepth);
+    const int64_t g = share.at.g;
+    const int tn = share.at.tn, m0 = share.at.tm * TILE, n0 = tn * TILE, first = share.first, last = share.last;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = (wave & 1) * (TILE / 2), wn = (wave >> 1) * (TILE / 2);
     float *la = lds, *lb = lds + A::kFloats;
     v16f acc[F][F];
@@ -134,8 +130,8 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
     A x;
     B w;
     if (first < last) {
-        x.load(a.a, g, m0, first * kDepth, a.M, a.K);
-        w.load(a.b, g, n0, first * kDepth, a.N, a.K);
+        x.load(a.a, g, m0, first * kDepth, a.t.M, a.K);
+        w.load(a.b, g, n0, first * kDepth, a.t.N, a.K);
     }
     for (int s = first; s < last; ++s) {
         x.shape(a.a);
@@ -145,7 +141,7 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
 #pragma unroll
             for (int i = 0; i < A::kChunks; ++i) {
                 const int m = m0 + A::major(i), k = s * kDepth + A::minor(i);
-                if (m >= a.M) continue;
+                if (m >= a.t.M) continue;
                 const int64_t at = g * a.copy_batch + m * a.copy_ld + k;
                 if (k + 4 <= a.K) write4<T>(a.copy, at, x.v[i]);
                 else
@@ -157,8 +153,8 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
             for (int i = 0; i < A::kChunks; ++i) sums += x.v[i];      // a thread's rows are the same in every chunk
         __syncthreads();
         if (s + 1 < last) {
-            x.load(a.a, g, m0, (s + 1) * kDepth, a.M, a.K);
-            w.load(a.b, g, n0, (s + 1) * kDepth, a.N, a.K);
+            x.load(a.a, g, m0, (s + 1) * kDepth, a.t.M, a.K);
+            w.load(a.b, g, n0, (s + 1) * kDepth, a.t.N, a.K);
         }
 #pragma unroll
         for (int t = 0; t < kDepth / 8; ++t) {
@@ -185,7 +181,7 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
 #pragma unroll
             for (int i = 0; i < groups; ++i) v += lds[i * TILE + threadIdx.x];
             const int m = m0 + static_cast<int>(threadIdx.x);
-            if (m < a.M) {
+            if (m < a.t.M) {
                 const int64_t at = g * a.sums_batch + m;
                 if (a.accumulate) v += load_one(a.sums, at, a.sums_type);
                 store_one(a.sums, at, a.sums_type, v);
@@ -193,7 +189,7 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         }
         __syncthreads();
     }
-    leave<TILE, TILE, 2, 2, false>(acc, lds, a, split, g, m0, n0);
+    leave<TILE, TILE, 2, 2, false>(acc, lds, a, share);
 }
 
 template <int T, int TILE>
@@ -209,20 +205,17 @@ __global__ __launch_bounds__(kThreads) void direct_backward_kernel(DirectArgs dx
 {
     __shared__ __align__(16) float lds[direct_lds<T, false, false, TILE>() / 4];
     static_assert(direct_lds<T, false, false, TILE>() >= direct_lds<T, true, false, TILE>(), "one piece of LDS for both");
-    const int n = dx.tiles_m * dx.tiles_n * dx.batch * dx.splits, id = static_cast<int>(blockIdx.x);
+    const int n = dx.t.blocks(), id = static_cast<int>(blockIdx.x);
     if (id < n) direct_tile<T, true, false, TILE, true>(dx, id, lds);
     else direct_tile<T, false, false, TILE, true>(dw, id - n, lds);
 }
-
-int64_t blocks_of(const DirectArgs &a) { return static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.batch * a.splits; }
 
 }  // namespace
 
 int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream_t stream)
 {
-    const int64_t blocks = blocks_of(a);
+    const int32_t blocks = a.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / kThreads) return GBMUF_EUNSUPPORTED;
     using Fn = void (*)(DirectArgs);
     static constexpr Fn fns[3][2] = {{direct_forward_kernel<kF32, 64>, direct_forward_kernel<kF32, 128>},
                                      {direct_forward_kernel<kBf16, 64>, direct_forward_kernel<kBf16, 128>},
@@ -236,9 +229,8 @@ int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream
 
 int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream)
 {
-    const int64_t blocks = blocks_of(dx) + blocks_of(dw);
+    const int32_t blocks = dx.t.blocks() + dw.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / kThreads) return GBMUF_EUNSUPPORTED;
     using Fn = void (*)(DirectArgs, DirectArgs);
     static constexpr Fn fns[3][2] = {{direct_backward_kernel<kF32, 64>, direct_backward_kernel<kF32, 128>},
                                      {direct_backward_kernel<kBf16, 64>, direct_backward_kernel<kBf16, 128>},

@@ -53,9 +53,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(DirectArgs a)
     constexpr size_t kBytes = sizeof(typename Num<T>::type);
     const char *xs[MT], *ws[NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) xs[i] = static_cast<const char *>(a.a.p) + (g * a.a.batch + min(i * 16 + (lane & 15), a.M - 1) * a.a.ld) * kBytes;
+    for (int i = 0; i < MT; ++i) xs[i] = static_cast<const char *>(a.a.p) + (g * a.a.batch + min(i * 16 + (lane & 15), a.t.M - 1) * a.a.ld) * kBytes;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) ws[j] = static_cast<const char *>(a.b.p) + (g * a.b.batch + min(n0 + j * 16 + (lane & 15), a.N - 1) * a.b.ld) * kBytes;
+    for (int j = 0; j < NT; ++j) ws[j] = static_cast<const char *>(a.b.p) + (g * a.b.batch + min(n0 + j * 16 + (lane & 15), a.t.N - 1) * a.b.ld) * kBytes;
     v4f acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -97,11 +97,11 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(DirectArgs a)
     __syncthreads();
     for (int at = threadIdx.x; at < MT * 16 * NT * 4; at += 64 * WAVES) {
         const int m = at / (NT * 4), n = at % (NT * 4) * 4;
-        if (m >= a.M || n0 + n >= a.N) continue;
+        if (m >= a.t.M || n0 + n >= a.t.N) continue;
         v4f s = *reinterpret_cast<const v4f *>(&part[0][m * kPitch + n]);
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const v4f *>(&part[v][m * kPitch + n]);
-        finish(a.e, g, m, n0 + n, a.N - n0 - n, s);
+        finish(a.e, g, m, n0 + n, a.t.N - n0 - n, s);
     }
 }
 
@@ -117,15 +117,15 @@ void (*pick(int mt, bool wide, bool many))(DirectArgs)
 
 int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream)
 {
-    if (a.M <= 0 || a.N <= 0 || a.batch <= 0) return GBMUF_OK;
-    const int mt = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
-    const int64_t narrow = (a.N + 15) / 16;
-    const bool wide = narrow * a.batch >= 2048, many = !wide && narrow * a.batch < 256 && a.K >= 1024;
-    const int64_t blocks = wide ? (a.N + 31) / 32 : narrow;
+    if (a.t.M <= 0 || a.t.N <= 0 || a.t.batch <= 0) return GBMUF_OK;
+    const int mt = a.t.M <= 16 ? 1 : a.t.M <= 32 ? 2 : 4;
+    const int64_t narrow = (a.t.N + 15) / 16;
+    const bool wide = narrow * a.t.batch >= 2048, many = !wide && narrow * a.t.batch < 256 && a.K >= 1024;
+    const int64_t blocks = wide ? (a.t.N + 31) / 32 : narrow;
     const auto fn = type == kF32 ? pick<kF32>(mt, wide, many) : type == kBf16 ? pick<kBf16>(mt, wide, many) : pick<kF16>(mt, wide, many);
     DirectArgs args = a;
     void *argv[] = {&args};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.batch)),
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.t.batch)),
                                            dim3(many ? 1024 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(few rows)", err, GBMUF_EDEVICE);
 }

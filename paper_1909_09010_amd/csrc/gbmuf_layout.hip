@@ -220,13 +220,21 @@ __global__ __launch_bounds__(256) void lay_kernel(LayArgs a)
         }
 }
 
+// 64 columns a workgroup, whose four waves take every fourth tile's sums.
 __global__ __launch_bounds__(256) void column_sums_kernel(SumArgs a)
 {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= static_cast<int64_t>(a.C) * a.batch) return;
-    const int64_t g = i / a.C, c = i - g * a.C;
+    __shared__ float part[4][64];
+    const int blocks = (a.C + 63) / 64, wave = threadIdx.x >> 6, c = static_cast<int>(blockIdx.x) % blocks * 64 + static_cast<int>(threadIdx.x & 63);
+    const int64_t g = blockIdx.x / blocks;
+    const float *from = a.sums + g * a.tiles * a.C + min(c, a.C - 1);
     float s = 0.0f;
-    for (int t = 0; t < a.tiles; ++t) s += a.sums[(g * a.tiles + t) * a.C + c];
+#pragma unroll 8
+    for (int t = wave; t < a.tiles; t += 4) s += from[static_cast<int64_t>(t) * a.C];
+    part[wave][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (wave != 0 || c >= a.C) return;
+    const int i = threadIdx.x;
+    s = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
     if (a.accumulate) s += load_one(a.out, g * a.out_batch + c, a.type);
     store_one(a.out, g * a.out_batch + c, a.type, s);
 }
@@ -273,7 +281,7 @@ int launch_copy(const LayArgs &a, hipStream_t stream)
 
 int launch_column_sums(const SumArgs &a, hipStream_t stream)
 {
-    return launch_256(column_sums_kernel, a, (static_cast<int64_t>(a.C) * a.batch + 255) / 256, "hipLaunchKernel(column sums)", stream);
+    return launch_256(column_sums_kernel, a, static_cast<int64_t>((a.C + 63) / 64) * a.batch, "hipLaunchKernel(column sums)", stream);
 }
 
 int launch_zero(uint32_t *p, int64_t words, hipStream_t stream)

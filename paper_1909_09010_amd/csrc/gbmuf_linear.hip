@@ -10,8 +10,8 @@ namespace gbmuf {
 namespace {
 
 constexpr int64_t kLargest = 0x7fffffff;
+constexpr double kMostTiles = 1 << 21;       // of 128 x 128 results or operands: four of 64 x 64 each are what a grid of 256 threads holds
 constexpr int64_t kStepWords = 64;
-constexpr double kForwardDirect = 2e10, kBackwardDirect = 2e10, kBackwardDirect16 = 2e9;
 
 // ---------------------------------------------------------------------------------------
 // Checks
@@ -72,13 +72,20 @@ bool valid_output(const gbmuf_matrix_t &m, const Extent &e, int32_t type)
     return rows_apart && (matrices_apart || inside);
 }
 
+bool too_many_tiles(int64_t rows, int64_t cols, int64_t batch)
+{
+    return static_cast<double>((rows + 127) / 128) * static_cast<double>((cols + 127) / 128) * static_cast<double>(batch) >= kMostTiles;
+}
+
 int check_desc(const gbmuf_linear_desc_t *d)
 {
     if (!d || d->struct_size < sizeof(gbmuf_linear_desc_t)) return GBMUF_EINVAL;
     if (d->dtype < GBMUF_F32 || d->dtype > GBMUF_F16 || d->activation < GBMUF_ACT_NONE || d->activation > GBMUF_ACT_TANH) return GBMUF_EINVAL;
     if (d->residual < GBMUF_RESIDUAL_NONE || d->residual > GBMUF_RESIDUAL_AFTER) return GBMUF_EINVAL;
     if (d->batch < 0 || d->rows < 0 || d->out_features < 0 || d->in_features < 0) return GBMUF_EINVAL;
-    if (d->batch > 65535 || d->rows > kLargest || d->out_features > kLargest || d->in_features > kLargest / 2 - 64) return GBMUF_EUNSUPPORTED;
+    if (d->batch > 65535 || d->rows > kLargest / 2 - 64 || d->out_features > kLargest / 2 - 64 || d->in_features > kLargest / 2 - 64) return GBMUF_EUNSUPPORTED;
+    const int64_t M = d->rows, N = d->out_features, K = d->in_features;
+    if (too_many_tiles(M, N, d->batch) || too_many_tiles(M, K, d->batch) || too_many_tiles(N, K, d->batch)) return GBMUF_EUNSUPPORTED;
     return GBMUF_OK;
 }
 
@@ -120,49 +127,62 @@ bool lies_well(const gbmuf_matrix_t &m)
     return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && m.ld % 8 == 0 && m.batch_stride % 8 == 0;
 }
 
-// What one product needs besides its operands.
-struct Shape {
-    int tile;
-    int32_t tiles_m, tiles_n, splits, steps;
-    int64_t partial;             // floats
+// How a product's tiles go to workgroups: rounds of `slots` workgroups work at a time, and where the last one is far from full, the sums of its
+// tiles are cut so that it is, in parts of 8 steps at least.  round: time of a step of a full round.
+struct Cut {
+    int tile = 0;
+    Tiles t{};
+    int64_t partial = 0;         // floats
+    double cost = 0.0;
 };
 
-Shape shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
+Cut cut(int tile, int64_t M, int64_t N, int64_t batch, int64_t steps, int64_t slots, double round)
 {
-    Shape s{};
-    // One workgroup of 256 x 256 or two of 128 x 128 a CU, whichever are done first: in rounds of the whole chip, a round of the first being 4
-    // tiles of 128 x 128, one of the second 2, which take 1.23 times as long each (8192 x 8192 x 8192 bf16: 886 and 1088 us).  Where rounds
-    // are few they decide, us for 256 / 128: 4 x 5120 x 1024 over 8192, 609 / 480; 16 x 5120 x 512 over 2048, 192 / 211.
-    const int64_t wide = (M + 255) / 256 * ((N + 255) / 256) * batch, small = (M + 127) / 128 * ((N + 127) / 128) * batch;
-    s.tile = 4.0 * static_cast<double>((wide + 255) / 256) <= 2.46 * static_cast<double>((small + 511) / 512) ? 256 : 128;
-    s.tiles_m = static_cast<int32_t>((M + s.tile - 1) / s.tile);
-    s.tiles_n = static_cast<int32_t>((N + s.tile - 1) / s.tile);
-    const int64_t all = packed_words(K, split_type) / kStepWords, tiles = static_cast<int64_t>(s.tiles_m) * s.tiles_n * batch;
-    // few tiles: the sum over k is cut so that two workgroups a CU have work, in parts of 8 steps at least
-    int64_t splits = tiles > 0 && tiles < 256 ? std::min<int64_t>(512 / tiles, all / 8) : 1;
-    splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
-    s.steps = static_cast<int32_t>(std::max<int64_t>(1, (all + splits - 1) / splits));
-    s.splits = static_cast<int32_t>(std::max<int64_t>(1, (all + s.steps - 1) / s.steps));
-    s.partial = s.splits > 1 ? static_cast<int64_t>(s.splits) * batch * M * N : 0;
-    return s;
+    Cut c;
+    c.tile = tile;
+    c.t.M = static_cast<int32_t>(M); c.t.N = static_cast<int32_t>(N); c.t.batch = static_cast<int32_t>(batch);
+    c.t.tiles_m = static_cast<int32_t>((M + tile - 1) / tile);
+    c.t.tiles_n = static_cast<int32_t>((N + tile - 1) / tile);
+    const int64_t tiles = static_cast<int64_t>(c.t.tiles_m) * c.t.tiles_n * batch, rest = tiles % slots;
+    c.t.whole = static_cast<int32_t>(tiles);
+    c.t.splits = 1;
+    c.t.steps = static_cast<int32_t>(std::max<int64_t>(steps, 1));
+    c.cost = static_cast<double>((tiles + slots - 1) / slots * steps) * round;
+    const int64_t most = rest > 0 ? std::min<int64_t>({slots / rest, steps / 8, 64}) : 1;
+    if (most < 2) return c;
+    const int64_t each = (steps + most - 1) / most, splits = (steps + each - 1) / each, partial = rest * splits * tile * tile;
+    // another launch, and writing and reading the parts at 4 TB/s
+    const double cost = static_cast<double>(tiles / slots * steps + each) * round + 5.0 + static_cast<double>(partial) * 8.0 / 4e6;
+    if (cost >= c.cost) return c;
+    c.t.whole = static_cast<int32_t>(tiles - rest);
+    c.t.splits = static_cast<int32_t>(splits);
+    c.t.steps = static_cast<int32_t>(each);
+    c.partial = partial;
+    c.cost = cost;
+    return c;
 }
 
-int run_product(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, int32_t batch, int32_t type, const Epilogue &e,
-                const Shape &s, float *partial, hipStream_t stream)
+// Tiles of 256 x 256, one a CU, or of 128 x 128, two a CU.  us for a step of a round: 8192 x 8192 x 8192 bf16 take 886 us in 4 rounds of 128
+// steps, and 1088 us in 8.
+Cut shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
+{
+    const int64_t steps = packed_words(K, split_type) / kStepWords;
+    const Cut wide = cut(256, M, N, batch, steps, 256, 1.73), small = cut(128, M, N, batch, steps, 512, 1.06);
+    return wide.cost <= small.cost ? wide : small;
+}
+
+int run_product(const Operand &a, const Operand &b, int64_t K, int32_t type, const Epilogue &e, const Cut &c, float *partial, hipStream_t stream)
 {
     ProductArgs p{};
     p.a = a.p; p.b = b.p; p.lda = a.ld; p.ldb = b.ld; p.a_batch = a.batch; p.b_batch = b.batch;
     p.a_max = a.max; p.b_max = b.max; p.a_max_batch = a.max_batch; p.b_max_batch = b.max_batch;
-    p.M = static_cast<int32_t>(M); p.N = static_cast<int32_t>(N);
     p.across = (a.across ? 1 : 0) | (b.across ? 2 : 0);
     p.K = static_cast<int32_t>(a.whole && b.whole && !p.across ? packed_words(K, type == kF32) : K);
-    p.batch = batch; p.tiles_m = s.tiles_m; p.tiles_n = s.tiles_n; p.splits = s.splits; p.steps = s.steps;
-    p.partial = partial; p.e = e;
-    int rc = launch_product(p, type, s.tile, stream);
-    if (rc != GBMUF_OK || s.splits <= 1) return rc;
-    JoinArgs j{};
-    j.partial = partial; j.M = M; j.N = N; j.batch = batch; j.splits = s.splits; j.e = e;
-    return launch_join(j, stream);
+    p.t = c.t;
+    p.t.partial = partial;
+    p.e = e;
+    const int rc = launch_product(p, type, c.tile, stream);
+    return rc != GBMUF_OK ? rc : launch_join(JoinArgs{p.t, c.tile, 0, e}, stream);
 }
 
 LayArgs source(const gbmuf_matrix_t &m, int64_t R, int64_t C, int32_t batch, int32_t type)
@@ -205,37 +225,21 @@ Source source_of(const gbmuf_matrix_t &m)
     return s;
 }
 
-DirectArgs direct_args(const Source &a, const Source &b, int64_t M, int64_t N, int64_t K, int32_t batch, int tile, const Epilogue &e)
+DirectArgs direct_args(const Source &a, const Source &b, int64_t K, const Cut &c, const Epilogue &e)
 {
     DirectArgs d{};
     d.a = a; d.b = b;
-    d.M = static_cast<int32_t>(M); d.N = static_cast<int32_t>(N); d.K = static_cast<int32_t>(K); d.batch = batch;
-    d.tiles_m = static_cast<int32_t>((M + tile - 1) / tile);
-    d.tiles_n = static_cast<int32_t>((N + tile - 1) / tile);
-    d.splits = 1;
-    d.steps = static_cast<int32_t>((K + 31) / 32);
+    d.K = static_cast<int32_t>(K);
+    d.t = c.t;
     d.e = e;
     return d;
 }
 
-// Cuts the sum over k where there are fewer tiles than CUs, in parts of 8 steps at least.  Returns the floats of partial sums.
-int64_t cut_sum(DirectArgs &d)
+// Tiles of 128 x 128 where there is one for every CU, else of 64 x 64, whose sums are cut (where `may_cut`) until there are two for every CU.  A step of a 64 x 64 tile takes 0.8 us or so, waits included.
+Cut direct_cut(int tile, int64_t M, int64_t N, int64_t K, int64_t batch, bool may_cut)
 {
-    const int64_t tiles = static_cast<int64_t>(d.tiles_m) * d.tiles_n * d.batch;
-    int64_t splits = tiles > 0 && tiles < 256 ? std::min<int64_t>(512 / tiles, d.steps / 8) : 1;
-    splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
-    const int64_t steps = std::max<int64_t>(1, (d.steps + splits - 1) / splits);
-    d.splits = static_cast<int32_t>(std::max<int64_t>(1, (d.steps + steps - 1) / steps));
-    d.steps = static_cast<int32_t>(steps);
-    return d.splits > 1 ? static_cast<int64_t>(d.splits) * d.batch * d.M * d.N : 0;
-}
-
-int join(const DirectArgs &d, hipStream_t stream)
-{
-    if (d.splits <= 1) return GBMUF_OK;
-    JoinArgs j{};
-    j.partial = d.partial; j.M = d.M; j.N = d.N; j.batch = d.batch; j.splits = d.splits; j.e = d.e;
-    return launch_join(j, stream);
+    const int64_t steps = (K + 31) / 32, tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile) * batch;
+    return cut(tile, M, N, batch, steps, may_cut && tiles < 256 ? 512 : std::max<int64_t>(tiles, 1), 0.8);
 }
 
 int tile_of(int64_t M, int64_t N, int64_t batch)
@@ -243,18 +247,21 @@ int tile_of(int64_t M, int64_t N, int64_t batch)
     return (M + 127) / 128 * ((N + 127) / 128) * batch >= 256 ? 128 : 64;
 }
 
-// Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions.
-bool takes_direct_forward(const gbmuf_linear_desc_t &d)
+// Operations of one product.
+double operations(const gbmuf_linear_desc_t &d)
 {
-    const double work = 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
-    return d.dtype == GBMUF_F32 && work <= kForwardDirect;
+    return 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
 }
 
-bool takes_direct_backward(const gbmuf_linear_desc_t &d)
-{
-    const double work = 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
-    return work <= (d.dtype == GBMUF_F32 ? kBackwardDirect : kBackwardDirect16);
-}
+// Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions, which costs launches and
+// passes over them.  us, as they lie / laid out, workers x rows x out x in:
+//   forward f32: 1 x 200 x 1024 x 512 13 / 22, 4 x 200 x 1024 x 512 18 / 28, 8 x 128 x 2600 x 650 51 / 55, 4 x 512 x 1024 x 1024 48 / 47,
+//     16 x 512 x 1024 x 512 84 / 54
+//   gradients f32: 1 x 200 x 1024 x 512 21 / 54, 4 x 200 x 1024 x 512 42 / 63, 8 x 128 x 2600 x 650 153 / 138, 4 x 512 x 1024 x 1024 129 / 92
+//   gradients bf16: 1 x 200 x 1024 x 512 23 / 36, 4 x 200 x 1024 x 512 47 / 38
+bool takes_direct_forward(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && operations(d) <= 4e9; }
+
+bool takes_direct_backward(const gbmuf_linear_desc_t &d) { return operations(d) <= (d.dtype == GBMUF_F32 ? 2.5e9 : 5e8); }
 
 // ---------------------------------------------------------------------------------------
 // Forward.  io nullptr: only count the workspace, for matrices that lie as badly as can be.
@@ -275,14 +282,15 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     }
     if (M <= kFewRows || takes_direct_forward(d)) {
         const int tile = tile_of(M, N, G);
-        DirectArgs f = direct_args(source_of(io ? io->x : none), source_of(io ? io->w : none), M, N, K, G, tile, e);
+        const Cut c = direct_cut(tile, M, N, K, G, M > kFewRows);
+        DirectArgs f = direct_args(source_of(io ? io->x : none), source_of(io ? io->w : none), K, c, e);
         if (M <= kFewRows) return io ? launch_few(f, type, stream) : GBMUF_OK;
-        f.partial = space.take<float>(cut_sum(f));
+        f.t.partial = space.take<float>(c.partial);
         if (!io) return GBMUF_OK;
         const int rc = launch_direct_forward(f, type, tile, stream);
-        return rc != GBMUF_OK ? rc : join(f, stream);
+        return rc != GBMUF_OK ? rc : launch_join(JoinArgs{f.t, tile, 0, e}, stream);
     }
-    const Shape s = shape_of(M, N, K, G, split);
+    const Cut s = shape_of(M, N, K, G, split);
     float *partial = space.take<float>(s.partial);
     uint32_t *max = space.take<uint32_t>(split ? G * (M + N) : 0);
     const gbmuf_matrix_t &xm = io ? io->x : none, &wm = io ? io->w : none;
@@ -306,12 +314,20 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
         else if ((rc = launch_stats(l, stream)) == GBMUF_OK) rc = launch_lay(l, stream);
         if (rc != GBMUF_OK) return rc;
     }
-    return run_product(x, w, M, N, K, G, type, e, s, partial, stream);
+    return run_product(x, w, K, type, e, s, partial, stream);
 }
 
 // ---------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------
+// dw's epilogue
+Epilogue weight_grad(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &m, int32_t type)
+{
+    Epilogue e = into(m, type);
+    if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = m.data; e.ldr = m.ld; e.r_batch = m.batch_stride; }
+    return e;
+}
+
 int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, Space &space, hipStream_t stream)
 {
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
@@ -322,24 +338,16 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
     const bool dx = !io || io->dx.data, dw = !io || io->dw.data;
     Source z = source_of(at.dy);
     if (d.activation) { z.pre = at.pre.data; z.ldp = at.pre.ld; z.p_batch = at.pre.batch_stride; z.act = d.activation; }
-    Epilogue e = into(at.dw, grad_type);
-    if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = at.dw.data; e.ldr = at.dw.ld; e.r_batch = at.dw.batch_stride; }
-    DirectArgs px = direct_args(z, source_of(at.w), M, dx ? K : 0, N, G, tile, into(at.dx, type));
-    DirectArgs pw = direct_args(z, source_of(at.x), N, dw ? K : 0, M, G, tile, e);
-    px.partial = space.take<float>(cut_sum(px));
+    const Cut cx = direct_cut(tile, M, dx ? K : 0, N, G, true), cw = direct_cut(tile, N, dw ? K : 0, M, G, false);
+    const Epilogue e = into(at.dx, type);
+    DirectArgs px = direct_args(z, source_of(at.w), N, cx, e);
+    DirectArgs pw = direct_args(z, source_of(at.x), M, cw, weight_grad(d, at.dw, grad_type));
+    px.t.partial = space.take<float>(cx.partial);
     if (!io) return GBMUF_OK;
     px.copy = at.dresidual.data; px.copy_ld = at.dresidual.ld; px.copy_batch = at.dresidual.batch_stride;
     pw.sums = at.dbias.data; pw.sums_batch = at.dbias.batch_stride; pw.sums_type = grad_type; pw.accumulate = d.accumulate;
     const int rc = launch_direct_backward(px, pw, type, tile, stream);
-    return rc != GBMUF_OK ? rc : join(px, stream);
-}
-
-// dw's epilogue
-Epilogue weight_grad(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &m, int32_t type)
-{
-    Epilogue e = into(m, type);
-    if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = m.data; e.ldr = m.ld; e.r_batch = m.batch_stride; }
-    return e;
+    return rc != GBMUF_OK ? rc : launch_join(JoinArgs{px.t, tile, 0, e}, stream);
 }
 
 int sum_columns(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &out, const float *sums, int32_t type, hipStream_t stream)
@@ -359,7 +367,7 @@ int backward_split(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *i
     const gbmuf_linear_grad_io_t none{};
     const gbmuf_linear_grad_io_t &at = io ? *io : none;
     const bool dx = !io || at.dx.data, dw = !io || at.dw.data, db = !io || at.dbias.data, dr = at.dresidual.data;
-    const Shape sx = shape_of(M, K, N, G, true), sw = shape_of(N, K, M, G, true);
+    const Cut sx = shape_of(M, K, N, G, true), sw = shape_of(N, K, M, G, true);
     float *partial = space.take<float>(std::max(dx ? sx.partial : 0, dw ? sw.partial : 0));     // one product after the other
     float *sums = space.take<float>(db ? G * ((M + kLayTile - 1) / kLayTile) * N : 0);
     const int64_t n_max = G * (M + N + 2 * K);             // largest magnitudes: rows and columns of dz, columns of w and of x
@@ -396,8 +404,8 @@ int backward_split(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *i
         l.trans = const_cast<uint16_t *>(o.p); l.trans_ld = o.ld; l.trans_batch = o.batch;
         if ((rc = launch_stats(l, stream)) != GBMUF_OK || (rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
     }
-    if (dx && (rc = run_product(z, wt, M, K, N, G, kF32, into(at.dx, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
-    return dw ? run_product(zt, xt, N, K, M, G, kF32, weight_grad(d, at.dw, kF32), sw, partial, stream) : rc;
+    if (dx && (rc = run_product(z, wt, N, kF32, into(at.dx, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
+    return dw ? run_product(zt, xt, M, kF32, weight_grad(d, at.dw, kF32), sw, partial, stream) : rc;
 }
 
 // bf16, f16: the products read w, x and dz across their rows where they need to, so that matrices whose rows lie on 16 bytes are taken as
@@ -409,7 +417,7 @@ int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, 
     const gbmuf_linear_grad_io_t none{};
     const gbmuf_linear_grad_io_t &at = io ? *io : none;
     const bool dx = !io || at.dx.data, dw = !io || at.dw.data, db = !io || at.dbias.data, dr = at.dresidual.data;
-    const Shape sx = shape_of(M, K, N, G, false), sw = shape_of(N, K, M, G, false);
+    const Cut sx = shape_of(M, K, N, G, false), sw = shape_of(N, K, M, G, false);
     float *partial = space.take<float>(std::max(dx ? sx.partial : 0, dw ? sw.partial : 0));
     float *sums = space.take<float>(db ? G * ((M + kLayTile - 1) / kLayTile) * N : 0);
 
@@ -440,8 +448,8 @@ int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, 
     if (rc == GBMUF_OK && db) rc = sum_columns(d, at.dbias, sums, grad_type, stream);
     if (rc == GBMUF_OK && copy_w) rc = copy(lw, w);
     if (rc == GBMUF_OK && copy_x) rc = copy(lx, x);
-    if (rc == GBMUF_OK && dx) rc = run_product(z, w, M, K, N, G, type, into(at.dx, type), sx, partial, stream);
-    if (rc == GBMUF_OK && dw) rc = run_product(zt, x, N, K, M, G, type, weight_grad(d, at.dw, grad_type), sw, partial, stream);
+    if (rc == GBMUF_OK && dx) rc = run_product(z, w, N, type, into(at.dx, type), sx, partial, stream);
+    if (rc == GBMUF_OK && dw) rc = run_product(zt, x, M, type, weight_grad(d, at.dw, grad_type), sw, partial, stream);
     return rc;
 }
 

@@ -19,6 +19,18 @@ struct Epilogue {
     int32_t reserved;
 };
 
+// Which tiles of a result there are and how workgroups take them: the first `whole` tiles one each, and the sum over k of every other one
+// goes to `splits` workgroups of `steps` steps each, whose parts lie [split][tile - whole][row][column].
+struct Tiles {
+    int32_t M, N, batch;
+    int32_t tiles_m, tiles_n;
+    int32_t whole, splits, steps;
+    float *partial;
+    __host__ __device__ int32_t count() const { return tiles_m * tiles_n * batch; }
+    __host__ __device__ int32_t rest() const { return count() - whole; }
+    __host__ __device__ int32_t blocks() const { return whole + rest() * splits; }
+};
+
 // out[g][m][n] = sum over k of a[g][m][k] * b[g][n][k], in 16-bit numbers whose k are contiguous.  Split: a row holds, for every 32
 // k, their 32 leading parts and then their 32 trailing parts, and `k` counts both; a_max and b_max hold the bits of the largest magnitude of
 // every row before the row was scaled.
@@ -27,11 +39,9 @@ struct ProductArgs {
     int64_t lda, ldb, a_batch, b_batch;
     const uint32_t *a_max, *b_max;
     int64_t a_max_batch, b_max_batch;
-    int32_t M, N, K, batch;
-    int32_t tiles_m, tiles_n;
-    int32_t splits, steps;   // the sum over k goes to `splits` workgroups of `steps` steps of 64 each
+    int32_t K;               // 16-bit words
     int32_t across;          // 16-bit types: bit 0, 1: a (b) is [k][m] ([k][n]) with rows lda (ldb) apart, whole pieces of 8 columns
-    float *partial;          // splits > 1: [split][g][m][n]
+    Tiles t;                 // steps of 64 words
     Epilogue e;
 };
 
@@ -46,23 +56,21 @@ struct Source {
 // m (n) is what lies side by side.
 struct DirectArgs {
     Source a, b;
-    int32_t M, N, K, batch;
-    int32_t tiles_m, tiles_n;
-    int32_t splits, steps;   // the sum over k goes to `splits` workgroups of `steps` steps of 32 each
-    float *partial;
+    int32_t K;
+    int32_t reserved;
+    Tiles t;                 // steps of 32 values
     Epilogue e;
     void *copy;              // a itself (dz), of the matrices' type, or nullptr
     int64_t copy_ld, copy_batch;
-    void *sums;              // sums[g][m] (+)= sum over k of a(m, k), or nullptr; splits == 1
+    void *sums;              // sums[g][m] (+)= sum over k of a(m, k), or nullptr; no tile is split
     int64_t sums_batch;
     int32_t sums_type, accumulate;
 };
 
-// The sums of `splits` partial products, and what is done with them.
+// The sums of the parts of split tiles, and what is done with them.
 struct JoinArgs {
-    const float *partial;
-    int64_t M, N;
-    int32_t batch, splits;
+    Tiles t;
+    int32_t tile, reserved;  // 64, 128 or 256
     Epilogue e;
 };
 

@@ -190,25 +190,14 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
     __shared__ __align__(1024) uint16_t lds[2][(TM + TN) * kStep];
     static_assert(leave_bytes<TM, TN, WM, WN>() <= sizeof(lds), "the result leaves through the stages");
 
-    const int per = a.tiles_m * a.tiles_n;
-    int id = static_cast<int>(blockIdx.x);
-    // workgroups go to the 8 XCDs in turns: each XCD takes a stretch of tiles, whose operands its L2 holds
-    const int whole = static_cast<int>(gridDim.x) / 8;
-    if (id < whole * 8) id = (id & 7) * whole + (id >> 3);
-    const int split = id / (per * a.batch);
-    id -= split * per * a.batch;
-    const int g = id / per;
-    id -= g * per;
-    // stretches run down 8 tiles, then to the next column
-    const int band = id / (8 * a.tiles_n), rows = min(8, a.tiles_m - band * 8), in = id - band * 8 * a.tiles_n;
-    const int m0 = (band * 8 + in % rows) * TM, n0 = in / rows * TN;
-
-    const int all = (a.K + kStep - 1) / kStep, first = split * a.steps, last = min(first + a.steps, all);
+    const Share share = share_of<TM, TN>(a.t, static_cast<int>(blockIdx.x), (a.K + kStep - 1) / kStep);
+    const int64_t g = share.at.g;
+    const int m0 = share.at.tm * TM, n0 = share.at.tn * TN, first = share.first, last = share.last;
     const int full = min(last, a.K / kStep);               // steps [first, full) are whole
     std::conditional_t<(ACROSS & 1) != 0, StageAcross<TM, THREADS>, Stage<TM, THREADS>> sa;
     std::conditional_t<(ACROSS & 2) != 0, StageAcross<TN, THREADS>, Stage<TN, THREADS>> sb;
-    sa.init(a.a + g * a.a_batch, a.lda, m0, a.M);
-    sb.init(a.b + g * a.b_batch, a.ldb, n0, a.N);
+    sa.init(a.a + g * a.a_batch, a.lda, m0, a.t.M);
+    sb.init(a.b + g * a.b_batch, a.ldb, n0, a.t.N);
 
     const int wave = threadIdx.x >> 6, wm = (wave % WM) * (TM / WM), wn = (wave / WM) * (TN / WN);
     v16f acc[FM][FN];
@@ -262,25 +251,31 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
         }
     }
     __syncthreads();
-    leave<TM, TN, WM, WN, SPLIT>(acc, &lds[0][0], a, split, g, m0, n0);
+    leave<TM, TN, WM, WN, SPLIT>(acc, &lds[0][0], a, share);
 }
 
-// Joins the parts of sums that were split, in their order.
+// Joins the parts of split tiles, in their order: 32 rows of a tile a workgroup, 8 columns a thread.
+template <int TILE>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
 {
-    const int64_t all = a.M * a.N * a.batch, fours = (a.N + 3) / 4, work = fours * a.M * a.batch;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < work; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / fours, n = (i - row * fours) * 4, g = row / a.M;
-        const int left = static_cast<int>(min(a.N - n, int64_t{4}));
-        const float *from = a.partial + row * a.N + n;
-        v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int p = 0; p < a.splits; ++p, from += all) {
-            if (left == 4) s += load4<kPlain>(from);
-            else
-                for (int c = 0; c < 3; ++c)
-                    if (c < left) s[c] += from[c];
+    constexpr int kChunks = TILE / 32, kLanes = TILE / 8;
+    const int rest = a.t.rest(), tile = static_cast<int>(blockIdx.x) / kChunks, chunk = static_cast<int>(blockIdx.x) % kChunks;
+    const TileAt at = tile_at(a.t, a.t.whole + tile);
+    const int column = static_cast<int>(threadIdx.x) % kLanes * 8, n = at.tn * TILE + column;
+    if (n >= a.t.N) return;
+    for (int r = chunk * 32 + static_cast<int>(threadIdx.x) / kLanes; r < chunk * 32 + 32; r += 256 / kLanes) {
+        const int m = at.tm * TILE + r;
+        if (m >= a.t.M) return;
+        const float *from = a.t.partial + static_cast<int64_t>(tile) * (TILE * TILE) + r * TILE + column;
+        const int64_t next = static_cast<int64_t>(rest) * (TILE * TILE);
+        Eight s = read8<kF32>(from, 0);
+#pragma unroll 4
+        for (int p = 1; p < a.t.splits; ++p) {
+            const Eight v = read8<kF32>(from, p * next);
+            s.v[0] += v.v[0];
+            s.v[1] += v.v[1];
         }
-        finish(a.e, g, row - g * a.M, n, left, s);
+        finish8(a.e, at.g, m, n, a.t.N - n, s);
     }
 }
 
@@ -288,9 +283,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a)
 
 int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t stream)
 {
-    if (a.M <= 0 || a.N <= 0 || a.batch <= 0) return GBMUF_OK;
-    const int64_t blocks = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.batch * a.splits;
-    if (blocks > 0x7fffffffLL / 512) return GBMUF_EUNSUPPORTED;
+    if (a.t.count() <= 0) return GBMUF_OK;
     ProductArgs args = a;
     void *argv[] = {&args};
     using Fn = void (*)(ProductArgs);
@@ -303,20 +296,19 @@ int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t str
          {product_kernel<kF16, false, 128, 128, 2, 2, 2>, product_kernel<kF16, false, 256, 256, 2, 4, 2>},
          {product_kernel<kF16, false, 128, 128, 2, 2, 3>, product_kernel<kF16, false, 256, 256, 2, 4, 3>}}};
     const Fn fn = type == kF32 ? split[tile == 256] : plain[type == kF16][a.across == 0 ? 0 : a.across - 1][tile == 256];
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)),
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(a.t.blocks())),
                                            dim3(tile == 256 ? 512 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(product)", err, GBMUF_EDEVICE);
 }
 
 int launch_join(const JoinArgs &a, hipStream_t stream)
 {
-    const int64_t all = (a.N + 3) / 4 * a.M * a.batch;
-    if (all <= 0) return GBMUF_OK;
+    if (a.t.splits <= 1 || a.t.rest() <= 0) return GBMUF_OK;
     JoinArgs args = a;
     void *argv[] = {&args};
-    const int64_t blocks = (all + 255) / 256;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(join_kernel), dim3(static_cast<unsigned>(blocks < 65536 ? blocks : 65536)),
-                                           dim3(256), argv, 0, stream);
+    const auto fn = a.tile == 64 ? join_kernel<64> : a.tile == 128 ? join_kernel<128> : join_kernel<256>;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(a.t.rest() * (a.tile / 32))), dim3(256), argv, 0,
+                                           stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(join)", err, GBMUF_EDEVICE);
 }
 

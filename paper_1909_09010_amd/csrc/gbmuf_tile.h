@@ -8,6 +8,41 @@ namespace {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
+// Tile number id: down 8 tiles, then the next column, which keeps what workgroups side by side read small.
+struct TileAt {
+    int64_t g;
+    int tm, tn;
+};
+__device__ __forceinline__ TileAt tile_at(const Tiles &t, int id)
+{
+    const int per = t.tiles_m * t.tiles_n;
+    TileAt at;
+    at.g = id / per;
+    id -= static_cast<int>(at.g) * per;
+    const int band = id / (8 * t.tiles_n), rows = min(8, t.tiles_m - band * 8), in = id - band * 8 * t.tiles_n;
+    at.tm = band * 8 + in % rows;
+    at.tn = in / rows;
+    return at;
+}
+
+// What workgroup b does.
+struct Share {
+    TileAt at;
+    int first, last;         // steps [first, last)
+    float *part;             // a split tile's: where its part goes, row by row
+};
+template <int TM, int TN>
+__device__ __forceinline__ Share share_of(const Tiles &t, int b, int all)
+{
+    // workgroups go to the 8 XCDs in turns: each XCD takes a stretch of tiles, whose operands its L2 holds
+    const auto stretch = [](int i, int n) { return i < n / 8 * 8 ? (i & 7) * (n / 8) + (i >> 3) : i; };
+    if (b < t.whole) return Share{tile_at(t, stretch(b, t.whole)), 0, all, nullptr};
+    const int rest = t.rest(), i = stretch(b - t.whole, rest * t.splits), split = i / rest, tile = i - split * rest;
+    Share s{tile_at(t, t.whole + tile), split * t.steps, min((split + 1) * t.steps, all), nullptr};
+    if (t.splits > 1) s.part = t.partial + static_cast<int64_t>(i) * (TM * TN);
+    return s;
+}
+
 // LDS that leave() needs: 32 rows of every wave's columns.
 template <int TM, int TN, int WM, int WN>
 constexpr size_t leave_bytes() { return static_cast<size_t>(WM) * WN * 32 * (TN / WN + 4) * sizeof(float); }
@@ -18,26 +53,25 @@ constexpr size_t leave_bytes() { return static_cast<size_t>(WM) * WN * 32 * (TN 
 // + 4 (lane / 32) + r % 4; afterwards 8 columns side by side, whose bias and scales it loads once.  (Tiles turned around by the
 // whole workgroup, row by row, cost 7 us where these cost 2: bf16, 256 x 256.)
 template <int TM, int TN, int WM, int WN, bool SPLIT, class Args>
-__device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Args &a, int split, int64_t g, int m0, int n0)
+__device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Args &a, const Share &share)
 {
+    const int64_t g = share.at.g;
+    const int m0 = share.at.tm * TM, n0 = share.at.tn * TN, M = a.t.M, N = a.t.N;
     constexpr int FM = TM / WM / 32, FN = TN / WN / 32, kColumns = TN / WN, kPitch = kColumns + 4, kLanes = kColumns / 8, kTogether = 64 / kLanes,
                   kTurns = 32 / kTogether;
     static_assert(FM == 1 || FM == 2 || FM == 4, "the cases below");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float *out = static_cast<float *>(lds) + wave * 32 * kPitch;
-    const int column = lane % kLanes * 8, first = lane / kLanes, n = n0 + (wave / WM) * kColumns + column, left = a.N - n;
+    const int column = lane % kLanes * 8, first = lane / kLanes, n = n0 + (wave / WM) * kColumns + column, left = N - n;
     const int mw = m0 + (wave % WM) * (TM / WM) + first;
-    const bool parts = a.splits > 1;
     const Epilogue &e = a.e;
-    const bool simple = parts || (!e.act && !e.place && !e.pre);
+    const bool parts = share.part != nullptr, simple = !e.act && !e.pre;
     Eight bias{};
     int scale[SPLIT ? 8 : 1];
-    if (left >= 8) {
-        if (e.bias && !parts) bias = load_eight(e.bias, g * e.bias_batch + n, e.type);
-        if constexpr (SPLIT)
+    if (left >= 8 && e.bias && !parts) bias = load_eight(e.bias, g * e.bias_batch + n, e.type);
+    if constexpr (SPLIT)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) scale[c] = row_exponent(a.b_max[g * a.b_max_batch + n + c]);
-    }
+        for (int c = 0; c < 8; ++c) scale[c] = row_exponent(a.b_max[g * a.b_max_batch + min(n + c, N - 1)]);
     const auto put = [&](const v16f (&rows)[FN]) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
@@ -66,7 +100,15 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
         uint32_t top[SPLIT ? kTurns : 1];
         if constexpr (SPLIT)
 #pragma unroll
-            for (int k = 0; k < kTurns; ++k) top[k] = a.a_max[g * a.a_max_batch + min(m_of(k), a.M - 1)];
+            for (int k = 0; k < kTurns; ++k) top[k] = a.a_max[g * a.a_max_batch + min(m_of(k), M - 1)];
+        const auto fetch = [&](int k) { return load_eight(e.res, g * e.r_batch + min(m_of(k), M - 1) * e.ldr + n, e.type); };
+        Eight r[kTurns] = {};
+        if (e.place && !parts && left >= 8) {
+            r[0] = fetch(0);
+            if (simple)
+#pragma unroll
+                for (int k = 1; k < kTurns; ++k) r[k] = fetch(k);
+        }
         if (i == 0) put(acc[0]);
         if constexpr (FM > 1)
             if (i == 1) put(acc[1]);
@@ -74,21 +116,22 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
             if (i == 2) put(acc[2]);
             if (i == 3) put(acc[3]);
         }
-        if (left >= 8 && simple) {
+        if (parts) {                                       // as they are, the whole tile
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) write8<kF32>(share.part, static_cast<int64_t>(m_of(k) - m0) * TN + (n - n0), scaled(get(k), top[SPLIT ? k : 0]));
+        } else if (left >= 8 && simple) {
             Eight z[kTurns];
 #pragma unroll
             for (int k = 0; k < kTurns; ++k) z[k] = get(k);
 #pragma unroll
             for (int k = 0; k < kTurns; ++k) {
                 z[k] = scaled(z[k], top[SPLIT ? k : 0]);
-                if (m_of(k) >= a.M) continue;
-                if (parts) write8<kF32>(a.partial, ((static_cast<int64_t>(split) * a.batch + g) * a.M + m_of(k)) * a.N + n, z[k]);
-                else store_eight(e.y, g * e.y_batch + m_of(k) * e.ldy + n, e.type, z[k]);
+                z[k].v[0] += r[k].v[0];
+                z[k].v[1] += r[k].v[1];
+                if (m_of(k) < M) store_eight(e.y, g * e.y_batch + m_of(k) * e.ldy + n, e.type, z[k]);
             }
         } else if (left >= 8) {
-            const auto fetch = [&](int k) { return load_eight(e.res, g * e.r_batch + min(m_of(k), a.M - 1) * e.ldr + n, e.type); };
-            Eight r{};
-            if (e.place) r = fetch(0);
+            Eight rk = r[0];
 #pragma unroll 1
             for (int k = 0; k < kTurns; ++k) {
                 uint32_t bits = top[0];
@@ -97,9 +140,9 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
                     for (int t = 1; t < kTurns; ++t) bits = k == t ? top[t] : bits;
                 Eight z = scaled(get(k), bits);
                 const int m = m_of(k);
-                const Eight now = r;
-                if (e.place && k + 1 < kTurns) r = fetch(k + 1);           // under this row's work
-                if (m >= a.M) continue;
+                const Eight now = rk;
+                if (e.place && k + 1 < kTurns) rk = fetch(k + 1);          // under this row's work
+                if (m >= M) continue;
                 if (e.place == GBMUF_RESIDUAL_BEFORE) {
                     z.v[0] += now.v[0];
                     z.v[1] += now.v[1];
@@ -116,7 +159,7 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
 #pragma unroll 1
             for (int k = 0; k < kTurns * 2; ++k) {
                 const int m = m_of(k >> 1), c0 = (k & 1) * 4, rest = left - c0;
-                if (m >= a.M || rest <= 0) continue;
+                if (m >= M || rest <= 0) continue;
                 v4f v = *reinterpret_cast<const v4f *>(out + (first + (k >> 1) * kTogether) * kPitch + column + c0);
                 if constexpr (SPLIT) {
                     const int em = row_exponent(a.a_max[g * a.a_max_batch + m]);
@@ -124,14 +167,7 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
                     for (int c = 0; c < 4; ++c)
                         if (c < rest) v[c] = ldexpf(v[c], em + row_exponent(a.b_max[g * a.b_max_batch + n + c0 + c]));
                 }
-                if (parts) {
-                    float *to = a.partial + ((static_cast<int64_t>(split) * a.batch + g) * a.M + m) * a.N + n + c0;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (c < rest) to[c] = v[c];
-                } else {
-                    finish(e, g, m, n + c0, rest, v);
-                }
+                finish(e, g, m, n + c0, rest, v);
             }
         }
     }

@@ -186,6 +186,28 @@ __device__ __forceinline__ Eight activate8(Eight z, int32_t act)
     return z;
 }
 
+// What follows 8 sums side by side, of which `left` are the matrix's.
+__device__ __forceinline__ void finish8(const Epilogue &e, int64_t g, int64_t m, int64_t n, int left, Eight z)
+{
+    if (left < 8) {
+        finish(e, g, m, n, left, z.v[0]);
+        if (left > 4) finish(e, g, m, n + 4, left - 4, z.v[1]);
+        return;
+    }
+    const auto add = [&](const Eight &o) {
+        z.v[0] += o.v[0];
+        z.v[1] += o.v[1];
+    };
+    Eight r{};
+    if (e.place) r = load_eight(e.res, g * e.r_batch + m * e.ldr + n, e.type);
+    if (e.bias) add(load_eight(e.bias, g * e.bias_batch + n, e.type));
+    if (e.place == GBMUF_RESIDUAL_BEFORE) add(r);
+    if (e.pre) store_eight(e.pre, g * e.p_batch + m * e.ldp + n, e.type, z);
+    z = activate8(z, e.act);
+    if (e.place == GBMUF_RESIDUAL_AFTER) add(r);
+    store_eight(e.y, g * e.y_batch + m * e.ldy + n, e.type, z);
+}
+
 // v times the slope at z
 __device__ __forceinline__ Eight slope8(Eight v, const Eight &z, int32_t act)
 {
