@@ -23,7 +23,9 @@ struct GradTile {                // one workgroup's share: values [start, start 
     int32_t tensor, n;
 };
 
-constexpr int kThreads = 256;
+// Workgroups take 4096 values each: every load of f32 is under way before the first value is used.  Clipping, Adagrad's step of 16 x 19.8 M f32, us:
+// tiles of 1 K 843, 1592; 2 K 712, 1527; 4 K 674, 1503; 8 K 692, 1510; 32 K 709, 1515.  Streamed accesses and tiles dealt in runs to the XCDs gain nothing.
+constexpr int kThreads = 256, kTile = 4096;
 
 __device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
 {
@@ -32,16 +34,62 @@ __device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
     return i + r * (t.ld - t.cols);
 }
 
-// do4(i) for four values of the tile from value i on that lie side by side in the tensor, do1(i) for single ones.
-template <class Do4, class Do1>
-__device__ __forceinline__ void each(const GradTensor &t, const GradTile &tile, Do4 do4, Do1 do1)
+// V values side by side: 16 bytes of f32 or of 16-bit numbers an instruction and lane, so that a wave's cover whole lines.
+template <int V>
+struct Some {
+    float v[V];
+};
+
+template <int T, int V>
+__device__ __forceinline__ Some<V> read_some(const void *p, int64_t i)
 {
-    for (int32_t k = static_cast<int32_t>(threadIdx.x) * 4; k < tile.n; k += kThreads * 4) {
+    Some<V> r;
+    if constexpr (V == 4) {
+        const v4f x = read4<T>(p, i);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) r.v[c] = x[c];
+    } else {
+        const Eight x = read8<T>(p, i);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) r.v[c] = x.v[c >> 2][c & 3];
+    }
+    return r;
+}
+
+template <int T, int V>
+__device__ __forceinline__ void write_some(void *p, int64_t i, const Some<V> &r)
+{
+    if constexpr (V == 4) write4<T>(p, i, v4f{r.v[0], r.v[1], r.v[2], r.v[3]});
+    else write8<T>(p, i, Eight{{v4f{r.v[0], r.v[1], r.v[2], r.v[3]}, v4f{r.v[4], r.v[5], r.v[6], r.v[7]}}});
+}
+
+// The tile's values, V at a time that lie side by side in the tensor: U times V are loaded, load(i), before the first are used, use(i, what was
+// loaded); one(i) for single values.
+template <int V, int U, class Load, class Use, class One>
+__device__ __forceinline__ void each(const GradTensor &t, const GradTile &tile, Load load, Use use, One one)
+{
+    constexpr int kAll = kThreads * V;
+    if (t.ld == t.cols) {
+        int32_t k = static_cast<int32_t>(threadIdx.x) * V;
+        for (; k + (U - 1) * kAll + V <= tile.n; k += U * kAll) {
+            decltype(load(tile.start)) v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load(tile.start + k + u * kAll);
+#pragma unroll
+            for (int u = 0; u < U; ++u) use(tile.start + k + u * kAll, v[u]);
+        }
+        for (; k < tile.n; k += kAll) {
+            if (k + V <= tile.n) use(tile.start + k, load(tile.start + k));
+            else
+                for (int32_t c = k; c < tile.n; ++c) one(tile.start + c);
+        }
+        return;
+    }
+    for (int32_t k = static_cast<int32_t>(threadIdx.x) * V; k < tile.n; k += kAll) {
         const int64_t i = tile.start + k;
-        const int left = min(4, tile.n - k);
-        if (left == 4 && (t.ld == t.cols || i % t.cols + 4 <= t.cols)) do4(i);
+        if (k + V <= tile.n && i % t.cols + V <= t.cols) use(i, load(i));
         else
-            for (int c = 0; c < left; ++c) do1(i + c);
+            for (int32_t c = k; c < min(k + V, tile.n); ++c) one(tile.start + c);
     }
 }
 
@@ -57,15 +105,14 @@ template <int T>
 __device__ __forceinline__ double tile_squares(const GradTensor &t, const GradTile &tile)
 {
     double s = 0.0;
-    each(t, tile,
-         [&](int64_t i) {
-             const v4f v = read4<T>(t.p, grad_at(t, i));
-             for (int c = 0; c < 4; ++c) s = fma(static_cast<double>(v[c]), static_cast<double>(v[c]), s);
-         },
-         [&](int64_t i) {
-             const double v = static_cast<double>(load_one(t.p, grad_at(t, i), T));
-             s = fma(v, v, s);
-         });
+    const auto add = [&](float v) { s = fma(static_cast<double>(v), static_cast<double>(v), s); };
+    constexpr int V = T == kF32 ? 4 : 8;
+    each<V, 4>(t, tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+            [&](int64_t, const Some<V> &v) {
+#pragma unroll
+                for (int c = 0; c < V; ++c) add(v.v[c]);
+            },
+            [&](int64_t i) { add(load_one(t.p, grad_at(t, i), T)); });
     return s;
 }
 
@@ -79,13 +126,35 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const GradTensor *tensor
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
+// A worker's norm from its tiles' sums, by a whole workgroup.
+__device__ __forceinline__ float join_norm(const double *partial, const int32_t *first, int32_t worker, double *lds)
+{
+    double s = 0.0;
+    for (int32_t i = first[worker] + static_cast<int32_t>(threadIdx.x); i < first[worker + 1]; i += kThreads) s += partial[i];
+    return static_cast<float>(sqrt(block_sum(s, lds)));
+}
+
 __global__ __launch_bounds__(kThreads) void norm_join_kernel(const double *partial, const int32_t *first, float *norms)
 {
     __shared__ double lds[4];
-    double s = 0.0;
-    for (int32_t i = first[blockIdx.x] + static_cast<int32_t>(threadIdx.x); i < first[blockIdx.x + 1]; i += kThreads) s += partial[i];
-    s = block_sum(s, lds);
-    if (threadIdx.x == 0) norms[blockIdx.x] = static_cast<float>(sqrt(s));
+    const float norm = join_norm(partial, first, static_cast<int32_t>(blockIdx.x), lds);
+    if (threadIdx.x == 0) norms[blockIdx.x] = norm;
+}
+
+// Where the norms are for the kernel after: joined already (partial nullptr), or to be joined by every workgroup for itself, which saves a
+// launch where a worker has few tiles; that of the worker's first tile writes it.
+struct Norms {
+    float *norms;
+    const double *partial;
+    const int32_t *first;
+};
+
+__device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t tile, double *lds)
+{
+    if (!n.partial) return n.norms[worker];
+    const float norm = join_norm(n.partial, n.first, worker, lds);
+    if (threadIdx.x == 0 && tile == n.first[worker]) n.norms[worker] = norm;
+    return norm;
 }
 
 __device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most ? 1.0f : most / norm; }
@@ -93,14 +162,17 @@ __device__ __forceinline__ float clip_factor(float norm, float most) { return no
 template <int T, int D>
 __device__ __forceinline__ void clip_tile(const GradTensor &t, const GradTensor &d, const GradTile &tile, float f)
 {
-    each(t, tile,
-         [&](int64_t i) {
-             const v4f v = read4<T>(t.p, grad_at(t, i)) * f;
-             if (d.ld == d.cols || i % d.cols + 4 <= d.cols) write4<D>(d.p, grad_at(d, i), v);
-             else
-                 for (int c = 0; c < 4; ++c) store_one(d.p, grad_at(d, i + c), D, v[c]);
-         },
-         [&](int64_t i) { store_one(d.p, grad_at(d, i), D, load_one(t.p, grad_at(t, i), T) * f); });
+    constexpr int V = T == kF32 || D == kF32 ? 4 : 8;
+    each<V, 4>(t, tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+            [&](int64_t i, Some<V> v) {
+#pragma unroll
+                for (int c = 0; c < V; ++c) v.v[c] *= f;
+                if (d.ld == d.cols || i % d.cols + V <= d.cols) write_some<D, V>(d.p, grad_at(d, i), v);
+                else
+#pragma unroll
+                    for (int c = 0; c < V; ++c) store_one(d.p, grad_at(d, i + c), D, v.v[c]);
+            },
+            [&](int64_t i) { store_one(d.p, grad_at(d, i), D, load_one(t.p, grad_at(t, i), T) * f); });
 }
 
 template <int T>
@@ -111,12 +183,14 @@ __device__ __forceinline__ void clip_to(const GradTensor &t, const GradTensor &d
     else clip_tile<T, kF16>(t, d, tile, f);
 }
 
-__global__ __launch_bounds__(kThreads) void clip_kernel(const GradTensor *tensors, const GradTensor *to, const GradTile *tiles, const float *norms,
-                                                        float most)
+// Tiles are taken from the last to the first: what the norm read last is still in the caches.
+__global__ __launch_bounds__(kThreads) void clip_kernel(const GradTensor *tensors, const GradTensor *to, const GradTile *tiles, Norms norms, float most)
 {
-    const GradTile tile = tiles[blockIdx.x];
+    __shared__ double lds[4];
+    const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);
+    const GradTile tile = tiles[number];
     const GradTensor t = tensors[tile.tensor];
-    const float f = clip_factor(norms[t.worker], most);
+    const float f = clip_factor(norm_of(norms, t.worker, number, lds), most);
     if (tensors == to && f == 1.0f) return;                // in place: nothing changes
     const GradTensor d = to[tile.tensor];
     if (t.type == kF32) clip_to<kF32>(t, d, tile, f);
@@ -127,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTensor *tensor
 struct StepArgs {
     const GradTensor *tensors;
     const GradTile *tiles;
-    const float *norms;          // nullptr: no clipping
+    Norms norms;                 // norms.norms nullptr: no clipping
     float *theta, *sums;         // sums nullptr: SGD
     Placement at, sums_at;
     float rate, eps, most;
@@ -145,6 +219,10 @@ __device__ __forceinline__ void update(float &theta, float &h, float g, const St
     }
 }
 
+struct StepFour {
+    Some<4> g, theta, h;
+};
+
 template <int T>
 __device__ __forceinline__ void step_tile(const GradTensor &t, const GradTile &tile, float f, const StepArgs &a)
 {
@@ -159,35 +237,41 @@ __device__ __forceinline__ void step_tile(const GradTensor &t, const GradTile &t
         *p = v;
         if (q) *q = h;
     };
-    each(t, tile,
-         [&](int64_t i) {
-             const int64_t e = t.offset + i;
-             if (((e ^ (e + 3)) >> a.at.logB) != 0 || (sums && ((e ^ (e + 3)) >> a.sums_at.logB) != 0)) {
-                 for (int c = 0; c < 4; ++c) one(i + c);
-                 return;
-             }
-             const v4f g = read4<T>(t.p, grad_at(t, i)) * f;
-             float *p = theta + placed(a.at, e), *q = sums ? sums + placed(a.sums_at, e) : nullptr;
-             v4f v = load4<kPlain>(p), h = q ? load4<kPlain>(q) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
-             for (int c = 0; c < 4; ++c) {
-                 float x = v[c], y = h[c];
-                 update(x, y, g[c], a);
-                 v[c] = x;
-                 h[c] = y;
-             }
-             store4<kPlain>(p, v);
-             if (q) store4<kPlain>(q, h);
-         },
-         one);
+    // four parameters that a block's edge parts are taken one by one
+    const auto together = [&](int64_t e) { return ((e ^ (e + 3)) >> a.at.logB) == 0 && (!sums || ((e ^ (e + 3)) >> a.sums_at.logB) == 0); };
+    each<4, 1>(t, tile,
+            [&](int64_t i) {
+                StepFour s{};
+                const int64_t e = t.offset + i;
+                if (!together(e)) return s;
+                s.g = read_some<T, 4>(t.p, grad_at(t, i));
+                s.theta = read_some<kF32, 4>(theta, placed(a.at, e));
+                if (sums) s.h = read_some<kF32, 4>(sums, placed(a.sums_at, e));
+                return s;
+            },
+            [&](int64_t i, StepFour s) {
+                const int64_t e = t.offset + i;
+                if (!together(e)) {
+                    for (int c = 0; c < 4; ++c) one(i + c);
+                    return;
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) update(s.theta.v[c], s.h.v[c], s.g.v[c] * f, a);
+                write_some<kF32, 4>(theta, placed(a.at, e), s.theta);
+                if (sums) write_some<kF32, 4>(sums, placed(a.sums_at, e), s.h);
+            },
+            one);
 }
 
 __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a)
 {
-    const GradTile tile = a.tiles[blockIdx.x];
+    __shared__ double lds[4];
+    const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);       // as clip_kernel
+    const GradTile tile = a.tiles[number];
     const GradTensor t = a.tensors[tile.tensor];
     float f = 1.0f;
-    if (a.norms) {
-        const float norm = a.norms[t.worker];
+    if (a.norms.norms) {
+        const float norm = norm_of(a.norms, t.worker, number, lds);
         if (a.skip_nonfinite && !(norm < INFINITY)) return;
         f = clip_factor(norm, a.most);
     }
@@ -205,6 +289,7 @@ struct gbmuf_grads_s {
     int32_t workers = 0;
     int device = -1;
     int64_t n_tiles = 0, reach = 0;              // reach: end of the last tensor among a worker's parameters
+    bool few = false;                            // every worker has tiles, one for a thread at most
     std::vector<GradTensor> tensors;             // by worker, in the order of the list
     GradTensor *d_tensors = nullptr;
     GradTile *d_tiles = nullptr;
@@ -237,7 +322,6 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
     h.workers = d.workers;
     std::vector<int64_t> next(static_cast<size_t>(d.workers), 0);
     std::vector<GradTensor> list(n);
-    int64_t values = 0;
     for (size_t i = 0; i < n; ++i) {
         const gbmuf_grad_tensor_t &t = d.tensors[i];
         if (t.worker < 0 || t.worker >= d.workers || t.dtype < GBMUF_F32 || t.dtype > GBMUF_F16 || t.rows < 0 || t.cols < 0 || t.offset < -1)
@@ -252,7 +336,6 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
         at = offset + count;
         list[i] = GradTensor{static_cast<char *>(t.data), t.cols, t.rows > 1 ? t.row_stride : t.cols, offset, t.worker, t.dtype, t.rows};
         if (count > 0) h.reach = std::max(h.reach, at);
-        values += count;
     }
     std::stable_sort(list.begin(), list.end(), [](const GradTensor &a, const GradTensor &b) { return a.worker < b.worker; });
     h.tensors = list;
@@ -263,9 +346,7 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
         if (before && before->worker == t.worker && before->offset + before->rows * before->cols > t.offset) return GBMUF_EINVAL;
         before = &t;
     }
-    // some 4096 tiles, of 2 K to 32 K values
-    int64_t size = 2048;
-    while (size < 32768 && values / size > 4096) size *= 2;
+    const int64_t size = kTile;
     std::vector<GradTile> tiles;
     std::vector<int32_t> first(static_cast<size_t>(d.workers) + 1, 0);
     int64_t count = 0;
@@ -279,6 +360,8 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
     }
     for (size_t w = 1; w < first.size(); ++w) first[w] = std::max(first[w], first[w - 1]);
     h.n_tiles = count;
+    h.few = true;
+    for (size_t w = 0; w + 1 < first.size(); ++w) h.few = h.few && first[w + 1] > first[w] && first[w + 1] - first[w] <= kThreads;
     int devices = 0;
     hipError_t err = hipGetDeviceCount(&devices);
     if (err != hipSuccess || devices < 1) return GBMUF_OK;  // host-side checks work without a GPU; the calls say EDEVICE
@@ -306,7 +389,8 @@ int launch(const void *fn, int64_t blocks, void **argv, const char *what, hipStr
     return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
 }
 
-int enqueue_norm(const gbmuf_grads_s *g, float *norms, hipStream_t stream)
+// The tiles' sums, and the norms unless the kernel after this one joins them (joined not nullptr).
+int enqueue_norm(const gbmuf_grads_s *g, float *norms, Norms *joined, hipStream_t stream)
 {
     const GradTensor *tensors = g->d_tensors;
     const GradTile *tiles = g->d_tiles;
@@ -314,7 +398,10 @@ int enqueue_norm(const gbmuf_grads_s *g, float *norms, hipStream_t stream)
     const int32_t *first = g->d_first;
     void *a1[] = {&tensors, &tiles, &partial}, *a2[] = {&partial, &first, &norms};
     const int rc = launch(reinterpret_cast<const void *>(norm_kernel), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
-    return rc != GBMUF_OK ? rc : launch(reinterpret_cast<const void *>(norm_join_kernel), g->workers, a2, "hipLaunchKernel(norm join)", stream);
+    if (rc != GBMUF_OK) return rc;
+    if (joined) *joined = Norms{norms, g->few ? partial : nullptr, first};
+    if (joined && g->few) return GBMUF_OK;
+    return launch(reinterpret_cast<const void *>(norm_join_kernel), g->workers, a2, "hipLaunchKernel(norm join)", stream);
 }
 
 // Where the arrays of a step lie.
@@ -398,7 +485,7 @@ int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream)
 {
     if (!grads || !norms) return GBMUF_EINVAL;
     const int rc = check_grads_device(grads);
-    return rc != GBMUF_OK ? rc : enqueue_norm(grads, norms, static_cast<hipStream_t>(stream));
+    return rc != GBMUF_OK ? rc : enqueue_norm(grads, norms, nullptr, static_cast<hipStream_t>(stream));
 }
 
 int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream)
@@ -414,10 +501,10 @@ int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float ma
     int rc = check_grads_device(src);
     if (rc != GBMUF_OK || (rc = check_grads_device(dst)) != GBMUF_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if ((rc = enqueue_norm(src, norms, s)) != GBMUF_OK) return rc;
+    Norms n{};
+    if ((rc = enqueue_norm(src, norms, &n, s)) != GBMUF_OK) return rc;
     const GradTensor *from = src->d_tensors, *to = dst->d_tensors;
     const GradTile *tiles = src->d_tiles;
-    const float *n = norms;
     void *argv[] = {&from, &to, &tiles, &n, &max_norm};
     return launch(reinterpret_cast<const void *>(clip_kernel), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
 }
@@ -442,9 +529,8 @@ int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, 
     }
     if ((rc = check_grads_device(grads)) != GBMUF_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (norms && (rc = enqueue_norm(grads, norms, s)) != GBMUF_OK) return rc;
+    if (norms && (rc = enqueue_norm(grads, norms, clip ? &a.norms : nullptr, s)) != GBMUF_OK) return rc;
     a.tensors = grads->d_tensors; a.tiles = grads->d_tiles;
-    a.norms = clip ? norms : nullptr;
     a.theta = theta->theta;
     a.rate = desc->rate; a.eps = desc->eps; a.most = desc->max_norm; a.skip_nonfinite = desc->skip_nonfinite;
     void *argv[] = {&a};
