@@ -5,7 +5,7 @@
 namespace gbmuf {
 namespace {
 
-constexpr int kDepth = 32;       // values of k per step
+constexpr int kDepth = 32;       // values of k per step (64 by tiles of 64 x 64 gain nothing, and cost the gradients half their waves)
 constexpr int kThreads = 256;
 
 template <int T>
@@ -20,7 +20,7 @@ __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
 }
 
 // One step's share of an operand: R rows of the result by kDepth values of k.  ALONG_K: k lies side by side in memory, LDS holds [row][k] with the 16-byte
-// chunk c of row r at place c ^ (r & 7); else rows do, and LDS holds [k][row].  Whatever lies beyond the matrix is zero.
+// chunk c of row r at place c ^ ((r / 2) & 7), 16 rows in all banks; else rows do, and LDS holds [k][row].  Whatever lies beyond the matrix is zero.
 template <int T, bool ALONG_K, int R, bool SLOPE = false>
 struct Stage {
     static constexpr int kChunks = R * kDepth / 4 / kThreads;
@@ -85,7 +85,7 @@ struct Stage {
     {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            float *to = ALONG_K ? lds + major(i) * kPitch + (((minor(i) >> 2) ^ (major(i) & 7)) << 2) : lds + major(i) * kPitch + minor(i);
+            float *to = ALONG_K ? lds + major(i) * kPitch + (((minor(i) >> 2) ^ ((major(i) >> 1) & 7)) << 2) : lds + major(i) * kPitch + minor(i);
             *reinterpret_cast<v4f *>(to) = v[i];
         }
     }
@@ -93,7 +93,7 @@ struct Stage {
     // the values of row `row` at k = 4 (2 t + half) + 0 .. 3
     static __device__ __forceinline__ v4f get(const float *lds, int row, int chunk)
     {
-        if constexpr (ALONG_K) return *reinterpret_cast<const v4f *>(lds + row * kPitch + ((chunk ^ (row & 7)) << 2));
+        if constexpr (ALONG_K) return *reinterpret_cast<const v4f *>(lds + row * kPitch + ((chunk ^ ((row >> 1) & 7)) << 2));
         const float *p = lds + chunk * 4 * kPitch + row;
         return v4f{p[0], p[kPitch], p[2 * kPitch], p[3 * kPitch]};
     }

@@ -73,8 +73,6 @@ __device__ __forceinline__ v4u chunk_of(const uint16_t *lds, int row, int chunk)
     return *reinterpret_cast<const v4u *>(lds + row * kStep + ((chunk ^ ((row >> 1) & 7)) * 8));
 }
 
-typedef short v4s __attribute__((ext_vector_type(4)));
-
 // The same for an operand whose k lie across its rows: a step is 64 rows of R columns, the 16-byte chunk c of row k at place c ^ ((k & 3) << 2), so
 // that 4 rows of 32 columns lie in all banks.  The transposing load hands 16 lanes the 4 x 16 values that their addresses cover, a column of 4 k each.
 template <int R, int THREADS>
@@ -116,18 +114,46 @@ struct StageAcross {
     }
 };
 
-// 8 k of column `first` + lane % 32, from k = 8 (2 turn + lane / 32) on
+// Where a lane's pieces of the columns first .. first + 31 lie in a stage, in bytes, for its first k of turn 0.
 template <int R>
-__device__ __forceinline__ v4u column_of(const uint16_t *lds, int first, int turn)
+__device__ __forceinline__ uint32_t column_place(int first)
 {
-    const int lane = threadIdx.x & 63, p = lane & 15, k = turn * 16 + (lane >> 5) * 8 + (p >> 2), c = first + ((lane >> 4) & 1) * 16 + (p & 3) * 4;
-    const auto at = [&](int row) {
-        return __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(
-                                                lds + row * R + (((c >> 3) ^ ((row & 3) << 2)) << 3) + (c & 4))));
-    };
-    const uint64_t lo = at(k), hi = at(k + 4);
-    return v4u{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+    const int lane = threadIdx.x & 63, p = lane & 15, k = (lane >> 5) * 8 + (p >> 2), c = first + ((lane >> 4) & 1) * 16 + (p & 3) * 4;
+    return static_cast<uint32_t>(k * R + (((c >> 3) ^ ((k & 3) << 2)) << 3) + (c & 4)) * 2;
 }
+
+// 8 k of a lane's column of each of N = 2, 4 or 6 fragments: four k at AT, four more 4 rows on.  One piece of assembly, with its wait: before
+// a transposing load that the compiler knows, it waits for every load on its way to LDS, and with that for the whole next step (4 x 8192 x 1024 over 5120
+// bf16 406 us).
+#define GBMUF_READ(lo, hi, at, k, k4) "ds_read_b64_tr_b16 %" #lo ", %" #at " offset:%" #k "\n\tds_read_b64_tr_b16 %" #hi ", %" #at " offset:%" #k4 "\n\t"
+#define GBMUF_TO(i) "=&v"(lo[i]), "=&v"(hi[i])
+template <int AT, int ROW>
+__device__ __forceinline__ void read_columns(const uint32_t (&at)[2], uint64_t (&lo)[2], uint64_t (&hi)[2])
+{
+    asm volatile(GBMUF_READ(0, 1, 4, 6, 7) GBMUF_READ(2, 3, 5, 6, 7) "s_waitcnt lgkmcnt(0)"
+                 : GBMUF_TO(0), GBMUF_TO(1)
+                 : "v"(at[0]), "v"(at[1]), "n"(AT), "n"(AT + 4 * ROW)
+                 : "memory");
+}
+template <int AT, int ROW>
+__device__ __forceinline__ void read_columns(const uint32_t (&at)[4], uint64_t (&lo)[4], uint64_t (&hi)[4])
+{
+    asm volatile(GBMUF_READ(0, 1, 8, 12, 13) GBMUF_READ(2, 3, 9, 12, 13) GBMUF_READ(4, 5, 10, 12, 13) GBMUF_READ(6, 7, 11, 12, 13) "s_waitcnt lgkmcnt(0)"
+                 : GBMUF_TO(0), GBMUF_TO(1), GBMUF_TO(2), GBMUF_TO(3)
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(AT), "n"(AT + 4 * ROW)
+                 : "memory");
+}
+template <int AT, int ROW>
+__device__ __forceinline__ void read_columns(const uint32_t (&at)[6], uint64_t (&lo)[6], uint64_t (&hi)[6])
+{
+    asm volatile(GBMUF_READ(0, 1, 12, 18, 19) GBMUF_READ(2, 3, 13, 18, 19) GBMUF_READ(4, 5, 14, 18, 19) GBMUF_READ(6, 7, 15, 18, 19)
+                     GBMUF_READ(8, 9, 16, 18, 19) GBMUF_READ(10, 11, 17, 18, 19) "s_waitcnt lgkmcnt(0)"
+                 : GBMUF_TO(0), GBMUF_TO(1), GBMUF_TO(2), GBMUF_TO(3), GBMUF_TO(4), GBMUF_TO(5)
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "n"(AT), "n"(AT + 4 * ROW)
+                 : "memory");
+}
+#undef GBMUF_READ
+#undef GBMUF_TO
 
 // What a wave needs of a step for one turn of matrix instructions: 16 of the 64 words of its rows (SPLIT: 16 leading and the 16
 // trailing parts).  m and n: the wave's first row of a and of b.
@@ -136,17 +162,39 @@ struct Turn {
     static constexpr int kParts = SPLIT ? 2 : 1;
     v4u x[kParts][FM], w[kParts][FN];
 
-    __device__ __forceinline__ void load(const uint16_t *lds, int m, int n, int turn)
+    template <int TURN>
+    __device__ __forceinline__ void load(const uint16_t *lds, int m, int n)
     {
         const int lane = threadIdx.x & 63;
         const uint16_t *la = lds, *lb = lds + TM * kStep;
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
-            const int c = p * 4 + turn * 2 + (lane >> 5);
+            const int c = p * 4 + TURN * 2 + (lane >> 5);
+            if constexpr (!(ACROSS & 2))
 #pragma unroll
-            for (int j = 0; j < FN; ++j) w[p][j] = ACROSS & 2 ? column_of<TN>(lb, n + j * 32, turn) : chunk_of(lb, n + j * 32 + (lane & 31), c);
+                for (int j = 0; j < FN; ++j) w[p][j] = chunk_of(lb, n + j * 32 + (lane & 31), c);
+            if constexpr (!(ACROSS & 1))
 #pragma unroll
-            for (int i = 0; i < FM; ++i) x[p][i] = ACROSS & 1 ? column_of<TM>(la, m + i * 32, turn) : chunk_of(la, m + i * 32 + (lane & 31), c);
+                for (int i = 0; i < FM; ++i) x[p][i] = chunk_of(la, m + i * 32 + (lane & 31), c);
+        }
+        if constexpr (ACROSS != 0) {
+            static_assert(ACROSS == 2 || (ACROSS == 3 && TM == TN), "b across its rows, or both");
+            constexpr int N = FN + (ACROSS & 1 ? FM : 0);
+            const uint32_t stage = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const uint16_t *)lds));
+            uint32_t at[N];
+            uint64_t lo[N], hi[N];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) at[j] = stage + TM * kStep * 2 + column_place<TN>(n + j * 32);
+#pragma unroll
+            for (int i = FN; i < N; ++i) at[i] = stage + column_place<TM>(m + (i - FN) * 32);
+            read_columns<TURN * 16 * TN * 2, TN * 2>(at, lo, hi);
+            const auto joined = [&](int i) {
+                return v4u{static_cast<uint32_t>(lo[i]), static_cast<uint32_t>(lo[i] >> 32), static_cast<uint32_t>(hi[i]), static_cast<uint32_t>(hi[i] >> 32)};
+            };
+#pragma unroll
+            for (int j = 0; j < FN; ++j) w[0][j] = joined(j);
+#pragma unroll
+            for (int i = FN; i < N; ++i) x[0][i - FN] = joined(i);
         }
     }
 
@@ -170,6 +218,16 @@ __device__ __forceinline__ void interleave()
         if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         interleave<READS, MFMAS, I + 1>();
+    }
+}
+
+// f(0), f(1) .. f(N - 1), the numbers known to the compiler
+template <int N, class F>
+__device__ __forceinline__ void repeat(F f)
+{
+    if constexpr (N > 0) {
+        repeat<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
     }
 }
 
@@ -208,7 +266,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    constexpr int kReads = (SPLIT ? 2 : 1) * (FM * (ACROSS & 1 ? 2 : 1) + FN * (ACROSS & 2 ? 2 : 1)), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
+    constexpr int kReads = (SPLIT ? 2 : 1) * ((ACROSS & 1 ? 0 : FM) + (ACROSS & 2 ? 0 : FN)), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
     Turn<T, SPLIT, TM, TN, FM, FN, ACROSS> turn[2];
     if (first < full) {
         sa.load(lds[0], first * kStep);
@@ -218,22 +276,21 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
             sa.load(lds[1], (first + 1) * kStep);
             sb.load(lds[1] + TM * kStep, (first + 1) * kStep);
         }
-        turn[0].load(lds[0], wm, wn, 0);
+        turn[0].template load<0>(lds[0], wm, wn);
         for (int s = first; s < full; ++s) {
             uint16_t *now = lds[(s - first) & 1], *next = lds[(s - first + 1) & 1];
-#pragma unroll
-            for (int t = 0; t + 1 < kTurns; ++t) {
-                turn[(t + 1) & 1].load(now, wm, wn, t + 1);
+            repeat<kTurns - 1>([&](auto t) {
+                turn[(t + 1) & 1].template load<t + 1>(now, wm, wn);
                 turn[t & 1].multiply(acc);
                 interleave<kReads, kMfmas>();
                 __builtin_amdgcn_sched_barrier(0);
-            }
+            });
             wait_and_meet();
             if (s + 2 < full) {
                 sa.load(now, (s + 2) * kStep);
                 sb.load(now + TM * kStep, (s + 2) * kStep);
             }
-            if (s + 1 < full) turn[0].load(next, wm, wn, 0);
+            if (s + 1 < full) turn[0].template load<0>(next, wm, wn);
             turn[(kTurns - 1) & 1].multiply(acc);
             interleave<kReads, kMfmas>();
             __builtin_amdgcn_sched_barrier(0);
@@ -244,11 +301,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
         sa.load_rest(lds[0], full * kStep, a.K);
         sb.load_rest(lds[0] + TM * kStep, full * kStep, a.K);
         __syncthreads();
-#pragma unroll
-        for (int t = 0; t < kTurns; ++t) {
-            turn[0].load(lds[0], wm, wn, t);
+        repeat<kTurns>([&](auto t) {
+            turn[0].template load<t>(lds[0], wm, wn);
             turn[0].multiply(acc);
-        }
+        });
     }
     __syncthreads();
     leave<TM, TN, WM, WN, SPLIT>(acc, &lds[0][0], a, share);
