@@ -21,6 +21,9 @@ __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
 
 // One step's share of an operand: R rows of the result by kDepth values of k.  ALONG_K: k lies side by side in memory, LDS holds [row][k] with the 16-byte
 // chunk c of row r at place c ^ ((r / 2) & 7), 16 rows in all banks; else rows do, and LDS holds [k][row].  Whatever lies beyond the matrix is zero.
+// Threads work in groups of 256, each on steps of its own.
+__device__ __forceinline__ int thread_of() { return static_cast<int>(threadIdx.x) & (kThreads - 1); }
+
 template <int T, bool ALONG_K, int R, bool SLOPE = false>
 struct Stage {
     static constexpr int kChunks = R * kDepth / 4 / kThreads;
@@ -31,12 +34,12 @@ struct Stage {
     static __device__ __forceinline__ int major(int i)
     {
         constexpr int per = (ALONG_K ? kDepth : R) / 4;
-        return (i * kThreads + static_cast<int>(threadIdx.x)) / per;
+        return (i * kThreads + thread_of()) / per;
     }
     static __device__ __forceinline__ int minor(int i)
     {
         constexpr int per = (ALONG_K ? kDepth : R) / 4;
-        return (i * kThreads + static_cast<int>(threadIdx.x)) % per * 4;
+        return (i * kThreads + thread_of()) % per * 4;
     }
 
     __device__ __forceinline__ void load(const Source &s, int64_t g, int row0, int k0, int rows, int K)
@@ -99,16 +102,18 @@ struct Stage {
     }
 };
 
-template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE>
+template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE, int GROUPS>
 constexpr size_t direct_lds()
 {
-    constexpr size_t stages = (Stage<T, A_ALONG_K, TILE>::kFloats + Stage<T, B_ALONG_K, TILE>::kFloats) * sizeof(float);
-    constexpr size_t out = leave_bytes<TILE, TILE, 2, 2>();
-    return stages > out ? stages : out;
+    constexpr size_t stages = GROUPS * (Stage<T, A_ALONG_K, TILE>::kFloats + Stage<T, B_ALONG_K, TILE>::kFloats) * sizeof(float);
+    constexpr size_t out = leave_bytes<TILE, TILE, 2, 2>(), parts = (GROUPS - 1) * TILE * TILE * sizeof(float), sums = GROUPS * kThreads * sizeof(v4f);
+    constexpr size_t most = stages > out ? stages : out, more = parts > sums ? parts : sums;
+    return most > more ? most : more;
 }
 
-// One tile of TILE x TILE by 2 x 2 waves.
-template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE, bool SLOPE>
+// One tile of TILE x TILE by 2 x 2 waves, or by GROUPS times as many that take every GROUPS-th step each and are added up in the end: a step
+// takes a microsecond or so however little it computes, and where there are few tiles nothing else hides that.
+template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE, bool SLOPE, int GROUPS>
 __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *lds)
 {
     constexpr int F = TILE / 64;
@@ -116,9 +121,11 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
     using B = Stage<T, B_ALONG_K, TILE>;
     const Share share = share_of<TILE, TILE>(a.t, id, (a.K + kDepth - 1) / kDepth);
     const int64_t g = share.at.g;
-    const int tn = share.at.tn, m0 = share.at.tm * TILE, n0 = tn * TILE, first = share.first, last = share.last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = (wave & 1) * (TILE / 2), wn = (wave >> 1) * (TILE / 2);
-    float *la = lds, *lb = lds + A::kFloats;
+    const int tn = share.at.tn, m0 = share.at.tm * TILE, n0 = tn * TILE;
+    const int group = GROUPS > 1 ? static_cast<int>(threadIdx.x) / kThreads : 0, first = share.first + group, last = share.last;
+    const int turns = (share.last - share.first + GROUPS - 1) / GROUPS;            // of every group, though its last may be empty
+    const int lane = threadIdx.x & 63, wave = thread_of() >> 6, wm = (wave & 1) * (TILE / 2), wn = (wave >> 1) * (TILE / 2);
+    float *la = lds + group * (A::kFloats + B::kFloats), *lb = la + A::kFloats;
     v16f acc[F][F];
 #pragma unroll
     for (int i = 0; i < F; ++i)
@@ -133,53 +140,57 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         x.load(a.a, g, m0, first * kDepth, a.t.M, a.K);
         w.load(a.b, g, n0, first * kDepth, a.t.N, a.K);
     }
-    for (int s = first; s < last; ++s) {
-        x.shape(a.a);
-        x.put(la);
-        w.put(lb);
-        if (A_ALONG_K && a.copy && tn == 0)
+    for (int turn = 0; turn < turns; ++turn) {
+        const int s = first + turn * GROUPS;
+        if (s < last) {
+            x.shape(a.a);
+            x.put(la);
+            w.put(lb);
+            if (A_ALONG_K && a.copy && tn == 0)
 #pragma unroll
-            for (int i = 0; i < A::kChunks; ++i) {
-                const int m = m0 + A::major(i), k = s * kDepth + A::minor(i);
-                if (m >= a.t.M) continue;
-                const int64_t at = g * a.copy_batch + m * a.copy_ld + k;
-                if (k + 4 <= a.K) write4<T>(a.copy, at, x.v[i]);
-                else
-                    for (int c = 0; c < 3; ++c)
-                        if (k + c < a.K) store_one(a.copy, at + c, T, x.v[i][c]);
-            }
-        if (!A_ALONG_K && a.sums)
+                for (int i = 0; i < A::kChunks; ++i) {
+                    const int m = m0 + A::major(i), k = s * kDepth + A::minor(i);
+                    if (m >= a.t.M) continue;
+                    const int64_t at = g * a.copy_batch + m * a.copy_ld + k;
+                    if (k + 4 <= a.K) write4<T>(a.copy, at, x.v[i]);
+                    else
+                        for (int c = 0; c < 3; ++c)
+                            if (k + c < a.K) store_one(a.copy, at + c, T, x.v[i][c]);
+                }
+            if (!A_ALONG_K && a.sums)
 #pragma unroll
-            for (int i = 0; i < A::kChunks; ++i) sums += x.v[i];      // a thread's rows are the same in every chunk
+                for (int i = 0; i < A::kChunks; ++i) sums += x.v[i];      // a thread's rows are the same in every chunk
+        }
         __syncthreads();
-        if (s + 1 < last) {
-            x.load(a.a, g, m0, (s + 1) * kDepth, a.t.M, a.K);
-            w.load(a.b, g, n0, (s + 1) * kDepth, a.t.N, a.K);
+        if (s + GROUPS < last) {
+            x.load(a.a, g, m0, (s + GROUPS) * kDepth, a.t.M, a.K);
+            w.load(a.b, g, n0, (s + GROUPS) * kDepth, a.t.N, a.K);
         }
+        if (s < last)
 #pragma unroll
-        for (int t = 0; t < kDepth / 8; ++t) {
-            v4f p[F], q[F];
+            for (int t = 0; t < kDepth / 8; ++t) {
+                v4f p[F], q[F];
 #pragma unroll
-            for (int i = 0; i < F; ++i) p[i] = A::get(la, wm + i * 32 + (lane & 31), 2 * t + (lane >> 5));
+                for (int i = 0; i < F; ++i) p[i] = A::get(la, wm + i * 32 + (lane & 31), 2 * t + (lane >> 5));
 #pragma unroll
-            for (int j = 0; j < F; ++j) q[j] = B::get(lb, wn + j * 32 + (lane & 31), 2 * t + (lane >> 5));
+                for (int j = 0; j < F; ++j) q[j] = B::get(lb, wn + j * 32 + (lane & 31), 2 * t + (lane >> 5));
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c)
 #pragma unroll
-                for (int i = 0; i < F; ++i)
+                    for (int i = 0; i < F; ++i)
 #pragma unroll
-                    for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[j][c], p[i][c], acc[i][j], 0, 0, 0);
-        }
+                        for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[j][c], p[i][c], acc[i][j], 0, 0, 0);
+            }
         __syncthreads();
     }
     if (!A_ALONG_K && a.sums && tn == 0) {
-        constexpr int per4 = TILE / 4, groups = kThreads / per4;     // threads t, t + per4 .. hold the same rows
+        constexpr int per4 = TILE / 4, same = GROUPS * kThreads / per4;      // threads t, t + per4 .. hold the same rows
         reinterpret_cast<v4f *>(lds)[threadIdx.x] = sums;
         __syncthreads();
         if (threadIdx.x < TILE) {
             float v = 0.0f;
-#pragma unroll
-            for (int i = 0; i < groups; ++i) v += lds[i * TILE + threadIdx.x];
+#pragma unroll 8
+            for (int i = 0; i < same; ++i) v += lds[i * TILE + threadIdx.x];
             const int m = m0 + static_cast<int>(threadIdx.x);
             if (m < a.t.M) {
                 const int64_t at = g * a.sums_batch + m;
@@ -189,41 +200,59 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         }
         __syncthreads();
     }
+    if constexpr (GROUPS > 1) {
+        static_assert(F == 1, "one result of 32 x 32 a wave");
+        v4f *part = reinterpret_cast<v4f *>(lds);
+        if (group > 0)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                part[((group - 1) * 4 + q) * kThreads + thread_of()] = v4f{acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int i = 0; i < (GROUPS - 1) * 4; ++i) {
+                const v4f v = part[i * kThreads + thread_of()];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[0][0][i % 4 * 4 + c] += v[c];
+            }
+        __syncthreads();
+        if (group > 0) return;
+    }
     leave<TILE, TILE, 2, 2, false>(acc, lds, a, share);
 }
 
-template <int T, int TILE>
-__global__ __launch_bounds__(kThreads) void direct_forward_kernel(DirectArgs a)
+template <int T, int GROUPS>
+__global__ __launch_bounds__(GROUPS *kThreads) void direct_forward_kernel(DirectArgs a)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, true, true, TILE>() / 4];
-    direct_tile<T, true, true, TILE, false>(a, static_cast<int>(blockIdx.x), lds);
+    __shared__ __align__(16) float lds[direct_lds<T, true, true, 64, GROUPS>() / 4];
+    direct_tile<T, true, true, 64, false, GROUPS>(a, static_cast<int>(blockIdx.x), lds);
 }
 
 // dx = dz w (dz lies along the sum, w across it) and dw = dz' x (both across), in one launch: the first workgroups are dx's.
-template <int T, int TILE>
-__global__ __launch_bounds__(kThreads) void direct_backward_kernel(DirectArgs dx, DirectArgs dw)
+template <int T, int TILE, int GROUPS>
+__global__ __launch_bounds__(GROUPS *kThreads) void direct_backward_kernel(DirectArgs dx, DirectArgs dw)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, false, false, TILE>() / 4];
-    static_assert(direct_lds<T, false, false, TILE>() >= direct_lds<T, true, false, TILE>(), "one piece of LDS for both");
+    __shared__ __align__(16) float lds[direct_lds<T, false, false, TILE, GROUPS>() / 4];
+    static_assert(direct_lds<T, false, false, TILE, GROUPS>() >= direct_lds<T, true, false, TILE, GROUPS>(), "one piece of LDS for both");
     const int n = dx.t.blocks(), id = static_cast<int>(blockIdx.x);
-    if (id < n) direct_tile<T, true, false, TILE, true>(dx, id, lds);
-    else direct_tile<T, false, false, TILE, true>(dw, id - n, lds);
+    if (id < n) direct_tile<T, true, false, TILE, true, GROUPS>(dx, id, lds);
+    else direct_tile<T, false, false, TILE, true, GROUPS>(dw, id - n, lds);
 }
+
+// Up to one workgroup a CU: four groups of threads each.
+int form_of(int tile, int32_t blocks) { return tile == 128 ? 2 : blocks <= 256 ? 0 : 1; }
 
 }  // namespace
 
-int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream_t stream)
+int launch_direct_forward(const DirectArgs &a, hipStream_t stream)
 {
     const int32_t blocks = a.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
-    using Fn = void (*)(DirectArgs);
-    static constexpr Fn fns[3][2] = {{direct_forward_kernel<kF32, 64>, direct_forward_kernel<kF32, 128>},
-                                     {direct_forward_kernel<kBf16, 64>, direct_forward_kernel<kBf16, 128>},
-                                     {direct_forward_kernel<kF16, 64>, direct_forward_kernel<kF16, 128>}};
+    const bool grouped = form_of(64, blocks) == 0;
     DirectArgs args = a;
     void *argv[] = {&args};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][tile == 128]), dim3(static_cast<unsigned>(blocks)), dim3(kThreads),
-                                           argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(grouped ? direct_forward_kernel<kF32, 4> : direct_forward_kernel<kF32, 1>),
+                                           dim3(static_cast<unsigned>(blocks)), dim3(grouped ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct product)", err, GBMUF_EDEVICE);
 }
 
@@ -232,13 +261,14 @@ int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t t
     const int32_t blocks = dx.t.blocks() + dw.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
     using Fn = void (*)(DirectArgs, DirectArgs);
-    static constexpr Fn fns[3][2] = {{direct_backward_kernel<kF32, 64>, direct_backward_kernel<kF32, 128>},
-                                     {direct_backward_kernel<kBf16, 64>, direct_backward_kernel<kBf16, 128>},
-                                     {direct_backward_kernel<kF16, 64>, direct_backward_kernel<kF16, 128>}};
+    static constexpr Fn fns[3][3] = {{direct_backward_kernel<kF32, 64, 4>, direct_backward_kernel<kF32, 64, 1>, direct_backward_kernel<kF32, 128, 1>},
+                                     {direct_backward_kernel<kBf16, 64, 4>, direct_backward_kernel<kBf16, 64, 1>, direct_backward_kernel<kBf16, 128, 1>},
+                                     {direct_backward_kernel<kF16, 64, 4>, direct_backward_kernel<kF16, 64, 1>, direct_backward_kernel<kF16, 128, 1>}};
+    const int form = form_of(tile, blocks);
     DirectArgs x = dx, w = dw;
     void *argv[] = {&x, &w};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][tile == 128]), dim3(static_cast<unsigned>(blocks)), dim3(kThreads),
-                                           argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][form]), dim3(static_cast<unsigned>(blocks)),
+                                           dim3(form == 0 ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct gradients)", err, GBMUF_EDEVICE);
 }
 

@@ -105,12 +105,15 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(DirectArgs a)
     }
 }
 
+// form 0: few tiles, 16 waves; 1: 16 rows of w a workgroup; 2, 3: 32, 64 rows
 template <int T>
-void (*pick(int mt, bool wide, bool many))(DirectArgs)
+void (*pick(int mt, int form))(DirectArgs)
 {
-    if (many) return mt == 1 ? few_kernel<T, 1, 1, 16> : mt == 2 ? few_kernel<T, 2, 1, 16> : few_kernel<T, 4, 1, 16>;
-    if (wide) return mt == 1 ? few_kernel<T, 1, 2, 4> : mt == 2 ? few_kernel<T, 2, 2, 4> : few_kernel<T, 4, 2, 4>;
-    return mt == 1 ? few_kernel<T, 1, 1, 4> : mt == 2 ? few_kernel<T, 2, 1, 4> : few_kernel<T, 4, 1, 4>;
+    static constexpr void (*fns[3][4])(DirectArgs) = {
+        {few_kernel<T, 1, 1, 16>, few_kernel<T, 1, 1, 4>, few_kernel<T, 1, 2, 4>, nullptr},
+        {few_kernel<T, 2, 1, 16>, few_kernel<T, 2, 1, 4>, T == kF32 ? few_kernel<T, 2, 2, 4> : nullptr, T == kF32 ? nullptr : few_kernel<T, 2, 4, 4>},
+        {few_kernel<T, 4, 1, 16>, few_kernel<T, 4, 1, 4>, nullptr, few_kernel<T, 4, 4, 4>}};
+    return fns[mt == 4 ? 2 : mt - 1][form];
 }
 
 }  // namespace
@@ -120,13 +123,18 @@ int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream)
     if (a.t.M <= 0 || a.t.N <= 0 || a.t.batch <= 0) return GBMUF_OK;
     const int mt = a.t.M <= 16 ? 1 : a.t.M <= 32 ? 2 : 4;
     const int64_t narrow = (a.t.N + 15) / 16;
-    const bool wide = narrow * a.t.batch >= 2048, many = !wide && narrow * a.t.batch < 256 && a.K >= 1024;
-    const int64_t blocks = wide ? (a.t.N + 31) / 32 : narrow;
-    const auto fn = type == kF32 ? pick<kF32>(mt, wide, many) : type == kBf16 ? pick<kBf16>(mt, wide, many) : pick<kF16>(mt, wide, many);
+    // A workgroup that takes more rows of w reads x less often.  us for 50,000 rows of 1024, 16 / 32 / 64 rows a workgroup: bf16, 8 rows of x 22 / 20 /
+    // 21, 20 rows 31 / 25 / 23, 64 rows 60 / 41 / 35; f32, 8 rows 48 / 47 / 46, 20 rows 72 / 57 / 64, 64 rows 131 / 112 / 108.  Few workgroups share
+    // long sums between 16 waves.
+    const bool many = narrow * a.t.batch >= 2048, widest = mt == 4 || (mt == 2 && type != kF32);
+    const int form = many ? (widest ? 3 : 2) : narrow * a.t.batch < 256 && a.K >= 1024 ? 0 : 1;
+    const int rows = form == 3 ? 64 : form == 2 ? 32 : 16;
+    const int64_t blocks = (a.t.N + rows - 1) / rows;
+    const auto fn = type == kF32 ? pick<kF32>(mt, form) : type == kBf16 ? pick<kBf16>(mt, form) : pick<kF16>(mt, form);
     DirectArgs args = a;
     void *argv[] = {&args};
     const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.t.batch)),
-                                           dim3(many ? 1024 : 256), argv, 0, stream);
+                                           dim3(form == 0 ? 1024 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(few rows)", err, GBMUF_EDEVICE);
 }
 

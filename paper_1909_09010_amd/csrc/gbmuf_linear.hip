@@ -152,7 +152,7 @@ Cut cut(int tile, int64_t M, int64_t N, int64_t batch, int64_t steps, int64_t sl
     if (most < 2) return c;
     const int64_t each = (steps + most - 1) / most, splits = (steps + each - 1) / each, partial = rest * splits * tile * tile;
     // another launch, and writing and reading the parts at 4 TB/s
-    const double cost = static_cast<double>(tiles / slots * steps + each) * round + 5.0 + static_cast<double>(partial) * 8.0 / 4e6;
+    const double cost = static_cast<double>(tiles / slots * steps + each) * round + 3.0 + static_cast<double>(partial) * 8.0 / 4e6;
     if (cost >= c.cost) return c;
     c.t.whole = static_cast<int32_t>(tiles - rest);
     c.t.splits = static_cast<int32_t>(splits);
@@ -235,13 +235,15 @@ DirectArgs direct_args(const Source &a, const Source &b, int64_t K, const Cut &c
     return d;
 }
 
-// Tiles of 128 x 128 where there is one for every CU, else of 64 x 64, whose sums are cut (where `may_cut`) until there are two for every CU.  A step of a 64 x 64 tile takes 0.8 us or so, waits included.
+// The sums of tiles are cut (where `may_cut`) where these are fewer than CUs and long.  A step of 64 x 64 is 0.43 us of a CU's f32 matrix instructions.
 Cut direct_cut(int tile, int64_t M, int64_t N, int64_t K, int64_t batch, bool may_cut)
 {
     const int64_t steps = (K + 31) / 32, tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile) * batch;
-    return cut(tile, M, N, batch, steps, may_cut && tiles < 256 ? 512 : std::max<int64_t>(tiles, 1), 0.8);
+    return cut(tile, M, N, batch, steps, may_cut && tiles < 256 ? 256 : std::max<int64_t>(tiles, 1), 0.5);
 }
 
+// Gradients: tiles of 128 x 128 where there is one for every CU, else of 64 x 64 (8 x 250 x 1000 x 400 f32 79 and 84 us).  The forward takes 64 x 64 always
+// (8 x 250 x 2000 x 400 f32 45 and 41 us).
 int tile_of(int64_t M, int64_t N, int64_t batch)
 {
     return (M + 127) / 128 * ((N + 127) / 128) * batch >= 256 ? 128 : 64;
@@ -260,6 +262,19 @@ double operations(const gbmuf_linear_desc_t &d)
 //   gradients f32: 1 x 200 x 1024 x 512 21 / 54, 4 x 200 x 1024 x 512 42 / 63, 8 x 128 x 2600 x 650 153 / 138, 4 x 512 x 1024 x 1024 129 / 92
 //   gradients bf16: 1 x 200 x 1024 x 512 23 / 36, 4 x 200 x 1024 x 512 47 / 38
 bool takes_direct_forward(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && operations(d) <= 4e9; }
+
+// What up to 64 rows take.  The kernel for few rows reads each matrix once in one launch, but for more than 16 rows of one the matrix cores (f32) or
+// the readings of x are what it waits for, where there are many outputs.  us, few rows / tiles of f32 / of 16 bits, 1024 to 50,000 outputs: f32, 20
+// rows 57 / - / -, 64 rows 108 / 90 / -; bf16, 8 rows 20 / - / 22, 20 rows 25 / - / 22, 64 rows 41 / - / 23 (without copies, where rows lie on 16 bytes).
+enum class Few { kNo, kAlways, kUnlessAligned, kDirect };
+Few few_of(const gbmuf_linear_desc_t &d)
+{
+    if (d.rows > kFewRows) return Few::kNo;
+    const int64_t tiles = (d.out_features + 127) / 128 * d.batch;
+    if (d.rows <= 16 || tiles < 256) return Few::kAlways;
+    if (d.dtype == GBMUF_F32) return d.rows > 32 ? Few::kDirect : Few::kAlways;
+    return Few::kUnlessAligned;
+}
 
 bool takes_direct_backward(const gbmuf_linear_desc_t &d) { return operations(d) <= (d.dtype == GBMUF_F32 ? 2.5e9 : 5e8); }
 
@@ -280,15 +295,16 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
         e.res = io->residual.data; e.ldr = io->residual.ld; e.r_batch = io->residual.batch_stride;
         e.act = d.activation; e.place = d.residual;
     }
-    if (M <= kFewRows || takes_direct_forward(d)) {
-        const int tile = tile_of(M, N, G);
-        const Cut c = direct_cut(tile, M, N, K, G, M > kFewRows);
+    const Few few = few_of(d);
+    const bool is_few = few == Few::kAlways || (few == Few::kUnlessAligned && io && !(lies_well(io->x) && lies_well(io->w)));
+    if (is_few || takes_direct_forward(d) || few == Few::kDirect) {
+        const Cut c = direct_cut(64, M, N, K, G, !is_few);
         DirectArgs f = direct_args(source_of(io ? io->x : none), source_of(io ? io->w : none), K, c, e);
-        if (M <= kFewRows) return io ? launch_few(f, type, stream) : GBMUF_OK;
+        if (is_few) return io ? launch_few(f, type, stream) : GBMUF_OK;
         f.t.partial = space.take<float>(c.partial);
         if (!io) return GBMUF_OK;
-        const int rc = launch_direct_forward(f, type, tile, stream);
-        return rc != GBMUF_OK ? rc : launch_join(JoinArgs{f.t, tile, 0, e}, stream);
+        const int rc = launch_direct_forward(f, stream);
+        return rc != GBMUF_OK ? rc : launch_join(JoinArgs{f.t, 64, 0, e}, stream);
     }
     const Cut s = shape_of(M, N, K, G, split);
     float *partial = space.take<float>(s.partial);
@@ -297,7 +313,7 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     const LayArgs lx = source(xm, M, K, G, type), lw = source(wm, N, K, G, type);
     Operand x{static_cast<const uint16_t *>(xm.data), xm.ld, xm.batch_stride, nullptr, 0, false, false};
     Operand w{static_cast<const uint16_t *>(wm.data), wm.ld, wm.batch_stride, nullptr, 0, false, false};
-    const bool lay_x = split || !io || !lies_well(xm), lay_w = split || !io || !lies_well(wm);
+    const bool may_lay = few == Few::kNo, lay_x = split || (may_lay && (!io || !lies_well(xm))), lay_w = split || (may_lay && (!io || !lies_well(wm)));
     if (lay_x) x = packed(space, M, K, G, lx.batch, split, max);
     if (lay_w) w = packed(space, N, K, G, lw.batch, split, max + G * M);
     if (!io) return GBMUF_OK;

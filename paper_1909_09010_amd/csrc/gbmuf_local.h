@@ -105,7 +105,7 @@ constexpr int64_t packed_words(int64_t n, bool split) { return split ? (n + 31) 
 int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t stream);   // tile: 128 or 256
 int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream);
 constexpr int kFewRows = 64;
-int launch_direct_forward(const DirectArgs &a, int32_t type, int tile, hipStream_t stream);
+int launch_direct_forward(const DirectArgs &a, hipStream_t stream);          // f32, tiles of 64 x 64
 int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream);
 int launch_join(const JoinArgs &a, hipStream_t stream);
 int launch_copy(const LayArgs &a, hipStream_t stream);
