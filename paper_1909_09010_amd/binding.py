@@ -158,6 +158,7 @@ def _load() -> ctypes.CDLL:
 
 
 _lib = _load()
+_linear, _linear_backward = _lib.gbmuf_linear, _lib.gbmuf_linear_backward        # calls that take microseconds: no look-up each time
 
 
 def lib() -> ctypes.CDLL:
@@ -399,19 +400,19 @@ class Linear:
                             _matrix(dy, G, M, N, t, "dy"), _matrix(dx, G, M, K, t, "dx"), _matrix(dw, G, N, K, gt, "dw"),
                             _vector(dbias, G, N, gt, "dbias"), _matrix(dresidual, G, M, N, t, "dresidual"))
 
-    @staticmethod
-    def _space(workspace):
-        return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-
     def forward(self, io: LinearIo, workspace=None, stream=None) -> None:
-        p, n = self._space(workspace)
-        rc = _lib.gbmuf_linear(self._at, ctypes.byref(io), p, n, _stream(stream))
+        if workspace is None:
+            rc = _linear(self._at, ctypes.byref(io), None, 0, _stream(stream))
+        else:
+            rc = _linear(self._at, ctypes.byref(io), workspace.data_ptr(), workspace.nbytes, _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_linear")
 
     def backward(self, io: LinearGradIo, workspace=None, stream=None) -> None:
-        p, n = self._space(workspace)
-        rc = _lib.gbmuf_linear_backward(self._at, ctypes.byref(io), p, n, _stream(stream))
+        if workspace is None:
+            rc = _linear_backward(self._at, ctypes.byref(io), None, 0, _stream(stream))
+        else:
+            rc = _linear_backward(self._at, ctypes.byref(io), workspace.data_ptr(), workspace.nbytes, _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_linear_backward")
 

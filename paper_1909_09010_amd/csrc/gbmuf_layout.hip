@@ -7,6 +7,15 @@ namespace {
 
 constexpr int kT = kLayTile;
 
+// The source that workgroup `block` works on, and its number among that source's.
+__device__ __forceinline__ const LayArgs &source_of(const LaySet &set, int &block)
+{
+    int i = 0;
+    while (i + 1 < set.n && block >= set.first[i + 1]) ++i;
+    block -= set.first[i];
+    return set.a[i];
+}
+
 // Up to 8 values (r, c) .. of a source, zeros behind the row's end.
 template <int T>
 __device__ __forceinline__ Eight row_read(const void *p, int64_t at, int left)
@@ -33,12 +42,13 @@ __device__ __forceinline__ void row_write(void *p, int64_t at, int left, const E
 // 256 columns, a thread 8 columns of every eighth row.  Bound by HBM: one reading (two with an activation) and one writing.
 // ---------------------------------------------------------------------------------------
 template <int T>
-__global__ __launch_bounds__(256) void copy_kernel(LayArgs a)
+__global__ __launch_bounds__(256) void copy_kernel(LaySet set)
 {
+    int id = static_cast<int>(blockIdx.x);
+    const LayArgs &a = source_of(set, id);
     __shared__ float sums[8][256];
     const int width = a.plain ? static_cast<int>(a.plain_ld) : a.C;        // zeros up to the end of the copy's rows
     const int tiles_c = (width + 255) / 256, tiles_r = (a.R + kT - 1) / kT;
-    int id = static_cast<int>(blockIdx.x);
     const int64_t g = id / (tiles_c * tiles_r);
     id -= static_cast<int>(g) * tiles_c * tiles_r;
     const int tr = id / tiles_c, c0 = id % tiles_c * 256, c = c0 + static_cast<int>(threadIdx.x & 31) * 8, left = a.C - c;
@@ -103,9 +113,11 @@ __device__ __forceinline__ uint32_t magnitude(const Eight &v)
 // Rows of up to 512 N values, a wave each, which holds its row in registers: read once, its largest magnitude found, taken apart and written
 // once.
 template <int N>
-__global__ __launch_bounds__(256) void rows_kernel(LayArgs a)
+__global__ __launch_bounds__(256) void rows_kernel(LaySet set)
 {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    int id = static_cast<int>(blockIdx.x);
+    const LayArgs &a = source_of(set, id);
+    const int64_t row = static_cast<int64_t>(id) * 4 + (threadIdx.x >> 6);
     if (row >= static_cast<int64_t>(a.R) * a.batch) return;
     const int64_t g = row / a.R, r = row - g * a.R;
     const int lane = threadIdx.x & 63, width = static_cast<int>(a.plain_ld / 2);
@@ -149,11 +161,12 @@ __device__ __forceinline__ void read_tile(const LayArgs &a, int64_t g, int r0, i
 
 // Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  Magnitudes compare as integers, and a maximum does not depend on
 // the order of the atomics.
-__global__ __launch_bounds__(256) void stats_kernel(LayArgs a)
+__global__ __launch_bounds__(256) void stats_kernel(LaySet set)
 {
+    int id = static_cast<int>(blockIdx.x);
+    const LayArgs &a = source_of(set, id);
     __shared__ float tile[kT][kT + 1];
     const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
-    int id = static_cast<int>(blockIdx.x);
     const int64_t g = id / (tiles_c * tiles_r);
     id -= static_cast<int>(g) * tiles_c * tiles_r;
     const int tr = id / tiles_c, r0 = tr * kT, c0 = id % tiles_c * kT;
@@ -189,11 +202,12 @@ __global__ __launch_bounds__(256) void stats_kernel(LayArgs a)
 }
 
 // The copies along rows and along columns from one reading.
-__global__ __launch_bounds__(256) void lay_kernel(LayArgs a)
+__global__ __launch_bounds__(256) void lay_kernel(LaySet set)
 {
+    int id = static_cast<int>(blockIdx.x);
+    const LayArgs &a = source_of(set, id);
     __shared__ float tile[kT][kT + 1];
     const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
-    int id = static_cast<int>(blockIdx.x);
     const int64_t g = id / (tiles_c * tiles_r);
     id -= static_cast<int>(g) * tiles_c * tiles_r;
     const int r0 = id / tiles_c * kT, c0 = id % tiles_c * kT;
@@ -256,27 +270,50 @@ int launch_256(void (*fn)(Args), const Args &a, int64_t blocks, const char *what
     return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
 }
 
-int64_t lay_blocks(const LayArgs &a)
+int64_t tiles_over(int64_t rows, int64_t columns, int64_t wide, int64_t batch) { return (columns + wide - 1) / wide * ((rows + kT - 1) / kT) * batch; }
+
+// One launch over the workgroups of all sources; blocks_of(l): how many l takes.
+template <class BlocksOf>
+int launch_set(void (*fn)(LaySet), const LaySet &set, BlocksOf blocks_of, const char *what, hipStream_t stream)
 {
-    return static_cast<int64_t>((a.C + kT - 1) / kT) * ((a.R + kT - 1) / kT) * a.batch;
+    LaySet s{};
+    int64_t blocks = 0;
+    for (int i = 0; i < set.n; ++i) {
+        const int64_t n = blocks_of(set.a[i]);
+        if (n <= 0) continue;
+        s.first[s.n] = static_cast<int32_t>(blocks);
+        s.add(set.a[i]);
+        blocks += n;
+        if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    }
+    return launch_256(fn, s, blocks, what, stream);
 }
 
 }  // namespace
 
-int launch_stats(const LayArgs &a, hipStream_t stream) { return launch_256(stats_kernel, a, lay_blocks(a), "hipLaunchKernel(stats)", stream); }
-int launch_lay(const LayArgs &a, hipStream_t stream) { return launch_256(lay_kernel, a, lay_blocks(a), "hipLaunchKernel(lay out)", stream); }
-
-int launch_rows(const LayArgs &a, hipStream_t stream)
+int launch_stats(const LaySet &set, hipStream_t stream)
 {
-    const int64_t blocks = (static_cast<int64_t>(a.R) * a.batch + 3) / 4;
-    const auto fn = a.C <= 1024 ? rows_kernel<2> : a.C <= 2048 ? rows_kernel<4> : rows_kernel<8>;
-    return launch_256(fn, a, blocks, "hipLaunchKernel(rows)", stream);
+    return launch_set(stats_kernel, set, [](const LayArgs &a) { return tiles_over(a.R, a.C, kT, a.batch); }, "hipLaunchKernel(stats)", stream);
 }
 
-int launch_copy(const LayArgs &a, hipStream_t stream)
+int launch_lay(const LaySet &set, hipStream_t stream)
 {
-    const int64_t width = a.plain ? a.plain_ld : a.C, blocks = (width + 255) / 256 * ((a.R + kT - 1) / kT) * a.batch;
-    return launch_256(a.type == kBf16 ? copy_kernel<kBf16> : copy_kernel<kF16>, a, blocks, "hipLaunchKernel(copy)", stream);
+    return launch_set(lay_kernel, set, [](const LayArgs &a) { return tiles_over(a.R, a.C, kT, a.batch); }, "hipLaunchKernel(lay out)", stream);
+}
+
+int launch_rows(const LaySet &set, hipStream_t stream)
+{
+    int32_t longest = 0;
+    for (int i = 0; i < set.n; ++i) longest = set.a[i].C > longest ? set.a[i].C : longest;
+    return launch_set(longest <= 1024 ? rows_kernel<2> : longest <= 2048 ? rows_kernel<4> : rows_kernel<8>, set,
+                      [](const LayArgs &a) { return (static_cast<int64_t>(a.R) * a.batch + 3) / 4; }, "hipLaunchKernel(rows)", stream);
+}
+
+int launch_copy(const LaySet &set, hipStream_t stream)
+{
+    if (set.n == 0) return GBMUF_OK;
+    return launch_set(set.a[0].type == kBf16 ? copy_kernel<kBf16> : copy_kernel<kF16>, set,
+                      [](const LayArgs &a) { return tiles_over(a.R, a.plain ? a.plain_ld : a.C, 256, a.batch); }, "hipLaunchKernel(copy)", stream);
 }
 
 int launch_column_sums(const SumArgs &a, hipStream_t stream)

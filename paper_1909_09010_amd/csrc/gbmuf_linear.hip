@@ -89,12 +89,15 @@ int check_desc(const gbmuf_linear_desc_t *d)
     return GBMUF_OK;
 }
 
+// Asked once: a process has a GPU or has none.
 int check_device()
 {
-    int n = 0;
-    const hipError_t err = hipGetDeviceCount(&n);
-    if (err != hipSuccess || n < 1) return hip_failed("hipGetDeviceCount", err == hipSuccess ? hipErrorNoDevice : err, GBMUF_EDEVICE);
-    return GBMUF_OK;
+    static const hipError_t status = [] {
+        int n = 0;
+        const hipError_t err = hipGetDeviceCount(&n);
+        return err == hipSuccess && n < 1 ? hipErrorNoDevice : err;
+    }();
+    return status == hipSuccess ? GBMUF_OK : hip_failed("hipGetDeviceCount", status, GBMUF_EDEVICE);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -319,17 +322,19 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     if (!io) return GBMUF_OK;
     int rc = GBMUF_OK;
     if (split && !(K > 0 && K <= kLongestRow) && (rc = launch_zero(max, G * (M + N), stream)) != GBMUF_OK) return rc;
+    LaySet set;
     for (int i = 0; i < 2; ++i) {
         if (!(i == 0 ? lay_x : lay_w)) continue;
         LayArgs l = i == 0 ? lx : lw;
         const Operand &o = i == 0 ? x : w;
         l.row_max = o.max;
         l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
-        if (!split) rc = launch_copy(l, stream);
-        else if (K > 0 && K <= kLongestRow) rc = launch_rows(l, stream);
-        else if ((rc = launch_stats(l, stream)) == GBMUF_OK) rc = launch_lay(l, stream);
-        if (rc != GBMUF_OK) return rc;
+        set.add(l);
     }
+    if (!split) rc = launch_copy(set, stream);
+    else if (K > 0 && K <= kLongestRow) rc = launch_rows(set, stream);
+    else if ((rc = launch_stats(set, stream)) == GBMUF_OK) rc = launch_lay(set, stream);
+    if (rc != GBMUF_OK) return rc;
     return run_product(x, w, K, type, e, s, partial, stream);
 }
 
@@ -406,20 +411,24 @@ int backward_split(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *i
     lz.row_max = dx ? z.max : nullptr;
     lz.col_max = dw ? zt.max : nullptr;
     lz.col_sums = db ? sums : nullptr;
-    if ((dx || dw || db) && (rc = launch_stats(lz, stream)) != GBMUF_OK) return rc;
-    if (db && (rc = sum_columns(d, at.dbias, sums, kF32, stream)) != GBMUF_OK) return rc;
     if (dx) { lz.plain = const_cast<uint16_t *>(z.p); lz.plain_ld = z.ld; lz.plain_batch = z.batch; }
     if (dw) { lz.trans = const_cast<uint16_t *>(zt.p); lz.trans_ld = zt.ld; lz.trans_batch = zt.batch; }
     lz.dz = at.dresidual.data; lz.dz_ld = at.dresidual.ld; lz.dz_batch = at.dresidual.batch_stride;
-    if ((dx || dw || dr) && (rc = launch_lay(lz, stream)) != GBMUF_OK) return rc;
+    LaySet stats, lay;
+    if (dx || dw || db) stats.add(lz);
+    if (dx || dw || dr) lay.add(lz);
     for (int i = 0; i < 2; ++i) {
         if (!(i == 0 ? dx : dw)) continue;
         LayArgs l = i == 0 ? lw : lx;
         const Operand &o = i == 0 ? wt : xt;
         l.col_max = o.max;
         l.trans = const_cast<uint16_t *>(o.p); l.trans_ld = o.ld; l.trans_batch = o.batch;
-        if ((rc = launch_stats(l, stream)) != GBMUF_OK || (rc = launch_lay(l, stream)) != GBMUF_OK) return rc;
+        stats.add(l);
+        lay.add(l);
     }
+    if ((rc = launch_stats(stats, stream)) != GBMUF_OK) return rc;
+    if (db && (rc = sum_columns(d, at.dbias, sums, kF32, stream)) != GBMUF_OK) return rc;
+    if ((rc = launch_lay(lay, stream)) != GBMUF_OK) return rc;
     if (dx && (rc = run_product(z, wt, N, kF32, into(at.dx, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
     return dw ? run_product(zt, xt, M, kF32, weight_grad(d, at.dw, kF32), sw, partial, stream) : rc;
 }
@@ -452,18 +461,18 @@ int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, 
     zt.across = w.across = x.across = true;
     if (!io) return GBMUF_OK;
 
-    const auto copy = [&](LayArgs l, const Operand &o) {
-        l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
-        return launch_copy(l, stream);
+    LaySet set;
+    const auto add = [&](LayArgs l, const Operand &o, bool copy) {
+        if (copy) { l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch; }
+        set.add(l);
     };
-    int rc = GBMUF_OK;
     lz.col_sums = db ? sums : nullptr;
     lz.dz = at.dresidual.data; lz.dz_ld = at.dresidual.ld; lz.dz_batch = at.dresidual.batch_stride;
-    if (copy_z) rc = copy(lz, z);
-    else if (db || dr) rc = launch_copy(lz, stream);
+    if (copy_z || db || dr) add(lz, z, copy_z);
+    if (copy_w) add(lw, w, true);
+    if (copy_x) add(lx, x, true);
+    int rc = launch_copy(set, stream);
     if (rc == GBMUF_OK && db) rc = sum_columns(d, at.dbias, sums, grad_type, stream);
-    if (rc == GBMUF_OK && copy_w) rc = copy(lw, w);
-    if (rc == GBMUF_OK && copy_x) rc = copy(lx, x);
     if (rc == GBMUF_OK && dx) rc = run_product(z, w, N, type, into(at.dx, type), sx, partial, stream);
     if (rc == GBMUF_OK && dw) rc = run_product(zt, x, M, type, weight_grad(d, at.dw, grad_type), sw, partial, stream);
     return rc;

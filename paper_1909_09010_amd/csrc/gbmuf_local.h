@@ -92,6 +92,15 @@ struct LayArgs {
 };
 constexpr int kLayTile = 64, kLongestRow = 4096;
 
+// Up to three sources of one type, laid out by one launch: those of one product or of a layer's gradients.
+struct LaySet {
+    LayArgs a[3];
+    int32_t first[4];            // first workgroup of each, set by the launch
+    int32_t n = 0;
+    int32_t reserved = 0;
+    void add(const LayArgs &l) { a[n++] = l; }
+};
+
 struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
     const float *sums;
     void *out;
@@ -108,10 +117,10 @@ constexpr int kFewRows = 64;
 int launch_direct_forward(const DirectArgs &a, hipStream_t stream);          // f32, tiles of 64 x 64
 int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream);
 int launch_join(const JoinArgs &a, hipStream_t stream);
-int launch_copy(const LayArgs &a, hipStream_t stream);
-int launch_rows(const LayArgs &a, hipStream_t stream);
-int launch_stats(const LayArgs &a, hipStream_t stream);
-int launch_lay(const LayArgs &a, hipStream_t stream);
+int launch_copy(const LaySet &set, hipStream_t stream);
+int launch_rows(const LaySet &set, hipStream_t stream);
+int launch_stats(const LaySet &set, hipStream_t stream);
+int launch_lay(const LaySet &set, hipStream_t stream);
 int launch_column_sums(const SumArgs &a, hipStream_t stream);
 int launch_zero(uint32_t *p, int64_t words, hipStream_t stream);
 
