@@ -18,14 +18,19 @@ struct GradTensor {              // on the device
     int64_t rows;
 };
 
-struct GradTile {                // one workgroup's share: values [start, start + n) of a tensor, counted row by row
+// One workgroup's share: values [start, start + n) of a tensor, counted row by row.  The tensor's own description is in it: what a workgroup waits
+// for before its first load is one load from this list.
+struct GradTile {
+    GradTensor t;
     int64_t start;
-    int32_t tensor, n;
+    int32_t n, tensor;
 };
+static_assert(sizeof(GradTile) == 64, "half a cache line");
 
-// Workgroups take 4096 values each: every load of f32 is under way before the first value is used.  Clipping, Adagrad's step of 16 x 19.8 M f32, us:
-// tiles of 1 K 843, 1592; 2 K 712, 1527; 4 K 674, 1503; 8 K 692, 1510; 32 K 709, 1515.  Streamed accesses and tiles dealt in runs to the XCDs gain nothing.
-constexpr int kThreads = 256, kTile = 4096;
+// Workgroups take 16 KB each, 4096 values of f32 or 8192 of 16-bit numbers: all loads are under way before the first value is used.  Clipping, Adagrad's
+// step of 16 x 19.8 M f32, us: tiles of 1 K 843, 1592; 2 K 712, 1527; 4 K 674, 1503; 8 K 692, 1510; 32 K 709, 1515.  The norm of 16 x 19.8 M bf16: 4 K 130,
+// 8 K 115.  Bound by HBM: the norm reads 6 TB/s.  Streamed accesses and tiles dealt in runs to the XCDs gain nothing.
+constexpr int kThreads = 256, kTile = 4096, kJoinThreads = 1024;
 
 __device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
 {
@@ -66,8 +71,9 @@ __device__ __forceinline__ void write_some(void *p, int64_t i, const Some<V> &r)
 // The tile's values, V at a time that lie side by side in the tensor: U times V are loaded, load(i), before the first are used, use(i, what was
 // loaded); one(i) for single values.
 template <int V, int U, class Load, class Use, class One>
-__device__ __forceinline__ void each(const GradTensor &t, const GradTile &tile, Load load, Use use, One one)
+__device__ __forceinline__ void each(const GradTile &tile, Load load, Use use, One one)
 {
+    const GradTensor &t = tile.t;
     constexpr int kAll = kThreads * V;
     if (t.ld == t.cols) {
         int32_t k = static_cast<int32_t>(threadIdx.x) * V;
@@ -93,21 +99,27 @@ __device__ __forceinline__ void each(const GradTensor &t, const GradTile &tile, 
     }
 }
 
+// The sum over a workgroup of THREADS, four waves at a time: more waves of zeros do not change it.
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double s, double *lds)
 {
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; i += 4) s += (lds[i] + lds[i + 1]) + (lds[i + 2] + lds[i + 3]);
+    return s;
 }
 
 template <int T>
-__device__ __forceinline__ double tile_squares(const GradTensor &t, const GradTile &tile)
+__device__ __forceinline__ double tile_squares(const GradTile &tile)
 {
+    const GradTensor &t = tile.t;
     double s = 0.0;
     const auto add = [&](float v) { s = fma(static_cast<double>(v), static_cast<double>(v), s); };
     constexpr int V = T == kF32 ? 4 : 8;
-    each<V, 4>(t, tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+    each<V, 4>(tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
             [&](int64_t, const Some<V> &v) {
 #pragma unroll
                 for (int c = 0; c < V; ++c) add(v.v[c]);
@@ -116,28 +128,30 @@ __device__ __forceinline__ double tile_squares(const GradTensor &t, const GradTi
     return s;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const GradTensor *tensors, const GradTile *tiles, double *partial)
+__global__ __launch_bounds__(kThreads) void norm_kernel(const GradTile *tiles, double *partial)
 {
     __shared__ double lds[4];
     const GradTile tile = tiles[blockIdx.x];
-    const GradTensor t = tensors[tile.tensor];
-    double s = t.type == kF32 ? tile_squares<kF32>(t, tile) : t.type == kBf16 ? tile_squares<kBf16>(t, tile) : tile_squares<kF16>(t, tile);
-    s = block_sum(s, lds);
+    double s = tile.t.type == kF32 ? tile_squares<kF32>(tile) : tile.t.type == kBf16 ? tile_squares<kBf16>(tile) : tile_squares<kF16>(tile);
+    s = block_sum<kThreads>(s, lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
 // A worker's norm from its tiles' sums, by a whole workgroup.
+template <int THREADS>
 __device__ __forceinline__ float join_norm(const double *partial, const int32_t *first, int32_t worker, double *lds)
 {
     double s = 0.0;
-    for (int32_t i = first[worker] + static_cast<int32_t>(threadIdx.x); i < first[worker + 1]; i += kThreads) s += partial[i];
-    return static_cast<float>(sqrt(block_sum(s, lds)));
+    const int32_t end = first[worker + 1];
+#pragma unroll 8
+    for (int32_t i = first[worker] + static_cast<int32_t>(threadIdx.x); i < end; i += THREADS) s += partial[i];
+    return static_cast<float>(sqrt(block_sum<THREADS>(s, lds)));
 }
 
-__global__ __launch_bounds__(kThreads) void norm_join_kernel(const double *partial, const int32_t *first, float *norms)
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const double *partial, const int32_t *first, float *norms)
 {
-    __shared__ double lds[4];
-    const float norm = join_norm(partial, first, static_cast<int32_t>(blockIdx.x), lds);
+    __shared__ double lds[kJoinThreads / 64];
+    const float norm = join_norm<kJoinThreads>(partial, first, static_cast<int32_t>(blockIdx.x), lds);
     if (threadIdx.x == 0) norms[blockIdx.x] = norm;
 }
 
@@ -152,7 +166,7 @@ struct Norms {
 __device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t tile, double *lds)
 {
     if (!n.partial) return n.norms[worker];
-    const float norm = join_norm(n.partial, n.first, worker, lds);
+    const float norm = join_norm<kThreads>(n.partial, n.first, worker, lds);
     if (threadIdx.x == 0 && tile == n.first[worker]) n.norms[worker] = norm;
     return norm;
 }
@@ -160,10 +174,11 @@ __device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t
 __device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most ? 1.0f : most / norm; }
 
 template <int T, int D>
-__device__ __forceinline__ void clip_tile(const GradTensor &t, const GradTensor &d, const GradTile &tile, float f)
+__device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor &d, float f)
 {
+    const GradTensor &t = tile.t;
     constexpr int V = T == kF32 || D == kF32 ? 4 : 8;
-    each<V, 4>(t, tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+    each<V, 4>(tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
             [&](int64_t i, Some<V> v) {
 #pragma unroll
                 for (int c = 0; c < V; ++c) v.v[c] *= f;
@@ -176,30 +191,28 @@ __device__ __forceinline__ void clip_tile(const GradTensor &t, const GradTensor 
 }
 
 template <int T>
-__device__ __forceinline__ void clip_to(const GradTensor &t, const GradTensor &d, const GradTile &tile, float f)
+__device__ __forceinline__ void clip_to(const GradTile &tile, const GradTensor &d, float f)
 {
-    if (d.type == kF32) clip_tile<T, kF32>(t, d, tile, f);
-    else if (d.type == kBf16) clip_tile<T, kBf16>(t, d, tile, f);
-    else clip_tile<T, kF16>(t, d, tile, f);
+    if (d.type == kF32) clip_tile<T, kF32>(tile, d, f);
+    else if (d.type == kBf16) clip_tile<T, kBf16>(tile, d, f);
+    else clip_tile<T, kF16>(tile, d, f);
 }
 
 // Tiles are taken from the last to the first: what the norm read last is still in the caches.
-__global__ __launch_bounds__(kThreads) void clip_kernel(const GradTensor *tensors, const GradTensor *to, const GradTile *tiles, Norms norms, float most)
+__global__ __launch_bounds__(kThreads) void clip_kernel(const GradTile *tiles, const GradTensor *to, Norms norms, float most, int32_t in_place)
 {
     __shared__ double lds[4];
     const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);
     const GradTile tile = tiles[number];
-    const GradTensor t = tensors[tile.tensor];
-    const float f = clip_factor(norm_of(norms, t.worker, number, lds), most);
-    if (tensors == to && f == 1.0f) return;                // in place: nothing changes
     const GradTensor d = to[tile.tensor];
-    if (t.type == kF32) clip_to<kF32>(t, d, tile, f);
-    else if (t.type == kBf16) clip_to<kBf16>(t, d, tile, f);
-    else clip_to<kF16>(t, d, tile, f);
+    const float f = clip_factor(norm_of(norms, tile.t.worker, number, lds), most);
+    if (in_place && f == 1.0f) return;                     // nothing changes
+    if (tile.t.type == kF32) clip_to<kF32>(tile, d, f);
+    else if (tile.t.type == kBf16) clip_to<kBf16>(tile, d, f);
+    else clip_to<kF16>(tile, d, f);
 }
 
 struct StepArgs {
-    const GradTensor *tensors;
     const GradTile *tiles;
     Norms norms;                 // norms.norms nullptr: no clipping
     float *theta, *sums;         // sums nullptr: SGD
@@ -224,8 +237,9 @@ struct StepFour {
 };
 
 template <int T>
-__device__ __forceinline__ void step_tile(const GradTensor &t, const GradTile &tile, float f, const StepArgs &a)
+__device__ __forceinline__ void step_tile(const GradTile &tile, float f, const StepArgs &a)
 {
+    const GradTensor &t = tile.t;
     float *theta = a.theta + t.worker * a.at.stride;
     float *sums = a.sums ? a.sums + t.worker * a.sums_at.stride : nullptr;
     const auto one = [&](int64_t i) {
@@ -239,7 +253,7 @@ __device__ __forceinline__ void step_tile(const GradTensor &t, const GradTile &t
     };
     // four parameters that a block's edge parts are taken one by one
     const auto together = [&](int64_t e) { return ((e ^ (e + 3)) >> a.at.logB) == 0 && (!sums || ((e ^ (e + 3)) >> a.sums_at.logB) == 0); };
-    each<4, 1>(t, tile,
+    each<4, 1>(tile,
             [&](int64_t i) {
                 StepFour s{};
                 const int64_t e = t.offset + i;
@@ -268,16 +282,15 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a)
     __shared__ double lds[4];
     const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);       // as clip_kernel
     const GradTile tile = a.tiles[number];
-    const GradTensor t = a.tensors[tile.tensor];
     float f = 1.0f;
     if (a.norms.norms) {
-        const float norm = norm_of(a.norms, t.worker, number, lds);
+        const float norm = norm_of(a.norms, tile.t.worker, number, lds);
         if (a.skip_nonfinite && !(norm < INFINITY)) return;
         f = clip_factor(norm, a.most);
     }
-    if (t.type == kF32) step_tile<kF32>(t, tile, f, a);
-    else if (t.type == kBf16) step_tile<kBf16>(t, tile, f, a);
-    else step_tile<kF16>(t, tile, f, a);
+    if (tile.t.type == kF32) step_tile<kF32>(tile, f, a);
+    else if (tile.t.type == kBf16) step_tile<kBf16>(tile, f, a);
+    else step_tile<kF16>(tile, f, a);
 }
 
 }  // namespace
@@ -346,7 +359,9 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
         if (before && before->worker == t.worker && before->offset + before->rows * before->cols > t.offset) return GBMUF_EINVAL;
         before = &t;
     }
-    const int64_t size = kTile;
+    int64_t size = 2 * kTile;                              // one size for a handle: f32 anywhere in it takes the smaller
+    for (const GradTensor &t : h.tensors)
+        if (t.type == kF32) size = kTile;
     std::vector<GradTile> tiles;
     std::vector<int32_t> first(static_cast<size_t>(d.workers) + 1, 0);
     int64_t count = 0;
@@ -355,7 +370,7 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
     tiles.reserve(static_cast<size_t>(count));
     for (size_t i = 0; i < h.tensors.size(); ++i) {
         const int64_t all = h.tensors[i].rows * h.tensors[i].cols;
-        for (int64_t s = 0; s < all; s += size) tiles.push_back(GradTile{s, static_cast<int32_t>(i), static_cast<int32_t>(std::min(size, all - s))});
+        for (int64_t s = 0; s < all; s += size) tiles.push_back(GradTile{h.tensors[i], s, static_cast<int32_t>(std::min(size, all - s)), static_cast<int32_t>(i)});
         first[static_cast<size_t>(h.tensors[i].worker) + 1] = static_cast<int32_t>(tiles.size());
     }
     for (size_t w = 1; w < first.size(); ++w) first[w] = std::max(first[w], first[w - 1]);
@@ -382,26 +397,25 @@ int check_grads_device(const gbmuf_grads_s *g)
     return now == g->device ? GBMUF_OK : hip_failed("another GPU than the handle's is current", hipErrorInvalidDevice, GBMUF_EDEVICE);
 }
 
-int launch(const void *fn, int64_t blocks, void **argv, const char *what, hipStream_t stream)
+int launch(const void *fn, int64_t blocks, void **argv, const char *what, hipStream_t stream, int threads = kThreads)
 {
     if (blocks <= 0) return GBMUF_OK;
-    const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(threads)), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
 }
 
 // The tiles' sums, and the norms unless the kernel after this one joins them (joined not nullptr).
 int enqueue_norm(const gbmuf_grads_s *g, float *norms, Norms *joined, hipStream_t stream)
 {
-    const GradTensor *tensors = g->d_tensors;
     const GradTile *tiles = g->d_tiles;
     double *partial = g->d_partial;
     const int32_t *first = g->d_first;
-    void *a1[] = {&tensors, &tiles, &partial}, *a2[] = {&partial, &first, &norms};
+    void *a1[] = {&tiles, &partial}, *a2[] = {&partial, &first, &norms};
     const int rc = launch(reinterpret_cast<const void *>(norm_kernel), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
     if (rc != GBMUF_OK) return rc;
     if (joined) *joined = Norms{norms, g->few ? partial : nullptr, first};
     if (joined && g->few) return GBMUF_OK;
-    return launch(reinterpret_cast<const void *>(norm_join_kernel), g->workers, a2, "hipLaunchKernel(norm join)", stream);
+    return launch(reinterpret_cast<const void *>(norm_join_kernel), g->workers, a2, "hipLaunchKernel(norm join)", stream, kJoinThreads);
 }
 
 // Where the arrays of a step lie.
@@ -503,9 +517,10 @@ int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float ma
     hipStream_t s = static_cast<hipStream_t>(stream);
     Norms n{};
     if ((rc = enqueue_norm(src, norms, &n, s)) != GBMUF_OK) return rc;
-    const GradTensor *from = src->d_tensors, *to = dst->d_tensors;
     const GradTile *tiles = src->d_tiles;
-    void *argv[] = {&from, &to, &tiles, &n, &max_norm};
+    const GradTensor *to = dst->d_tensors;
+    int32_t in_place = src == dst ? 1 : 0;
+    void *argv[] = {&tiles, &to, &n, &max_norm, &in_place};
     return launch(reinterpret_cast<const void *>(clip_kernel), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
 }
 
@@ -530,7 +545,7 @@ int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, 
     if ((rc = check_grads_device(grads)) != GBMUF_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (norms && (rc = enqueue_norm(grads, norms, clip ? &a.norms : nullptr, s)) != GBMUF_OK) return rc;
-    a.tensors = grads->d_tensors; a.tiles = grads->d_tiles;
+    a.tiles = grads->d_tiles;
     a.theta = theta->theta;
     a.rate = desc->rate; a.eps = desc->eps; a.most = desc->max_norm; a.skip_nonfinite = desc->skip_nonfinite;
     void *argv[] = {&a};
