@@ -416,7 +416,7 @@ typedef struct gbmuf_linear_io {
  *   two and its values are taken apart into two f16 numbers, of whose four products the matrix cores form three: a value keeps 22 bits or
  *   more, or 2^-40 of its row's largest where that is more, so results are as near as those of f32 products whose
  *   values lie within 2^16 of their row's largest.  An infinity or NaN in x or w makes NaN of the results that it reaches
- *   (in f32; in bf16 and f16 infinities stay what IEEE says).  Few rows: plain f32 products.
+ *   (in f32; in bf16 and f16 infinities stay what IEEE says).  Up to 64 rows, and small sizes: plain f32 products.
  *   workspace  device memory of gbmuf_linear_workspace bytes, 256-byte aligned, that nothing else uses until the call's work
  *              is done; NULL if that is 0.  Calls that share one must be in order.
  * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,
