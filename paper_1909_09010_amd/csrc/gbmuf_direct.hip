@@ -20,7 +20,7 @@ __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
 }
 
 // One step's share of an operand: R rows of the result by kDepth values of k.  ALONG_K: k lies side by side in memory, LDS holds [row][k] with the 16-byte
-// chunk c of row r at place c ^ ((r / 2) & 7), 16 rows in all banks; else rows do, and LDS holds [k][row].  Whatever lies beyond the matrix is zero.
+// chunk c of row r at place c ^ ((r / 2) & 7), 16 rows in all banks; else rows do, and LDS holds [k][row].  What lies beyond the matrix along k is zero.
 // Threads work in groups of 256, each on steps of its own.
 __device__ __forceinline__ int thread_of() { return static_cast<int>(threadIdx.x) & (kThreads - 1); }
 
@@ -42,17 +42,32 @@ struct Stage {
         return (i * kThreads + thread_of()) % per * 4;
     }
 
+    using Value = typename Num<T>::type;
+    const Value *p[kChunks], *pre[kChunks];
+
+    // Where the chunks of step 0 are read; those of rows beyond the matrix, whose results are not stored, at its end.
+    __device__ __forceinline__ void init(const Source &s, int64_t g, int row0, int rows)
+    {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int64_t row = ALONG_K ? min(row0 + major(i), rows - 1) : major(i), side = ALONG_K ? minor(i) : min(row0 + minor(i), max(rows - 4, 0));
+            p[i] = static_cast<const Value *>(s.p) + g * s.batch + row * s.ld + side;
+            if (SLOPE && s.act) pre[i] = static_cast<const Value *>(s.pre) + g * s.p_batch + row * s.ldp + side;
+        }
+    }
+
     __device__ __forceinline__ void load(const Source &s, int64_t g, int row0, int k0, int rows, int K)
     {
-        const int64_t first = static_cast<int64_t>(ALONG_K ? row0 : k0), side = ALONG_K ? k0 : row0;
-        if (row0 + R <= rows && k0 + kDepth <= K) {            // no guard between the loads: they are all in flight
+        if (k0 + kDepth <= K && (ALONG_K || row0 + R <= rows || rows % 4 == 0)) {            // no guard between the loads: they are all in flight
+            const int64_t k = k0;
 #pragma unroll
-            for (int i = 0; i < kChunks; ++i) v[i] = read4<T>(s.p, g * s.batch + (first + major(i)) * s.ld + side + minor(i));
+            for (int i = 0; i < kChunks; ++i) v[i] = read4<T>(p[i], ALONG_K ? k : k * s.ld);
             if (SLOPE && s.act)
 #pragma unroll
-                for (int i = 0; i < kChunks; ++i) z[i] = read4<T>(s.pre, g * s.p_batch + (first + major(i)) * s.ldp + side + minor(i));
+                for (int i = 0; i < kChunks; ++i) z[i] = read4<T>(pre[i], ALONG_K ? k : k * s.ldp);
             return;
         }
+        const int64_t first = static_cast<int64_t>(ALONG_K ? row0 : k0), side = ALONG_K ? k0 : row0;
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int left = first + major(i) < (ALONG_K ? rows : K) ? static_cast<int>((ALONG_K ? K : rows) - side) - minor(i) : 0;
@@ -70,7 +85,7 @@ struct Stage {
             for (int c = 0; c < 4; ++c) v[i][c] *= slope(z[i][c], ACT);
     }
 
-    // applies the slope; what was beyond the matrix stays zero
+    // applies the slope
     __device__ __forceinline__ void shape(const Source &s)
     {
         if (!SLOPE) return;
@@ -136,6 +151,8 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
     v4f sums = {0.0f, 0.0f, 0.0f, 0.0f};
     A x;
     B w;
+    x.init(a.a, g, m0, a.t.M);
+    w.init(a.b, g, n0, a.t.N);
     if (first < last) {
         x.load(a.a, g, m0, first * kDepth, a.t.M, a.K);
         w.load(a.b, g, n0, first * kDepth, a.t.N, a.K);
