@@ -7,6 +7,7 @@ namespace {
 
 constexpr int kDepth = 32;       // values of k per step (64 by tiles of 64 x 64 gain nothing, and cost the gradients half their waves)
 constexpr int kThreads = 256;
+constexpr int kTile = 64;        // (128 x 128: gradients of 8 x 128 x 650 x 650 f32 88 us where these take 44, and nowhere less than these)
 
 template <int T>
 __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
@@ -24,21 +25,21 @@ __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
 // Threads work in groups of 256, each on steps of its own.
 __device__ __forceinline__ int thread_of() { return static_cast<int>(threadIdx.x) & (kThreads - 1); }
 
-template <int T, bool ALONG_K, int R, bool SLOPE = false>
+template <int T, bool ALONG_K, bool SLOPE = false>
 struct Stage {
-    static constexpr int kChunks = R * kDepth / 4 / kThreads;
-    static constexpr int kPitch = ALONG_K ? kDepth : R + 8;        // + 8: the two halves of a wave read k 4 apart, in other banks
-    static constexpr int kFloats = ALONG_K ? R * kDepth : kDepth * kPitch;
+    static constexpr int kChunks = kTile * kDepth / 4 / kThreads;
+    static constexpr int kPitch = ALONG_K ? kDepth : kTile + 8;        // + 8: the two halves of a wave read k 4 apart, in other banks
+    static constexpr int kFloats = ALONG_K ? kTile * kDepth : kDepth * kPitch;
     v4f v[kChunks], z[kChunks];
 
     static __device__ __forceinline__ int major(int i)
     {
-        constexpr int per = (ALONG_K ? kDepth : R) / 4;
+        constexpr int per = (ALONG_K ? kDepth : kTile) / 4;
         return (i * kThreads + thread_of()) / per;
     }
     static __device__ __forceinline__ int minor(int i)
     {
-        constexpr int per = (ALONG_K ? kDepth : R) / 4;
+        constexpr int per = (ALONG_K ? kDepth : kTile) / 4;
         return (i * kThreads + thread_of()) % per * 4;
     }
 
@@ -58,7 +59,7 @@ struct Stage {
 
     __device__ __forceinline__ void load(const Source &s, int64_t g, int row0, int k0, int rows, int K)
     {
-        if (k0 + kDepth <= K && (ALONG_K || row0 + R <= rows || rows % 4 == 0)) {            // no guard between the loads: they are all in flight
+        if (k0 + kDepth <= K && (ALONG_K || row0 + kTile <= rows || rows % 4 == 0)) {            // no guard between the loads: they are all in flight
             const int64_t k = k0;
 #pragma unroll
             for (int i = 0; i < kChunks; ++i) v[i] = read4<T>(p[i], ALONG_K ? k : k * s.ld);
@@ -117,37 +118,32 @@ struct Stage {
     }
 };
 
-template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE, int GROUPS>
+template <int T, bool A_ALONG_K, bool B_ALONG_K, int GROUPS>
 constexpr size_t direct_lds()
 {
-    constexpr size_t stages = GROUPS * (Stage<T, A_ALONG_K, TILE>::kFloats + Stage<T, B_ALONG_K, TILE>::kFloats) * sizeof(float);
-    constexpr size_t out = leave_bytes<TILE, TILE, 2, 2>(), parts = (GROUPS - 1) * TILE * TILE * sizeof(float), sums = GROUPS * kThreads * sizeof(v4f);
+    constexpr size_t stages = GROUPS * (Stage<T, A_ALONG_K>::kFloats + Stage<T, B_ALONG_K>::kFloats) * sizeof(float);
+    constexpr size_t out = leave_bytes<kTile, kTile, 2, 2>(), parts = (GROUPS - 1) * kTile * kTile * sizeof(float), sums = GROUPS * kThreads * sizeof(v4f);
     constexpr size_t most = stages > out ? stages : out, more = parts > sums ? parts : sums;
     return most > more ? most : more;
 }
 
-// One tile of TILE x TILE by 2 x 2 waves, or by GROUPS times as many that take every GROUPS-th step each and are added up in the end: a step
+// One tile of 64 x 64 by 2 x 2 waves, or by GROUPS times as many that take every GROUPS-th step each and are added up in the end: a step
 // takes a microsecond or so however little it computes, and where there are few tiles nothing else hides that.
-template <int T, bool A_ALONG_K, bool B_ALONG_K, int TILE, bool SLOPE, int GROUPS>
+template <int T, bool A_ALONG_K, bool B_ALONG_K, bool SLOPE, int GROUPS>
 __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *lds)
 {
-    constexpr int F = TILE / 64;
-    using A = Stage<T, A_ALONG_K, TILE, SLOPE>;
-    using B = Stage<T, B_ALONG_K, TILE>;
-    const Share share = share_of<TILE, TILE>(a.t, id, (a.K + kDepth - 1) / kDepth);
+    using A = Stage<T, A_ALONG_K, SLOPE>;
+    using B = Stage<T, B_ALONG_K>;
+    const Share share = share_of<kTile, kTile>(a.t, id, (a.K + kDepth - 1) / kDepth);
     const int64_t g = share.at.g;
-    const int tn = share.at.tn, m0 = share.at.tm * TILE, n0 = tn * TILE;
+    const int tn = share.at.tn, m0 = share.at.tm * kTile, n0 = tn * kTile;
     const int group = GROUPS > 1 ? static_cast<int>(threadIdx.x) / kThreads : 0, first = share.first + group, last = share.last;
     const int turns = (share.last - share.first + GROUPS - 1) / GROUPS;            // of every group, though its last may be empty
-    const int lane = threadIdx.x & 63, wave = thread_of() >> 6, wm = (wave & 1) * (TILE / 2), wn = (wave >> 1) * (TILE / 2);
+    const int lane = threadIdx.x & 63, wave = thread_of() >> 6, wm = (wave & 1) * (kTile / 2), wn = (wave >> 1) * (kTile / 2);
     float *la = lds + group * (A::kFloats + B::kFloats), *lb = la + A::kFloats;
-    v16f acc[F][F];
+    v16f acc[1][1];
 #pragma unroll
-    for (int i = 0; i < F; ++i)
-#pragma unroll
-        for (int j = 0; j < F; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.0f;
     v4f sums = {0.0f, 0.0f, 0.0f, 0.0f};
     A x;
     B w;
@@ -186,28 +182,20 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         if (s < last)
 #pragma unroll
             for (int t = 0; t < kDepth / 8; ++t) {
-                v4f p[F], q[F];
+                const v4f p = A::get(la, wm + (lane & 31), 2 * t + (lane >> 5)), q = B::get(lb, wn + (lane & 31), 2 * t + (lane >> 5));
 #pragma unroll
-                for (int i = 0; i < F; ++i) p[i] = A::get(la, wm + i * 32 + (lane & 31), 2 * t + (lane >> 5));
-#pragma unroll
-                for (int j = 0; j < F; ++j) q[j] = B::get(lb, wn + j * 32 + (lane & 31), 2 * t + (lane >> 5));
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < F; ++i)
-#pragma unroll
-                        for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[j][c], p[i][c], acc[i][j], 0, 0, 0);
+                for (int c = 0; c < 4; ++c) acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[c], p[c], acc[0][0], 0, 0, 0);
             }
         __syncthreads();
     }
     if (!A_ALONG_K && a.sums && tn == 0) {
-        constexpr int per4 = TILE / 4, same = GROUPS * kThreads / per4;      // threads t, t + per4 .. hold the same rows
+        constexpr int per4 = kTile / 4, same = GROUPS * kThreads / per4;      // threads t, t + per4 .. hold the same rows
         reinterpret_cast<v4f *>(lds)[threadIdx.x] = sums;
         __syncthreads();
-        if (threadIdx.x < TILE) {
+        if (threadIdx.x < kTile) {
             float v = 0.0f;
 #pragma unroll 8
-            for (int i = 0; i < same; ++i) v += lds[i * TILE + threadIdx.x];
+            for (int i = 0; i < same; ++i) v += lds[i * kTile + threadIdx.x];
             const int m = m0 + static_cast<int>(threadIdx.x);
             if (m < a.t.M) {
                 const int64_t at = g * a.sums_batch + m;
@@ -218,7 +206,6 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         __syncthreads();
     }
     if constexpr (GROUPS > 1) {
-        static_assert(F == 1, "one result of 32 x 32 a wave");
         v4f *part = reinterpret_cast<v4f *>(lds);
         if (group > 0)
 #pragma unroll
@@ -235,29 +222,29 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         __syncthreads();
         if (group > 0) return;
     }
-    leave<TILE, TILE, 2, 2, false>(acc, lds, a, share);
+    leave<kTile, kTile, 2, 2, false>(acc, lds, a, share);
 }
 
 template <int T, int GROUPS>
 __global__ __launch_bounds__(GROUPS *kThreads) void direct_forward_kernel(DirectArgs a)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, true, true, 64, GROUPS>() / 4];
-    direct_tile<T, true, true, 64, false, GROUPS>(a, static_cast<int>(blockIdx.x), lds);
+    __shared__ __align__(16) float lds[direct_lds<T, true, true, GROUPS>() / 4];
+    direct_tile<T, true, true, false, GROUPS>(a, static_cast<int>(blockIdx.x), lds);
 }
 
 // dx = dz w (dz lies along the sum, w across it) and dw = dz' x (both across), in one launch: the first workgroups are dx's.
-template <int T, int TILE, int GROUPS>
+template <int T, int GROUPS>
 __global__ __launch_bounds__(GROUPS *kThreads) void direct_backward_kernel(DirectArgs dx, DirectArgs dw)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, false, false, TILE, GROUPS>() / 4];
-    static_assert(direct_lds<T, false, false, TILE, GROUPS>() >= direct_lds<T, true, false, TILE, GROUPS>(), "one piece of LDS for both");
+    __shared__ __align__(16) float lds[direct_lds<T, false, false, GROUPS>() / 4];
+    static_assert(direct_lds<T, false, false, GROUPS>() >= direct_lds<T, true, false, GROUPS>(), "one piece of LDS for both");
     const int n = dx.t.blocks(), id = static_cast<int>(blockIdx.x);
-    if (id < n) direct_tile<T, true, false, TILE, true, GROUPS>(dx, id, lds);
-    else direct_tile<T, false, false, TILE, true, GROUPS>(dw, id - n, lds);
+    if (id < n) direct_tile<T, true, false, true, GROUPS>(dx, id, lds);
+    else direct_tile<T, false, false, true, GROUPS>(dw, id - n, lds);
 }
 
 // Up to one workgroup a CU: four groups of threads each.
-int form_of(int tile, int32_t blocks) { return tile == 128 ? 2 : blocks <= 256 ? 0 : 1; }
+bool grouped(int32_t blocks) { return blocks <= 256; }
 
 }  // namespace
 
@@ -265,27 +252,25 @@ int launch_direct_forward(const DirectArgs &a, hipStream_t stream)
 {
     const int32_t blocks = a.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
-    const bool grouped = form_of(64, blocks) == 0;
     DirectArgs args = a;
     void *argv[] = {&args};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(grouped ? direct_forward_kernel<kF32, 4> : direct_forward_kernel<kF32, 1>),
-                                           dim3(static_cast<unsigned>(blocks)), dim3(grouped ? 4 * kThreads : kThreads), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(grouped(blocks) ? direct_forward_kernel<kF32, 4> : direct_forward_kernel<kF32, 1>),
+                                           dim3(static_cast<unsigned>(blocks)), dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct product)", err, GBMUF_EDEVICE);
 }
 
-int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream)
+int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream)
 {
     const int32_t blocks = dx.t.blocks() + dw.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
     using Fn = void (*)(DirectArgs, DirectArgs);
-    static constexpr Fn fns[3][3] = {{direct_backward_kernel<kF32, 64, 4>, direct_backward_kernel<kF32, 64, 1>, direct_backward_kernel<kF32, 128, 1>},
-                                     {direct_backward_kernel<kBf16, 64, 4>, direct_backward_kernel<kBf16, 64, 1>, direct_backward_kernel<kBf16, 128, 1>},
-                                     {direct_backward_kernel<kF16, 64, 4>, direct_backward_kernel<kF16, 64, 1>, direct_backward_kernel<kF16, 128, 1>}};
-    const int form = form_of(tile, blocks);
+    static constexpr Fn fns[3][2] = {{direct_backward_kernel<kF32, 1>, direct_backward_kernel<kF32, 4>},
+                                     {direct_backward_kernel<kBf16, 1>, direct_backward_kernel<kBf16, 4>},
+                                     {direct_backward_kernel<kF16, 1>, direct_backward_kernel<kF16, 4>}};
     DirectArgs x = dx, w = dw;
     void *argv[] = {&x, &w};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][form]), dim3(static_cast<unsigned>(blocks)),
-                                           dim3(form == 0 ? 4 * kThreads : kThreads), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][grouped(blocks) ? 1 : 0]), dim3(static_cast<unsigned>(blocks)),
+                                           dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct gradients)", err, GBMUF_EDEVICE);
 }
 

@@ -238,18 +238,30 @@ DirectArgs direct_args(const Source &a, const Source &b, int64_t K, const Cut &c
     return d;
 }
 
-// The sums of tiles are cut (where `may_cut`) where these are fewer than CUs and long.  A step of 64 x 64 is 0.43 us of a CU's f32 matrix instructions.
-Cut direct_cut(int tile, int64_t M, int64_t N, int64_t K, int64_t batch, bool may_cut)
+// Forward, tiles of 64 x 64: the sums are cut (where `may_cut`) where there are fewer tiles than CUs and they are long.  A step is 0.43 us of a CU's f32
+// matrix instructions.
+Cut direct_cut(int64_t M, int64_t N, int64_t K, int64_t batch, bool may_cut)
 {
-    const int64_t steps = (K + 31) / 32, tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile) * batch;
-    return cut(tile, M, N, batch, steps, may_cut && tiles < 256 ? 256 : std::max<int64_t>(tiles, 1), 0.5);
+    const int64_t steps = (K + 31) / 32, tiles = (M + 63) / 64 * ((N + 63) / 64) * batch;
+    return cut(64, M, N, batch, steps, may_cut && tiles < 256 ? 256 : std::max<int64_t>(tiles, 1), 0.5);
 }
 
-// Gradients: tiles of 128 x 128 where there is one for every CU, else of 64 x 64 (8 x 250 x 1000 x 400 f32 79 and 84 us).  The forward takes 64 x 64 always
-// (8 x 250 x 2000 x 400 f32 45 and 41 us).
-int tile_of(int64_t M, int64_t N, int64_t batch)
+// Gradients: dx's sums are usually the longer ones, and a workgroup that shares its CU with others takes 1.2 us a step or so, so they are cut to last
+// no longer than the matrix instructions of both products (f32: 4 x 128 x 2600 x 650, 82 steps of 88 tiles and 4 of 1804, 79 us in two parts, 65 in
+// four; 16 x 128 x 512 x 512, 16 steps of 256 tiles and 4 of 1024, 34 whole, 40 in two; 1 x 64 x 200,000 x 64 141 in 64 parts, 87 in 358).
+Cut chain_cut(int64_t M, int64_t N, int64_t K, int64_t batch, const Cut &other)
 {
-    return (M + 127) / 128 * ((N + 127) / 128) * batch >= 256 ? 128 : 64;
+    const int64_t steps = (K + 31) / 32, tiles = (M + 63) / 64 * ((N + 63) / 64) * batch;
+    Cut c = cut(64, M, N, batch, steps, std::max<int64_t>(tiles, 1), 0.5);
+    const int64_t all = tiles * steps + static_cast<int64_t>(other.t.whole) * other.t.steps;
+    const int64_t parts = tiles > 0 ? std::min(steps / 8, steps * 256 * 14 / (5 * (all + 1))) : 1;
+    if (parts < 2) return c;
+    const int64_t each = (steps + parts - 1) / parts, splits = (steps + each - 1) / each;
+    c.t.whole = 0;
+    c.t.splits = static_cast<int32_t>(splits);
+    c.t.steps = static_cast<int32_t>(each);
+    c.partial = tiles * splits * 64 * 64;
+    return c;
 }
 
 // Operations of one product.
@@ -260,10 +272,11 @@ double operations(const gbmuf_linear_desc_t &d)
 
 // Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions, which costs launches and
 // passes over them.  us, as they lie / laid out, workers x rows x out x in:
-//   forward f32: 1 x 200 x 1024 x 512 13 / 22, 4 x 200 x 1024 x 512 18 / 28, 8 x 128 x 2600 x 650 51 / 55, 4 x 512 x 1024 x 1024 48 / 47,
-//     16 x 512 x 1024 x 512 84 / 54
-//   gradients f32: 1 x 200 x 1024 x 512 21 / 54, 4 x 200 x 1024 x 512 42 / 63, 8 x 128 x 2600 x 650 153 / 138, 4 x 512 x 1024 x 1024 129 / 92
-//   gradients bf16: 1 x 200 x 1024 x 512 23 / 36, 4 x 200 x 1024 x 512 47 / 38
+//   forward f32: 1 x 200 x 1024 x 512 15 / 20, 4 x 200 x 1024 x 512 17 / 28, 8 x 250 x 1500 x 400 30 / 41, 8 x 128 x 2600 x 650 45 / 45 (with tanh and z kept, operands in HBM before the call, 45 / 57),
+//     8 x 250 x 2000 x 400 39 / 35, 4 x 512 x 1024 x 1024 46 / 41, 16 x 512 x 1024 x 512 83 / 51
+//   gradients f32: 1 x 200 x 1024 x 512 16 / 42, 4 x 200 x 1024 x 512 32 / 50, 8 x 200 x 1024 x 512 53 / 60, 1 x 1000 x 1000 x 1000 64 / 64,
+//     8 x 128 x 2600 x 650 121 / 117, 8 x 250 x 2000 x 400 113 / 85
+//   gradients bf16: 1 x 200 x 1024 x 512 16 / 28, 8 x 128 x 400 x 400 22 / 26, 4 x 200 x 1024 x 512 34 / 30, 8 x 128 x 652 x 652 37 / 45
 bool takes_direct_forward(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && operations(d) <= 4e9; }
 
 // What up to 64 rows take.  The kernel for few rows reads each matrix once in one launch, but for more than 16 rows of one the matrix cores (f32) or
@@ -279,7 +292,7 @@ Few few_of(const gbmuf_linear_desc_t &d)
     return Few::kUnlessAligned;
 }
 
-bool takes_direct_backward(const gbmuf_linear_desc_t &d) { return operations(d) <= (d.dtype == GBMUF_F32 ? 2.5e9 : 5e8); }
+bool takes_direct_backward(const gbmuf_linear_desc_t &d) { return operations(d) <= (d.dtype == GBMUF_F32 ? 2e9 : 1e9); }
 
 // ---------------------------------------------------------------------------------------
 // Forward.  io nullptr: only count the workspace, for matrices that lie as badly as can be.
@@ -301,7 +314,7 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     const Few few = few_of(d);
     const bool is_few = few == Few::kAlways || (few == Few::kUnlessAligned && io && !(lies_well(io->x) && lies_well(io->w)));
     if (is_few || takes_direct_forward(d) || few == Few::kDirect) {
-        const Cut c = direct_cut(64, M, N, K, G, !is_few);
+        const Cut c = direct_cut(M, N, K, G, !is_few);
         DirectArgs f = direct_args(source_of(io ? io->x : none), source_of(io ? io->w : none), K, c, e);
         if (is_few) return io ? launch_few(f, type, stream) : GBMUF_OK;
         f.t.partial = space.take<float>(c.partial);
@@ -353,13 +366,13 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
 {
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
     const int32_t G = d.batch, type = d.dtype, grad_type = d.weight_grad_f32 ? kF32 : type;
-    const int tile = std::max(tile_of(M, K, G), tile_of(N, K, G));
     const gbmuf_linear_grad_io_t none{};
     const gbmuf_linear_grad_io_t &at = io ? *io : none;
     const bool dx = !io || io->dx.data, dw = !io || io->dw.data;
     Source z = source_of(at.dy);
     if (d.activation) { z.pre = at.pre.data; z.ldp = at.pre.ld; z.p_batch = at.pre.batch_stride; z.act = d.activation; }
-    const Cut cx = direct_cut(tile, M, dx ? K : 0, N, G, true), cw = direct_cut(tile, N, dw ? K : 0, M, G, false);
+    const Cut both = direct_cut(N, K, M, G, false), cw = direct_cut(N, dw ? K : 0, M, G, false);
+    const Cut cx = chain_cut(M, dx ? K : 0, N, G, both);           // as for both products, so that the workspace is the same for one
     const Epilogue e = into(at.dx, type);
     DirectArgs px = direct_args(z, source_of(at.w), N, cx, e);
     DirectArgs pw = direct_args(z, source_of(at.x), M, cw, weight_grad(d, at.dw, grad_type));
@@ -367,8 +380,8 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
     if (!io) return GBMUF_OK;
     px.copy = at.dresidual.data; px.copy_ld = at.dresidual.ld; px.copy_batch = at.dresidual.batch_stride;
     pw.sums = at.dbias.data; pw.sums_batch = at.dbias.batch_stride; pw.sums_type = grad_type; pw.accumulate = d.accumulate;
-    const int rc = launch_direct_backward(px, pw, type, tile, stream);
-    return rc != GBMUF_OK ? rc : launch_join(JoinArgs{px.t, tile, 0, e}, stream);
+    const int rc = launch_direct_backward(px, pw, type, stream);
+    return rc != GBMUF_OK ? rc : launch_join(JoinArgs{px.t, 64, 0, e}, stream);
 }
 
 int sum_columns(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &out, const float *sums, int32_t type, hipStream_t stream)

@@ -115,7 +115,7 @@ int launch_product(const ProductArgs &a, int32_t type, int tile, hipStream_t str
 int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream);
 constexpr int kFewRows = 64;
 int launch_direct_forward(const DirectArgs &a, hipStream_t stream);          // f32, tiles of 64 x 64
-int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, int tile, hipStream_t stream);
+int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream);
 int launch_join(const JoinArgs &a, hipStream_t stream);
 int launch_copy(const LaySet &set, hipStream_t stream);
 int launch_rows(const LaySet &set, hipStream_t stream);
