@@ -420,7 +420,8 @@ typedef struct gbmuf_linear_io {
  *   workspace  device memory of gbmuf_linear_workspace bytes, 256-byte aligned, that nothing else uses until the call's work
  *              is done; NULL if that is 0.  Calls that share one must be in order.
  * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,
- * pointers that are not aligned to their type, outputs that overlap inputs or each other, a workspace that is too small),
+ * pointers that are not aligned to their type, outputs that overlap inputs or each other, a workspace that is too small or overlaps a matrix,
+ * strides that span more than 2^48 elements),
  * EUNSUPPORTED (sizes near 2^30 and above, batch above 65535, a matrix of all workers with 2^21 tiles of 128 x 128 or more), EDEVICE.
  */
 int gbmuf_linear_workspace(const gbmuf_linear_desc_t *desc, int32_t backward, int64_t *bytes);
@@ -489,7 +490,7 @@ int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream);
  * (a norm that is NaN makes NaN of the worker's gradients).  dst has the tensors of src, in the same order and with the same
  * rows, cols and worker; it may be src, or lie elsewhere and have other dtypes.  Tensors of dst must not share values with each
  * other or, unless dst is src, with src.
- * EINVAL also for max_norm < 0 or NaN (INFINITY: copies) and for a dst whose tensors differ.
+ * EINVAL also for max_norm < 0 or NaN (INFINITY: copies, whatever the norm) and for a dst whose tensors differ.
  */
 int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream);
 

@@ -171,7 +171,7 @@ __device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t
     return norm;
 }
 
-__device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most ? 1.0f : most / norm; }
+__device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most || most == INFINITY ? 1.0f : most / norm; }
 
 template <int T, int D>
 __device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor &d, float f)
@@ -423,6 +423,9 @@ int place(const gbmuf_state_t &s, int64_t K, int64_t P, Placement *at, int64_t *
 {
     if (reinterpret_cast<uintptr_t>(s.theta) % 4 != 0) return GBMUF_EINVAL;
     const int64_t B = s.block_floats;
+    constexpr int64_t kMost = static_cast<int64_t>(1) << 48;       // floats: what any memory holds, and no product below overflows
+    if (P > kMost || s.worker_stride > kMost || s.block_stride > kMost) return GBMUF_EINVAL;
+    if (B > 0 && static_cast<double>(P) / static_cast<double>(B) * static_cast<double>(s.block_stride) > static_cast<double>(kMost)) return GBMUF_EINVAL;
     if (B == 0) {
         if (s.worker_stride < P) return GBMUF_EINVAL;
         *at = Placement{s.worker_stride, 0, 62, 0};

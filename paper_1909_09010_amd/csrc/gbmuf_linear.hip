@@ -4,6 +4,7 @@
 #include "../../include/gbmuf.h"
 
 #include <algorithm>
+#include <initializer_list>
 #include <numeric>
 
 namespace gbmuf {
@@ -30,8 +31,9 @@ Extent extent(const gbmuf_matrix_t &m, int64_t rows, int64_t cols, int64_t batch
     const int64_t b = static_cast<int64_t>(type_bytes(type));
     Extent e;
     e.at = reinterpret_cast<uintptr_t>(m.data);
-    e.rows = rows; e.row = cols * b; e.ld = rows > 1 ? m.ld * b : 0;
-    e.batch = batch; e.stride = batch > 1 ? m.batch_stride * b : 0;
+    constexpr int64_t kMost = static_cast<int64_t>(1) << 52;       // more is refused below
+    e.rows = rows; e.row = cols * b; e.ld = rows > 1 ? std::min(m.ld, kMost) * b : 0;
+    e.batch = batch; e.stride = batch > 1 ? std::min(m.batch_stride, kMost) * b : 0;
     return e;
 }
 
@@ -55,9 +57,11 @@ bool overlap(const Extent &a, const Extent &b)
     return !side_by_side(a.at, a.matrix(), b.at, b.matrix(), matrices) && !side_by_side(a.at, a.row, b.at, b.row, rows);
 }
 
+// Nothing spans more than 2^48 elements, and no product of strides and sizes overflows.
 bool valid_input(const gbmuf_matrix_t &m, const Extent &e, int32_t type)
 {
     if (m.ld < 0 || m.batch_stride < 0) return false;
+    if (static_cast<double>(e.rows) * static_cast<double>(e.ld) + static_cast<double>(e.batch) * static_cast<double>(e.stride) > 0x1p48 * 4.0) return false;
     if (e.rows <= 0 || e.row <= 0 || e.batch <= 0) return true;
     return m.data && reinterpret_cast<uintptr_t>(m.data) % type_bytes(type) == 0;
 }
@@ -518,10 +522,17 @@ int64_t backward_bytes(const gbmuf_linear_desc_t &d)
     return std::max(direct.used, laid.used);
 }
 
-int check_workspace(const void *workspace, int64_t have, int64_t need)
+int check_workspace(const void *workspace, int64_t have, int64_t need, std::initializer_list<const Extent *> matrices)
 {
     if (need == 0) return GBMUF_OK;
-    return workspace && have >= need && reinterpret_cast<uintptr_t>(workspace) % 256 == 0 ? GBMUF_OK : GBMUF_EINVAL;
+    if (!workspace || have < need || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return GBMUF_EINVAL;
+    Extent space;
+    space.at = reinterpret_cast<uintptr_t>(workspace);
+    space.rows = space.batch = 1;
+    space.row = need;
+    for (const Extent *m : matrices)
+        if (overlap(space, *m)) return GBMUF_EINVAL;
+    return GBMUF_OK;
 }
 
 }  // namespace
@@ -563,7 +574,8 @@ int gbmuf_linear(const gbmuf_linear_desc_t *desc, const gbmuf_linear_io_t *io, v
     int64_t need = 0;
     if ((rc = gbmuf_linear_workspace(desc, 0, &need)) != GBMUF_OK) return rc;
     if (M == 0 || N == 0 || G == 0) return GBMUF_OK;
-    if ((rc = check_workspace(workspace, workspace_bytes, need)) != GBMUF_OK) return rc;
+    const Extent none, &res = desc->residual != GBMUF_RESIDUAL_NONE ? r : none;
+    if ((rc = check_workspace(workspace, workspace_bytes, need, {&x, &w, &b, &res, &y, &p})) != GBMUF_OK) return rc;
     if ((rc = check_device()) != GBMUF_OK) return rc;
     Space space{static_cast<char *>(workspace)};
     return forward(*desc, io, space, static_cast<hipStream_t>(stream));
@@ -595,7 +607,8 @@ int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_gr
     int64_t need = 0;
     if ((rc = gbmuf_linear_workspace(desc, 1, &need)) != GBMUF_OK) return rc;
     if (G == 0) return GBMUF_OK;
-    if ((rc = check_workspace(workspace, workspace_bytes, need)) != GBMUF_OK) return rc;
+    const Extent none, &pre = desc->activation ? z : none, &xs = io->dw.data ? x : none, &ws = io->dx.data ? w : none;
+    if ((rc = check_workspace(workspace, workspace_bytes, need, {&xs, &ws, &pre, &dy, &dx, &dw, &db, &dr})) != GBMUF_OK) return rc;
     if ((rc = check_device()) != GBMUF_OK) return rc;
     Space space{static_cast<char *>(workspace)};
     return backward(*desc, *io, space, static_cast<hipStream_t>(stream));

@@ -114,6 +114,17 @@ def test_clip_with_infinite_and_nan_gradients():
 
 
 @gpu
+def test_clip_without_a_bound_copies_whatever_the_norm():
+    ts = [[torch.tensor([1.0, float("inf"), -2.0], device=DEV)], [torch.tensor([1.0, float("nan")], device=DEV)], [torch.ones(4, device=DEV)]]
+    out = [[torch.zeros_like(t) for t in tt] for tt in ts]
+    n = torch.empty(3, device=DEV)
+    B.Grads(ts).clip(math.inf, n, out=B.Grads(out), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for a, b in zip(ts, out):
+        np.testing.assert_array_equal(a[0].cpu().numpy(), b[0].cpu().numpy())
+
+
+@gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shift", [0, 1, 3])
 def test_strided_and_unaligned_tensors(dtype, shift):
@@ -357,6 +368,8 @@ def test_calls_that_are_refused():
     assert code(lambda: step(a=B.make_state(theta.data_ptr() + 2, None, None, 30))) == E
     for B_, ws, bs in ((6, 6, 12), (2, 2, 4), (8, 7, 16), (8, 8, 15), (-8, 8, 16)):
         assert code(lambda: step(a=B.make_state(theta, None, None, ws, B_, bs))) == E
+    for ws, bs in (((1 << 61) + 1, 0), (30, (1 << 61) + 1)):
+        assert code(lambda: step(a=B.make_state(theta, None, None, ws, 0 if bs == 0 else 8, bs))) == E
     # side by side in one arena: the checks pass, and the device is what is missing
     arena = torch.zeros(2, 2, 32)
     assert code(lambda: step(a=B.make_state(arena[:, 0], None, None, 64), b=B.make_state(arena[:, 1], None, None, 64))) == B.GBMUF_EDEVICE

@@ -481,6 +481,63 @@ def test_large_placements_and_each_output_alone(dtype, monkeypatch):
         backward_case(G, M, N, K, dtype, B.ACT_RELU, B.RESIDUAL_BEFORE, want=want)
 
 
+# -- sizes whose gradients' sums are cut between few and many workgroups, with ragged edges -----------
+MIDDLE = [(1, 64, 20000, 64), (4, 128, 2600, 66), (3, 100, 513, 301), (2, 66, 1030, 3), (8, 128, 650, 650), (2, 70, 2, 1500), (1, 65, 4100, 2)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", MIDDLE)
+def test_middle_sizes(size, dtype):
+    forward_case(*size, dtype, B.ACT_TANH, B.RESIDUAL_BEFORE, True, True, seed=9)
+    backward_case(*size, dtype, B.ACT_GELU, B.RESIDUAL_BEFORE, seed=9, want=("dx", "dw", "dbias", "dresidual"))
+    backward_case(*size, dtype, B.ACT_NONE, B.RESIDUAL_BEFORE, f32_grads=True, accumulate=True, seed=10)
+
+
+@gpu
+@pytest.mark.parametrize("size", [(1, 900, 1100, 2050), (1, 700, 750, 4500)])
+def test_f32_rows_of_very_different_sizes_in_large_products(size):
+    """Rows and columns over 60 and 14 powers of ten: each has a scale of its own, in both directions."""
+    G, M, N, K = size
+    g = torch.Generator().manual_seed(12)
+    over = lambda e, n: 10.0 ** torch.linspace(-e, e, n)
+    x, w = torch.randn(G, M, K, generator=g) * over(15, M)[None, :, None], torch.randn(G, N, K, generator=g) * over(7, N)[None, :, None]
+    lin = B.Linear(M, N, K, G)
+    ws = torch.empty(max(lin.workspace_bytes(), lin.workspace_bytes(True)), dtype=torch.uint8, device=DEV)
+    y = torch.empty(G, M, N, device=DEV)
+    lin.forward(lin.forward_io(x.to(DEV), w.to(DEV), y), ws)
+    X, W = x.double(), w.double()
+    S = product64(X.abs(), W.abs())
+    check(y, product64(X, W), sum_bound(K, S, torch.float32, spread(X, W)) + 2.0 ** -126, 2.0 ** -21 * S, "y")
+    # dx sums over n, dw over the rows: dz has a scale for each of its rows, then for each of its columns
+    dy = torch.randn(G, M, N, generator=g)
+    for d, b, what in ((dy * over(15, M)[None, :, None], torch.randn(G, N, K, generator=g) * over(7, K)[None, None], "dx"),
+                       (dy * over(15, N)[None, None], torch.randn(G, M, K, generator=g) * over(7, K)[None, None], "dw")):
+        out = torch.empty(G, M if what == "dx" else N, K, device=DEV)
+        io = lin.backward_io(d.to(DEV), w=b.to(DEV), dx=out) if what == "dx" else lin.backward_io(d.to(DEV), x=b.to(DEV), dw=out)
+        lin.backward(io, ws)
+        p, q = (d if what == "dx" else d.transpose(1, 2)).double(), b.transpose(1, 2).double()
+        S = product64(p.abs(), q.abs())
+        check(out, product64(p, q), sum_bound(p.shape[2], S, torch.float32, spread(p, q)) + 2.0 ** -126, 2.0 ** -21 * S, what)
+
+
+@gpu
+def test_infinities_in_large_f32_products_reach_only_their_rows():
+    G, M, N, K = 2, 800, 900, 3001
+    g = torch.Generator().manual_seed(13)
+    x, w = (torch.randn(s, generator=g).to(DEV) for s in ((G, M, K), (G, N, K)))
+    lin = B.Linear(M, N, K, G)
+    ws = torch.empty(lin.workspace_bytes(), dtype=torch.uint8, device=DEV)
+    clean, got = torch.empty(G, M, N, device=DEV), torch.empty(G, M, N, device=DEV)
+    lin.forward(lin.forward_io(x, w, clean), ws)
+    x[0, 5, 7], x[1, 700, 3000], w[1, 899, 0] = float("inf"), float("nan"), float("-inf")
+    lin.forward(lin.forward_io(x, w, got), ws)
+    torch.cuda.synchronize()
+    bad = torch.zeros(G, M, N, dtype=torch.bool, device=DEV)
+    bad[0, 5], bad[1, 700], bad[1, :, 899] = True, True, True
+    assert not torch.isfinite(got[bad]).any() and torch.equal(got[~bad], clean[~bad])
+
+
 # -- streams, graphs, equal bits ------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -581,6 +638,26 @@ def test_matrices_that_are_refused():
     assert code_of(lambda: back(dresidual=dy)) == B.GBMUF_EINVAL
     after = B.Linear(M, N, K, G, torch.float32, B.ACT_NONE, B.RESIDUAL_AFTER)
     assert code_of(lambda: after.backward(after.backward_io(dy, dresidual=z), space)) == B.GBMUF_EINVAL
+
+
+def test_workspaces_that_overlap_and_strides_beyond_any_memory_are_refused():
+    G, M, N, K = 2, 1500, 1500, 1500                       # a size that takes a workspace
+    lin = B.Linear(M, N, K, G)
+    need = lin.workspace_bytes()
+    assert need > 0
+    at = lambda k: B.Matrix((1 << 40) + (k << 30), K, M * K)           # places that are only compared
+    io = B.LinearIo()
+    io.x, io.w, io.y = at(0), at(1), at(2)
+    lib, d = B.lib(), lin.desc
+    call = lambda space: lib.gbmuf_linear(ctypes.byref(d), ctypes.byref(io), space, need, None)
+    for k in range(3):
+        assert call((1 << 40) + (k << 30)) == B.GBMUF_EINVAL and call((1 << 40) + (k << 30) + 70312 * 256) == B.GBMUF_EINVAL
+    for k in range(3):
+        for field in ("ld", "batch_stride"):
+            io = B.LinearIo()
+            io.x, io.w, io.y = at(0), at(1), at(2)
+            setattr((io.x, io.w, io.y)[k], field, (1 << 62) + 5)
+            assert call(1 << 45) == B.GBMUF_EINVAL
 
 
 def test_outputs_side_by_side_are_taken():
