@@ -437,6 +437,46 @@ def test_gradient_against_differences(act):
         assert abs(got - want) <= tol + 1e-3 * abs(want), (i, got, want, tol)
 
 
+@gpu
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_activations_and_slopes_over_the_range(act):
+    """z = x * 1, f32: the exponentials and reciprocals are within 2 units and 1, a handful of roundings around them: 16 half units of
+    the value itself, of 1 + |z| where a slope's two terms cancel.  Nothing is asked below 2^-120."""
+    z = torch.cat([torch.linspace(-12, 12, 4001), torch.tensor([0.0, 1e-30, -1e-30, 0.25, -0.25, 0.2499999, -0.2499999, 3e-5, 19.0, -30.0, 31.0, 86.0, -86.0,
+                                                               1e4, -1e4, 1e20, -1e20, 3e38, -3e38])])
+    M = z.numel()
+    lin = B.Linear(M, 1, 1, 1, torch.float32, act, B.RESIDUAL_BEFORE)
+    ws = torch.empty(max(lin.workspace_bytes(), lin.workspace_bytes(True), 256), dtype=torch.uint8, device=DEV)
+    one, r = torch.ones(1, 1, device=DEV), torch.zeros(M, 1, device=DEV)
+    x, y, d = z.view(M, 1).to(DEV), torch.empty(M, 1, device=DEV), torch.empty(M, 1, device=DEV)
+    lin.forward(lin.forward_io(x, one, y, residual=r), ws)
+    lin.backward(lin.backward_io(torch.ones(M, 1, device=DEV), x, one, pre=x, dresidual=d), ws)
+    got, slope = y.cpu().double().view(-1), d.cpu().double().view(-1)
+    Z = z.double()
+    want = act64(Z, act)
+    finite = torch.isfinite(got)
+    assert finite.all() and ((got - want).abs() <= 16 * U * want.abs() + 2.0 ** -120).all(), (got - want).abs().max()
+    inside = Z.abs() <= 100
+    w = slope64(Z, act)[inside]
+    if act == B.ACT_SIGMOID:                               # y (1 - y) has no bits left in 64 where y is near 1
+        w = 1 / (2 * torch.cosh(Z[inside] / 2)) ** 2
+    if act == B.ACT_TANH:
+        w = 1 / torch.cosh(Z[inside]) ** 2
+    size = w.abs() if act in (B.ACT_RELU, B.ACT_SIGMOID, B.ACT_TANH) else 1 + Z[inside].abs()
+    assert ((slope[inside] - w).abs() <= 16 * U * size + 2.0 ** -120).all()
+    far = {B.ACT_SIGMOID: (0.0, 0.0), B.ACT_TANH: (0.0, 0.0)}.get(act, (0.0, 1.0))
+    assert (slope[Z < -100] == far[0]).all() and (slope[Z > 100] == far[1]).all()
+    x[:] = float("nan")
+    lin.forward(lin.forward_io(x, one, y, residual=r), ws)
+    lin.backward(lin.backward_io(torch.ones(M, 1, device=DEV), x, one, pre=x, dresidual=d), ws)
+    assert torch.isnan(y).all() and torch.isnan(d).all()
+    for value, wanted in ((float("inf"), {B.ACT_SIGMOID: 1.0, B.ACT_TANH: 1.0}.get(act, float("inf"))), (float("-inf"), {B.ACT_TANH: -1.0}.get(act, 0.0))):
+        x[:] = value
+        lin.forward(lin.forward_io(x, one, y, residual=r), ws)
+        if value > 0 or act in (B.ACT_RELU, B.ACT_SIGMOID, B.ACT_TANH):             # -inf * 0 is NaN in the others' formulas
+            assert (y == wanted).all()
+
+
 # -- sizes that take the larger tiles, operands laid out, split sums ---------------------------------
 LARGE = [(16, 1030, 1031, 1029), (16, 1024, 1040, 1032), (2, 4100, 2056, 136), (1, 2049, 4104, 3001), (1, 200, 6000, 2500), (3, 300, 128, 9000),
          (1, 70, 3000, 10240), (16, 1024, 776, 1016), (16, 1021, 775, 1013)]
