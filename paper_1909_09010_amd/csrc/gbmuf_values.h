@@ -51,8 +51,8 @@ __device__ __forceinline__ void store_one(void *p, int64_t i, int32_t type, floa
 
 // e^x for x <= 0, within 2 units: 2^(x / ln 2), the quotient in two parts, of which the second is put in as 1 + r ln 2.  Nothing is left of it below -200.
 // With it and the reciprocal instruction (1 unit) a logistic function takes 14 instructions, where expf and a division that rounds exactly take 27.  An
-// epilogue's activation is done while the CU does nothing else: 4 x 5120 x 8192 x 1024 bf16, us without one 405, with silu 413 (expf: 468), sigmoid 410
-// (458), tanh 448 (468), gelu 477 (545); its gradients with silu 825 (918), gelu 860 (966).
+// epilogue's activation is done while the CU does nothing else: 4 x 5120 x 8192 x 1024 bf16, us without one 365, with relu 375, silu 410 (expf: 468),
+// sigmoid 403 (458), tanh 430 (468), gelu 465 (545); its gradients with silu 825 (918), gelu 860 (966).
 __device__ __forceinline__ float exp_below(float x)
 {
     x = x < -200.0f ? -200.0f : x;
@@ -215,11 +215,14 @@ __device__ __forceinline__ void store_eight(void *p, int64_t i, int32_t type, co
     else write8<kF16>(p, i, v);
 }
 
-__device__ __forceinline__ Eight activate8(Eight z, int32_t act)
+template <int N>
+__device__ __forceinline__ void activate_all(Eight (&z)[N], int32_t act)
 {
     const auto all = [&](auto f) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z.v[c >> 2][c & 3] = f(z.v[c >> 2][c & 3]);
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[k].v[c >> 2][c & 3] = f(z[k].v[c >> 2][c & 3]);
     };
     switch (act) {
         case GBMUF_ACT_RELU: all([](float v) { return activate(v, GBMUF_ACT_RELU); }); break;
@@ -229,7 +232,6 @@ __device__ __forceinline__ Eight activate8(Eight z, int32_t act)
         case GBMUF_ACT_TANH: all([](float v) { return activate(v, GBMUF_ACT_TANH); }); break;
         default: break;
     }
-    return z;
 }
 
 // What follows 8 sums side by side, of which `left` are the matrix's.
@@ -249,7 +251,9 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t g, int64_t m,
     if (e.bias) add(load_eight(e.bias, g * e.bias_batch + n, e.type));
     if (e.place == GBMUF_RESIDUAL_BEFORE) add(r);
     if (e.pre) store_eight(e.pre, g * e.p_batch + m * e.ldp + n, e.type, z);
-    z = activate8(z, e.act);
+    Eight one[1] = {z};
+    activate_all(one, e.act);
+    z = one[0];
     if (e.place == GBMUF_RESIDUAL_AFTER) add(r);
     store_eight(e.y, g * e.y_batch + m * e.ldy + n, e.type, z);
 }
