@@ -29,8 +29,16 @@ static_assert(sizeof(GradTile) == 64, "half a cache line");
 
 // Workgroups take 16 KB each, 4096 values of f32 or 8192 of 16-bit numbers: all loads are under way before the first value is used.  Clipping, Adagrad's
 // step of 16 x 19.8 M f32, us: tiles of 1 K 843, 1592; 2 K 712, 1527; 4 K 674, 1503; 8 K 692, 1510; 32 K 709, 1515.  The norm of 16 x 19.8 M bf16: 4 K 130,
-// 8 K 115.  Bound by HBM: the norm reads 6 TB/s.  Streamed accesses and tiles dealt in runs to the XCDs gain nothing.
+// 8 K 115.  Handles that make less than 1024 workgroups take half as much, down to 1024 values, as long as no worker has more tiles than a workgroup has
+// threads, which lets the kernel after the norm join its sums: the step of 4 x 100,000 bf16, clipped, 12.6 with 8 K, 7.1 with 1 K, 7.7 with 512.
+// Above what the caches hold bound by HBM, and by how its pages are met: accesses are streamed, which keeps neighbours together on their way, and a CU holds few workgroups at a
+// time, by LDS that they declare and do not use, so that what is in flight is one short moving range.  us, the norm, clipping in place and Adagrad's step
+// with it in blocks, 16 x 19.8 M f32: plain accesses 209, 682, 1505; streamed 189, 620, 1401; and 6, 3, 3 workgroups a CU 183, 585, 1385 (4 for all 190, 592,
+// 1402; 3 for all 235, 626, 1425).  The norm reads 6.9 TB/s, clipping moves 6.5, the step alone 5.3.
+// Below, plain accesses: the step of 8 x 2 M f32 in rows 63 where streamed ones take 70, of 16 x 2 M 134 and 129, of 16 x 4 M 280 and 249.
 constexpr int kThreads = 256, kTile = 4096, kJoinThreads = 1024;
+constexpr int64_t kCached = 24 << 20, kManyTiles = 1024, kLeastTile = 1024;       // values, workgroups, values
+constexpr int kSixPerCu = 24 * 128, kThreePerCu = 50 * 128;        // doubles of LDS
 
 __device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
 {
@@ -46,26 +54,30 @@ struct Some {
 };
 
 template <int T, int V>
+struct Piece {                   // at any address that the type allows
+    typedef typename Num<T>::type type __attribute__((ext_vector_type(V), aligned(sizeof(typename Num<T>::type))));
+};
+
+template <bool S, int T, int V>
 __device__ __forceinline__ Some<V> read_some(const void *p, int64_t i)
 {
+    const auto at = reinterpret_cast<const typename Piece<T, V>::type *>(static_cast<const typename Num<T>::type *>(p) + i);
+    const typename Piece<T, V>::type x = S ? __builtin_nontemporal_load(at) : *at;
     Some<V> r;
-    if constexpr (V == 4) {
-        const v4f x = read4<T>(p, i);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) r.v[c] = x[c];
-    } else {
-        const Eight x = read8<T>(p, i);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) r.v[c] = x.v[c >> 2][c & 3];
-    }
+    for (int c = 0; c < V; ++c) r.v[c] = static_cast<float>(x[c]);
     return r;
 }
 
-template <int T, int V>
+template <bool S, int T, int V>
 __device__ __forceinline__ void write_some(void *p, int64_t i, const Some<V> &r)
 {
-    if constexpr (V == 4) write4<T>(p, i, v4f{r.v[0], r.v[1], r.v[2], r.v[3]});
-    else write8<T>(p, i, Eight{{v4f{r.v[0], r.v[1], r.v[2], r.v[3]}, v4f{r.v[4], r.v[5], r.v[6], r.v[7]}}});
+    const auto at = reinterpret_cast<typename Piece<T, V>::type *>(static_cast<typename Num<T>::type *>(p) + i);
+    typename Piece<T, V>::type x;
+#pragma unroll
+    for (int c = 0; c < V; ++c) x[c] = static_cast<typename Num<T>::type>(r.v[c]);
+    if constexpr (S) __builtin_nontemporal_store(x, at);
+    else *at = x;
 }
 
 // The tile's values, V at a time that lie side by side in the tensor: U times V are loaded, load(i), before the first are used, use(i, what was
@@ -112,14 +124,14 @@ __device__ __forceinline__ double block_sum(double s, double *lds)
     return s;
 }
 
-template <int T>
+template <bool S, int T>
 __device__ __forceinline__ double tile_squares(const GradTile &tile)
 {
     const GradTensor &t = tile.t;
     double s = 0.0;
     const auto add = [&](float v) { s = fma(static_cast<double>(v), static_cast<double>(v), s); };
     constexpr int V = T == kF32 ? 4 : 8;
-    each<V, 4>(tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+    each<V, 4>(tile, [&](int64_t i) { return read_some<S, T, V>(t.p, grad_at(t, i)); },
             [&](int64_t, const Some<V> &v) {
 #pragma unroll
                 for (int c = 0; c < V; ++c) add(v.v[c]);
@@ -128,11 +140,12 @@ __device__ __forceinline__ double tile_squares(const GradTile &tile)
     return s;
 }
 
+template <bool S>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const GradTile *tiles, double *partial)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[S ? kSixPerCu : 4];
     const GradTile tile = tiles[blockIdx.x];
-    double s = tile.t.type == kF32 ? tile_squares<kF32>(tile) : tile.t.type == kBf16 ? tile_squares<kBf16>(tile) : tile_squares<kF16>(tile);
+    double s = tile.t.type == kF32 ? tile_squares<S, kF32>(tile) : tile.t.type == kBf16 ? tile_squares<S, kBf16>(tile) : tile_squares<S, kF16>(tile);
     s = block_sum<kThreads>(s, lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -173,16 +186,16 @@ __device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t
 
 __device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most || most == INFINITY ? 1.0f : most / norm; }
 
-template <int T, int D>
+template <bool S, int T, int D>
 __device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor &d, float f)
 {
     const GradTensor &t = tile.t;
     constexpr int V = T == kF32 || D == kF32 ? 4 : 8;
-    each<V, 4>(tile, [&](int64_t i) { return read_some<T, V>(t.p, grad_at(t, i)); },
+    each<V, 4>(tile, [&](int64_t i) { return read_some<S, T, V>(t.p, grad_at(t, i)); },
             [&](int64_t i, Some<V> v) {
 #pragma unroll
                 for (int c = 0; c < V; ++c) v.v[c] *= f;
-                if (d.ld == d.cols || i % d.cols + V <= d.cols) write_some<D, V>(d.p, grad_at(d, i), v);
+                if (d.ld == d.cols || i % d.cols + V <= d.cols) write_some<S, D, V>(d.p, grad_at(d, i), v);
                 else
 #pragma unroll
                     for (int c = 0; c < V; ++c) store_one(d.p, grad_at(d, i + c), D, v.v[c]);
@@ -190,26 +203,27 @@ __device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor
             [&](int64_t i) { store_one(d.p, grad_at(d, i), D, load_one(t.p, grad_at(t, i), T) * f); });
 }
 
-template <int T>
+template <bool S, int T>
 __device__ __forceinline__ void clip_to(const GradTile &tile, const GradTensor &d, float f)
 {
-    if (d.type == kF32) clip_tile<T, kF32>(tile, d, f);
-    else if (d.type == kBf16) clip_tile<T, kBf16>(tile, d, f);
-    else clip_tile<T, kF16>(tile, d, f);
+    if (d.type == kF32) clip_tile<S, T, kF32>(tile, d, f);
+    else if (d.type == kBf16) clip_tile<S, T, kBf16>(tile, d, f);
+    else clip_tile<S, T, kF16>(tile, d, f);
 }
 
 // Tiles are taken from the last to the first: what the norm read last is still in the caches.
+template <bool S>
 __global__ __launch_bounds__(kThreads) void clip_kernel(const GradTile *tiles, const GradTensor *to, Norms norms, float most, int32_t in_place)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[S ? kThreePerCu : 4];
     const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);
     const GradTile tile = tiles[number];
     const GradTensor d = to[tile.tensor];
     const float f = clip_factor(norm_of(norms, tile.t.worker, number, lds), most);
     if (in_place && f == 1.0f) return;                     // nothing changes
-    if (tile.t.type == kF32) clip_to<kF32>(tile, d, f);
-    else if (tile.t.type == kBf16) clip_to<kBf16>(tile, d, f);
-    else clip_to<kF16>(tile, d, f);
+    if (tile.t.type == kF32) clip_to<S, kF32>(tile, d, f);
+    else if (tile.t.type == kBf16) clip_to<S, kBf16>(tile, d, f);
+    else clip_to<S, kF16>(tile, d, f);
 }
 
 struct StepArgs {
@@ -236,7 +250,7 @@ struct StepFour {
     Some<4> g, theta, h;
 };
 
-template <int T>
+template <bool S, int T>
 __device__ __forceinline__ void step_tile(const GradTile &tile, float f, const StepArgs &a)
 {
     const GradTensor &t = tile.t;
@@ -253,14 +267,14 @@ __device__ __forceinline__ void step_tile(const GradTile &tile, float f, const S
     };
     // four parameters that a block's edge parts are taken one by one
     const auto together = [&](int64_t e) { return ((e ^ (e + 3)) >> a.at.logB) == 0 && (!sums || ((e ^ (e + 3)) >> a.sums_at.logB) == 0); };
-    each<4, 1>(tile,
+    each<4, 4>(tile,
             [&](int64_t i) {
                 StepFour s{};
                 const int64_t e = t.offset + i;
                 if (!together(e)) return s;
-                s.g = read_some<T, 4>(t.p, grad_at(t, i));
-                s.theta = read_some<kF32, 4>(theta, placed(a.at, e));
-                if (sums) s.h = read_some<kF32, 4>(sums, placed(a.sums_at, e));
+                s.g = read_some<S, T, 4>(t.p, grad_at(t, i));
+                s.theta = read_some<S, kF32, 4>(theta, placed(a.at, e));
+                if (sums) s.h = read_some<S, kF32, 4>(sums, placed(a.sums_at, e));
                 return s;
             },
             [&](int64_t i, StepFour s) {
@@ -271,15 +285,16 @@ __device__ __forceinline__ void step_tile(const GradTile &tile, float f, const S
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) update(s.theta.v[c], s.h.v[c], s.g.v[c] * f, a);
-                write_some<kF32, 4>(theta, placed(a.at, e), s.theta);
-                if (sums) write_some<kF32, 4>(sums, placed(a.sums_at, e), s.h);
+                write_some<S, kF32, 4>(theta, placed(a.at, e), s.theta);
+                if (sums) write_some<S, kF32, 4>(sums, placed(a.sums_at, e), s.h);
             },
             one);
 }
 
+template <bool S>
 __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a)
 {
-    __shared__ double lds[4];
+    __shared__ double lds[S ? kThreePerCu : 4];
     const int32_t number = static_cast<int32_t>(gridDim.x - 1 - blockIdx.x);       // as clip_kernel
     const GradTile tile = a.tiles[number];
     float f = 1.0f;
@@ -288,9 +303,9 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs a)
         if (a.skip_nonfinite && !(norm < INFINITY)) return;
         f = clip_factor(norm, a.most);
     }
-    if (tile.t.type == kF32) step_tile<kF32>(tile, f, a);
-    else if (tile.t.type == kBf16) step_tile<kBf16>(tile, f, a);
-    else step_tile<kF16>(tile, f, a);
+    if (tile.t.type == kF32) step_tile<S, kF32>(tile, f, a);
+    else if (tile.t.type == kBf16) step_tile<S, kBf16>(tile, f, a);
+    else step_tile<S, kF16>(tile, f, a);
 }
 
 }  // namespace
@@ -302,6 +317,7 @@ struct gbmuf_grads_s {
     int32_t workers = 0;
     int device = -1;
     int64_t n_tiles = 0, reach = 0;              // reach: end of the last tensor among a worker's parameters
+    bool streamed = false;                       // more than the caches hold
     bool few = false;                            // every worker has tiles, one for a thread at most
     std::vector<GradTensor> tensors;             // by worker, in the order of the list
     GradTensor *d_tensors = nullptr;
@@ -359,13 +375,27 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
         if (before && before->worker == t.worker && before->offset + before->rows * before->cols > t.offset) return GBMUF_EINVAL;
         before = &t;
     }
-    int64_t size = 2 * kTile;                              // one size for a handle: f32 anywhere in it takes the smaller
-    for (const GradTensor &t : h.tensors)
+    int64_t size = 2 * kTile, values = 0;                  // one size for a handle: f32 anywhere in it takes the smaller
+    for (const GradTensor &t : h.tensors) {
         if (t.type == kF32) size = kTile;
+        values += t.rows * t.cols;
+    }
+    int64_t most = 0;                                      // of one worker
+    const auto count_tiles = [&](int64_t of) {
+        int64_t all = 0;
+        std::fill(next.begin(), next.end(), 0);
+        for (const GradTensor &t : h.tensors) {
+            const int64_t n = (t.rows * t.cols + of - 1) / of;
+            all += n;
+            next[static_cast<size_t>(t.worker)] += n;
+        }
+        most = *std::max_element(next.begin(), next.end());
+        return all;
+    };
+    while (size > kLeastTile && count_tiles(size) < kManyTiles && count_tiles(size / 2) >= 0 && most <= kThreads) size /= 2;
     std::vector<GradTile> tiles;
     std::vector<int32_t> first(static_cast<size_t>(d.workers) + 1, 0);
-    int64_t count = 0;
-    for (const GradTensor &t : h.tensors) count += (t.rows * t.cols + size - 1) / size;
+    const int64_t count = count_tiles(size);
     if (count > 0x7fffffffLL / kThreads) return GBMUF_EUNSUPPORTED;
     tiles.reserve(static_cast<size_t>(count));
     for (size_t i = 0; i < h.tensors.size(); ++i) {
@@ -375,6 +405,7 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
     }
     for (size_t w = 1; w < first.size(); ++w) first[w] = std::max(first[w], first[w - 1]);
     h.n_tiles = count;
+    h.streamed = values > kCached;
     h.few = true;
     for (size_t w = 0; w + 1 < first.size(); ++w) h.few = h.few && first[w + 1] > first[w] && first[w + 1] - first[w] <= kThreads;
     int devices = 0;
@@ -411,7 +442,7 @@ int enqueue_norm(const gbmuf_grads_s *g, float *norms, Norms *joined, hipStream_
     double *partial = g->d_partial;
     const int32_t *first = g->d_first;
     void *a1[] = {&tiles, &partial}, *a2[] = {&partial, &first, &norms};
-    const int rc = launch(reinterpret_cast<const void *>(norm_kernel), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
+    const int rc = launch(reinterpret_cast<const void *>(g->streamed ? norm_kernel<true> : norm_kernel<false>), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
     if (rc != GBMUF_OK) return rc;
     if (joined) *joined = Norms{norms, g->few ? partial : nullptr, first};
     if (joined && g->few) return GBMUF_OK;
@@ -524,7 +555,7 @@ int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float ma
     const GradTensor *to = dst->d_tensors;
     int32_t in_place = src == dst ? 1 : 0;
     void *argv[] = {&tiles, &to, &n, &max_norm, &in_place};
-    return launch(reinterpret_cast<const void *>(clip_kernel), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
+    return launch(reinterpret_cast<const void *>(src->streamed ? clip_kernel<true> : clip_kernel<false>), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
 }
 
 int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, const gbmuf_state_t *theta, const gbmuf_state_t *sums, float *norms,
@@ -552,7 +583,7 @@ int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, 
     a.theta = theta->theta;
     a.rate = desc->rate; a.eps = desc->eps; a.most = desc->max_norm; a.skip_nonfinite = desc->skip_nonfinite;
     void *argv[] = {&a};
-    return launch(reinterpret_cast<const void *>(step_kernel), grads->n_tiles, argv, "hipLaunchKernel(local step)", s);
+    return launch(reinterpret_cast<const void *>(grads->streamed ? step_kernel<true> : step_kernel<false>), grads->n_tiles, argv, "hipLaunchKernel(local step)", s);
 }
 
 }  // extern "C"
