@@ -487,9 +487,9 @@ int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream);
 
 /*
  * gbmuf_grad_clip -- the norms, and dst = c_w * src with c_w = 1 where norms[w] <= max_norm and max_norm / norms[w] elsewhere
- * (a norm that is NaN makes NaN of the worker's gradients).  dst has the tensors of src, in the same order and with the same
- * rows, cols and worker; it may be src, or lie elsewhere and have other dtypes.  Tensors of dst must not share values with each
- * other or, unless dst is src, with src.
+ * (a norm that is NaN makes NaN of the worker's gradients).  dst has the tensors of src, in the same order, of the same worker and with
+ * as many values, which are counted row by row; it may be src, or lie elsewhere with other strides and dtypes.  Tensors of dst must not
+ * share values with each other or, unless dst is src, with src.
  * EINVAL also for max_norm < 0 or NaN (INFINITY: copies, whatever the norm) and for a dst whose tensors differ.
  */
 int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream);

@@ -543,7 +543,7 @@ int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float ma
         if (src->workers != dst->workers || src->tensors.size() != dst->tensors.size()) return GBMUF_EINVAL;
         for (size_t i = 0; i < src->tensors.size(); ++i) {
             const GradTensor &a = src->tensors[i], &b = dst->tensors[i];
-            if (a.worker != b.worker || a.rows != b.rows || a.cols != b.cols) return GBMUF_EINVAL;
+            if (a.worker != b.worker || a.rows * a.cols != b.rows * b.cols) return GBMUF_EINVAL;
         }
     }
     int rc = check_grads_device(src);

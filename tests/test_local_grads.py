@@ -341,6 +341,45 @@ def test_handles_that_are_refused():
         B.Grads([[torch.zeros(4, 5, 6)[:, :, 1:]]])
 
 
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("layout", ["rows", "blocked"])
+def test_more_than_the_caches_hold(dtype, layout):
+    """26 M values of 2 workers, tensors of odd sizes, rows with gaps and unaligned views: norm, clipping apart and in place, the step."""
+    K, P = 2, 13_000_040
+    rng = np.random.default_rng(11)
+    flat = torch.tensor(rng.standard_normal((K, P + 3), dtype=np.float32)).to(dtype)
+    dev = flat.to(DEV)
+    wide = torch.zeros(K, 1000, 40, dtype=dtype, device=DEV)
+    wide[:, :, 1:34] = dev[:, 1: 33001].view(K, 1000, 33)
+    ts = [[wide[w, :, 1:34], dev[w, 33001: 8_000_000], dev[w, 8_000_000: P + 1]] for w in range(K)]
+    values = flat[:, 1: P + 1]
+    h, n = B.Grads(ts), torch.empty(K, device=DEV)
+    out = [[torch.empty(t.shape, dtype=torch.float32, device=DEV) for t in w] for w in ts]
+    h.clip(3.0, n, out=B.Grads(out), stream=torch.cuda.current_stream())
+    norms = n.cpu().numpy()
+    want = np.array([math.sqrt(float(values[w].double().square().sum())) for w in range(K)])
+    assert np.all(np.abs(norms - want) <= 2.0 ** -23 * want)
+    clipped = [values[w].float() * torch.tensor(factor(norms[w], 3.0)) for w in range(K)]
+    for w in range(K):
+        assert torch.equal(torch.cat([t.reshape(-1) for t in out[w]]).cpu(), clipped[w])
+    theta, sums = rng.standard_normal((K, P), dtype=np.float32), rng.random((K, P), dtype=np.float32) + np.float32(0.1)
+    t, s = Placed(torch.tensor(theta), layout), Placed(torch.tensor(sums), layout)
+    h.local_step(t.state, s.state, P, 0.1, 1e-7, 3.0, n, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert np.array_equal(n.cpu().numpy(), norms)
+    got, got_sums = t.get(), s.get()
+    for w in range(K):
+        a, b = step_numpy(theta[w], sums[w], values[w].float().numpy(), factor(norms[w], 3.0), 0.1, 1e-7)
+        assert np.array_equal(got[w], a) and np.array_equal(got_sums[w], b)
+    assert t.rest() and s.rest()
+    h.clip(3.0, n, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for w in range(K):
+        assert torch.equal(torch.cat([x.reshape(-1) for x in ts[w]]).cpu(), clipped[w].to(dtype))
+    assert (wide[:, :, 0] == 0).all() and (wide[:, :, 34:] == 0).all() and torch.equal(dev[:, 0].cpu(), flat[:, 0])
+
+
 def test_calls_that_are_refused():
     ts = [[torch.zeros(10), torch.zeros(4, 5)], [torch.zeros(30)]]
     h, n, theta, sums = B.Grads(ts) if not torch.cuda.is_available() else None, torch.zeros(2), torch.zeros(2, 30), torch.zeros(2, 30)
