@@ -13,6 +13,7 @@ namespace {
 constexpr int64_t kLargest = 0x7fffffff;
 constexpr double kMostTiles = 1 << 21;       // of 128 x 128 results or operands: four of 64 x 64 each are what a grid of 256 threads holds
 constexpr int64_t kStepWords = 64;
+constexpr int64_t kCached = 128 << 20;        // bytes
 
 // ---------------------------------------------------------------------------------------
 // Checks
@@ -215,10 +216,12 @@ Operand packed(Space &space, int64_t R, int64_t C, int32_t batch, int32_t writte
     return o;
 }
 
-Epilogue into(const gbmuf_matrix_t &m, int32_t type)
+// values: of all workers
+Epilogue into(const gbmuf_matrix_t &m, int64_t values, int32_t type)
 {
     Epilogue e{};
     e.y = m.data; e.ldy = m.ld; e.y_batch = m.batch_stride; e.type = type;
+    e.streamed = values * static_cast<int64_t>(type_bytes(type)) > kCached ? 1 : 0;
     return e;
 }
 
@@ -309,7 +312,7 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
     const gbmuf_matrix_t none{};
     Epilogue e{};
     if (io) {
-        e = into(io->y, type);
+        e = into(io->y, G * M * N, type);
         e.pre = io->pre.data; e.ldp = io->pre.ld; e.p_batch = io->pre.batch_stride;
         e.bias = io->bias.data; e.bias_batch = io->bias.batch_stride;
         e.res = io->residual.data; e.ldr = io->residual.ld; e.r_batch = io->residual.batch_stride;
@@ -361,7 +364,7 @@ int forward(const gbmuf_linear_desc_t &d, const gbmuf_linear_io_t *io, Space &sp
 // dw's epilogue
 Epilogue weight_grad(const gbmuf_linear_desc_t &d, const gbmuf_matrix_t &m, int32_t type)
 {
-    Epilogue e = into(m, type);
+    Epilogue e = into(m, d.batch * d.out_features * d.in_features, type);
     if (d.accumulate) { e.place = GBMUF_RESIDUAL_AFTER; e.res = m.data; e.ldr = m.ld; e.r_batch = m.batch_stride; }
     return e;
 }
@@ -377,7 +380,7 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
     if (d.activation) { z.pre = at.pre.data; z.ldp = at.pre.ld; z.p_batch = at.pre.batch_stride; z.act = d.activation; }
     const Cut both = direct_cut(N, K, M, G, false), cw = direct_cut(N, dw ? K : 0, M, G, false);
     const Cut cx = chain_cut(M, dx ? K : 0, N, G, both);           // as for both products, so that the workspace is the same for one
-    const Epilogue e = into(at.dx, type);
+    const Epilogue e = into(at.dx, G * M * K, type);
     DirectArgs px = direct_args(z, source_of(at.w), N, cx, e);
     DirectArgs pw = direct_args(z, source_of(at.x), M, cw, weight_grad(d, at.dw, grad_type));
     px.t.partial = space.take<float>(cx.partial);
@@ -446,7 +449,7 @@ int backward_split(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *i
     if ((rc = launch_stats(stats, stream)) != GBMUF_OK) return rc;
     if (db && (rc = sum_columns(d, at.dbias, sums, kF32, stream)) != GBMUF_OK) return rc;
     if ((rc = launch_lay(lay, stream)) != GBMUF_OK) return rc;
-    if (dx && (rc = run_product(z, wt, N, kF32, into(at.dx, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
+    if (dx && (rc = run_product(z, wt, N, kF32, into(at.dx, G * M * K, kF32), sx, partial, stream)) != GBMUF_OK) return rc;
     return dw ? run_product(zt, xt, M, kF32, weight_grad(d, at.dw, kF32), sw, partial, stream) : rc;
 }
 
@@ -490,7 +493,7 @@ int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, 
     if (copy_x) add(lx, x, true);
     int rc = launch_copy(set, stream);
     if (rc == GBMUF_OK && db) rc = sum_columns(d, at.dbias, sums, grad_type, stream);
-    if (rc == GBMUF_OK && dx) rc = run_product(z, w, N, type, into(at.dx, type), sx, partial, stream);
+    if (rc == GBMUF_OK && dx) rc = run_product(z, w, N, type, into(at.dx, G * M * K, type), sx, partial, stream);
     if (rc == GBMUF_OK && dw) rc = run_product(zt, x, M, type, weight_grad(d, at.dw, grad_type), sw, partial, stream);
     return rc;
 }

@@ -16,7 +16,7 @@ struct Epilogue {
     int64_t ldy, y_batch, ldp, p_batch, bias_batch, ldr, r_batch;
     int32_t act, place;      // GBMUF_ACT_*, GBMUF_RESIDUAL_*
     int32_t type;            // of all of them
-    int32_t reserved;
+    int32_t streamed;        // y is more than the caches hold
 };
 
 // Which tiles of a result there are and how workgroups take them: the first `whole` tiles one each, and the sum over k of every other one

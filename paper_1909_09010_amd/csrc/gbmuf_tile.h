@@ -126,7 +126,7 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
                 z[k] = scaled(z[k], top[SPLIT ? k : 0]);
                 z[k].v[0] += r[k].v[0];
                 z[k].v[1] += r[k].v[1];
-                if (m_of(k) < M) store_eight(e.y, g * e.y_batch + m_of(k) * e.ldy + n, e.type, z[k]);
+                if (m_of(k) < M) store_result(e, e.y, g * e.y_batch + m_of(k) * e.ldy + n, z[k]);
             }
         } else if (left >= 8) {
             // two rows at a time (with tanh 430 us where one took 446, bf16, 4 x 5120 x 8192 x 1024; four do not fit the registers)
@@ -147,7 +147,7 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
                 const auto store = [&](void *to, int64_t batch, int64_t ld) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
-                        if (m(u) < M) store_eight(to, g * batch + m(u) * ld + n, e.type, z[u]);
+                        if (m(u) < M) store_result(e, to, g * batch + m(u) * ld + n, z[u]);
                 };
 #pragma unroll
                 for (int u = 0; u < 2; ++u) z[u] = get(k0 + u);

@@ -187,19 +187,20 @@ __device__ __forceinline__ Eight read8(const void *p, int64_t i)
     return e;
 }
 
-template <int T>
+template <int T, bool STREAMED = false>
 __device__ __forceinline__ void write8(void *p, int64_t i, const Eight &e)
 {
     using N = typename Num<T>::type;
-    if constexpr (T == kF32) {
-        write4<T>(p, i, e.v[0]);
-        write4<T>(p, i + 4, e.v[1]);
-    } else {
-        typedef N N8 __attribute__((ext_vector_type(8), aligned(2)));
-        N8 r;
+    constexpr int V = T == kF32 ? 4 : 8;
+    typedef N Piece __attribute__((ext_vector_type(V), aligned(sizeof(N))));
 #pragma unroll
-        for (int c = 0; c < 8; ++c) r[c] = static_cast<N>(e.v[c >> 2][c & 3]);
-        *reinterpret_cast<N8 *>(static_cast<N *>(p) + i) = r;
+    for (int k = 0; k < 8; k += V) {
+        Piece r;
+#pragma unroll
+        for (int c = 0; c < V; ++c) r[c] = static_cast<N>(e.v[(k + c) >> 2][(k + c) & 3]);
+        Piece *to = reinterpret_cast<Piece *>(static_cast<N *>(p) + i + k);
+        if constexpr (STREAMED) __builtin_nontemporal_store(r, to);
+        else *to = r;
     }
 }
 
@@ -208,11 +209,20 @@ __device__ __forceinline__ Eight load_eight(const void *p, int64_t i, int32_t ty
     return type == kF32 ? read8<kF32>(p, i) : type == kBf16 ? read8<kBf16>(p, i) : read8<kF16>(p, i);
 }
 
+template <bool STREAMED = false>
 __device__ __forceinline__ void store_eight(void *p, int64_t i, int32_t type, const Eight &v)
 {
-    if (type == kF32) write8<kF32>(p, i, v);
-    else if (type == kBf16) write8<kBf16>(p, i, v);
-    else write8<kF16>(p, i, v);
+    if (type == kF32) write8<kF32, STREAMED>(p, i, v);
+    else if (type == kBf16) write8<kBf16, STREAMED>(p, i, v);
+    else write8<kF16, STREAMED>(p, i, v);
+}
+
+// An epilogue's y or pre.  Streamed, where that is more than the caches hold, it leaves them to the operands: 8 x 5120 x 8192 x 512 bf16 (671 MB) 474 us
+// before, 430 now, x 8197 514 and 477.
+__device__ __forceinline__ void store_result(const Epilogue &e, void *p, int64_t i, const Eight &v)
+{
+    if (e.streamed) store_eight<true>(p, i, e.type, v);
+    else store_eight(p, i, e.type, v);
 }
 
 template <int N>
@@ -250,12 +260,12 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t g, int64_t m,
     if (e.place) r = load_eight(e.res, g * e.r_batch + m * e.ldr + n, e.type);
     if (e.bias) add(load_eight(e.bias, g * e.bias_batch + n, e.type));
     if (e.place == GBMUF_RESIDUAL_BEFORE) add(r);
-    if (e.pre) store_eight(e.pre, g * e.p_batch + m * e.ldp + n, e.type, z);
+    if (e.pre) store_result(e, e.pre, g * e.p_batch + m * e.ldp + n, z);
     Eight one[1] = {z};
     activate_all(one, e.act);
     z = one[0];
     if (e.place == GBMUF_RESIDUAL_AFTER) add(r);
-    store_eight(e.y, g * e.y_batch + m * e.ldy + n, e.type, z);
+    store_result(e, e.y, g * e.y_batch + m * e.ldy + n, z);
 }
 
 // v times the slope at z

@@ -578,6 +578,37 @@ def test_infinities_in_large_f32_products_reach_only_their_rows():
     assert not torch.isfinite(got[bad]).any() and torch.equal(got[~bad], clean[~bad])
 
 
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("act,N", [(B.ACT_NONE, 4104), (B.ACT_GELU, 4099)])
+def test_results_above_what_the_caches_hold_are_those_of_their_rows(dtype, act, N):
+    """Every element's sum has one order, so a call gives the bits of calls on its rows, whose results are small (but of more than 4e9 operations, from
+    where on f32 is taken apart)."""
+    G, M, K = 2, 8232, 160
+    g = torch.Generator().manual_seed(15)
+    x, w, b, r = (make(s, dtype, g).to(DEV) for s in ((G, M, K), (G, N, K), (G, N), (G, 1, N)))
+    r = r.expand(G, M, N)
+
+    def run(x, r):
+        lin = B.Linear(x.shape[1], N, K, G, dtype, act, B.RESIDUAL_AFTER)
+        y = torch.empty(G, x.shape[1], N, dtype=dtype, device=DEV)
+        z = torch.empty_like(y) if act else None
+        ws = torch.empty(max(lin.workspace_bytes(), 256), dtype=torch.uint8, device=DEV)
+        lin.forward(lin.forward_io(x, w, y, bias=b, residual=r, pre=z), ws, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        return y, z
+    y, z = run(x, r)
+    for i in range(0, M, 2058):
+        part = [t.contiguous() for t in (x[:, i: i + 2058], r[:, i: i + 2058])]
+        py, pz = run(*part)
+        assert torch.equal(y[:, i: i + 2058], py) and (z is None or torch.equal(z[:, i: i + 2058], pz))
+    X, W, rows = x[:, 4000:4050].cpu().double(), w.cpu().double(), slice(4000, 4050)
+    s, S = mm(X, W) + b.cpu().double()[:, None], mm(X.abs(), W.abs()) + b.cpu().double().abs()[:, None]
+    out, h = act64(s, act) + r[:, rows].cpu().double(), HALF[dtype]
+    bound = 1.2 * sum_bound(K, S, dtype, spread(X, W)) + 16 * U * (s.abs() + out.abs() + 1)
+    assert ((y[:, rows].cpu().double() - out).abs() <= bound + h * (out.abs() + bound) + 2.0 ** -25).all()
+
+
 # -- streams, graphs, equal bits ------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", DTYPES)
