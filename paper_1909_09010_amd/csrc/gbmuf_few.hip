@@ -42,7 +42,8 @@ __device__ __forceinline__ v4f product(v4u w, v4u x, v4f acc)
     }
 }
 
-// A workgroup takes 16 NT rows of w for all rows of x (up to 16 MT); its waves share the sum over k in turns of UNROLL steps.
+// A workgroup takes 16 NT rows of w for all rows of x (up to 16 MT); its waves share the sum over k in turns of UNROLL steps.  Bound by the reading of w: 8 x
+// 50,000 x 1024 bf16, w out of HBM, 21.6 us, 4.75 TB/s (twice the steps under way 21.7, streamed loads 23.6).
 template <int T, int MT, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(DirectArgs a)
 {
