@@ -253,15 +253,18 @@ Cut direct_cut(int64_t M, int64_t N, int64_t K, int64_t batch, bool may_cut)
     return cut(64, M, N, batch, steps, may_cut && tiles < 256 ? 256 : std::max<int64_t>(tiles, 1), 0.5);
 }
 
-// Gradients: dx's sums are usually the longer ones, and a workgroup that shares its CU with others takes 1.2 us a step or so, so they are cut to last
-// no longer than the matrix instructions of both products (f32: 4 x 128 x 2600 x 650, 82 steps of 88 tiles and 4 of 1804, 79 us in two parts, 65 in
-// four; 16 x 128 x 512 x 512, 16 steps of 256 tiles and 4 of 1024, 34 whole, 40 in two; 1 x 64 x 200,000 x 64 141 in 64 parts, 87 in 358).
+// Gradients: dx's sums are usually the longer ones, and a workgroup that shares its CU with others takes 1.2 us a step or more.  Sums that would last as
+// long as the matrix instructions of both products at their rate, or longer, are cut to last half of that (us, f32: 4 x 128 x 2600 x 650, 82 steps of 88 tiles and
+// 4 of 1804, 79 in two parts, 65 in four, 62 in eight; 8 x 128 x 2600 x 650 152 whole, 124 in two, 105 in four; 11 x 16 x 28173 x 942, 881 steps of 165 tiles and one
+// of 72,765, 1890 in two, 1324 in four; 16 x 128 x 512 x 512, 16 steps of 256 tiles and 4 of 1024, 34 whole, 40 in two), but not into more than 64 parts
+// for that (1 x 64 x 200,000 x 64 141 in 64, 87 in 358, 116 in 716).
 Cut chain_cut(int64_t M, int64_t N, int64_t K, int64_t batch, const Cut &other)
 {
     const int64_t steps = (K + 31) / 32, tiles = (M + 63) / 64 * ((N + 63) / 64) * batch;
     Cut c = cut(64, M, N, batch, steps, std::max<int64_t>(tiles, 1), 0.5);
     const int64_t all = tiles * steps + static_cast<int64_t>(other.t.whole) * other.t.steps;
-    const int64_t parts = tiles > 0 ? std::min(steps / 8, steps * 256 * 14 / (5 * (all + 1))) : 1;
+    int64_t parts = tiles > 0 ? steps * 256 * 14 / (5 * (all + 1)) : 1;
+    if (parts >= 2) parts = std::min(steps / 8, std::max(parts, std::min<int64_t>(2 * parts, 64)));
     if (parts < 2) return c;
     const int64_t each = (steps + parts - 1) / parts, splits = (steps + each - 1) / each;
     c.t.whole = 0;
@@ -271,20 +274,32 @@ Cut chain_cut(int64_t M, int64_t N, int64_t K, int64_t batch, const Cut &other)
     return c;
 }
 
-// Operations of one product.
-double operations(const gbmuf_linear_desc_t &d)
+// Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions, which costs launches and passes
+// over them.  Both are estimated, in us: as they lie, by the steps of 64 x 64 x 32, of which the chip does 256 in 0.43 at best; laid out, by the launches, the values
+// that are laid out and the operations.  As they lie / laid out, workers x rows x out x in:
+//   forward f32: 1 x 200 x 1024 x 512 15 / 20, 4 x 200 x 1024 x 512 17 / 28, 8 x 250 x 1500 x 400 30 / 41, 8 x 128 x 2600 x 650 45 / 45 (with tanh and z
+//     kept, operands in HBM before the call, 45 / 57), 8 x 250 x 2000 x 400 39 / 35, 4 x 512 x 1024 x 1024 46 / 41, 16 x 512 x 1024 x 512 83 / 51
+//   gradients f32: 1 x 200 x 1024 x 512 16 / 42, 4 x 200 x 1024 x 512 32 / 50, 8 x 200 x 1024 x 512 53 / 60, 1 x 1000 x 1000 x 1000 64 / 64,
+//     8 x 128 x 2600 x 650 105 / 117, 8 x 250 x 2000 x 400 99 / 86, 11 x 16 x 28173 x 942 1233 / 1714
+//   gradients bf16: 1 x 200 x 1024 x 512 16 / 28, 8 x 128 x 400 x 400 22 / 26, 4 x 200 x 1024 x 512 34 / 30, 8 x 128 x 652 x 652 37 / 45,
+//     16 x 16 x 10000 x 650 420 / 277, 1 x 3 x 31296 x 768 92 / 53
+double steps_us(int64_t M, int64_t N, int64_t K, int64_t batch)
 {
-    return 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
+    return static_cast<double>((M + 63) / 64 * ((N + 63) / 64) * batch) * static_cast<double>((K + 31) / 32) * (0.43 / 256);
 }
 
-// Whether f32 arithmetic on the matrices as they lie is faster than laying them out for the 16-bit instructions, which costs launches and
-// passes over them.  us, as they lie / laid out, workers x rows x out x in:
-//   forward f32: 1 x 200 x 1024 x 512 15 / 20, 4 x 200 x 1024 x 512 17 / 28, 8 x 250 x 1500 x 400 30 / 41, 8 x 128 x 2600 x 650 45 / 45 (with tanh and z kept, operands in HBM before the call, 45 / 57),
-//     8 x 250 x 2000 x 400 39 / 35, 4 x 512 x 1024 x 1024 46 / 41, 16 x 512 x 1024 x 512 83 / 51
-//   gradients f32: 1 x 200 x 1024 x 512 16 / 42, 4 x 200 x 1024 x 512 32 / 50, 8 x 200 x 1024 x 512 53 / 60, 1 x 1000 x 1000 x 1000 64 / 64,
-//     8 x 128 x 2600 x 650 121 / 117, 8 x 250 x 2000 x 400 113 / 85
-//   gradients bf16: 1 x 200 x 1024 x 512 16 / 28, 8 x 128 x 400 x 400 22 / 26, 4 x 200 x 1024 x 512 34 / 30, 8 x 128 x 652 x 652 37 / 45
-bool takes_direct_forward(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && operations(d) <= 4e9; }
+double products_us(const gbmuf_linear_desc_t &d)
+{
+    return 2.0 * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features) *
+           (d.dtype == GBMUF_F32 ? 3.0 : 1.0) / 0.9e9;
+}
+
+bool takes_direct_forward(const gbmuf_linear_desc_t &d)
+{
+    if (d.dtype != GBMUF_F32) return false;
+    const double values = 1e-6 * d.batch * static_cast<double>(d.rows + d.out_features) * static_cast<double>(d.in_features);
+    return 9.0 + 1.4 * steps_us(d.rows, d.out_features, d.in_features, d.batch) <= 18.0 + 1.5 * values + products_us(d);
+}
 
 // What up to 64 rows take.  The kernel for few rows reads each matrix once in one launch, but for more than 16 rows of one the matrix cores (f32) or
 // the readings of x are what it waits for, where there are many outputs.  us, few rows / tiles of f32 / of 16 bits, 1024 to 50,000 outputs: f32, 20
@@ -299,7 +314,23 @@ Few few_of(const gbmuf_linear_desc_t &d)
     return Few::kUnlessAligned;
 }
 
-bool takes_direct_backward(const gbmuf_linear_desc_t &d) { return operations(d) <= (d.dtype == GBMUF_F32 ? 2e9 : 1e9); }
+// What a gradient of 16-bit types takes as it lies: matrices whose rows lie on 16 bytes and are whole pieces of that.
+bool as_it_lies(const gbmuf_matrix_t &m, int64_t cols) { return lies_well(m) && cols % 8 == 0; }
+
+bool takes_direct_backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t &io)
+{
+    const bool split = d.dtype == GBMUF_F32;
+    const double M = static_cast<double>(d.rows), N = static_cast<double>(d.out_features), K = static_cast<double>(d.in_features);
+    const bool dx = io.dx.data, dw = io.dw.data;
+    double values = 0.0;                                   // that are laid out
+    if (split) values = M * N * ((dx ? 1 : 0) + (dw ? 1 : 0)) + (dx ? N * K : 0.0) + (dw ? M * K : 0.0);
+    else values = (d.activation || !as_it_lies(io.dy, d.out_features) ? M * N : 0.0) + (dx && !as_it_lies(io.w, d.in_features) ? N * K : 0.0) +
+                  (dw && !as_it_lies(io.x, d.in_features) ? M * K : 0.0);
+    const double steps = (dx ? steps_us(d.rows, d.in_features, d.out_features, d.batch) : 0.0) +
+                         (dw ? steps_us(d.out_features, d.in_features, d.rows, d.batch) : 0.0);
+    const double laid = (split ? 38.0 : 28.0) + (split ? 3e-6 : 2e-6) * d.batch * values + ((dx ? 1 : 0) + (dw ? 1 : 0)) * products_us(d);
+    return 10.0 + 2.2 * steps <= laid;
+}
 
 // ---------------------------------------------------------------------------------------
 // Forward.  io nullptr: only count the workspace, for matrices that lie as badly as can be.
@@ -383,6 +414,7 @@ int backward_direct(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *
     const Epilogue e = into(at.dx, G * M * K, type);
     DirectArgs px = direct_args(z, source_of(at.w), N, cx, e);
     DirectArgs pw = direct_args(z, source_of(at.x), M, cw, weight_grad(d, at.dw, grad_type));
+    pw.e.streamed = 0;                                     // tiles of 64 columns: pieces of lines, which the caches join (11 x 16 x 28173 x 942 f32 1326 streamed, 1233 plain)
     px.t.partial = space.take<float>(cx.partial);
     if (!io) return GBMUF_OK;
     px.copy = at.dresidual.data; px.copy_ld = at.dresidual.ld; px.copy_batch = at.dresidual.batch_stride;
@@ -470,12 +502,12 @@ int backward_16(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io, 
     if (d.activation) { lz.pre = at.pre.data; lz.ldp = at.pre.ld; lz.p_batch = at.pre.batch_stride; lz.act = d.activation; }
     if (d.activation || dr || db) lz.batch = G;            // a matrix for each worker even where dy is shared
     const LayArgs lw = source(at.w, N, K, G, type), lx = source(at.x, M, K, G, type);
-    const auto as_it_lies = [&](const gbmuf_matrix_t &m, int64_t cols) { return io && lies_well(m) && cols % 8 == 0; };
     const auto take = [&](const gbmuf_matrix_t &m, const LayArgs &l, bool copy) {
         if (copy) return packed(space, l.R, l.C, G, l.batch, false, nullptr);
         return Operand{static_cast<const uint16_t *>(m.data), m.ld, m.batch_stride, nullptr, 0, false, false};
     };
-    const bool copy_z = (dx || dw) && (d.activation || !as_it_lies(at.dy, N)), copy_w = dx && !as_it_lies(at.w, K), copy_x = dw && !as_it_lies(at.x, K);
+    const bool copy_z = (dx || dw) && (d.activation || !io || !as_it_lies(at.dy, N)), copy_w = dx && (!io || !as_it_lies(at.w, K)),
+               copy_x = dw && (!io || !as_it_lies(at.x, K));
     const Operand z = take(at.dy, lz, copy_z);
     Operand w = take(at.w, lw, copy_w), x = take(at.x, lx, copy_x), zt = z;
     zt.across = w.across = x.across = true;
@@ -507,7 +539,7 @@ int backward_laid(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t *io
 int backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t &io, Space &space, hipStream_t stream)
 {
     const bool sums = !io.dbias.data || (io.dw.data && d.in_features > 0), copy = !io.dresidual.data || (io.dx.data && d.in_features > 0);
-    return takes_direct_backward(d) && sums && copy ? backward_direct(d, &io, space, stream) : backward_laid(d, &io, space, stream);
+    return takes_direct_backward(d, io) && sums && copy ? backward_direct(d, &io, space, stream) : backward_laid(d, &io, space, stream);
 }
 
 int64_t forward_bytes(const gbmuf_linear_desc_t &d)
@@ -520,7 +552,7 @@ int64_t forward_bytes(const gbmuf_linear_desc_t &d)
 int64_t backward_bytes(const gbmuf_linear_desc_t &d)
 {
     Space direct{nullptr}, laid{nullptr};
-    if (takes_direct_backward(d)) (void)backward_direct(d, nullptr, direct, nullptr);
+    (void)backward_direct(d, nullptr, direct, nullptr);
     (void)backward_laid(d, nullptr, laid, nullptr);
     return std::max(direct.used, laid.used);
 }

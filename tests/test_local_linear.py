@@ -582,8 +582,8 @@ def test_infinities_in_large_f32_products_reach_only_their_rows():
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("act,N", [(B.ACT_NONE, 4104), (B.ACT_GELU, 4099)])
 def test_results_above_what_the_caches_hold_are_those_of_their_rows(dtype, act, N):
-    """Every element's sum has one order, so a call gives the bits of calls on its rows, whose results are small (but of more than 4e9 operations, from
-    where on f32 is taken apart)."""
+    """Every element's sum has one order, so a call gives the bits of calls on its rows, whose results are small (but whose
+    products are large enough for f32 to be taken apart)."""
     G, M, K = 2, 8232, 160
     g = torch.Generator().manual_seed(15)
     x, w, b, r = (make(s, dtype, g).to(DEV) for s in ((G, M, K), (G, N, K), (G, N), (G, 1, N)))
