@@ -186,6 +186,15 @@ __device__ __forceinline__ float norm_of(const Norms &n, int32_t worker, int32_t
 
 __device__ __forceinline__ float clip_factor(float norm, float most) { return norm <= most || most == INFINITY ? 1.0f : most / norm; }
 
+// A product rounded to f32, whatever follows: without the barrier a product that f16 takes one by one becomes v_fma_mixlo_f16, which rounds the exact
+// product once, to other bits than those of the values taken side by side, and makes +0 of -0.
+__device__ __forceinline__ float times(float v, float f)
+{
+    float p = v * f;
+    asm("" : "+v"(p));
+    return p;
+}
+
 template <bool S, int T, int D>
 __device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor &d, float f)
 {
@@ -194,13 +203,13 @@ __device__ __forceinline__ void clip_tile(const GradTile &tile, const GradTensor
     each<V, 4>(tile, [&](int64_t i) { return read_some<S, T, V>(t.p, grad_at(t, i)); },
             [&](int64_t i, Some<V> v) {
 #pragma unroll
-                for (int c = 0; c < V; ++c) v.v[c] *= f;
+                for (int c = 0; c < V; ++c) v.v[c] = times(v.v[c], f);
                 if (d.ld == d.cols || i % d.cols + V <= d.cols) write_some<S, D, V>(d.p, grad_at(d, i), v);
                 else
 #pragma unroll
                     for (int c = 0; c < V; ++c) store_one(d.p, grad_at(d, i + c), D, v.v[c]);
             },
-            [&](int64_t i) { store_one(d.p, grad_at(d, i), D, load_one(t.p, grad_at(t, i), T) * f); });
+            [&](int64_t i) { store_one(d.p, grad_at(d, i), D, times(load_one(t.p, grad_at(t, i), T), f)); });
 }
 
 template <bool S, int T>

@@ -413,3 +413,59 @@ def test_calls_that_are_refused():
     arena = torch.zeros(2, 2, 32)
     assert code(lambda: step(a=B.make_state(arena[:, 0], None, None, 64), b=B.make_state(arena[:, 1], None, None, 64))) == B.GBMUF_EDEVICE
     assert code(lambda: step()) == B.GBMUF_EDEVICE and code(lambda: h.norm(n)) == B.GBMUF_EDEVICE and code(lambda: h.clip(1.0, n)) == B.GBMUF_EDEVICE
+
+
+# -- clipping into tensors of other shapes: as many values, counted row by row ------------------------------------------------
+def shaped(values, shape, dtype):
+    """A view of `shape` = (rows, columns, pitch, first column) with 5.0 in the gaps; (n,): a vector."""
+    if len(shape) == 1:
+        return values.to(dtype).clone()
+    rows, cols, pitch, first = shape
+    buf = torch.full((rows, pitch), 5.0, dtype=dtype, device=DEV)
+    v = buf[:, first: first + cols]
+    v.copy_(values.view(rows, cols))
+    return v
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("out_dtype", DTYPES)
+@pytest.mark.parametrize("times", [1, 1250])             # 55 thousand values, and 69 million, which no cache holds
+def test_clip_into_other_shapes(dtype, out_dtype, times):
+    pairs = [((11100,), (300, 37, 50, 7)), ((60, 185, 200, 3), (300, 37, 41, 1)), ((300, 37, 40, 0), (100, 111, 120, 9)), ((300, 37, 41, 2), (11100,)),
+             ((5550, 2, 3, 0), (3700, 3, 7, 1))]
+    grow = lambda s: (s[0] * times, *s[1:])
+    g = torch.Generator(device=DEV).manual_seed(21)
+    values = [torch.randn(11100 * times, generator=g, device=DEV).to(dtype) for _ in pairs]
+    src = [shaped(v, grow(a), dtype) for v, (a, _) in zip(values, pairs)]
+    dst = [shaped(torch.zeros_like(v), grow(b), out_dtype) for v, (_, b) in zip(values, pairs)]
+    n = torch.empty(2, device=DEV)
+    B.Grads([src[:2], src[2:]]).clip(3.0, n, out=B.Grads([dst[:2], dst[2:]]), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for w, part in enumerate((slice(0, 2), slice(2, 5))):
+        want = math.sqrt(sum(float(v.double().square().sum()) for v in values[part]))
+        assert abs(n[w].item() - want) <= 2.0 ** -23 * want
+        f = torch.tensor(factor(n[w].item(), 3.0), device=DEV)
+        for v, d, (_, b) in zip(values[part], dst[part], pairs[part]):
+            assert torch.equal(d.reshape(-1), (v.float() * f).to(out_dtype))
+            if len(b) > 1:
+                assert (d._base[:, :b[3]] == 5.0).all() and (d._base[:, b[3] + b[1]:] == 5.0).all()
+    for v, s, (a, _) in zip(values, src, pairs):
+        assert torch.equal(s.reshape(-1), v)
+        if len(a) > 1:
+            assert (s._base[:, :a[3]] == 5.0).all() and (s._base[:, a[3] + a[1]:] == 5.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_clipped_values_are_the_same_wherever_they_lie(dtype):
+    """In f16: an f32 product, then its rounding, for values taken side by side and one by one, zeros' signs among them."""
+    g = torch.Generator(device=DEV).manual_seed(22)
+    v = torch.randn(200001, generator=g, device=DEV).to(dtype)
+    v[::1000] = -0.0
+    n, out, column = torch.empty(2, device=DEV), torch.empty(200001, dtype=torch.float16, device=DEV), torch.empty(200001, 2, dtype=torch.float16, device=DEV)
+    B.Grads([[v], [v]]).clip(3.0, n, out=B.Grads([[out], [column[:, 0]]]), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    f = torch.tensor(factor(n[0].item(), 3.0))
+    want = (v.cpu().float() * f).to(torch.float16).view(torch.int16)
+    assert torch.equal(out.cpu().view(torch.int16), want) and torch.equal(column[:, 0].cpu().view(torch.int16), want)
