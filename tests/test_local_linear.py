@@ -770,3 +770,77 @@ def test_workspace_that_is_missing_or_too_small_is_refused():
         assert L.gbmuf_linear(d, ctypes.byref(io), 1 << 50, need, None) == B.GBMUF_EDEVICE
         assert L.gbmuf_linear_backward(d, ctypes.byref(grad), 1 << 50, back, None) == B.GBMUF_EDEVICE
     assert B.Linear(0, 8, 8, 1).workspace_bytes() < 1 << 20
+
+
+# -- few rows against many outputs: the wide forms, tiles for 33 to 64 rows, and 16-bit rows that lie on 16 bytes or do not ------
+WIDE = [(1, 8, 32801, 72), (1, 16, 32803, 66), (1, 17, 32771, 40), (1, 20, 32803, 136), (2, 32, 16400, 44), (1, 33, 32769, 24), (1, 64, 32801, 130),
+        (16, 40, 2100, 264), (16, 17, 2050, 65)]
+
+
+def whole_pieces(n):
+    return (n + 7) // 8 * 8
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("size", WIDE)
+def test_few_rows_against_many_outputs(size, aligned, dtype):
+    """Every act and residual in turn; what lies beside the outputs stays."""
+    G, M, N, K = size
+    i = WIDE.index(size) + (3 if aligned else 0)
+    if aligned:
+        place = {"x": columns_of(whole_pieces(K) + 8, 8), "w": columns_of(whole_pieces(K), 0)}
+    else:
+        place = {"x": columns_of(K + 3, 1), "w": in_rows(5, N * K + 7)}
+    place.update({"y": columns_of(N + 5, 3), "pre": columns_of(N + 4, 1), "residual": columns_of(N + 9, 2)})
+    y, z = forward_case(*size, dtype, ACTS[i % 6], i % 3, True, i % 2 == 0, seed=20 + i, place=place)
+    for t, first in ((y, 3), (z, 1)):
+        if t is not None:
+            buf = t._base
+            assert buf.shape[2] > N and (buf[:, :, :first] == 7.0).all() and (buf[:, :, first + N:] == 7.0).all()
+
+
+# -- f32 taken apart: what a wide range inside a row and infinities leave ------------------------------------------------
+def wide_rows(shape, g):
+    """Magnitudes from 1 down to 2^-35 along the last axis."""
+    n = shape[-1]
+    return torch.randn(shape, generator=g).sign() * (0.5 + 0.5 * torch.rand(shape, generator=g)) * 2.0 ** torch.linspace(0, -35, n)
+
+
+def small_part_only(shape, g):
+    """Zero where wide_rows is above 2^-28."""
+    t = torch.randn(shape, generator=g)
+    t[..., : shape[-1] * 4 // 5] = 0
+    return t
+
+
+@gpu
+@pytest.mark.parametrize("swap", [False, True])
+@pytest.mark.parametrize("size", [(1, 900, 1100, 2050), (1, 700, 750, 4500)])
+def test_f32_values_far_below_their_rows_largest(size, swap):
+    """Only values below 2^-28 of their row's largest meet anything but zeros: what is kept of them, 2^-39 of the largest, is all
+    that results have.  Forward, dx and dw, the wide rows on either side."""
+    G, M, N, K = size
+    g = torch.Generator().manual_seed(31)
+    f, h = (small_part_only, wide_rows) if swap else (wide_rows, small_part_only)
+    lin = B.Linear(M, N, K, G)
+    ws = torch.empty(max(lin.workspace_bytes(), lin.workspace_bytes(True)), dtype=torch.uint8, device=DEV)
+    x, w = f((G, M, K), g), h((G, N, K), g)
+    y = torch.empty(G, M, N, device=DEV)
+    lin.forward(lin.forward_io(x.to(DEV), w.to(DEV), y), ws)
+    results = [(y, x, w, "y")]
+    dz, w = f((G, M, N), g), h((G, K, N), g)
+    dx = torch.empty(G, M, K, device=DEV)
+    lin.backward(lin.backward_io(dz.to(DEV), w=w.transpose(1, 2).contiguous().to(DEV), dx=dx), ws)
+    results.append((dx, dz, w, "dx"))
+    dz, x = f((G, N, M), g), h((G, K, M), g)
+    dw = torch.empty(G, N, K, device=DEV)
+    lin.backward(lin.backward_io(dz.transpose(1, 2).contiguous().to(DEV), x=x.transpose(1, 2).contiguous().to(DEV), dw=dw), ws)
+    results.append((dw, dz, x, "dw"))
+    for got, a, b, what in results:
+        a, b = a.double(), b.double()
+        S = product64(a.abs(), b.abs())
+        bound = sum_bound(a.shape[2], S, torch.float32, spread(a, b))
+        check(got, product64(a, b), bound, bound, what)
+        assert (product64(a, b).abs() > 4 * bound).double().mean() > 0.3, what          # the bound is not the result itself
