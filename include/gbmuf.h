@@ -414,9 +414,10 @@ typedef struct gbmuf_linear_io {
  * gbmuf_linear -- the product, its bias, activation and residual: y, and z where asked for.
  *   Sums of products are held in f32, rounded once to dtype.  GBMUF_F32: each row of x and w is scaled by a power of
  *   two and its values are taken apart into two f16 numbers, of whose four products the matrix cores form three: a value keeps 22 bits or
- *   more, or 2^-40 of its row's largest where that is more, so results are as near as those of f32 products whose
- *   values lie within 2^16 of their row's largest.  An infinity or NaN in x or w makes NaN of the results that it reaches
- *   (in f32; in bf16 and f16 infinities stay what IEEE says).  Up to 64 rows, and small sizes: plain f32 products.
+ *   more, or 2^-39 of its row's largest finite one where that is more, so results are as near as those of f32 products whose
+ *   values lie within 2^16 of their row's largest.  Up to 64 rows, and small sizes: plain f32 products.
+ *   Infinities and NaN in x or w reach the results that IEEE says, as it says (in the products taken apart an infinity meets 0 where the other value
+ *   is below 2^-39 of its row's largest: NaN).
  *   workspace  device memory of gbmuf_linear_workspace bytes, 256-byte aligned, that nothing else uses until the call's work
  *              is done; NULL if that is 0.  Calls that share one must be in order.
  * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,

@@ -79,13 +79,15 @@ __global__ __launch_bounds__(256) void copy_kernel(LaySet set)
 // ---------------------------------------------------------------------------------------
 // f32 sources, taken apart.
 // ---------------------------------------------------------------------------------------
-// The two f16 numbers of a value that its row's exponent has scaled.
+// The two f16 numbers of a value that its row's exponent has scaled.  An infinity is +-1 and, trailing, itself: of the three products with another
+// value's two numbers that leaves the infinity that is due, also with another infinity, and NaN where the other's leading number is 0.
 __device__ __forceinline__ void take_apart(float v, uint16_t &lead, uint16_t &trail)
 {
     const _Float16 h = static_cast<_Float16>(v);
     const float f = static_cast<float>(h);
-    const _Float16 l = fabsf(f) <= 65504.0f ? static_cast<_Float16>(v - f) : static_cast<_Float16>(0.0f);
-    lead = __builtin_bit_cast(uint16_t, h);
+    const bool finite = fabsf(f) <= 65504.0f;
+    const _Float16 l = finite ? static_cast<_Float16>(v - f) : h;
+    lead = __builtin_bit_cast(uint16_t, finite ? h : static_cast<_Float16>(copysignf(1.0f, v)));
     trail = __builtin_bit_cast(uint16_t, l);
 }
 
@@ -102,11 +104,18 @@ __device__ __forceinline__ void write_apart(uint16_t *row, int k, int exponent, 
     *reinterpret_cast<v4u *>(to + 32) = __builtin_bit_cast(v4u, t);
 }
 
+// The bits of a finite value's magnitude, which compare as integers.  Infinities and NaN have no part in their row's exponent.
+__device__ __forceinline__ uint32_t magnitude(float v)
+{
+    const uint32_t m = __float_as_uint(v) & 0x7fffffffu;
+    return m < 0x7f800000u ? m : 0u;
+}
+
 __device__ __forceinline__ uint32_t magnitude(const Eight &v)
 {
     uint32_t m = 0;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) m = max(m, __float_as_uint(v.v[c >> 2][c & 3]) & 0x7fffffffu);
+    for (int c = 0; c < 8; ++c) m = max(m, magnitude(v.v[c >> 2][c & 3]));
     return m;
 }
 
@@ -159,8 +168,7 @@ __device__ __forceinline__ void read_tile(const LayArgs &a, int64_t g, int r0, i
     __syncthreads();
 }
 
-// Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  Magnitudes compare as integers, and a maximum does not depend on
-// the order of the atomics.
+// Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  A maximum does not depend on the order of the atomics.
 __global__ __launch_bounds__(256) void stats_kernel(LaySet set)
 {
     int id = static_cast<int>(blockIdx.x);
@@ -176,7 +184,7 @@ __global__ __launch_bounds__(256) void stats_kernel(LaySet set)
     if (a.row_max) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(tile[line][part + i]) & 0x7fffffffu);
+        for (int i = 0; i < 16; ++i) m = max(m, magnitude(tile[line][part + i]));
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 2)));
         if (part == 0 && r0 + line < a.R && m) atomicMax(a.row_max + g * a.R + r0 + line, m);
@@ -187,7 +195,7 @@ __global__ __launch_bounds__(256) void stats_kernel(LaySet set)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float v = tile[part + i][line];
-            m = max(m, __float_as_uint(v) & 0x7fffffffu);
+            m = max(m, magnitude(v));
             s += v;
         }
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 1)));

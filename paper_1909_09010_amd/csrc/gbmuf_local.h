@@ -32,7 +32,7 @@ struct Tiles {
 };
 
 // out[g][m][n] = sum over k of a[g][m][k] * b[g][n][k], in 16-bit numbers whose k are contiguous.  Split: a row holds, for every 32
-// k, their 32 leading parts and then their 32 trailing parts, and `k` counts both; a_max and b_max hold the bits of the largest magnitude of
+// k, their 32 leading parts and then their 32 trailing parts, and `k` counts both; a_max and b_max hold the bits of the largest finite magnitude of
 // every row before the row was scaled.
 struct ProductArgs {
     const uint16_t *a, *b;
@@ -83,7 +83,7 @@ struct LayArgs {
     int32_t R, C, batch;
     int32_t type, act;       // act: GBMUF_ACT_NONE = no factor
     // any of these nullptr
-    uint32_t *row_max, *col_max;          // [batch][R], [batch][C]: bits of the largest magnitude, zeroed before launch_stats
+    uint32_t *row_max, *col_max;          // [batch][R], [batch][C]: bits of the largest finite magnitude, zeroed before launch_stats
     float *col_sums;                      // [batch][row tiles][C]
     uint16_t *plain, *trans;              // rows of R (C) values along C (R), in 16 bits or taken apart; their whole length is written
     int64_t plain_ld, plain_batch, trans_ld, trans_batch;

@@ -287,11 +287,11 @@ __device__ __forceinline__ Eight slope8(Eight v, const Eight &z, int32_t act)
 }
 
 // The exponent of a scaled row of a split matrix: values are taken times 2^-row_exponent, the largest lies in [2^14, 2^15)
-// then.  bits: of the largest magnitude (infinity and NaN count as the largest finite exponent).
+// then.  bits: of the largest finite magnitude.
 __device__ __forceinline__ int row_exponent(uint32_t bits)
 {
     const int e = static_cast<int>(bits >> 23);
-    return (e > 254 ? 254 : e < 1 ? 1 : e) - 127 - 14;
+    return (e < 1 ? 1 : e) - 127 - 14;
 }
 
 }  // namespace

@@ -844,3 +844,46 @@ def test_f32_values_far_below_their_rows_largest(size, swap):
         bound = sum_bound(a.shape[2], S, torch.float32, spread(a, b))
         check(got, product64(a, b), bound, bound, what)
         assert (product64(a, b).abs() > 4 * bound).double().mean() > 0.3, what          # the bound is not the result itself
+
+
+@gpu
+@pytest.mark.parametrize("size", [(2, 800, 900, 3001), (1, 700, 750, 4500)])
+def test_infinities_in_large_f32_products_are_those_of_the_definition(size):
+    """Infinities against values, zeros, each other at the same place and at others, and NaN: the pattern that 64 bits give, and finite
+    results as they are without."""
+    G, M, N, K = size
+    inf, nan = float("inf"), float("nan")
+    g = torch.Generator().manual_seed(32)
+
+    def spoil(a, b):                                         # a product over the last axis of both
+        a[0, 5, 7], a[0, 6, 11], a[0, 9, 20], a[0, 30, 40], a[0, 31, 41], a[G - 1, 50, 60] = inf, -inf, inf, -inf, 1e6, nan
+        b[0, 3, 9], b[0, 4, 11], b[0, 10, 7], b[0, 11, 20], b[0, 12, 40] = inf, inf, 0.0, -inf, -inf
+        return a, b
+
+    def same(got, clean, a, b, what):
+        want = torch.matmul(a.double(), b.double().transpose(1, 2))
+        got = got.cpu()
+        finite = torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+        assert torch.equal(got == inf, want == inf) and torch.equal(got == -inf, want == -inf), what
+        assert 500 < (~finite).sum() < finite.sum(), what
+        rows = torch.ones(got.shape, dtype=torch.bool)
+        rows[0, 31], rows[0, :, 10] = False, False           # other finite values than before
+        assert torch.equal(got[finite & rows], clean.cpu()[finite & rows]), what
+    lin = B.Linear(M, N, K, G)
+    ws = torch.empty(max(lin.workspace_bytes(), lin.workspace_bytes(True)), dtype=torch.uint8, device=DEV)
+    turn = lambda t: t.transpose(1, 2).contiguous().to(DEV)
+    for what, rows, columns, over in (("y", M, N, K), ("dx", M, K, N), ("dw", N, K, M)):
+        a, b = torch.randn((G, rows, over), generator=g), torch.randn((G, columns, over), generator=g)
+        out = []
+        for p, q in ((a, b), spoil(a.clone(), b.clone())):
+            o = torch.empty(G, rows, columns, device=DEV)
+            if what == "y":
+                lin.forward(lin.forward_io(p.to(DEV), q.to(DEV), o), ws)
+            elif what == "dx":
+                lin.backward(lin.backward_io(p.to(DEV), w=turn(q), dx=o), ws)
+            else:
+                lin.backward(lin.backward_io(turn(p), x=turn(q), dw=o), ws)
+            torch.cuda.synchronize()
+            out.append((o, p, q))
+        same(out[1][0], out[0][0], out[1][1], out[1][2], what)
