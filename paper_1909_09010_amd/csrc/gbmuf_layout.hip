@@ -7,6 +7,10 @@ namespace {
 
 constexpr int kT = kLayTile;
 
+// More workgroups than a grid's first dimension holds lie in two; the last row's surplus has nothing to do.
+constexpr int64_t kGridRow = 1 << 22;
+__device__ __forceinline__ int block_number() { return static_cast<int>(blockIdx.y * gridDim.x + blockIdx.x); }
+
 // The source that workgroup `block` works on, and its number among that source's.
 __device__ __forceinline__ const LayArgs &source_of(const LaySet &set, int &block)
 {
@@ -44,7 +48,8 @@ __device__ __forceinline__ void row_write(void *p, int64_t at, int left, const E
 template <int T>
 __global__ __launch_bounds__(256) void copy_kernel(LaySet set)
 {
-    int id = static_cast<int>(blockIdx.x);
+    int id = block_number();
+    if (id >= set.first[set.n]) return;
     const LayArgs &a = source_of(set, id);
     __shared__ float sums[8][256];
     const int width = a.plain ? static_cast<int>(a.plain_ld) : a.C;        // zeros up to the end of the copy's rows
@@ -124,7 +129,8 @@ __device__ __forceinline__ uint32_t magnitude(const Eight &v)
 template <int N>
 __global__ __launch_bounds__(256) void rows_kernel(LaySet set)
 {
-    int id = static_cast<int>(blockIdx.x);
+    int id = block_number();
+    if (id >= set.first[set.n]) return;
     const LayArgs &a = source_of(set, id);
     const int64_t row = static_cast<int64_t>(id) * 4 + (threadIdx.x >> 6);
     if (row >= static_cast<int64_t>(a.R) * a.batch) return;
@@ -171,7 +177,8 @@ __device__ __forceinline__ void read_tile(const LayArgs &a, int64_t g, int r0, i
 // Largest magnitudes of rows and columns, and sums of columns over the tile's rows.  A maximum does not depend on the order of the atomics.
 __global__ __launch_bounds__(256) void stats_kernel(LaySet set)
 {
-    int id = static_cast<int>(blockIdx.x);
+    int id = block_number();
+    if (id >= set.first[set.n]) return;
     const LayArgs &a = source_of(set, id);
     __shared__ float tile[kT][kT + 1];
     const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
@@ -212,7 +219,8 @@ __global__ __launch_bounds__(256) void stats_kernel(LaySet set)
 // The copies along rows and along columns from one reading.
 __global__ __launch_bounds__(256) void lay_kernel(LaySet set)
 {
-    int id = static_cast<int>(blockIdx.x);
+    int id = block_number();
+    if (id >= set.first[set.n]) return;
     const LayArgs &a = source_of(set, id);
     __shared__ float tile[kT][kT + 1];
     const int tiles_c = (a.C + kT - 1) / kT, tiles_r = (a.R + kT - 1) / kT;
@@ -292,9 +300,15 @@ int launch_set(void (*fn)(LaySet), const LaySet &set, BlocksOf blocks_of, const 
         s.first[s.n] = static_cast<int32_t>(blocks);
         s.add(set.a[i]);
         blocks += n;
-        if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
     }
-    return launch_256(fn, s, blocks, what, stream);
+    if (blocks <= 0) return GBMUF_OK;
+    if (blocks > 0x7fffffffLL - kGridRow) return GBMUF_EUNSUPPORTED;
+    s.first[s.n] = static_cast<int32_t>(blocks);
+    void *argv[] = {&s};
+    const int64_t across = blocks < kGridRow ? blocks : kGridRow;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
+                                           dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
 }
 
 }  // namespace

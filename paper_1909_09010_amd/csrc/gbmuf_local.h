@@ -95,7 +95,7 @@ constexpr int kLayTile = 64, kLongestRow = 4096;
 // Up to three sources of one type, laid out by one launch: those of one product or of a layer's gradients.
 struct LaySet {
     LayArgs a[3];
-    int32_t first[4];            // first workgroup of each, set by the launch
+    int32_t first[4];            // first workgroup of each, and how many there are, set by the launch
     int32_t n = 0;
     int32_t reserved = 0;
     void add(const LayArgs &l) { a[n++] = l; }

@@ -887,3 +887,29 @@ def test_infinities_in_large_f32_products_are_those_of_the_definition(size):
             torch.cuda.synchronize()
             out.append((o, p, q))
         same(out[1][0], out[0][0], out[1][1], out[1][2], what)
+
+
+@gpu
+def test_more_rows_than_one_dimension_of_a_grid():
+    """36 M rows of f32 that are taken apart, 9 M workgroups, 56 GB: every value is written, and rows are those of calls on few of them."""
+    M, N, K, part = 36_000_000, 256, 64, 1_000_000
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("memory")
+    lin, small = B.Linear(M, N, K), B.Linear(part, N, K)
+    g = torch.Generator(device=DEV).manual_seed(33)
+    x, y, w = torch.empty(M, K, device=DEV), torch.empty(M, N, device=DEV), torch.randn(N, K, generator=g, device=DEV)
+    for i in range(0, M, part):
+        x[i: i + part].normal_(generator=g)
+        y[i: i + part].fill_(float("nan"))
+    ws = torch.empty(lin.workspace_bytes(), dtype=torch.uint8, device=DEV)
+    lin.forward(lin.forward_io(x, w, y), ws, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    few = torch.empty(part, N, device=DEV)
+    for i in range(0, M, part):
+        if i % (5 * part) == 0 or i in (33 * part, 34 * part, 16 * part, 17 * part):
+            small.forward(small.forward_io(x[i: i + part], w, few), ws, torch.cuda.current_stream())
+            assert torch.equal(y[i: i + part], few), i
+        assert torch.isfinite(y[i: i + part]).all(), i
+    X, W = x[None, -1000:].cpu().double(), w[None].cpu().double()
+    S = mm(X.abs(), W.abs())
+    check(y[None, -1000:], mm(X, W), sum_bound(K, S, torch.float32, spread(X, W)), 2.0 ** -21 * S, "y")
