@@ -500,7 +500,7 @@ typedef struct gbmuf_step_desc {
     int32_t skip_nonfinite;  /* 1: a worker whose norm is infinite or NaN is left as it is                 */
     int64_t P;               /* parameters per worker                                                     */
     float rate;              /* alpha_t                                                                   */
-    float eps;               /* Adagrad only                                                              */
+    float eps;               /* Adagrad only; > 0 if sums may be 0: a zero gradient on a zero sum is 0 / (0 + eps) */
     float max_norm;          /* gradients are clipped at this norm; INFINITY: not                         */
     float reserved0;
 } gbmuf_step_desc_t;

@@ -469,9 +469,9 @@ class Grads:
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_grad_clip")
 
-    def local_step(self, theta: State, sums: Optional[State], P: int, rate: float, eps: float = 0.0,
+    def local_step(self, theta: State, sums: Optional[State], P: int, rate: float, eps: float = 1e-7,
                    max_norm: float = float("inf"), norms=None, skip_nonfinite: bool = False, stream=None) -> None:
-        """Adagrad with ``sums`` (a state whose theta holds them), SGD with None."""
+        """Adagrad with ``sums`` (a state whose theta holds them), SGD with None.  ``eps`` 0 makes NaN of a parameter whose sum is 0."""
         d = StepDesc(ctypes.sizeof(StepDesc), int(skip_nonfinite), P, rate, eps, max_norm, 0.0)
         rc = _lib.gbmuf_local_step(self._h, ctypes.byref(d), ctypes.byref(theta), ctypes.byref(sums) if sums is not None else None,
                                    _dev(norms), _stream(stream))

@@ -469,3 +469,20 @@ def test_clipped_values_are_the_same_wherever_they_lie(dtype):
     f = torch.tensor(factor(n[0].item(), 3.0))
     want = (v.cpu().float() * f).to(torch.float16).view(torch.int16)
     assert torch.equal(out.cpu().view(torch.int16), want) and torch.equal(column[:, 0].cpu().view(torch.int16), want)
+
+
+@gpu
+def test_zero_gradients_on_fresh_sums_leave_theta_as_it_is():
+    """Embedding rows that a batch does not touch, before any step: the default eps makes 0 / eps of them.  An eps of 0 is the caller's word."""
+    g = torch.randn(3, 1000, generator=torch.Generator().manual_seed(23))
+    g[:, ::3] = 0
+    theta = np.ones((3, 1000), dtype=np.float32)
+    t, s, n = Placed(torch.tensor(theta), "rows"), Placed(torch.zeros(3, 1000), "rows"), torch.empty(3, device=DEV)
+    h = B.Grads([[v.to(DEV)] for v in g])
+    h.local_step(t.state, s.state, 1000, 0.1, max_norm=1.0, norms=n, stream=torch.cuda.current_stream())
+    got = t.get()
+    assert (got[:, ::3] == 1).all() and np.isfinite(got).all() and (got[:, 1::3] != 1).all()
+    t, s = Placed(torch.tensor(theta), "rows"), Placed(torch.zeros(3, 1000), "rows")
+    h.local_step(t.state, s.state, 1000, 0.1, 0.0, 1.0, n, stream=torch.cuda.current_stream())
+    got = t.get()
+    assert np.isnan(got[:, ::3]).all() and np.isfinite(got[:, 1::3]).all()
