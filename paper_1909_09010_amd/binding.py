@@ -77,11 +77,16 @@ class Matrix(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("batch_stride", ctypes.c_int64)]
 
 
-class LinearIo(ctypes.Structure):
+class _LinearIo(ctypes.Structure):
+    tensors = ()                    # kept alive as long as their addresses are here
+    on_host = False
+
+
+class LinearIo(_LinearIo):
     _fields_ = [(n, Matrix) for n in ("x", "w", "bias", "residual", "y", "pre")]
 
 
-class LinearGradIo(ctypes.Structure):
+class LinearGradIo(_LinearIo):
     _fields_ = [(n, Matrix) for n in ("x", "w", "pre", "dy", "dx", "dw", "dbias", "dresidual")]
 
 
@@ -158,7 +163,9 @@ def _load() -> ctypes.CDLL:
 
 
 _lib = _load()
-_linear, _linear_backward = _lib.gbmuf_linear, _lib.gbmuf_linear_backward        # calls that take microseconds: no look-up each time
+# calls that take microseconds: no look-up each time
+_linear, _linear_backward = _lib.gbmuf_linear, _lib.gbmuf_linear_backward
+_grad_norm, _grad_clip, _local_step = _lib.gbmuf_grad_norm, _lib.gbmuf_grad_clip, _lib.gbmuf_local_step
 
 
 def lib() -> ctypes.CDLL:
@@ -180,9 +187,7 @@ def _dev(x) -> Optional[int]:
 def _stream(s) -> Optional[int]:
     if s is None:
         return None
-    if hasattr(s, "cuda_stream"):
-        return int(s.cuda_stream) or None
-    return int(s) or None
+    return int(getattr(s, "cuda_stream", s)) or None
 
 
 def recommend_layout(P: int, K: int, kind: int = LAYOUT_BLOCKED, plan: "Optional[Plan]" = None) -> Layout:
@@ -344,6 +349,30 @@ class Plan:
             raise GbmufError(rc, "gbmuf_state_copy")
 
 
+def _on_host(tensors, what: str) -> bool:
+    """Whether tensors lie where no GPU reads them (pinned memory it does); all of them have to lie on one device."""
+    devices = {t.device for t in tensors if t is not None and t.numel() and not (t.device.type == "cpu" and t.is_pinned())}
+    if len(devices) > 1:
+        raise GbmufError(GBMUF_EINVAL, what + ": tensors of several devices")
+    return any(d.type != "cuda" for d in devices)
+
+
+def _refuse_host(what: str) -> None:
+    """Without a GPU the library itself says what is missing."""
+    if torch.cuda.is_available():
+        raise GbmufError(GBMUF_EINVAL, what + ": a tensor in the host's memory")
+
+
+def _norms(t, workers: int, what: str) -> Optional[int]:
+    if not isinstance(t, torch.Tensor):
+        return _dev(t)
+    if t.dtype is not torch.float32 or t.numel() < workers or not t.is_contiguous():
+        raise GbmufError(GBMUF_EINVAL, what + ": norms are `workers` floats")
+    if not t.is_cuda and not t.is_pinned():
+        _refuse_host(what)
+    return t.data_ptr()
+
+
 def _matrix(t, batch: int, rows: int, cols: int, dtype, what: str) -> Matrix:
     """A [batch, rows, cols] tensor (or [rows, cols] where batch is 1) whose last axis is contiguous, as gbmuf_matrix_t."""
     if t is None:
@@ -367,8 +396,8 @@ def _vector(t, batch: int, cols: int, dtype, what: str) -> Matrix:
 
 class Linear:
     """gbmuf_linear_desc_t: one product y = act(x w' + bias ...) for each of ``batch`` workers.  Tensors are [batch, rows, columns] (or
-    [rows, columns] where batch is 1), views with strides among them; ``forward_io`` / ``backward_io`` check them and
-    return what ``forward`` / ``backward`` take, as often as the tensors stay where they are."""
+    [rows, columns] where batch is 1), views with strides among them; ``forward_io`` / ``backward_io`` check them, keep them alive
+    and return what ``forward`` / ``backward`` take, as often as is wanted."""
 
     def __init__(self, rows: int, out_features: int, in_features: int, batch: int = 1, dtype=torch.float32,
                  activation: int = ACT_NONE, residual: int = RESIDUAL_NONE, weight_grad_f32: bool = False, accumulate: bool = False):
@@ -390,17 +419,25 @@ class Linear:
     def forward_io(self, x, w, y, bias=None, residual=None, pre=None) -> LinearIo:
         d, t = self.desc, self.dtype
         G, M, N, K = d.batch, d.rows, d.out_features, d.in_features
-        return LinearIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _vector(bias, G, N, t, "bias"),
-                        _matrix(residual, G, M, N, t, "residual"), _matrix(y, G, M, N, t, "y"), _matrix(pre, G, M, N, t, "pre"))
+        io = LinearIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _vector(bias, G, N, t, "bias"),
+                      _matrix(residual, G, M, N, t, "residual"), _matrix(y, G, M, N, t, "y"), _matrix(pre, G, M, N, t, "pre"))
+        io.tensors = (x, w, y, bias, residual, pre)
+        io.on_host = _on_host(io.tensors, "gbmuf_linear")
+        return io
 
     def backward_io(self, dy, x=None, w=None, pre=None, dx=None, dw=None, dbias=None, dresidual=None) -> LinearGradIo:
         d, t, gt = self.desc, self.dtype, self.grad_dtype
         G, M, N, K = d.batch, d.rows, d.out_features, d.in_features
-        return LinearGradIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _matrix(pre, G, M, N, t, "pre"),
-                            _matrix(dy, G, M, N, t, "dy"), _matrix(dx, G, M, K, t, "dx"), _matrix(dw, G, N, K, gt, "dw"),
-                            _vector(dbias, G, N, gt, "dbias"), _matrix(dresidual, G, M, N, t, "dresidual"))
+        io = LinearGradIo(_matrix(x, G, M, K, t, "x"), _matrix(w, G, N, K, t, "w"), _matrix(pre, G, M, N, t, "pre"),
+                          _matrix(dy, G, M, N, t, "dy"), _matrix(dx, G, M, K, t, "dx"), _matrix(dw, G, N, K, gt, "dw"),
+                          _vector(dbias, G, N, gt, "dbias"), _matrix(dresidual, G, M, N, t, "dresidual"))
+        io.tensors = (dy, x, w, pre, dx, dw, dbias, dresidual)
+        io.on_host = _on_host(io.tensors, "gbmuf_linear_backward")
+        return io
 
     def forward(self, io: LinearIo, workspace=None, stream=None) -> None:
+        if io.on_host or (workspace is not None and not workspace.is_cuda and not workspace.is_pinned()):
+            _refuse_host("gbmuf_linear")
         if workspace is None:
             rc = _linear(self._at, ctypes.byref(io), None, 0, _stream(stream))
         else:
@@ -409,6 +446,8 @@ class Linear:
             raise GbmufError(rc, "gbmuf_linear")
 
     def backward(self, io: LinearGradIo, workspace=None, stream=None) -> None:
+        if io.on_host or (workspace is not None and not workspace.is_cuda and not workspace.is_pinned()):
+            _refuse_host("gbmuf_linear_backward")
         if workspace is None:
             rc = _linear_backward(self._at, ctypes.byref(io), None, 0, _stream(stream))
         else:
@@ -437,6 +476,8 @@ class Grads:
                 else:
                     raise GbmufError(GBMUF_EINVAL, "gbmuf_grads_create")
                 rows.append(GradTensor(t.data_ptr(), *shape, -1 if offsets is None else int(offsets[w][i]), w, _TYPES[t.dtype]))
+        if _on_host([t for ts in tensors for t in ts], "gbmuf_grads_create"):
+            _refuse_host("gbmuf_grads_create")
         table = (GradTensor * max(len(rows), 1))(*rows)
         d = GradsDesc(ctypes.sizeof(GradsDesc), len(tensors), len(rows), ctypes.addressof(table))
         self._h = ctypes.c_void_p()
@@ -459,13 +500,13 @@ class Grads:
             pass
 
     def norm(self, norms, stream=None) -> None:
-        rc = _lib.gbmuf_grad_norm(self._h, _dev(norms), _stream(stream))
+        rc = _grad_norm(self._h, _norms(norms, self.workers, "gbmuf_grad_norm"), _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_grad_norm")
 
     def clip(self, max_norm: float, norms, out: "Optional[Grads]" = None, stream=None) -> None:
         """In place, or into the tensors of ``out``."""
-        rc = _lib.gbmuf_grad_clip(self._h, (out or self)._h, max_norm, _dev(norms), _stream(stream))
+        rc = _grad_clip(self._h, (out or self)._h, max_norm, _norms(norms, self.workers, "gbmuf_grad_clip"), _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_grad_clip")
 
@@ -473,7 +514,7 @@ class Grads:
                    max_norm: float = float("inf"), norms=None, skip_nonfinite: bool = False, stream=None) -> None:
         """Adagrad with ``sums`` (a state whose theta holds them), SGD with None.  ``eps`` 0 makes NaN of a parameter whose sum is 0."""
         d = StepDesc(ctypes.sizeof(StepDesc), int(skip_nonfinite), P, rate, eps, max_norm, 0.0)
-        rc = _lib.gbmuf_local_step(self._h, ctypes.byref(d), ctypes.byref(theta), ctypes.byref(sums) if sums is not None else None,
-                                   _dev(norms), _stream(stream))
+        rc = _local_step(self._h, ctypes.byref(d), ctypes.byref(theta), ctypes.byref(sums) if sums is not None else None,
+                         _norms(norms, self.workers, "gbmuf_local_step"), _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_local_step")

@@ -486,3 +486,23 @@ def test_zero_gradients_on_fresh_sums_leave_theta_as_it_is():
     h.local_step(t.state, s.state, 1000, 0.1, 0.0, 1.0, n, stream=torch.cuda.current_stream())
     got = t.get()
     assert np.isnan(got[:, ::3]).all() and np.isfinite(got[:, 1::3]).all()
+
+
+def test_tensors_of_the_host_and_norms_of_another_form_are_refused(monkeypatch):
+    if torch.cuda.is_available():
+        pytest.skip("host memory")
+    h, theta = B.Grads([[torch.zeros(8)], [torch.zeros(8)]]), torch.zeros(2, 8)
+    st = B.make_state(theta, None, None, 8)
+    calls = (lambda n: h.norm(n), lambda n: h.clip(1.0, n), lambda n: h.local_step(st, None, 8, 0.1, max_norm=1.0, norms=n))
+    for call in calls:
+        for n, want in ((torch.zeros(2), B.GBMUF_EDEVICE), (torch.zeros(3), B.GBMUF_EDEVICE), (torch.zeros(1), B.GBMUF_EINVAL),
+                        (torch.zeros(2, dtype=torch.float64), B.GBMUF_EINVAL), (torch.zeros(4)[::2], B.GBMUF_EINVAL)):
+            with pytest.raises(B.GbmufError) as e:
+                call(n)
+            assert e.value.code == want
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    for call in (*(lambda c=c: c(torch.zeros(2)) for c in calls), lambda: B.Grads([[torch.zeros(8)]]),
+                 lambda: B.Grads([[torch.zeros(8), torch.zeros(8, device="meta")]])):
+        with pytest.raises(B.GbmufError) as e:
+            call()
+        assert e.value.code == B.GBMUF_EINVAL

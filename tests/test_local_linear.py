@@ -10,7 +10,9 @@ Bounds, derived before any run (u = 2^-24, S = the sum of the magnitudes of what
 Errors of many roundings do not add up all one way: their root mean square is held to 2^-21 of S's (and the roundings above).
 """
 import ctypes
+import gc
 import math
+import weakref
 
 import numpy as np
 import pytest
@@ -913,3 +915,32 @@ def test_more_rows_than_one_dimension_of_a_grid():
     X, W = x[None, -1000:].cpu().double(), w[None].cpu().double()
     S = mm(X.abs(), W.abs())
     check(y[None, -1000:], mm(X, W), sum_bound(K, S, torch.float32, spread(X, W)), 2.0 ** -21 * S, "y")
+
+
+def test_tensors_of_the_host_and_of_several_devices_are_refused(monkeypatch):
+    """Before the call: a kernel that read them would fault.  (Without a GPU the library says that one is missing, as before.)"""
+    G, M, N, K = 2, 70, 80, 90
+    lin = B.Linear(M, N, K, G)
+    space = lambda n: (lambda t: t[-t.data_ptr() % 256:][:n])(torch.zeros(n + 256, dtype=torch.uint8))
+    x, w, y, dw = torch.zeros(G, M, K), torch.zeros(G, N, K), torch.zeros(G, M, N), torch.zeros(G, N, K)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    io, grad = lin.forward_io(x, w, y), lin.backward_io(y, x, dw=dw)
+    assert code_of(lambda: lin.forward(io, space(lin.workspace_bytes()))) == B.GBMUF_EINVAL
+    assert code_of(lambda: lin.backward(grad, space(lin.workspace_bytes(True)))) == B.GBMUF_EINVAL
+    bare = B.LinearIo(x=B.Matrix(1 << 40, K, M * K), w=B.Matrix(1 << 41, K, N * K), y=B.Matrix(1 << 42, N, M * N))      # as if on the GPU
+    assert code_of(lambda: lin.forward(bare, torch.zeros(1 << 20, dtype=torch.uint8))) == B.GBMUF_EINVAL
+    elsewhere = torch.zeros(G, M, K, device="meta")
+    assert code_of(lambda: lin.forward_io(elsewhere, w, y)) == B.GBMUF_EINVAL
+
+
+def test_a_calls_tensors_live_as_long_as_it_can_be_made():
+    lin = B.Linear(3, 4, 5)
+    x, w, y, dw = torch.zeros(3, 5), torch.zeros(4, 5), torch.zeros(3, 4), torch.zeros(4, 5)
+    seen = [weakref.ref(t) for t in (x, w, y, dw)]
+    io, grad = lin.forward_io(x, w, y), lin.backward_io(y, x, dw=dw)
+    del x, w, y, dw
+    gc.collect()
+    assert all(r() is not None for r in seen)
+    del io, grad
+    gc.collect()
+    assert all(r() is None for r in seen)
