@@ -476,7 +476,7 @@ typedef struct gbmuf_grads_s gbmuf_grads_t;   /* opaque */
  * that stay where they are.  It owns small device tables and the scratch of its sums: calls with one handle must
  * not be in flight at the same time on different streams.
  * gbmuf_grads_create  EINVAL (NULLs, struct_size, workers, an unknown dtype, a worker out of range, negative sizes, a row_stride
- *                     below cols, data not aligned to its type or NULL for a tensor that holds values, tensors of one
+ *                     below cols or rows that span more than 2^48 elements, data not aligned to its type or NULL for a tensor that holds values, tensors of one
  *                     worker whose places overlap), EUNSUPPORTED (workers > GBMUF_MAX_K; above 2^31 work items), ENOMEM, EDEVICE.
  * gbmuf_grads_destroy synchronises the device first; NULL is OK.
  */

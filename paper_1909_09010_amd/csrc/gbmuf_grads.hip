@@ -366,6 +366,7 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
             return GBMUF_EINVAL;
         if (t.rows > 1 && t.row_stride < t.cols) return GBMUF_EINVAL;
         if (t.rows > 0 && t.cols > (static_cast<int64_t>(1) << 48) / t.rows) return GBMUF_EUNSUPPORTED;
+        if (t.rows > 1 && static_cast<double>(t.rows) * static_cast<double>(t.row_stride) > 0x1p48) return GBMUF_EINVAL;     // no place overflows
         const int64_t count = t.rows * t.cols;
         if (count > 0 && (!t.data || reinterpret_cast<uintptr_t>(t.data) % type_bytes(t.dtype) != 0)) return GBMUF_EINVAL;
         int64_t &at = next[static_cast<size_t>(t.worker)];

@@ -506,3 +506,12 @@ def test_tensors_of_the_host_and_norms_of_another_form_are_refused(monkeypatch):
         with pytest.raises(B.GbmufError) as e:
             call()
         assert e.value.code == B.GBMUF_EINVAL
+
+
+def test_rows_that_span_more_than_any_memory_are_refused():
+    """Their places would overflow 64 bits."""
+    p = 4096
+    for rows, cols, stride in ((2, 8, 1 << 62), (3, 8, 1 << 61), (2, 8, (1 << 63) - 1), (1 << 20, 8, 1 << 29), (1 << 30, 0, 1 << 40)):
+        assert raw([(p, rows, cols, stride, -1, 0, 0)]) == B.GBMUF_EINVAL, (rows, cols, stride)
+    assert raw([(p, 1, 8, 1 << 62, -1, 0, 0)]) == B.GBMUF_OK              # one row has no stride
+    assert raw([(p, 1 << 20, 1, 1 << 28, -1, 0, 0)]) == B.GBMUF_OK
