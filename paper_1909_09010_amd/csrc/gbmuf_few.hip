@@ -106,15 +106,23 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(DirectArgs a)
     }
 }
 
-// form 0: few tiles, 16 waves; 1: 16 rows of w a workgroup; 2, 3: 32, 64 rows
+// form 0: few tiles, 16 waves; 1: 16 rows of w a workgroup; 2, 3: 32, 64 rows.  What no call takes is nullptr: f32 of more than 32 rows against many outputs
+// goes to tiles.
 template <int T>
 void (*pick(int mt, int form))(DirectArgs)
 {
-    static constexpr void (*fns[3][4])(DirectArgs) = {
-        {few_kernel<T, 1, 1, 16>, few_kernel<T, 1, 1, 4>, few_kernel<T, 1, 2, 4>, nullptr},
-        {few_kernel<T, 2, 1, 16>, few_kernel<T, 2, 1, 4>, T == kF32 ? few_kernel<T, 2, 2, 4> : nullptr, T == kF32 ? nullptr : few_kernel<T, 2, 4, 4>},
-        {few_kernel<T, 4, 1, 16>, few_kernel<T, 4, 1, 4>, nullptr, few_kernel<T, 4, 4, 4>}};
-    return fns[mt == 4 ? 2 : mt - 1][form];
+    using Fn = void (*)(DirectArgs);
+    static constexpr Fn one[] = {few_kernel<T, 1, 1, 16>, few_kernel<T, 1, 1, 4>, few_kernel<T, 1, 2, 4>, nullptr};
+    if (mt == 1) return one[form];
+    if constexpr (T == kF32) {
+        static constexpr Fn more[2][4] = {{few_kernel<T, 2, 1, 16>, few_kernel<T, 2, 1, 4>, few_kernel<T, 2, 2, 4>, nullptr},
+                                          {few_kernel<T, 4, 1, 16>, few_kernel<T, 4, 1, 4>, nullptr, nullptr}};
+        return more[mt == 4][form];
+    } else {
+        static constexpr Fn more[2][4] = {{few_kernel<T, 2, 1, 16>, few_kernel<T, 2, 1, 4>, nullptr, few_kernel<T, 2, 4, 4>},
+                                          {few_kernel<T, 4, 1, 16>, few_kernel<T, 4, 1, 4>, nullptr, few_kernel<T, 4, 4, 4>}};
+        return more[mt == 4][form];
+    }
 }
 
 }  // namespace
@@ -125,8 +133,8 @@ int launch_few(const DirectArgs &a, int32_t type, hipStream_t stream)
     const int mt = a.t.M <= 16 ? 1 : a.t.M <= 32 ? 2 : 4;
     const int64_t narrow = (a.t.N + 15) / 16;
     // A workgroup that takes more rows of w reads x less often.  us for 50,000 rows of 1024, 16 / 32 / 64 rows a workgroup: bf16, 8 rows of x 22 / 20 /
-    // 21, 20 rows 31 / 25 / 23, 64 rows 60 / 41 / 35; f32, 8 rows 48 / 47 / 46, 20 rows 72 / 57 / 64, 64 rows 131 / 112 / 108.  Few workgroups share
-    // long sums between 16 waves.
+    // 21, 20 rows 31 / 25 / 23, 64 rows 60 / 41 / 35; f32, 8 rows 48 / 47 / 46, 20 rows 72 / 57 / 64 (64 rows 131 / 112 / 108: tiles
+    // take 90).  Few workgroups share long sums between 16 waves.
     const bool many = narrow * a.t.batch >= 2048, widest = mt == 4 || (mt == 2 && type != kF32);
     const int form = many ? (widest ? 3 : 2) : narrow * a.t.batch < 256 && a.K >= 1024 ? 0 : 1;
     const int rows = form == 3 ? 64 : form == 2 ? 32 : 16;
