@@ -35,9 +35,14 @@ static_assert(sizeof(GradTile) == 64, "half a cache line");
 // time, by LDS that they declare and do not use, so that what is in flight is one short moving range.  us, the norm, clipping in place and Adagrad's step
 // with it in blocks, 16 x 19.8 M f32: plain accesses 209, 682, 1505; streamed 189, 620, 1401; and 6, 3, 3 workgroups a CU 183, 585, 1385 (4 for all 190, 592,
 // 1402; 3 for all 235, 626, 1425).  The norm reads 6.9 TB/s, clipping moves 6.5, the step alone 5.3.
-// Below, plain accesses: the step of 8 x 2 M f32 in rows 63 where streamed ones take 70, of 16 x 2 M 134 and 129, of 16 x 4 M 280 and 249.
+// Which of the two goes by the bytes that a call's arrays cover.  us plain / streamed: clipping into others 16 x 2 M f32 and 16 x 4 M bf16 (244 MB) 60 / 64 and 61 / 64,
+// 16 x 3 M and 16 x 6 M (366 MB) 94 / 91 and 95 / 91; in place 16 x 4 M f32 and 16 x 8 M bf16 (244 MB) 117 / 122 and 116 / 121, 16 x 6 M and 16 x 12 M (366 MB) 184 / 179 and
+// 183 / 179; Adagrad in rows 16 x 1.5 M f32 (275 MB) 94 / 100, 16 x 2 M bf16 (305 MB) 112 / 120, 16 x 2 M f32 (366 MB) 137 / 131, 16 x 3 M bf16 (458 MB) 182 / 168; SGD
+// 16 x 2 M f32 (244 MB) 83 / 88, 16 x 3 M (366 MB) 131 / 127, bf16 (366 MB) 134 / 140, 16 x 6 M bf16 (549 MB) 212 / 204.  The norm alone, which leaves
+// nothing to find: 8 x 2 M bf16 (31 MB) 7.5 / 7.9, 16 x 1.5 M bf16 (46 MB) 11.7 / 10.3, 8 x 2 M f32 (61 MB) 13.3 / 12.0.  (MB of 2^20.)
 constexpr int kThreads = 256, kTile = 4096, kJoinThreads = 1024;
-constexpr int64_t kCached = 24 << 20, kManyTiles = 1024, kLeastTile = 1024;       // values, workgroups, values
+constexpr int64_t kCached = 320 << 20, kReadOnce = 40 << 20;       // bytes: of the calls that write, of the norm alone
+constexpr int64_t kManyTiles = 1024, kLeastTile = 1024;            // workgroups, values
 constexpr int kSixPerCu = 24 * 128, kThreePerCu = 50 * 128;        // doubles of LDS
 
 __device__ __forceinline__ int64_t grad_at(const GradTensor &t, int64_t i)
@@ -326,7 +331,7 @@ struct gbmuf_grads_s {
     int32_t workers = 0;
     int device = -1;
     int64_t n_tiles = 0, reach = 0;              // reach: end of the last tensor among a worker's parameters
-    bool streamed = false;                       // more than the caches hold
+    int64_t values = 0, bytes = 0;               // of all tensors
     bool few = false;                            // every worker has tiles, one for a thread at most
     std::vector<GradTensor> tensors;             // by worker, in the order of the list
     GradTensor *d_tensors = nullptr;
@@ -385,10 +390,11 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
         if (before && before->worker == t.worker && before->offset + before->rows * before->cols > t.offset) return GBMUF_EINVAL;
         before = &t;
     }
-    int64_t size = 2 * kTile, values = 0;                  // one size for a handle: f32 anywhere in it takes the smaller
+    int64_t size = 2 * kTile;                              // one size for a handle: f32 anywhere in it takes the smaller
     for (const GradTensor &t : h.tensors) {
         if (t.type == kF32) size = kTile;
-        values += t.rows * t.cols;
+        h.values += t.rows * t.cols;
+        h.bytes += t.rows * t.cols * static_cast<int64_t>(type_bytes(t.type));
     }
     int64_t most = 0;                                      // of one worker
     const auto count_tiles = [&](int64_t of) {
@@ -415,7 +421,6 @@ int make_grads(gbmuf_grads_s &h, const gbmuf_grads_desc_t &d)
     }
     for (size_t w = 1; w < first.size(); ++w) first[w] = std::max(first[w], first[w - 1]);
     h.n_tiles = count;
-    h.streamed = values > kCached;
     h.few = true;
     for (size_t w = 0; w + 1 < first.size(); ++w) h.few = h.few && first[w + 1] > first[w] && first[w + 1] - first[w] <= kThreads;
     int devices = 0;
@@ -446,13 +451,13 @@ int launch(const void *fn, int64_t blocks, void **argv, const char *what, hipStr
 }
 
 // The tiles' sums, and the norms unless the kernel after this one joins them (joined not nullptr).
-int enqueue_norm(const gbmuf_grads_s *g, float *norms, Norms *joined, hipStream_t stream)
+int enqueue_norm(const gbmuf_grads_s *g, float *norms, Norms *joined, bool streamed, hipStream_t stream)
 {
     const GradTile *tiles = g->d_tiles;
     double *partial = g->d_partial;
     const int32_t *first = g->d_first;
     void *a1[] = {&tiles, &partial}, *a2[] = {&partial, &first, &norms};
-    const int rc = launch(reinterpret_cast<const void *>(g->streamed ? norm_kernel<true> : norm_kernel<false>), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
+    const int rc = launch(reinterpret_cast<const void *>(streamed ? norm_kernel<true> : norm_kernel<false>), g->n_tiles, a1, "hipLaunchKernel(norm)", stream);
     if (rc != GBMUF_OK) return rc;
     if (joined) *joined = Norms{norms, g->few ? partial : nullptr, first};
     if (joined && g->few) return GBMUF_OK;
@@ -543,7 +548,7 @@ int gbmuf_grad_norm(const gbmuf_grads_t *grads, float *norms, void *stream)
 {
     if (!grads || !norms) return GBMUF_EINVAL;
     const int rc = check_grads_device(grads);
-    return rc != GBMUF_OK ? rc : enqueue_norm(grads, norms, nullptr, static_cast<hipStream_t>(stream));
+    return rc != GBMUF_OK ? rc : enqueue_norm(grads, norms, nullptr, grads->bytes > kReadOnce, static_cast<hipStream_t>(stream));
 }
 
 int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float max_norm, float *norms, void *stream)
@@ -560,12 +565,13 @@ int gbmuf_grad_clip(const gbmuf_grads_t *src, const gbmuf_grads_t *dst, float ma
     if (rc != GBMUF_OK || (rc = check_grads_device(dst)) != GBMUF_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Norms n{};
-    if ((rc = enqueue_norm(src, norms, &n, s)) != GBMUF_OK) return rc;
+    const bool streamed = src->bytes + (src == dst ? 0 : dst->bytes) > kCached;
+    if ((rc = enqueue_norm(src, norms, &n, streamed, s)) != GBMUF_OK) return rc;
     const GradTile *tiles = src->d_tiles;
     const GradTensor *to = dst->d_tensors;
     int32_t in_place = src == dst ? 1 : 0;
     void *argv[] = {&tiles, &to, &n, &max_norm, &in_place};
-    return launch(reinterpret_cast<const void *>(src->streamed ? clip_kernel<true> : clip_kernel<false>), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
+    return launch(reinterpret_cast<const void *>(streamed ? clip_kernel<true> : clip_kernel<false>), src->n_tiles, argv, "hipLaunchKernel(clip)", s);
 }
 
 int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, const gbmuf_state_t *theta, const gbmuf_state_t *sums, float *norms,
@@ -588,12 +594,13 @@ int gbmuf_local_step(const gbmuf_grads_t *grads, const gbmuf_step_desc_t *desc, 
     }
     if ((rc = check_grads_device(grads)) != GBMUF_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (norms && (rc = enqueue_norm(grads, norms, clip ? &a.norms : nullptr, s)) != GBMUF_OK) return rc;
+    const bool streamed = grads->bytes + grads->values * (sums ? 8 : 4) > kCached;
+    if (norms && (rc = enqueue_norm(grads, norms, clip ? &a.norms : nullptr, streamed, s)) != GBMUF_OK) return rc;
     a.tiles = grads->d_tiles;
     a.theta = theta->theta;
     a.rate = desc->rate; a.eps = desc->eps; a.most = desc->max_norm; a.skip_nonfinite = desc->skip_nonfinite;
     void *argv[] = {&a};
-    return launch(reinterpret_cast<const void *>(grads->streamed ? step_kernel<true> : step_kernel<false>), grads->n_tiles, argv, "hipLaunchKernel(local step)", s);
+    return launch(reinterpret_cast<const void *>(streamed ? step_kernel<true> : step_kernel<false>), grads->n_tiles, argv, "hipLaunchKernel(local step)", s);
 }
 
 }  // extern "C"

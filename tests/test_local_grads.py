@@ -515,3 +515,40 @@ def test_rows_that_span_more_than_any_memory_are_refused():
         assert raw([(p, rows, cols, stride, -1, 0, 0)]) == B.GBMUF_EINVAL, (rows, cols, stride)
     assert raw([(p, 1, 8, 1 << 62, -1, 0, 0)]) == B.GBMUF_OK              # one row has no stride
     assert raw([(p, 1 << 20, 1, 1 << 28, -1, 0, 0)]) == B.GBMUF_OK
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_call_above_what_the_caches_hold_gives_the_bits_of_calls_for_each_worker(dtype):
+    """200 M values of 20 workers, rows with gaps and unaligned views: norms, clipping apart and in place, both steps, against 20 handles of
+    10 M values whose arrays the caches hold."""
+    K, P = 20, 10_000_040
+    gen = torch.Generator(device=DEV).manual_seed(24)
+    flat = torch.empty(K, P + 3, dtype=dtype, device=DEV)
+    for w in range(K):
+        flat[w] = torch.randn(P + 3, generator=gen, device=DEV) * (0.001 if w % 3 == 0 else 1.0)
+    wide = torch.zeros(K, 1000, 40, dtype=dtype, device=DEV)
+    wide[:, :, 1:34] = flat[:, 1: 33001].view(K, 1000, 33)
+    parts = lambda f, w, v: [w[v, :, 1:34], f[v, 33001: 8_000_000], f[v, 8_000_000: P + 1]]
+
+    def calls(groups):
+        """Every call for each group of workers in turn; what they leave, in the order of the workers."""
+        f, v = flat.clone(), wide.clone()
+        clipped = torch.full((K, P + 3), 5.0, dtype=dtype, device=DEV)
+        theta, sums, sgd = torch.ones(K, P, device=DEV), torch.full((K, P), 0.1, device=DEV), torch.ones(K, P, device=DEV)
+        n = torch.empty(4, K, device=DEV)
+        at = lambda t, g: B.make_state(t[g.start:], None, None, P)
+        for g in groups:
+            h = B.Grads([parts(f, v, w) for w in g])
+            out = B.Grads([[clipped[w, 1: 33001], clipped[w, 33001: 8_000_000], clipped[w, 8_000_000: P + 1]] for w in g])
+            s, k = torch.cuda.current_stream(), slice(g.start, g.stop)
+            h.norm(n[0, k], s)
+            h.clip(3.0, n[1, k], out=out, stream=s)
+            h.local_step(at(theta, g), at(sums, g), P, 0.1, 1e-7, 3.0, n[2, k], stream=s)
+            h.local_step(at(sgd, g), None, P, 0.1, max_norm=3.0, norms=n[3, k], stream=s)
+            h.clip(3.0, n[1, k], stream=s)
+            torch.cuda.synchronize()
+        return f, v, clipped, theta, sums, sgd, n
+    for a, b in zip(calls([range(K)]), calls([range(w, w + 1) for w in range(K)])):
+        assert torch.equal(a, b)
+        del a, b
