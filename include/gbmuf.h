@@ -419,7 +419,8 @@ typedef struct gbmuf_linear_io {
  *   Infinities and NaN in x or w reach the results that IEEE says, as it says (in the products taken apart an infinity meets 0 where the other value
  *   is below 2^-39 of its row's largest: NaN).
  *   workspace  device memory of gbmuf_linear_workspace bytes, 256-byte aligned, that nothing else uses until the call's work
- *              is done; NULL if that is 0.  Calls that share one must be in order.
+ *              is done; NULL if that is 0.  Calls that share one must be in order.  The bytes are those of matrices that lie as badly as
+ *              can be: 16-bit matrices whose rows lie on 16 bytes are read where they are and leave part of them unused.
  * Errors: EINVAL (NULLs, struct_size, unknown enum, negative sizes or strides, an output whose elements are not apart,
  * pointers that are not aligned to their type, outputs that overlap inputs or each other, a workspace that is too small or overlaps a matrix,
  * strides that span more than 2^48 elements),
@@ -445,8 +446,8 @@ typedef struct gbmuf_linear_grad_io {
  * gbmuf_linear_backward -- with dz = dy * act'(z):
  *     dx = dz w,   dw = dz' x,   dbias[n] = sum_i dz[i,n],   dresidual = dz
  * for each worker by itself (the gradient of an input that workers share is the sum of theirs).  relu'(0) = 0.  With bf16
- * and f16, dz is rounded to dtype before the products (the matrix cores take 16 bits, and dy has no more); dbias sums what
- * was not rounded.  Workspace and errors as above.
+ * and f16, large sizes round dz = dy * act'(z) to dtype once before dx's and dw's products (the matrix cores take 16 bits, and dy has no more); small
+ * ones, which multiply in f32, do not.  dbias sums what was not rounded.  Workspace and errors as above.
  */
 int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_grad_io_t *io, void *workspace,
                           int64_t workspace_bytes, void *stream);

@@ -44,6 +44,8 @@ __device__ __forceinline__ void row_write(void *p, int64_t at, int left, const E
 // ---------------------------------------------------------------------------------------
 // 16-bit sources: rows at aligned places with zeros behind them, dz on the way, and its column sums.  A workgroup takes kT rows of
 // 256 columns, a thread 8 columns of every eighth row.  Bound by HBM: one reading (two with an activation) and one writing.
+// dz is rounded to the type here, since that is what the 16-bit matrix instructions take: against 64 bits the gradients of 4 x 5120 x 8192 x 1024 bf16 with tanh are off by 0.0023 of their
+// size where products of the f32 dz, rounded at the end alike, are off by 0.0017.  A second product with what the rounding leaves would double the products' time.
 // ---------------------------------------------------------------------------------------
 template <int T>
 __global__ __launch_bounds__(256) void copy_kernel(LaySet set)
