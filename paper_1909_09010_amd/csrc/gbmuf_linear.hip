@@ -171,7 +171,10 @@ Cut cut(int tile, int64_t M, int64_t N, int64_t batch, int64_t steps, int64_t sl
 }
 
 // Tiles of 256 x 256, one a CU, or of 128 x 128, two a CU.  us for a step of a round: 8192 x 8192 x 8192 bf16 take 886 us in 4 rounds of 128
-// steps, and 1088 us in 8.
+// steps, and 1088 us in 8.  Tiles of 256 / of 128, us, * what is taken, workers x rows x out x in: forward bf16 1 x 2048 x 2048 x 2048 44 / 29*, 1 x 4096 x 4096 x 1024 39* / 46,
+// 8 x 700 x 2600 x 656 62 / 47*, 4 x 1024 x 4096 x 1024 38* / 45, 8 x 5120 x 8192 x 512 430* / 498; f32 16 x 512 x 1024 x 512 64 / 52*, 16 x 5120 x 512 x 2048 736* / 754,
+// 1 x 5120 x 10000 x 512 222* / 192; gradients bf16 1 x 4096 x 4096 x 1024 126 / 117*, 8 x 700 x 2600 x 656 115 / 97*, 4 x 5120 x 8192 x 1024 739* / 819; f32
+// 8 x 1000 x 2048 x 400 226 / 199*.
 Cut shape_of(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
 {
     const int64_t steps = packed_words(K, split_type) / kStepWords;

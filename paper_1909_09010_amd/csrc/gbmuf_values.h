@@ -217,8 +217,8 @@ __device__ __forceinline__ void store_eight(void *p, int64_t i, int32_t type, co
     else write8<kF16, STREAMED>(p, i, v);
 }
 
-// An epilogue's y or pre.  Streamed, where that is more than the caches hold, it leaves them to the operands: 8 x 5120 x 8192 x 512 bf16 (671 MB) 476 us
-// plain, 410 streamed, x 8197, whose rows end inside lines, 530 and 476.
+// An epilogue's y or pre.  Streamed, where that is more than the caches hold, it leaves them to the operands: 8 x 5120 x 8192 x 512 bf16 (671 MB) 469 us
+// plain, 411 streamed, x 8197, whose rows end inside lines, 517 and 469.
 __device__ __forceinline__ void store_result(const Epilogue &e, void *p, int64_t i, const Eight &v)
 {
     if (e.streamed) store_eight<true>(p, i, e.type, v);
