@@ -452,6 +452,82 @@ typedef struct gbmuf_linear_grad_io {
 int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_grad_io_t *io, void *workspace,
                           int64_t workspace_bytes, void *stream);
 
+/*
+ * Losses over a vocabulary, for each of `batch` workers g, from the rows x that go into its output matrix: with the logits
+ *     z[g,i,v] = sum_k x[g,i,k] w[g,v,k] + bias[g,v]          i < rows, v < vocab, k < in_features
+ * a row i is held to a word (cross entropy) or to what a teacher says of some words (distillation).  The logits are formed tile by
+ * tile and never kept; a call's workspace does not grow with rows * vocab beyond half a gigabyte of their gradient.
+ * Any of the sizes may be 0.  Zero the struct, set struct_size, fill in what is needed.
+ */
+#define GBMUF_MAX_TOP 1024
+
+typedef struct gbmuf_loss_desc {
+    uint32_t struct_size;    /* sizeof(gbmuf_loss_desc_t) of the caller's header                                  */
+    int32_t dtype;           /* GBMUF_F32, _BF16, _F16: x, w, bias, dx, dw, dbias                                 */
+    int32_t batch;           /* workers, 0 .. 65535                                                               */
+    int32_t top;             /* distillation: words of the teacher in a row, 1 .. GBMUF_MAX_TOP; else 0           */
+    int32_t weight_grad_f32; /* backward: 1 = dw and dbias are f32 whatever dtype is                              */
+    int32_t accumulate;      /* backward: 1 = dw and dbias are added to what is there                             */
+    float temperature;       /* distillation: tau, 2^-40 .. 2^40; else unused                                     */
+    int32_t reserved0;
+    int64_t rows;            /* tokens per worker                                                                 */
+    int64_t vocab;
+    int64_t in_features;
+} gbmuf_loss_desc_t;
+
+/* What a row is held to and what comes of it are matrices as well: of one column where nothing else is said, so that ld is the step from
+   row to row. */
+typedef struct gbmuf_loss_io {
+    gbmuf_matrix_t x;        /* in,  rows x in_features                                                           */
+    gbmuf_matrix_t w;        /* in,  vocab x in_features, as the models' tensors lie in theta                     */
+    gbmuf_matrix_t bias;     /* in,  vocab (ld unused), or NULL                                                   */
+    gbmuf_matrix_t target;   /* in,  int64: the row's word; distillation: rows x top, the teacher's words         */
+    gbmuf_matrix_t teacher;  /* in,  distillation, f32: rows x top, the teacher's logits of those words           */
+    gbmuf_matrix_t loss;     /* out, f32                                                                          */
+    gbmuf_matrix_t lse;      /* out, f32: log of the sum of exp(z / tau), which the backward takes; or NULL        */
+} gbmuf_loss_io_t;
+
+typedef struct gbmuf_loss_grad_io {
+    gbmuf_matrix_t x;        /* in,  as in the forward, and so are the next four                                   */
+    gbmuf_matrix_t w;
+    gbmuf_matrix_t bias;
+    gbmuf_matrix_t target;
+    gbmuf_matrix_t teacher;
+    gbmuf_matrix_t lse;      /* in,  f32, as the forward wrote it                                                  */
+    gbmuf_matrix_t dloss;    /* in,  f32: the gradient of each row's loss (of a mean: 1 / rows for all, ld 0)      */
+    gbmuf_matrix_t dx;       /* out, rows x in_features, or NULL                                                   */
+    gbmuf_matrix_t dw;       /* out, vocab x in_features, or NULL                                                  */
+    gbmuf_matrix_t dbias;    /* out, vocab (ld unused), or NULL                                                    */
+} gbmuf_loss_grad_io_t;
+
+/*
+ * gbmuf_cross_entropy -- with the row's word t (tau = 1):
+ *     lse = log sum_v exp z[v],   loss = lse - z[t]                (minus the log of the word's probability)
+ * gbmuf_distill -- with the row's words t_j and the teacher's logits s_j of them, q = softmax of s / tau over j:
+ *     lse = log sum_v exp(z[v] / tau),   loss = tau^2 sum_j q_j (log q_j - z[t_j] / tau + lse)
+ *   the divergence of the student's distribution over the whole vocabulary from the teacher's over its words, times tau^2 so that gradients
+ *   keep their size whatever tau is.  A word with a negative number or a logit of -infinity is not there; a word may be there more than once.
+ * Rows: one whose word is negative, or that has no words there, does not count: its loss, lse and gradients are 0, whatever its x, dloss and lse
+ * hold, NaN among it.  One that names a word of `vocab` or above gets NaN for its loss and lse, and its gradients are NaN.
+ * Logits of -infinity (a word that a bias forbids) have the probability 0; a row of nothing else, and NaN anywhere, follow IEEE arithmetic.
+ * Sums of products and everything that comes of them are held in f32; operands of type f32 are taken apart as in gbmuf_linear.
+ * Backward: dz[v] = dloss tau (exp(z[v] / tau - lse) - sum of the q_j with t_j = v)   (cross entropy: q = 1 for the word, tau = 1)
+ *     dx = dz w,   dw = dz' x,   dbias[v] = sum_i dz[i,v]
+ *   for each worker by itself.  With bf16 and f16 large sizes round dz to dtype once before the products of dx and dw (f16: times a power of two, the same
+ *   for all rows of a worker, that takes its largest below 2^15; values below 2^-39 of the largest |dloss tau| are lost), small ones do not; dbias sums what was
+ *   not rounded.  No gradient is formed of the teacher's logits.
+ * Equal calls give equal bits.
+ * Workspace and errors as for gbmuf_linear; EINVAL also for a top or temperature that the loss does not take (top 0 asks gbmuf_loss_workspace for
+ * cross entropy's bytes), EUNSUPPORTED for top above GBMUF_MAX_TOP, temperatures beyond 2^-40 .. 2^40 and batch * rows above 2^29.
+ */
+int gbmuf_loss_workspace(const gbmuf_loss_desc_t *desc, int32_t backward, int64_t *bytes);
+int gbmuf_cross_entropy(const gbmuf_loss_desc_t *desc, const gbmuf_loss_io_t *io, void *workspace, int64_t workspace_bytes, void *stream);
+int gbmuf_cross_entropy_backward(const gbmuf_loss_desc_t *desc, const gbmuf_loss_grad_io_t *io, void *workspace,
+                                 int64_t workspace_bytes, void *stream);
+int gbmuf_distill(const gbmuf_loss_desc_t *desc, const gbmuf_loss_io_t *io, void *workspace, int64_t workspace_bytes, void *stream);
+int gbmuf_distill_backward(const gbmuf_loss_desc_t *desc, const gbmuf_loss_grad_io_t *io, void *workspace, int64_t workspace_bytes,
+                           void *stream);
+
 /* One gradient tensor of one worker: rows x cols values, row r at data + r * row_stride (a vector: rows = 1). */
 typedef struct gbmuf_grad_tensor {
     void *data;              /* device                                                                   */

@@ -24,6 +24,7 @@ SWEEP_AUTO, SWEEP_FORWARD = 0, 1
 LAYOUT_ROWS, LAYOUT_BLOCKED = 0, 1
 MAX_K = 1024
 STATIC_TABLE_ENTRIES = 1 << 19
+MAX_TOP = 1024
 F32, BF16, F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, ACT_SIGMOID, ACT_TANH = range(6)
 RESIDUAL_NONE, RESIDUAL_BEFORE, RESIDUAL_AFTER = 0, 1, 2
@@ -90,6 +91,20 @@ class LinearGradIo(_LinearIo):
     _fields_ = [(n, Matrix) for n in ("x", "w", "pre", "dy", "dx", "dw", "dbias", "dresidual")]
 
 
+class LossDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("top", ctypes.c_int32),
+                ("weight_grad_f32", ctypes.c_int32), ("accumulate", ctypes.c_int32), ("temperature", ctypes.c_float),
+                ("reserved0", ctypes.c_int32), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("in_features", ctypes.c_int64)]
+
+
+class LossIo(_LinearIo):
+    _fields_ = [(n, Matrix) for n in ("x", "w", "bias", "target", "teacher", "loss", "lse")]
+
+
+class LossGradIo(_LinearIo):
+    _fields_ = [(n, Matrix) for n in ("x", "w", "bias", "target", "teacher", "lse", "dloss", "dx", "dw", "dbias")]
+
+
 class GradTensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
                 ("offset", ctypes.c_int64), ("worker", ctypes.c_int32), ("dtype", ctypes.c_int32)]
@@ -143,10 +158,15 @@ def _load() -> ctypes.CDLL:
         getattr(L, name).restype = ctypes.c_int
     L.gbmuf_probe_copy.argtypes = [vp, vp, i64, i32, vp]
     L.gbmuf_probe_copy.restype = ctypes.c_int
-    ld, gp = ctypes.POINTER(LinearDesc), ctypes.POINTER(vp)
+    ld, lo, gp = ctypes.POINTER(LinearDesc), ctypes.POINTER(LossDesc), ctypes.POINTER(vp)
     for name, args in (("gbmuf_linear_workspace", [ld, i32, ctypes.POINTER(i64)]),
                        ("gbmuf_linear", [ld, ctypes.POINTER(LinearIo), vp, i64, vp]),
                        ("gbmuf_linear_backward", [ld, ctypes.POINTER(LinearGradIo), vp, i64, vp]),
+                       ("gbmuf_loss_workspace", [lo, i32, ctypes.POINTER(i64)]),
+                       ("gbmuf_cross_entropy", [lo, ctypes.POINTER(LossIo), vp, i64, vp]),
+                       ("gbmuf_cross_entropy_backward", [lo, ctypes.POINTER(LossGradIo), vp, i64, vp]),
+                       ("gbmuf_distill", [lo, ctypes.POINTER(LossIo), vp, i64, vp]),
+                       ("gbmuf_distill_backward", [lo, ctypes.POINTER(LossGradIo), vp, i64, vp]),
                        ("gbmuf_grads_create", [gp, ctypes.POINTER(GradsDesc)]), ("gbmuf_grads_destroy", [vp]),
                        ("gbmuf_grad_norm", [vp, vp, vp]), ("gbmuf_grad_clip", [vp, vp, f32, vp, vp]),
                        ("gbmuf_local_step", [vp, ctypes.POINTER(StepDesc), sp, sp, vp, vp])):
@@ -454,6 +474,119 @@ class Linear:
             rc = _linear_backward(self._at, ctypes.byref(io), workspace.data_ptr(), workspace.nbytes, _stream(stream))
         if rc != GBMUF_OK:
             raise GbmufError(rc, "gbmuf_linear_backward")
+
+
+def _column(t, batch: int, rows: int, dtype, what: str) -> Matrix:
+    """A [batch, rows] tensor (or [rows] where batch is 1) with any strides, as a gbmuf_matrix_t of one column."""
+    if t is None:
+        return Matrix()
+    if t.dim() == 1 and batch == 1:
+        t = t.unsqueeze(0)
+    if tuple(t.shape) != (batch, rows) or t.dtype != dtype:
+        raise GbmufError(GBMUF_EINVAL, what)
+    return Matrix(t.data_ptr(), t.stride(1), t.stride(0))
+
+
+class _Loss:
+    """gbmuf_loss_desc_t: a loss over a vocabulary for each of ``batch`` workers, from the rows x that go into its output matrix w, whose
+    logits are never kept.  Tensors are [batch, rows, columns], [batch, rows] or, the bias, [batch, vocab] (without the first where batch is 1), views with
+    strides among them; ``forward_io`` / ``backward_io`` check them, keep them alive and return what ``forward`` / ``backward``
+    take, as often as is wanted."""
+
+    _top = 0
+
+    def __init__(self, rows: int, vocab: int, in_features: int, batch: int, dtype, weight_grad_f32: bool, accumulate: bool, temperature: float):
+        if dtype not in _TYPES:
+            raise GbmufError(GBMUF_EINVAL, "gbmuf_loss_desc_t")
+        self.dtype, self.grad_dtype = dtype, torch.float32 if weight_grad_f32 else dtype
+        self.desc = LossDesc(ctypes.sizeof(LossDesc), _TYPES[dtype], batch, self._top, int(weight_grad_f32), int(accumulate), temperature, 0,
+                             rows, vocab, in_features)
+        self._at = ctypes.byref(self.desc)
+        self.workspace_bytes()                               # the description's own checks
+
+    def workspace_bytes(self, backward: bool = False) -> int:
+        n = ctypes.c_int64()
+        rc = _lib.gbmuf_loss_workspace(self._at, int(backward), ctypes.byref(n))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, "gbmuf_loss_workspace")
+        return n.value
+
+    def _inputs(self, x, w, bias, target, teacher):
+        d, t = self.desc, self.dtype
+        G, M, V, K, T = d.batch, d.rows, d.vocab, d.in_features, self._top
+        return (_matrix(x, G, M, K, t, "x"), _matrix(w, G, V, K, t, "w"), _vector(bias, G, V, t, "bias"),
+                _matrix(target, G, M, T, torch.int64, "words") if T else _column(target, G, M, torch.int64, "target"),
+                _matrix(teacher, G, M, T, torch.float32, "teacher"))
+
+    def _forward_io(self, x, w, target, teacher, loss, lse, bias) -> LossIo:
+        G, M = self.desc.batch, self.desc.rows
+        io = LossIo(*self._inputs(x, w, bias, target, teacher), _column(loss, G, M, torch.float32, "loss"), _column(lse, G, M, torch.float32, "lse"))
+        io.tensors = (x, w, target, teacher, loss, lse, bias)
+        io.on_host = _on_host(io.tensors, self._names[0])
+        return io
+
+    def _backward_io(self, x, w, target, teacher, lse, dloss, bias, dx, dw, dbias) -> LossGradIo:
+        d, t, gt = self.desc, self.dtype, self.grad_dtype
+        G, M, V, K = d.batch, d.rows, d.vocab, d.in_features
+        io = LossGradIo(*self._inputs(x, w, bias, target, teacher), _column(lse, G, M, torch.float32, "lse"),
+                        _column(dloss, G, M, torch.float32, "dloss"), _matrix(dx, G, M, K, t, "dx"), _matrix(dw, G, V, K, gt, "dw"),
+                        _vector(dbias, G, V, gt, "dbias"))
+        io.tensors = (x, w, target, teacher, lse, dloss, bias, dx, dw, dbias)
+        io.on_host = _on_host(io.tensors, self._names[1])
+        return io
+
+    def _call(self, fn, name, io, workspace, stream) -> None:
+        if io.on_host or (workspace is not None and not workspace.is_cuda and not workspace.is_pinned()):
+            _refuse_host(name)
+        if workspace is None:
+            rc = fn(self._at, ctypes.byref(io), None, 0, _stream(stream))
+        else:
+            rc = fn(self._at, ctypes.byref(io), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+        if rc != GBMUF_OK:
+            raise GbmufError(rc, name)
+
+    def forward(self, io: LossIo, workspace=None, stream=None) -> None:
+        self._call(self._forward, self._names[0], io, workspace, stream)
+
+    def backward(self, io: LossGradIo, workspace=None, stream=None) -> None:
+        self._call(self._backward, self._names[1], io, workspace, stream)
+
+
+class CrossEntropy(_Loss):
+    """Each row is held to one word: target is int64, negative where a row does not count."""
+
+    _forward, _backward = _lib.gbmuf_cross_entropy, _lib.gbmuf_cross_entropy_backward
+    _names = ("gbmuf_cross_entropy", "gbmuf_cross_entropy_backward")
+
+    def __init__(self, rows: int, vocab: int, in_features: int, batch: int = 1, dtype=torch.float32, weight_grad_f32: bool = False,
+                 accumulate: bool = False):
+        super().__init__(rows, vocab, in_features, batch, dtype, weight_grad_f32, accumulate, 1.0)
+
+    def forward_io(self, x, w, target, loss, lse=None, bias=None) -> LossIo:
+        return self._forward_io(x, w, target, None, loss, lse, bias)
+
+    def backward_io(self, x, w, target, lse, dloss, bias=None, dx=None, dw=None, dbias=None) -> LossGradIo:
+        return self._backward_io(x, w, target, None, lse, dloss, bias, dx, dw, dbias)
+
+
+class Distill(_Loss):
+    """Each row is held to a teacher's logits (f32) of ``top`` words (int64, negative: not there), [batch, rows, top] both, at a temperature."""
+
+    _forward, _backward = _lib.gbmuf_distill, _lib.gbmuf_distill_backward
+    _names = ("gbmuf_distill", "gbmuf_distill_backward")
+
+    def __init__(self, rows: int, vocab: int, in_features: int, top: int, temperature: float = 1.0, batch: int = 1, dtype=torch.float32,
+                 weight_grad_f32: bool = False, accumulate: bool = False):
+        if top < 1:
+            raise GbmufError(GBMUF_EINVAL, "gbmuf_loss_desc_t")
+        self._top = top
+        super().__init__(rows, vocab, in_features, batch, dtype, weight_grad_f32, accumulate, temperature)
+
+    def forward_io(self, x, w, words, teacher, loss, lse=None, bias=None) -> LossIo:
+        return self._forward_io(x, w, words, teacher, loss, lse, bias)
+
+    def backward_io(self, x, w, words, teacher, lse, dloss, bias=None, dx=None, dw=None, dbias=None) -> LossGradIo:
+        return self._backward_io(x, w, words, teacher, lse, dloss, bias, dx, dw, dbias)
 
 
 class Grads:

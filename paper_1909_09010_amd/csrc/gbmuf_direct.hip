@@ -1,6 +1,8 @@
 // gbmuf_direct.hip -- products in f32 arithmetic straight from where the matrices lie, in tiles: no pass over the operands goes before
 // them, so they are what small and ordinary sizes take.
-#include "gbmuf_tile.h"
+#include "gbmuf_loss.h"
+
+#include <algorithm>
 
 namespace gbmuf {
 namespace {
@@ -25,12 +27,13 @@ __device__ __forceinline__ v4f read_left(const void *p, int64_t i, int left)
 // Threads work in groups of 256, each on steps of its own.
 __device__ __forceinline__ int thread_of() { return static_cast<int>(threadIdx.x) & (kThreads - 1); }
 
-template <int T, bool ALONG_K, bool SLOPE = false>
+template <int T, bool ALONG_K, bool SLOPE = false, bool LIVE = false>
 struct Stage {
     static constexpr int kChunks = kTile * kDepth / 4 / kThreads;
     static constexpr int kPitch = ALONG_K ? kDepth : kTile + 8;        // + 8: the two halves of a wave read k 4 apart, in other banks
     static constexpr int kFloats = ALONG_K ? kTile * kDepth : kDepth * kPitch;
     v4f v[kChunks], z[kChunks];
+    int32_t live[LIVE ? kChunks : 1];
 
     static __device__ __forceinline__ int major(int i)
     {
@@ -100,6 +103,23 @@ struct Stage {
         }
     }
 
+    __device__ __forceinline__ void load_live(const DirectArgs &a, int64_t g, int k0)
+    {
+        static_assert(!LIVE || !ALONG_K, "a chunk has one k");
+        if constexpr (LIVE)
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) live[i] = a.live[g * a.live_batch + min(k0 + major(i), a.K - 1)];
+    }
+
+    __device__ __forceinline__ void keep_live()
+    {
+        if constexpr (LIVE)
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[i][c] = live[i] ? v[i][c] : 0.0f;
+    }
+
     __device__ __forceinline__ void put(float *lds) const
     {
 #pragma unroll
@@ -118,30 +138,29 @@ struct Stage {
     }
 };
 
-template <int T, bool A_ALONG_K, bool B_ALONG_K, int GROUPS>
+template <bool A_ALONG_K, bool B_ALONG_K, int GROUPS>
 constexpr size_t direct_lds()
 {
-    constexpr size_t stages = GROUPS * (Stage<T, A_ALONG_K>::kFloats + Stage<T, B_ALONG_K>::kFloats) * sizeof(float);
+    constexpr size_t stages = GROUPS * (Stage<kF32, A_ALONG_K>::kFloats + Stage<kF32, B_ALONG_K>::kFloats) * sizeof(float);
     constexpr size_t out = leave_bytes<kTile, kTile, 2, 2>(), parts = (GROUPS - 1) * kTile * kTile * sizeof(float), sums = GROUPS * kThreads * sizeof(v4f);
     constexpr size_t most = stages > out ? stages : out, more = parts > sums ? parts : sums;
     return most > more ? most : more;
 }
 
-// One tile of 64 x 64 by 2 x 2 waves, or by GROUPS times as many that take every GROUPS-th step each and are added up in the end: a step
-// takes a microsecond or so however little it computes, and where there are few tiles nothing else hides that.
-template <int T, bool A_ALONG_K, bool B_ALONG_K, bool SLOPE, int GROUPS>
-__device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *lds)
+// The sums of one tile of 64 x 64 by 2 x 2 waves, or by GROUPS times as many that take every GROUPS-th step each and are added up in the end: a step
+// takes a microsecond or so however little it computes, and where there are few tiles nothing else hides that.  false: for a group whose sums another has.
+// T, TB: types of a and b; LIVE: values of b at k that do not count are zero.
+template <int T, int TB, bool A_ALONG_K, bool B_ALONG_K, bool SLOPE, bool LIVE, int GROUPS>
+__device__ __forceinline__ bool direct_sums(v16f (&acc)[1][1], const DirectArgs &a, const Share &share, float *lds)
 {
     using A = Stage<T, A_ALONG_K, SLOPE>;
-    using B = Stage<T, B_ALONG_K>;
-    const Share share = share_of<kTile, kTile>(a.t, id, (a.K + kDepth - 1) / kDepth);
+    using B = Stage<TB, B_ALONG_K, false, LIVE>;
     const int64_t g = share.at.g;
     const int tn = share.at.tn, m0 = share.at.tm * kTile, n0 = tn * kTile;
     const int group = GROUPS > 1 ? static_cast<int>(threadIdx.x) / kThreads : 0, first = share.first + group, last = share.last;
     const int turns = (share.last - share.first + GROUPS - 1) / GROUPS;            // of every group, though its last may be empty
     const int lane = threadIdx.x & 63, wave = thread_of() >> 6, wm = (wave & 1) * (kTile / 2), wn = (wave >> 1) * (kTile / 2);
     float *la = lds + group * (A::kFloats + B::kFloats), *lb = la + A::kFloats;
-    v16f acc[1][1];
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.0f;
     v4f sums = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -152,12 +171,14 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
     if (first < last) {
         x.load(a.a, g, m0, first * kDepth, a.t.M, a.K);
         w.load(a.b, g, n0, first * kDepth, a.t.N, a.K);
+        w.load_live(a, g, first * kDepth);
     }
     for (int turn = 0; turn < turns; ++turn) {
         const int s = first + turn * GROUPS;
         if (s < last) {
             x.shape(a.a);
             x.put(la);
+            w.keep_live();
             w.put(lb);
             if (A_ALONG_K && a.copy && tn == 0)
 #pragma unroll
@@ -178,6 +199,7 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
         if (s + GROUPS < last) {
             x.load(a.a, g, m0, (s + GROUPS) * kDepth, a.t.M, a.K);
             w.load(a.b, g, n0, (s + GROUPS) * kDepth, a.t.N, a.K);
+            w.load_live(a, g, (s + GROUPS) * kDepth);
         }
         if (s < last)
 #pragma unroll
@@ -220,27 +242,61 @@ __device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *
                 for (int c = 0; c < 4; ++c) acc[0][0][i % 4 * 4 + c] += v[c];
             }
         __syncthreads();
-        if (group > 0) return;
+        if (group > 0) return false;
     }
-    leave<kTile, kTile, 2, 2, false>(acc, lds, a, share);
+    return true;
+}
+
+template <int T, int TB, bool A_ALONG_K, bool B_ALONG_K, bool SLOPE, bool LIVE, int GROUPS>
+__device__ __forceinline__ void direct_tile(const DirectArgs &a, int id, float *lds)
+{
+    const Share share = share_of<kTile, kTile>(a.t, id, (a.K + kDepth - 1) / kDepth);
+    v16f acc[1][1];
+    if (direct_sums<T, TB, A_ALONG_K, B_ALONG_K, SLOPE, LIVE, GROUPS>(acc, a, share, lds)) leave<kTile, kTile, 2, 2, false>(acc, lds, a, share);
 }
 
 template <int T, int GROUPS>
 __global__ __launch_bounds__(GROUPS *kThreads) void direct_forward_kernel(DirectArgs a)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, true, true, GROUPS>() / 4];
-    direct_tile<T, true, true, false, GROUPS>(a, static_cast<int>(blockIdx.x), lds);
+    __shared__ __align__(16) float lds[direct_lds<true, true, GROUPS>() / 4];
+    direct_tile<T, T, true, true, false, false, GROUPS>(a, static_cast<int>(blockIdx.x), lds);
 }
 
 // dx = dz w (dz lies along the sum, w across it) and dw = dz' x (both across), in one launch: the first workgroups are dx's.
 template <int T, int GROUPS>
 __global__ __launch_bounds__(GROUPS *kThreads) void direct_backward_kernel(DirectArgs dx, DirectArgs dw)
 {
-    __shared__ __align__(16) float lds[direct_lds<T, false, false, GROUPS>() / 4];
-    static_assert(direct_lds<T, false, false, GROUPS>() >= direct_lds<T, true, false, GROUPS>(), "one piece of LDS for both");
+    __shared__ __align__(16) float lds[direct_lds<false, false, GROUPS>() / 4];
+    static_assert(direct_lds<false, false, GROUPS>() >= direct_lds<true, false, GROUPS>(), "one piece of LDS for both");
     const int n = dx.t.blocks(), id = static_cast<int>(blockIdx.x);
-    if (id < n) direct_tile<T, true, false, true, GROUPS>(dx, id, lds);
-    else direct_tile<T, false, false, true, GROUPS>(dw, id - n, lds);
+    if (id < n) direct_tile<T, T, true, false, true, false, GROUPS>(dx, id, lds);
+    else direct_tile<T, T, false, false, true, false, GROUPS>(dw, id - n, lds);
+}
+
+// Logits of losses, and what becomes of them.
+template <int T, bool BACKWARD, int GROUPS>
+__global__ __launch_bounds__(GROUPS *kThreads) void loss_direct_kernel(DirectArgs a, LossArgs l)
+{
+    constexpr size_t kBytes = std::max(direct_lds<true, true, GROUPS>(), loss_bytes<kTile, kTile, 2, 2>());
+    __shared__ __align__(16) float lds[kBytes / 4];
+    const Share share = share_of<kTile, kTile>(a.t, static_cast<int>(blockIdx.x), (a.K + kDepth - 1) / kDepth);
+    v16f acc[1][1];
+    if (direct_sums<T, T, true, true, false, false, GROUPS>(acc, a, share, lds))
+        leave_loss<kTile, kTile, 2, 2, false, BACKWARD>(acc, lds, a.t, l, Scales{}, share.at);
+    if constexpr (!BACKWARD) {
+        __syncthreads();
+        store_parts<kTile, kTile, 2, 2, GROUPS * kThreads>(lds, a.t, l, share.at);
+    }
+}
+
+// A loss's gradients: dz in f32, w and x as they are, and the rows of x that count.
+template <int T, int GROUPS>
+__global__ __launch_bounds__(GROUPS *kThreads) void loss_grads_kernel(DirectArgs dx, DirectArgs dw)
+{
+    __shared__ __align__(16) float lds[direct_lds<false, false, GROUPS>() / 4];
+    const int n = dx.t.blocks(), id = static_cast<int>(blockIdx.x);
+    if (id < n) direct_tile<kF32, T, true, false, false, false, GROUPS>(dx, id, lds);
+    else direct_tile<kF32, T, false, false, false, true, GROUPS>(dw, id - n, lds);
 }
 
 // Up to one workgroup a CU: four groups of threads each.
@@ -272,6 +328,38 @@ int launch_direct_backward(const DirectArgs &dx, const DirectArgs &dw, int32_t t
     const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][grouped(blocks) ? 1 : 0]), dim3(static_cast<unsigned>(blocks)),
                                            dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct gradients)", err, GBMUF_EDEVICE);
+}
+
+int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, bool backward, hipStream_t stream)
+{
+    const int32_t blocks = a.t.blocks();
+    if (blocks <= 0) return GBMUF_OK;
+    using Fn = void (*)(DirectArgs, LossArgs);
+    static constexpr Fn fns[3][2][2] = {
+        {{loss_direct_kernel<kF32, false, 1>, loss_direct_kernel<kF32, false, 4>}, {loss_direct_kernel<kF32, true, 1>, loss_direct_kernel<kF32, true, 4>}},
+        {{loss_direct_kernel<kBf16, false, 1>, loss_direct_kernel<kBf16, false, 4>}, {loss_direct_kernel<kBf16, true, 1>, loss_direct_kernel<kBf16, true, 4>}},
+        {{loss_direct_kernel<kF16, false, 1>, loss_direct_kernel<kF16, false, 4>}, {loss_direct_kernel<kF16, true, 1>, loss_direct_kernel<kF16, true, 4>}}};
+    DirectArgs args = a;
+    LossArgs loss = l;
+    void *argv[] = {&args, &loss};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][grouped(blocks) ? 1 : 0]), dim3(static_cast<unsigned>(blocks)),
+                                           dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct logits)", err, GBMUF_EDEVICE);
+}
+
+int launch_loss_grads(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream)
+{
+    const int32_t blocks = dx.t.blocks() + dw.t.blocks();
+    if (blocks <= 0) return GBMUF_OK;
+    using Fn = void (*)(DirectArgs, DirectArgs);
+    static constexpr Fn fns[3][2] = {{loss_grads_kernel<kF32, 1>, loss_grads_kernel<kF32, 4>},
+                                     {loss_grads_kernel<kBf16, 1>, loss_grads_kernel<kBf16, 4>},
+                                     {loss_grads_kernel<kF16, 1>, loss_grads_kernel<kF16, 4>}};
+    DirectArgs x = dx, w = dw;
+    void *argv[] = {&x, &w};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][grouped(blocks) ? 1 : 0]), dim3(static_cast<unsigned>(blocks)),
+                                           dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(a loss's gradients)", err, GBMUF_EDEVICE);
 }
 
 }  // namespace gbmuf

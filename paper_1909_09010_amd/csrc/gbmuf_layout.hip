@@ -267,6 +267,7 @@ __global__ __launch_bounds__(256) void column_sums_kernel(SumArgs a)
     if (wave != 0 || c >= a.C) return;
     const int i = threadIdx.x;
     s = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+    if (a.factor) s *= a.factor[g];
     if (a.accumulate) s += load_one(a.out, g * a.out_batch + c, a.type);
     store_one(a.out, g * a.out_batch + c, a.type, s);
 }

@@ -6,8 +6,8 @@
 
 namespace gbmuf {
 
-enum : int32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };          // = GBMUF_F32 ..
-constexpr size_t type_bytes(int32_t t) { return t == kF32 ? 4 : 2; }
+enum : int32_t { kF32 = 0, kBf16 = 1, kF16 = 2, kI64 = 3 };          // = GBMUF_F32 .., and the words of rows
+constexpr size_t type_bytes(int32_t t) { return t == kI64 ? 8 : t == kF32 ? 4 : 2; }
 
 // What is done with a sum s of products: z = s + bias (+ r), y = act(z) (+ r).
 struct Epilogue {
@@ -17,6 +17,7 @@ struct Epilogue {
     int32_t act, place;      // GBMUF_ACT_*, GBMUF_RESIDUAL_*
     int32_t type;            // of all of them
     int32_t streamed;        // y is more than the caches hold
+    const float *factor;     // [g] of the sums, or nullptr
 };
 
 // Which tiles of a result there are and how workgroups take them: the first `whole` tiles one each, and the sum over k of every other one
@@ -60,6 +61,8 @@ struct DirectArgs {
     int32_t reserved;
     Tiles t;                 // steps of 32 values
     Epilogue e;
+    const int32_t *live;     // [g][k]: b's values at k count as 0 where this is 0, whatever they are (gradients of losses); or nullptr
+    int64_t live_batch;
     void *copy;              // a itself (dz), of the matrices' type, or nullptr
     int64_t copy_ld, copy_batch;
     void *sums;              // sums[g][m] (+)= sum over k of a(m, k), or nullptr; no tile is split
@@ -106,6 +109,88 @@ struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
     void *out;
     int64_t out_batch;
     int32_t C, tiles, batch, type, accumulate;
+    const float *factor;     // [g] of the sums, or nullptr
+};
+
+// The words that rows are held to.  target: one of them each, negative where a row does not count.  Else lists of `top`: words in ascending order, kNoWord
+// behind the last, and the share of each.
+enum : int32_t { kDead = 0, kLive = 1, kBad = 2 };         // what a row counts; kBad: it names a word that the vocabulary does not have
+constexpr int32_t kNoWord = 0x7fffffff;
+struct Words {
+    const int64_t *target;
+    int64_t ld, batch;
+    const int32_t *id;       // [g][row][top], and share
+    const float *share;
+    const int32_t *state;    // [g][row]
+    int32_t top;             // 1 where target is
+    int32_t rows, vocab;     // of a worker, whole
+};
+
+// What is done with logits z = s + bias of the words `first` .. of the vocabulary.
+struct LossArgs {
+    const void *bias;        // of `type`, or nullptr
+    int64_t bias_batch;
+    Words words;
+    int32_t type;
+    int32_t first;
+    float inv_tau, tau;
+    // forward: parts[g][tile][row], tiles counted over the vocabulary from first_tile on, and z of the rows' words, at[g][row][top]
+    float2 *parts;
+    float *at;
+    int32_t part_tiles, first_tile;
+    // backward: dz[g][row][column], rows dz_ld apart, whole pieces of 8 up to there
+    const float *lse, *dloss;
+    int64_t lse_ld, lse_batch, dloss_ld, dloss_batch;
+    const float *sigma;      // [g]: a power of two that dz is multiplied with, or nullptr
+    void *dz;
+    int64_t dz_ld, dz_batch;
+    int32_t dz_type, reserved;
+    float *col_sums;         // [g][parts of 64 or 128 rows][column], or nullptr
+    int32_t *live;           // out: [g][row], or nullptr
+};
+
+// A teacher's words of every row, as it gives them, made lists of Words.
+struct TeacherArgs {
+    const int64_t *id;
+    const float *logit;
+    int64_t id_ld, id_batch, logit_ld, logit_batch;
+    int32_t *out_id, *out_state;
+    float *out_share;
+    int32_t rows, batch, top, vocab;
+    float inv_tau, reserved;
+};
+
+// Losses from their parts.
+struct LossJoin {
+    Words words;
+    const float2 *parts;
+    const float *at;
+    float *loss, *lse;       // lse nullptr: not wanted
+    int64_t loss_ld, loss_batch, lse_ld, lse_batch;
+    int32_t tiles, batch;
+    float inv_tau, tau;
+};
+
+// Rows of x that count, at aligned places with zeros behind them, zeros in place of the others; and for f16 the power of two that a worker's dz takes.
+struct KeepArgs {
+    Words words;
+    const void *x;
+    int64_t ld, batch_stride;
+    void *out;               // [batch][rows][out_ld]
+    int64_t out_ld;
+    int32_t columns, batch, type, reserved;
+    const float *dloss;
+    int64_t dloss_ld, dloss_batch;
+    float tau;
+    int32_t reserved1;
+    float *sigma;            // [batch], and behind them 1 / sigma; or nullptr
+};
+
+struct CastArgs {            // out = from, [batch][rows][columns]
+    const float *from;
+    void *out;
+    int64_t ld, batch_stride;
+    int32_t rows, columns, batch, type;
 };
 
 // values of a packed row of n numbers, in 16-bit words: whole steps of 64
@@ -122,6 +207,16 @@ int launch_rows(const LaySet &set, hipStream_t stream);
 int launch_stats(const LaySet &set, hipStream_t stream);
 int launch_lay(const LaySet &set, hipStream_t stream);
 int launch_column_sums(const SumArgs &a, hipStream_t stream);
+int launch_vocab(const ProductArgs &a, const LossArgs &l, int32_t type, int tile, bool backward, hipStream_t stream);
+int launch_loss_few(const DirectArgs &a, const LossArgs &l, int32_t type, hipStream_t stream);
+int few_columns(const DirectArgs &a, int32_t type);        // of a tile of launch_loss_few
+int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, bool backward, hipStream_t stream);
+int launch_loss_grads(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream);   // dz in f32
+int launch_teacher(const TeacherArgs &a, hipStream_t stream);
+int launch_loss_join(const LossJoin &a, hipStream_t stream);
+int launch_keep(const KeepArgs &a, hipStream_t stream);
+int launch_cast(const CastArgs &a, hipStream_t stream);
+constexpr int kMostTop = 1024;
 int launch_zero(uint32_t *p, int64_t words, hipStream_t stream);
 
 }  // namespace gbmuf

@@ -1,0 +1,257 @@
+// gbmuf_rows.hip -- what losses do row by row: a teacher's words put in order, losses from the parts of their logits, the rows of x that count.
+#include "gbmuf_loss.h"
+
+namespace gbmuf {
+namespace {
+
+// Sums and maxima of WIDTH neighbouring lanes.
+template <int WIDTH>
+__device__ __forceinline__ float sum_of(float v)
+{
+#pragma unroll
+    for (int d = 1; d < WIDTH; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+template <int WIDTH>
+__device__ __forceinline__ float max_of(float v)
+{
+#pragma unroll
+    for (int d = 1; d < WIDTH; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+// ---------------------------------------------------------------------------------------
+// A teacher's words.  One wave a row: the shares are a softmax over the words that are there (id not negative, logit not -infinity), and the words are
+// sorted by a bitonic network in LDS, the place in the teacher's list behind the word, so that equal words keep their order and every
+// key is another.
+// ---------------------------------------------------------------------------------------
+template <int MOST>
+__global__ __launch_bounds__(256) void teacher_kernel(TeacherArgs a, int32_t padded)
+{
+    __shared__ uint64_t keys[4][MOST];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t all = static_cast<int64_t>(a.rows) * a.batch, at = static_cast<int64_t>(blockIdx.x) * 4 + wave, row = at < all ? at : all - 1;
+    const int64_t g = row / a.rows, i = row - g * a.rows;
+    const int64_t *id = a.id + g * a.id_batch + i * a.id_ld;
+    const float *logit = a.logit + g * a.logit_batch + i * a.logit_ld;
+    uint64_t *key = keys[wave];
+    const float inf = __builtin_inff();
+    float most = -inf;
+    int state = kDead;
+    for (int j = lane; j < padded; j += 64) {
+        int32_t word = kNoWord;
+        if (j < a.top) {
+            const int64_t v = id[j];
+            const float l = logit[j];
+            if (v >= 0 && l != -inf) {
+                word = v < a.vocab ? static_cast<int32_t>(v) : a.vocab;          // behind every word that there is
+                most = fmaxf(most, l);
+                state = max(state, v < a.vocab ? kLive : kBad);
+            }
+        }
+        key[j] = (static_cast<uint64_t>(static_cast<uint32_t>(word)) << 32) | static_cast<uint32_t>(j);
+    }
+    most = max_of<64>(most);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) state = max(state, __shfl_xor(state, d));
+    const float from = most == -inf ? 0.0f : most;
+    float total = 0.0f;
+    for (int j = lane; j < a.top; j += 64)
+        if (static_cast<int32_t>(key[j] >> 32) != kNoWord) total += expf((logit[j] - from) * a.inv_tau);
+    total = sum_of<64>(total);
+    __syncthreads();
+    for (int size = 2; size <= padded; size *= 2)
+        for (int d = size / 2; d; d /= 2) {
+            for (int p = lane; p < padded / 2; p += 64) {
+                const int lo = (p / d) * 2 * d + p % d, hi = lo + d;
+                const uint64_t x = key[lo], y = key[hi];
+                if ((x > y) == ((lo & size) == 0)) {
+                    key[lo] = y;
+                    key[hi] = x;
+                }
+            }
+            __syncthreads();
+        }
+    if (at >= all) return;
+    for (int p = lane; p < a.top; p += 64) {
+        const uint64_t k = key[p];
+        const int32_t word = static_cast<int32_t>(k >> 32);
+        a.out_id[row * a.top + p] = word;
+        a.out_share[row * a.top + p] = word == kNoWord ? 0.0f : expf((logit[static_cast<uint32_t>(k)] - from) * a.inv_tau) / total;
+    }
+    if (lane == 0) a.out_state[row] = state;
+}
+
+// ---------------------------------------------------------------------------------------
+// Losses.  A workgroup takes ROWS rows: 256 / ROWS threads share the parts of a row, side by side in memory with its neighbours', and then its words.
+// ---------------------------------------------------------------------------------------
+template <int ROWS>
+__global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
+{
+    constexpr int kThreads = 256 / ROWS;
+    __shared__ float2 shared[kThreads][ROWS];
+    __shared__ float sums[ROWS];
+    const Words &w = a.words;
+    const int blocks = (w.rows + ROWS - 1) / ROWS, m0 = static_cast<int>(blockIdx.x % blocks) * ROWS;
+    const int64_t g = blockIdx.x / blocks;
+    const float inf = __builtin_inff(), scale = a.inv_tau * kLog2E;
+    {
+        const int r = threadIdx.x % ROWS, first = threadIdx.x / ROWS, m = min(m0 + r, w.rows - 1);
+        const float2 *from = a.parts + g * a.tiles * w.rows + m;
+        float2 s = {-inf, 0.0f};
+#pragma unroll 4
+        for (int t = first; t < a.tiles; t += kThreads) s = join_stats(s, from[static_cast<int64_t>(t) * w.rows], scale);
+        shared[first][r] = s;
+        __syncthreads();
+        for (int n = kThreads / 2; n; n /= 2) {
+            if (first < n) shared[first][r] = join_stats(shared[first][r], shared[first + n][r], scale);
+            __syncthreads();
+        }
+        if (first == 0) {
+            const float2 s = shared[0][r];
+            sums[r] = (fabsf(s.x) < inf ? s.x * a.inv_tau : 0.0f) + logf(s.y);
+        }
+        __syncthreads();
+    }
+    const int r = threadIdx.x / kThreads, first = threadIdx.x % kThreads, m = m0 + r;
+    const bool inside = m < w.rows;
+    const int state = inside ? row_state(w, g, m) : kDead;
+    const float lse = sums[r];
+    const int64_t row = g * w.rows + m;
+    float loss = 0.0f;
+    if (w.target) loss = state == kLive ? lse - a.at[row] : 0.0f;
+    else {
+        if (state == kLive)
+            for (int j = first; j < w.top; j += kThreads) {
+                const int64_t at = row * w.top + j;
+                const float share = w.share[at];
+                // nothing is lost by a word that the teacher gives no share
+                if (w.id[at] != kNoWord && share != 0.0f) loss += share * (logf(share) - fmaf(a.at[at], a.inv_tau, -lse));
+            }
+        loss = sum_of<(kThreads < 64 ? kThreads : 64)>(loss);
+        if constexpr (kThreads > 64) {
+            __shared__ float waves[4];
+            if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = loss;
+            __syncthreads();
+            loss = 0.0f;
+            for (int v = 0; v < kThreads / 64; ++v) loss += waves[r * (kThreads / 64) + v];
+        }
+        loss *= a.tau * a.tau;
+    }
+    if (!inside || first != 0) return;
+    const float bad = __builtin_nanf("");
+    a.loss[g * a.loss_batch + m * a.loss_ld] = state == kBad ? bad : loss;
+    if (a.lse) a.lse[g * a.lse_batch + m * a.lse_ld] = state == kBad ? bad : state == kDead ? 0.0f : lse;
+}
+
+// ---------------------------------------------------------------------------------------
+// Rows of x: zeros where a row does not count, whatever it holds, since 0 times that is not always 0.  8 columns a thread.  The last `batch` workgroups, where
+// sigma is wanted, find the power of two that takes the largest finite weight of a worker's rows below 2^15: with it dz, whose values are
+// at most that, fills f16's range from above, and what a row has below 2^-39 of the largest weight is nothing.
+// ---------------------------------------------------------------------------------------
+template <int T>
+__global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
+{
+    const int64_t block = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    if (block < copies) {
+        const int64_t id = block * 256 + threadIdx.x, per_row = a.out_ld / 8, row = id / per_row;
+        if (row >= static_cast<int64_t>(a.words.rows) * a.batch) return;
+        const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
+        const int64_t g = row / a.words.rows, from = g * a.batch_stride + (row - g * a.words.rows) * a.ld + c;
+        Eight v{};
+        if (row_state(a.words, g, static_cast<int>(row - g * a.words.rows)) != kDead) {
+            if (left >= 8) v = read8<T>(a.x, from);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < left) v.v[k >> 2][k & 3] = load_one(a.x, from + k, T);
+        }
+        write8<T>(a.out, row * a.out_ld + c, v);
+        return;
+    }
+    const int64_t g = block - copies;
+    if (g >= a.batch || !a.sigma) return;
+    __shared__ float waves[4];
+    float most = 0.0f;
+    for (int m = threadIdx.x; m < a.words.rows; m += 256) {
+        const float d = fabsf(a.dloss[g * a.dloss_batch + m * a.dloss_ld] * a.tau);
+        if (d < __builtin_inff() && row_state(a.words, g, m) == kLive) most = fmaxf(most, d);
+    }
+    most = max_of<64>(most);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    const int e = most > 0.0f ? 14 - ilogbf(most) : 0;
+    const int s = e > 126 ? 126 : e < -112 ? -112 : e;
+    a.sigma[g] = ldexpf(1.0f, s);
+    a.sigma[a.batch + g] = ldexpf(1.0f, -s);
+}
+
+__global__ __launch_bounds__(256) void cast_kernel(CastArgs a)
+{
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per_row = (a.columns + 7) / 8, row = id / per_row;
+    if (row >= static_cast<int64_t>(a.rows) * a.batch) return;
+    const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
+    const int64_t g = row / a.rows, to = g * a.batch_stride + (row - g * a.rows) * a.ld + c, from = row * a.columns + c;
+    if (left >= 8) return store_eight(a.out, to, a.type, read8<kF32>(a.from, from));
+    for (int k = 0; k < left; ++k) store_one(a.out, to + k, a.type, a.from[from + k]);
+}
+
+}  // namespace
+
+int launch_teacher(const TeacherArgs &a, hipStream_t stream)
+{
+    const int64_t blocks = (static_cast<int64_t>(a.rows) * a.batch + 3) / 4;
+    if (blocks <= 0) return GBMUF_OK;
+    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    TeacherArgs args = a;
+    int32_t padded = 1;
+    while (padded < a.top) padded *= 2;
+    void *argv[] = {&args, &padded};
+    const auto fn = padded <= 128 ? teacher_kernel<128> : teacher_kernel<kMostTop>;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(teacher)", err, GBMUF_EDEVICE);
+}
+
+// Few rows: more threads for the parts of each.
+int launch_loss_join(const LossJoin &a, hipStream_t stream)
+{
+    if (a.words.rows <= 0 || a.batch <= 0) return GBMUF_OK;
+    const int rows = a.words.rows <= 2 ? 1 : static_cast<int64_t>(a.words.rows) * a.batch <= 4096 ? 4 : 32;
+    const int64_t blocks = static_cast<int64_t>((a.words.rows + rows - 1) / rows) * a.batch;
+    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    LossJoin args = a;
+    void *argv[] = {&args};
+    const auto fn = rows == 1 ? loss_join_kernel<1> : rows == 4 ? loss_join_kernel<4> : loss_join_kernel<32>;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(losses)", err, GBMUF_EDEVICE);
+}
+
+int launch_keep(const KeepArgs &a, hipStream_t stream)
+{
+    int64_t copies = (static_cast<int64_t>(a.words.rows) * a.batch * (a.out_ld / 8) + 255) / 256;
+    const int64_t blocks = copies + (a.sigma ? a.batch : 0);
+    if (blocks <= 0) return GBMUF_OK;
+    KeepArgs args = a;
+    void *argv[] = {&args, &copies};
+    const int64_t across = blocks < (1 << 22) ? blocks : 1 << 22;
+    const auto fn = a.type == kF32 ? keep_kernel<kF32> : a.type == kBf16 ? keep_kernel<kBf16> : keep_kernel<kF16>;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
+                                           dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(rows of x)", err, GBMUF_EDEVICE);
+}
+
+int launch_cast(const CastArgs &a, hipStream_t stream)
+{
+    const int64_t blocks = (static_cast<int64_t>(a.rows) * a.batch * ((a.columns + 7) / 8) + 255) / 256;
+    if (blocks <= 0) return GBMUF_OK;
+    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    CastArgs args = a;
+    void *argv[] = {&args};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(cast_kernel), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(cast)", err, GBMUF_EDEVICE);
+}
+
+}  // namespace gbmuf

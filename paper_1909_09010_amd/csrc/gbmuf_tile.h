@@ -84,7 +84,12 @@ __device__ __forceinline__ void leave(const v16f (&acc)[TM / WM / 32][TN / WN / 
         const float *from = out + (first + k * kTogether) * kPitch + column;
         return Eight{{*reinterpret_cast<const v4f *>(from), *reinterpret_cast<const v4f *>(from + 4)}};
     };
+    const float factor = !SPLIT && e.factor && !parts ? e.factor[g] : 1.0f;
     const auto scaled = [&](Eight z, uint32_t row_bits) {
+        if constexpr (!SPLIT) {
+            z.v[0] *= factor;
+            z.v[1] *= factor;
+        }
         if constexpr (SPLIT) {
             const int em = row_exponent(row_bits);
 #pragma unroll

@@ -160,6 +160,7 @@ __device__ __forceinline__ void finish(const Epilogue &e, int64_t g, int64_t m, 
         if (left > 1) store_one(p, i + 1, e.type, v[1]);
         if (left > 2) store_one(p, i + 2, e.type, v[2]);
     };
+    if (e.factor) z *= e.factor[g];
     if (e.bias) z += load(e.bias, g * e.bias_batch + n);
     v4f r = {0.0f, 0.0f, 0.0f, 0.0f};
     if (e.place) r = load(e.res, g * e.r_batch + m * e.ldr + n);
@@ -257,6 +258,11 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t g, int64_t m,
         z.v[1] += o.v[1];
     };
     Eight r{};
+    if (e.factor) {
+        const float f = e.factor[g];
+        z.v[0] *= f;
+        z.v[1] *= f;
+    }
     if (e.place) r = load_eight(e.res, g * e.r_batch + m * e.ldr + n, e.type);
     if (e.bias) add(load_eight(e.bias, g * e.bias_batch + n, e.type));
     if (e.place == GBMUF_RESIDUAL_BEFORE) add(r);
