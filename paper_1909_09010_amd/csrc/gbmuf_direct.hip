@@ -282,7 +282,7 @@ __global__ __launch_bounds__(GROUPS *kThreads) void loss_direct_kernel(DirectArg
     const Share share = share_of<kTile, kTile>(a.t, static_cast<int>(blockIdx.x), (a.K + kDepth - 1) / kDepth);
     v16f acc[1][1];
     if (direct_sums<T, T, true, true, false, false, GROUPS>(acc, a, share, lds))
-        leave_loss<kTile, kTile, 2, 2, false, BACKWARD>(acc, lds, a.t, l, Scales{}, share.at);
+        leave_loss<kTile, kTile, 2, 2, BACKWARD>(acc, lds, a.t, l, share.at);
     if constexpr (!BACKWARD) {
         __syncthreads();
         store_parts<kTile, kTile, 2, 2, GROUPS * kThreads>(lds, a.t, l, share.at);

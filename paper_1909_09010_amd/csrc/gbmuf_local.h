@@ -126,6 +126,16 @@ struct Words {
     int32_t rows, vocab;     // of a worker, whole
 };
 
+// The words of lists by where they meet a tile of logits: for every block of block_rows rows the words of each window of 64 << shift, one behind the
+// other, as (word, row of the block << 16 | place in the row's list, share); a word that a row has more than once is there once, with all its shares.
+// starts: [g][block][windows + 1].
+struct WordLists {
+    int32_t *word, *row, *starts;
+    float *share;            // nullptr: not wanted
+    int32_t blocks, block_rows, windows, shift;          // shift: log2 of a window
+};
+constexpr int kMostWindows = 8192;
+
 // What is done with logits z = s + bias of the words `first` .. of the vocabulary.
 struct LossArgs {
     const void *bias;        // of `type`, or nullptr
@@ -134,7 +144,9 @@ struct LossArgs {
     int32_t type;
     int32_t first;
     float inv_tau, tau;
-    // forward: parts[g][tile][row], tiles counted over the vocabulary from first_tile on, and z of the rows' words, at[g][row][top]
+    WordLists lists;         // of tiles of many rows; word nullptr: rows have one word each
+    int32_t walk, reserved1; // tiles of logits that a workgroup takes one after the other
+    // forward: parts[g][part][row], counted over the vocabulary from first_tile on, and z of the rows' words, at[g][row][top]
     float2 *parts;
     float *at;
     int32_t part_tiles, first_tile;
@@ -213,6 +225,7 @@ int few_columns(const DirectArgs &a, int32_t type);        // of a tile of launc
 int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, bool backward, hipStream_t stream);
 int launch_loss_grads(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream);   // dz in f32
 int launch_teacher(const TeacherArgs &a, hipStream_t stream);
+int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStream_t stream);
 int launch_loss_join(const LossJoin &a, hipStream_t stream);
 int launch_keep(const KeepArgs &a, hipStream_t stream);
 int launch_cast(const CastArgs &a, hipStream_t stream);

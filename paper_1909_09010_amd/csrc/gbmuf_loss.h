@@ -45,21 +45,14 @@ __device__ __forceinline__ void in_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-// Row scales of operands that were taken apart.
-struct Scales {
-    const uint32_t *a_max, *b_max;
-    int64_t a_batch, b_batch;
-};
-
 // A tile of TM x TN logits by WM x WN waves; all waves are past what LDS held before.  A lane holds, of row lane % 32 of acc[i][j], the columns
 // 8 (r / 4) + 4 (lane / 32) + r % 4, so that what belongs to a row is a lane's own, and its sums need one exchange between the two
 // halves of the wave.  Words whose logits or shares are wanted are few (64 of 8197 words: 1 in 2 lanes and tile): their rows go through LDS, where a lane
 // finds any column, only where the wave has one.
 // Forward: (largest logit, sum of exp of the others less that) of every row of the tile, and the logits of the row's words.
 // Backward: dz = weight (exp(z / tau - lse) - share), through LDS so that stores follow rows, and its column sums before it is rounded.
-template <int TM, int TN, int WM, int WN, bool SPLIT, bool BACKWARD>
-__device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Tiles &t, const LossArgs &a, const Scales &scales,
-                                           const TileAt &tile)
+template <int TM, int TN, int WM, int WN, bool BACKWARD>
+__device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Tiles &t, const LossArgs &a, const TileAt &tile)
 {
     constexpr int FM = TM / WM / 32, FN = TN / WN / 32, kColumns = TN / WN, kPitch = kColumns + 4;
     const int64_t g = tile.g;
@@ -71,7 +64,6 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
     const auto row_of = [&](int i) { return m_wave + i * 32 + (lane & 31); };
 
     v4f bias[FN][4];
-    int exponent[SPLIT ? FN * 16 : 1];
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -87,9 +79,6 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
                         if (n + c < N) b[c] = load_one(a.bias, at + c, a.type);
             }
             bias[j][q] = b;
-            if constexpr (SPLIT)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) exponent[j * 16 + q * 4 + c] = row_exponent(scales.b_max[g * scales.b_batch + min(n + c, N - 1)]);
         }
 
     // the words of each of the lane's rows: where the list of them reaches this wave's columns
@@ -146,15 +135,10 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int m = row_of(i), mc = min(m, M - 1);
-        const int em = SPLIT ? row_exponent(scales.a_max[g * scales.a_batch + mc]) : 0;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float z = acc[i][j][r];
-                if constexpr (SPLIT) z = ldexpf(z, em + exponent[j * 16 + r]);
-                acc[i][j][r] = z + bias[j][r >> 2][r & 3];
-            }
+            for (int r = 0; r < 16; ++r) acc[i][j][r] += bias[j][r >> 2][r & 3];
         if (!whole)
 #pragma unroll
             for (int j = 0; j < FN; ++j)

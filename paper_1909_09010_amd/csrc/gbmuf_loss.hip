@@ -131,6 +131,37 @@ int order_words(const Loss &l, const Words &w, const Inputs &in, hipStream_t str
     return launch_teacher(a, stream);
 }
 
+// Lists by window for tiles of `tile` rows, whose waves take half of them each.
+WordLists lists_of(const Loss &l, const Words &w, int tile, bool shares, Space &space)
+{
+    WordLists lists{};
+    if (l.top == 0) return lists;
+    lists.block_rows = tile / 2;
+    lists.blocks = (w.rows + lists.block_rows - 1) / lists.block_rows;
+    lists.shift = 6;
+    while ((static_cast<int64_t>(w.vocab) >> lists.shift) >= kMostWindows) ++lists.shift;
+    lists.windows = (w.vocab >> lists.shift) + 1;
+    const int64_t blocks = static_cast<int64_t>(l.linear.batch) * lists.blocks, n = blocks * lists.block_rows * w.top;
+    lists.word = space.take<int32_t>(n);
+    lists.row = space.take<int32_t>(n);
+    lists.share = space.take<float>(shares ? n : 0);
+    if (!shares) lists.share = nullptr;
+    lists.starts = space.take<int32_t>(blocks * (lists.windows + 1));
+    return lists;
+}
+
+WordLists lists_from(const WordLists &lists, const Words &w, int64_t g)
+{
+    WordLists p = lists;
+    if (!p.word) return p;
+    const int64_t n = g * p.blocks * p.block_rows * w.top;
+    p.word += n;
+    p.row += n;
+    if (p.share) p.share += n;
+    p.starts += g * p.blocks * (p.windows + 1);
+    return p;
+}
+
 LossArgs loss_args(const Loss &l, const Inputs &in, const Words &w, const Piece &p)
 {
     LossArgs a{};
@@ -143,19 +174,42 @@ LossArgs loss_args(const Loss &l, const Inputs &in, const Words &w, const Piece 
     return a;
 }
 
-// Tiles of logits, none of them cut along the sum: the same two shapes as a product's, whose times a step they take.
-Cut logits_shape(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type)
+// Tiles of logits: of 256 x 256, one workgroup a CU, or of 128 x 128, two, as a product's, and how many of them a workgroup walks: as many as
+// fill the rounds of the chip best.  us: a product's step, what leaving a tile takes, and what a workgroup pays before its first step.
+Cut logits_shape(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type, bool backward)
 {
-    const int64_t steps = packed_words(K, split_type) / kStepWords;
-    const auto whole = [&](int tile, int64_t slots, double round) {
-        Cut c = cut(tile, M, N, batch, 1, std::max<int64_t>((M + tile - 1) / tile * ((N + tile - 1) / tile) * batch, 1), round);
-        const int64_t tiles = c.t.count();
-        c.t.steps = static_cast<int32_t>(std::max<int64_t>(steps, 1));
-        c.cost = static_cast<double>((tiles + slots - 1) / slots) * (static_cast<double>(steps) * round + 3.0);
-        return c;
-    };
-    const Cut wide = whole(256, 256, 1.73), small = whole(128, 512, 1.06);
-    return wide.cost <= small.cost ? wide : small;
+    const int64_t steps = std::max<int64_t>(packed_words(K, split_type) / kStepWords, 1);
+    Cut best;
+    for (const int tile : {256, 128}) {
+        const bool wide = tile == 256;
+        const int64_t rows = (M + tile - 1) / tile * batch, words = (N + tile - 1) / tile, slots = wide ? 256 : 512;
+        const double each = static_cast<double>(steps) * (wide ? 1.73 : 1.06) + (wide ? 4.0 : 2.5) * (backward ? 2.0 : 1.0);
+        for (int64_t walk = 1; walk <= std::min<int64_t>(words, 64); ++walk) {
+            const int64_t groups = rows * ((words + walk - 1) / walk);
+            const double cost = static_cast<double>((groups + slots - 1) / slots) * (static_cast<double>(walk) * each + 3.0);
+            if (best.tile != 0 && cost >= best.cost) continue;
+            best = Cut{};
+            best.tile = tile;
+            best.cost = cost;
+            best.t.M = static_cast<int32_t>(M); best.t.N = static_cast<int32_t>(N); best.t.batch = static_cast<int32_t>(batch);
+            best.t.tiles_m = static_cast<int32_t>((M + tile - 1) / tile);
+            best.t.steps = static_cast<int32_t>(walk);
+        }
+    }
+    best.t.splits = 1;
+    best.t.tiles_n = static_cast<int32_t>(((N + best.tile - 1) / best.tile + best.t.steps - 1) / best.t.steps);
+    best.t.whole = best.t.count();
+    return best;
+}
+
+// The same tiles for fewer words or workers.
+Cut same_shape(const Cut &c, int64_t N, int64_t batch)
+{
+    Cut s = c;
+    s.t.N = static_cast<int32_t>(N); s.t.batch = static_cast<int32_t>(batch);
+    s.t.tiles_n = static_cast<int32_t>(((N + c.tile - 1) / c.tile + c.t.steps - 1) / c.t.steps);
+    s.t.whole = s.t.count();
+    return s;
 }
 
 ProductArgs logits_args(const Operand &x, const Operand &w, int64_t K, int32_t type, const Cut &c)
@@ -241,15 +295,18 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
     // w is laid out a piece at a time, x once
     const bool may_lay = few == Few::kNo, lay_x = split || (may_lay && (!in || !lies_well(at.x))), lay_w = split || (may_lay && (!in || !lies_well(at.w)));
     const Pieces pieces = lay_w ? pieces_of(G, N, packed_words(K, split) * 2, kLaidBytes) : Pieces{std::max(G, 1), std::max<int64_t>(N, 1)};
-    const Cut shape = logits_shape(M, pieces.words, K, pieces.workers, split);
-    float2 *parts = parts_of((N + shape.tile - 1) / shape.tile);
+    const Cut shape = logits_shape(M, pieces.words, K, pieces.workers, split, false);
+    const int64_t whole_pieces = N / pieces.words;
+    float2 *parts = parts_of(whole_pieces * shape.t.tiles_n + same_shape(shape, N - whole_pieces * pieces.words, 1).t.tiles_n);
+    const WordLists lists = lists_of(l, words, shape.tile, false, space);
     const LayArgs lx = source(at.x, M, K, G, type);
     Operand x = operand_of(at.x), w = operand_of(at.w);
     if (lay_x) x = packed(space, M, K, G, in ? lx.batch : G, split, space.take<uint32_t>(split ? G * M : 0));
     if (lay_w) w = packed(space, pieces.words, K, static_cast<int32_t>(pieces.workers), static_cast<int32_t>(pieces.workers), split,
-                          space.take<uint32_t>(split ? pieces.workers * pieces.words : 0));
+                          space.take<uint32_t>(split ? pieces.workers * pieces.words + 256 : 0));
     if (!in) return GBMUF_OK;
     if ((rc = order_words(l, words, at, stream)) != GBMUF_OK) return rc;
+    if (lists.word && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK) return rc;
     if (lay_x && (rc = lay_rows(lx, x, K, type, stream)) != GBMUF_OK) return rc;
     rc = each_piece(pieces, G, N, [&](const Piece &p) {
         Operand px = x, pw = w;
@@ -263,14 +320,14 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
             const int r = lay_rows(lw, pw, K, type, stream);
             if (r != GBMUF_OK) return r;
         } else pw = operand_of(wm);
-        Cut c = logits_shape(M, p.words, K, p.workers, split);
-        if (c.tile != shape.tile) c = cut(shape.tile, M, p.words, p.workers, 1, 0x7fffffff, 1.0);
+        const Cut c = same_shape(shape, p.words, p.workers);
         LossArgs a = loss_args(l, at, words, p);
+        a.lists = lists_from(lists, words, p.g);
+        a.walk = c.t.steps;
         a.part_tiles = j.tiles;
-        a.first_tile = static_cast<int32_t>(p.v / shape.tile);
+        a.first_tile = static_cast<int32_t>(p.v / pieces.words) * shape.t.tiles_n;
         a.parts = parts + p.g * j.tiles * M;
         a.at = word_logits + p.g * M * words.top;
-        c.t.steps = static_cast<int32_t>(std::max<int64_t>(packed_words(K, split) / kStepWords, 1));
         return launch_vocab(logits_args(px, pw, K, type, c), a, type, shape.tile, false, stream);
     });
     return rc == GBMUF_OK ? launch_loss_join(j, stream) : rc;
@@ -356,6 +413,8 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     const int64_t PG = pieces.workers, PN = pieces.words, ld = (PN + 63) / 64 * 64;
     const bool copy_w = !split && (!io || !as_it_lies(at.w, K));
     const int64_t kept = packed_words(K, false);                 // columns of a row of x that is kept
+    const Cut shape = logits_shape(M, PN, K, PG, split, true);
+    const WordLists lists = lists_of(l, words, shape.tile, true, space);
     // the last workers or words may be fewer, and cut otherwise
     int64_t parts = 0;
     for (const int64_t workers : {PG, G % PG})
@@ -378,7 +437,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         x = packed(space, M, K, G, G, true, space.take<uint32_t>(G * M));
         xt = packed(space, K, M, G, G, true, x_max);
         const int32_t workers = static_cast<int32_t>(PG);
-        w = packed(space, PN, K, workers, workers, true, space.take<uint32_t>(PG * PN));
+        w = packed(space, PN, K, workers, workers, true, space.take<uint32_t>(PG * PN + 256));
         wt = packed(space, K, PN, workers, workers, true, max + PG * (M + PN));
         z = packed(space, M, PN, workers, workers, true, max);
         zt = packed(space, PN, M, workers, workers, true, max + PG * M);
@@ -388,7 +447,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     if (!io) return GBMUF_OK;
 
     int rc = order_words(l, words, at, stream);
-    if (rc != GBMUF_OK) return rc;
+    if (rc != GBMUF_OK || (lists.word && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK)) return rc;
     KeepArgs keep{};
     keep.words = words;
     keep.x = at.x.data; keep.ld = at.x.ld; keep.batch_stride = at.x.batch_stride;
@@ -426,8 +485,10 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
             if ((r = lay_rows(lw, pw, K, type, stream)) != GBMUF_OK) return r;
         } else pw = operand_of(wm);
 
-        Cut c = logits_shape(M, p.words, K, workers, split);
+        const Cut c = same_shape(shape, p.words, workers);
         LossArgs a = grad_args(l, at, io, words, p);
+        a.lists = lists_from(lists, words, p.g);
+        a.walk = c.t.steps;
         a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld; a.dz_type = type;
         if (type == kF16) a.sigma = sigma + p.g;
         if (db && !split) a.col_sums = sums;

@@ -4,15 +4,74 @@
 namespace gbmuf {
 namespace {
 
-// One tile of TM x TN by WM x WN waves.
+// One tile of TM x TN, WM x WN waves.  Two stages in LDS: while one is multiplied the next step arrives in the other.  A wave
+// loads a turn's operands while it multiplies the turn before, and the waves meet before the last turn of a step, whose operands they then
+// all hold: the next step's first turn is loaded, and the step after it sent for, under that last turn.
 template <int T, bool SPLIT, int TM, int TN, int WM, int WN, int ACROSS>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 {
+    constexpr int THREADS = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kTurns = SPLIT ? 2 : 4;
     __shared__ __align__(1024) uint16_t lds[2][(TM + TN) * kStep];
     static_assert(leave_bytes<TM, TN, WM, WN>() <= sizeof(lds), "the result leaves through the stages");
+
     const Share share = share_of<TM, TN>(a.t, static_cast<int>(blockIdx.x), (a.K + kStep - 1) / kStep);
-    v16f acc[TM / WM / 32][TN / WN / 32];
-    sum_tile<T, SPLIT, TM, TN, WM, WN, ACROSS>(acc, lds, a, share);
+    const int64_t g = share.at.g;
+    const int m0 = share.at.tm * TM, n0 = share.at.tn * TN, first = share.first, last = share.last;
+    const int full = min(last, a.K / kStep);               // steps [first, full) are whole
+    std::conditional_t<(ACROSS & 1) != 0, StageAcross<TM, THREADS>, Stage<TM, THREADS>> sa;
+    std::conditional_t<(ACROSS & 2) != 0, StageAcross<TN, THREADS>, Stage<TN, THREADS>> sb;
+    sa.init(a.a + g * a.a_batch, a.lda, m0, a.t.M);
+    sb.init(a.b + g * a.b_batch, a.ldb, n0, a.t.N);
+
+    const int wave = threadIdx.x >> 6, wm = (wave % WM) * (TM / WM), wn = (wave / WM) * (TN / WN);
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    constexpr int kReads = (SPLIT ? 2 : 1) * ((ACROSS & 1 ? 0 : FM) + (ACROSS & 2 ? 0 : FN)), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
+    Turn<T, SPLIT, TM, TN, FM, FN, ACROSS> turn[2];
+    if (first < full) {
+        sa.load(lds[0], first * kStep);
+        sb.load(lds[0] + TM * kStep, first * kStep);
+        wait_and_meet();
+        if (first + 1 < full) {
+            sa.load(lds[1], (first + 1) * kStep);
+            sb.load(lds[1] + TM * kStep, (first + 1) * kStep);
+        }
+        turn[0].template load<0>(lds[0], wm, wn);
+        for (int s = first; s < full; ++s) {
+            uint16_t *now = lds[(s - first) & 1], *next = lds[(s - first + 1) & 1];
+            repeat<kTurns - 1>([&](auto t) {
+                turn[(t + 1) & 1].template load<t + 1>(now, wm, wn);
+                turn[t & 1].multiply(acc);
+                interleave<kReads, kMfmas>();
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            wait_and_meet();
+            if (s + 2 < full) {
+                sa.load(now, (s + 2) * kStep);
+                sb.load(now + TM * kStep, (s + 2) * kStep);
+            }
+            if (s + 1 < full) turn[0].template load<0>(next, wm, wn);
+            turn[(kTurns - 1) & 1].multiply(acc);
+            interleave<kReads, kMfmas>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (full < last) {                                     // at most one step; nothing is in flight, the waves may be in the last turn
+        __syncthreads();
+        sa.load_rest(lds[0], full * kStep, a.K);
+        sb.load_rest(lds[0] + TM * kStep, full * kStep, a.K);
+        __syncthreads();
+        repeat<kTurns>([&](auto t) {
+            turn[0].template load<t>(lds[0], wm, wn);
+            turn[0].multiply(acc);
+        });
+    }
     __syncthreads();
     leave<TM, TN, WM, WN, SPLIT>(acc, &lds[0][0], a, share);
 }

@@ -84,6 +84,63 @@ __global__ __launch_bounds__(256) void teacher_kernel(TeacherArgs a, int32_t pad
 }
 
 // ---------------------------------------------------------------------------------------
+// Lists of words by window: a workgroup takes the lists of a block of rows, counts the words of each window, and puts them there.  Within a window they lie in no
+// certain order, which no result depends on: no two are the same word of the same row.
+// ---------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void word_lists_kernel(Words w, WordLists l)
+{
+    __shared__ int32_t count[kMostWindows];
+    __shared__ int32_t sums[4];
+    const int64_t g = blockIdx.x / l.blocks;
+    const int block = static_cast<int>(blockIdx.x % l.blocks), m0 = block * l.block_rows, rows = min(l.block_rows, w.rows - m0), n = rows * w.top;
+    const int64_t first = (g * w.rows + m0) * w.top, out = static_cast<int64_t>(blockIdx.x) * l.block_rows * w.top;
+    const int32_t *id = w.id + first;
+    const float *share = w.share + first;
+    int32_t *starts = l.starts + static_cast<int64_t>(blockIdx.x) * (l.windows + 1);
+    for (int i = threadIdx.x; i < l.windows; i += 256) count[i] = 0;
+    __syncthreads();
+    const auto each = [&](auto f) {
+        for (int e = threadIdx.x; e < n; e += 256) {
+            const int word = id[e], p = e % w.top;
+            if (word < w.vocab && (p == 0 || id[e - 1] != word)) f(word, e, p);
+        }
+    };
+    each([&](int word, int, int) { atomicAdd(&count[word >> l.shift], 1); });
+    __syncthreads();
+    // where each window begins: a thread's windows lie side by side
+    const int per = (l.windows + 255) / 256, from = threadIdx.x * per, to = min(from + per, l.windows);
+    int mine = 0;
+    for (int i = from; i < to; ++i) mine += count[i];
+    int before = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int v = __shfl_up(before, d);
+        if (static_cast<int>(threadIdx.x & 63) >= d) before += v;
+    }
+    if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = before;
+    __syncthreads();
+    for (int v = 0; v < static_cast<int>(threadIdx.x >> 6); ++v) before += sums[v];
+    int at = before - mine;
+    for (int i = from; i < to; ++i) {
+        const int c = count[i];
+        starts[i] = at;
+        count[i] = at;
+        at += c;
+    }
+    if (threadIdx.x == 255) starts[l.windows] = before;
+    __syncthreads();
+    each([&](int word, int e, int p) {
+        const int place = atomicAdd(&count[word >> l.shift], 1);
+        l.word[out + place] = word;
+        l.row[out + place] = ((e / w.top) << 16) | p;
+        if (!l.share) return;
+        float s = share[e];
+        for (int q = 1; p + q < w.top && id[e + q] == word; ++q) s += share[e + q];
+        l.share[out + place] = s;
+    });
+}
+
+// ---------------------------------------------------------------------------------------
 // Losses.  A workgroup takes ROWS rows: 256 / ROWS threads share the parts of a row, side by side in memory with its neighbours', and then its words.
 // ---------------------------------------------------------------------------------------
 template <int ROWS>
@@ -127,7 +184,10 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
                 const int64_t at = row * w.top + j;
                 const float share = w.share[at];
                 // nothing is lost by a word that the teacher gives no share
-                if (w.id[at] != kNoWord && share != 0.0f) loss += share * (logf(share) - fmaf(a.at[at], a.inv_tau, -lse));
+                if (w.id[at] == kNoWord || share == 0.0f) continue;
+                int64_t one = at;                           // a word's logit stands at its first place
+                while (one > row * w.top && w.id[one - 1] == w.id[at]) --one;
+                loss += share * (logf(share) - fmaf(a.at[one], a.inv_tau, -lse));
             }
         loss = sum_of<(kThreads < 64 ? kThreads : 64)>(loss);
         if constexpr (kThreads > 64) {
@@ -213,6 +273,18 @@ int launch_teacher(const TeacherArgs &a, hipStream_t stream)
     const auto fn = padded <= 128 ? teacher_kernel<128> : teacher_kernel<kMostTop>;
     const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(teacher)", err, GBMUF_EDEVICE);
+}
+
+int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStream_t stream)
+{
+    const int64_t blocks = static_cast<int64_t>(l.blocks) * batch;
+    if (blocks <= 0) return GBMUF_OK;
+    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    Words words = w;
+    WordLists lists = l;
+    void *argv[] = {&words, &lists};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(word_lists_kernel), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(lists of words)", err, GBMUF_EDEVICE);
 }
 
 // Few rows: more threads for the parts of each.

@@ -6,20 +6,398 @@
 namespace gbmuf {
 namespace {
 
-// One tile of TM x TN logits by WM x WN waves.
-template <int T, bool SPLIT, int TM, int TN, int WM, int WN, bool BACKWARD>
-__global__ __launch_bounds__(64 * WM * WN) void vocab_kernel(ProductArgs a, LossArgs l)
+// 32 x 32 values of a wave on their way between lanes that hold a row and lanes that hold 8 columns: the 16-byte chunk c of row r at place
+// c ^ ((r / 2) & 7), so that 16 lanes meet all banks both ways.
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(4)));
+constexpr float kPlain = 65536.0f;       // up to here the rounding of what an exponent subtracts is a small one
+constexpr int kScratch = 32 * 32;
+__device__ __forceinline__ int scratch_at(int r, int c) { return r * 32 + (((c >> 2) ^ ((r >> 1) & 7)) << 2) + (c & 3); }
+
+// Sends R rows of one step to LDS as Stage does.  Where the rows are is worked out for every step from one address a lane: Stage's addresses, kept over a
+// tile's steps, would go to memory and back (f32 by tiles of 256 8 x 700 x 10000 x 650: 436 us, where these take 3TODO).
+template <int R, int THREADS>
+struct Sender {
+    static constexpr int kPass = THREADS / 8, kPasses = R / kPass;
+    static_assert(kPass % 16 == 0, "a thread's chunk lies at the same place in every pass");
+    const uint16_t *base;        // of the matrix
+    int64_t ld;
+    int first, count;
+
+    // whatever is derived from this number is derived anew
+    __device__ __forceinline__ static int thread()
+    {
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return t;
+    }
+    __device__ __forceinline__ static int chunk(int t) { return ((t & 7) ^ ((t >> 4) & 7)) * 8; }
+
+    // rows behind the last are read as the last one
+    __device__ __forceinline__ void load(uint16_t *lds, int k0) const
+    {
+        const int t = thread(), r = t >> 3;
+        const uint16_t *at = base + k0 + chunk(t);
+        uint16_t *to = lds + static_cast<int>(threadIdx.x >> 6) * 8 * kStep;
+        const auto send = [&](int i, const uint16_t *from) {
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)from,
+                                             (__attribute__((address_space(3))) void *)(to + i * kPass * kStep), 16, 0, 0);
+        };
+        if (first + R <= count) {
+            at += static_cast<int64_t>(first + r) * ld;
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) send(i, at + i * kPass * ld);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) send(i, at + static_cast<int64_t>(min(first + r + i * kPass, count - 1)) * ld);
+        }
+    }
+
+    __device__ __forceinline__ void load_rest(uint16_t *lds, int k0, int K) const
+    {
+        const int t = thread(), r = t >> 3, left = K - (k0 + chunk(t));
+#pragma unroll 1
+        for (int i = 0; i < kPasses; ++i) {
+            uint32_t v[4] = {0u, 0u, 0u, 0u};
+            const uint16_t *from = base + static_cast<int64_t>(min(first + r + i * kPass, count - 1)) * ld + k0 + chunk(t);
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c < left) v[c >> 1] |= static_cast<uint32_t>(from[c]) << (16 * (c & 1));
+            *reinterpret_cast<v4u *>(lds + (i * kPass + r) * kStep + (t & 7) * 8) = v4u{v[0], v[1], v[2], v[3]};
+        }
+    }
+};
+
+// A workgroup takes one block of TM rows and walks `walk` tiles of TN words, as one stream of steps: while a tile is left the first two steps of the
+// next are on their way, so that only the arithmetic of leaving is paid.  Everything that a row needs is a lane's own (leave_loss): its statistics
+// stay in registers over all of the tiles, and lse and weight are loaded once.
+// Forward, per logit: a maximum, a multiply-add, an exponential and an addition.
+template <int T, bool SPLIT, int TM, int TN, int WM, int WN, bool BACKWARD, bool LISTS>
+__global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, LossArgs l)
 {
+    constexpr int THREADS = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, kColumns = TN / WN, kTurns = SPLIT ? 2 : 4;
     __shared__ __align__(1024) uint16_t lds[2][(TM + TN) * kStep];
-    static_assert(loss_bytes<TM, TN, WM, WN>() <= sizeof(lds), "what follows takes the stages' place");
-    const Share share = share_of<TM, TN>(a.t, static_cast<int>(blockIdx.x), (a.K + kStep - 1) / kStep);
-    v16f acc[TM / WM / 32][TN / WN / 32];
-    sum_tile<T, SPLIT, TM, TN, WM, WN, 0>(acc, lds, a, share);
-    __syncthreads();
-    leave_loss<TM, TN, WM, WN, SPLIT, BACKWARD>(acc, &lds[0][0], a.t, l, Scales{a.a_max, a.b_max, a.a_max_batch, a.b_max_batch}, share.at);
+    __shared__ __align__(16) float scratches[WM * WN][kScratch];
+    static_assert(sizeof(float2) * TM * WN <= sizeof(lds), "the rows' statistics take the stages' place");
+    const Share share = share_of<TM, TN>(a.t, static_cast<int>(blockIdx.x), 0);
+    const int64_t g = share.at.g;
+    const int M = a.t.M, N = a.t.N, m0 = share.at.tm * TM, tiles = (N + TN - 1) / TN, first = share.at.tn * l.walk, last = min(first + l.walk, tiles);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6, wm = (wave % WM) * (TM / WM), wn = (wave / WM) * kColumns;
+    const Words &w = l.words;
+    float *scratch = scratches[wave];
+
+    // the stream of steps
+    const int full = a.K / kStep, steps = (a.K + kStep - 1) / kStep;
+    const Sender<TM, THREADS> sa{a.a + g * a.a_batch, a.lda, m0, M};
+    int send_tile = steps > 0 ? first : last, send_step = 0, t = 0;
+    const auto send = [&](uint16_t *to) {
+        if (send_tile >= last) return;
+        const Sender<TN, THREADS> sb{a.b + g * a.b_batch, a.ldb, send_tile * TN, N};
+        if (send_step < full) {
+            sa.load(to, send_step * kStep);
+            sb.load(to + TM * kStep, send_step * kStep);
+        } else {
+            sa.load_rest(to, send_step * kStep, a.K);
+            sb.load_rest(to + TM * kStep, send_step * kStep, a.K);
+        }
+        if (++send_step == steps) {
+            send_step = 0;
+            ++send_tile;
+        }
+    };
+    send(lds[0]);
+
+    // what a row brings along
+    const float scale = l.inv_tau * kLog2E;
+    float2 stats[FM];                                     // forward: as join_stats has them, of the lane's own columns
+    float weight[FM], p_weight[FM], lse[FM];              // backward
+    int32_t target[LISTS ? 1 : FM];
+    bool near[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int m = m0 + wm + i * 32 + (lane & 31), mc = min(m, M - 1);
+        stats[i] = float2{-__builtin_inff(), 0.0f};
+        if constexpr (!LISTS) {
+            const int64_t word = w.target[g * w.batch + mc * w.ld];
+            target[i] = m < M && word < w.vocab ? static_cast<int32_t>(word < 0 ? -1 : word) : -1;
+        }
+        if constexpr (BACKWARD) {
+            const int state = m < M ? row_state(w, g, mc) : kDead;
+            const float sigma = l.sigma ? l.sigma[g] : 1.0f;
+            weight[i] = row_weight(l, g, mc, state) * sigma;
+            // a row that does not count: exp of something far below, times 0
+            const float n = state == kDead ? 1e30f : l.lse[g * l.lse_batch + mc * l.lse_ld];
+            near[i] = state == kDead || fabsf(n) <= kPlain;
+            lse[i] = near[i] ? n * kLog2E : n;
+            p_weight[i] = state == kDead ? 0.0f : near[i] ? weight[i] * exp2_of(-fmaf(n, kLog2E, -lse[i])) : weight[i];       // what the product rounded away
+        }
+    }
+
+    // the logits' sums begin with the bias, loaded while the tile before is left
+    typedef typename Four<T>::type Raw;
+    Raw bias[SPLIT ? 1 : FN][SPLIT ? 1 : 4];
+    const auto load_bias = [&](int tile) {
+        if constexpr (!SPLIT) {
+            const int n_wave = tile * TN + wn;
+            const typename Num<T>::type *from = static_cast<const typename Num<T>::type *>(l.bias) + g * l.bias_batch;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n_wave + j * 32 + q * 8 + half * 4;
+                    bias[j][q] = Raw{};
+                    if (!l.bias || tile >= last) continue;
+                    if (n_wave + kColumns <= N) bias[j][q] = *reinterpret_cast<const Raw *>(from + n);
+                    else
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (n + c < N) bias[j][q][c] = from[n + c];
+                }
+        }
+    };
+    if (!BACKWARD) load_bias(first);
+
+    wait_and_meet();
+    send(lds[1]);
+    constexpr int kReads = (SPLIT ? 2 : 1) * (FM + FN), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
+    for (int tile = first; tile < last; ++tile) {
+        v16f acc[FM][FN];
+        if (BACKWARD) load_bias(tile);                      // the registers that hold it while a tile is left are not to be had
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = SPLIT ? 0.0f : static_cast<float>(bias[j][r >> 2][r & 3]);
+        Turn<T, SPLIT, TM, TN, FM, FN, 0> turn[2];
+        if (steps > 0) turn[0].template load<0>(lds[t & 1], wm, wn);
+        for (int s = 0; s < steps; ++s, ++t) {
+            uint16_t *now = lds[t & 1], *next = lds[(t + 1) & 1];
+            repeat<kTurns - 1>([&](auto k) {
+                turn[(k + 1) & 1].template load<k + 1>(now, wm, wn);
+                turn[k & 1].multiply(acc);
+                interleave<kReads, kMfmas>();
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            wait_and_meet();
+            send(now);
+            if (s + 1 < steps) turn[0].template load<0>(next, wm, wn);
+            turn[(kTurns - 1) & 1].multiply(acc);
+            interleave<kReads, kMfmas>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!BACKWARD) load_bias(tile + 1);
+
+        // what leaving derives from the lane is derived anew for every tile: kept over the steps, it would take the registers of the sums
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        const int half = lane >> 5;
+        const int n_wave = tile * TN + wn, lo = l.first + n_wave, hi = l.first + min(n_wave + kColumns, N);
+        const bool whole = n_wave + kColumns <= N;
+        const int left = N - n_wave - half * 4;             // columns from the lane's first on
+        // words of the wave's rows among its columns, 64 of them at hand
+        int entries = 0, entry_word = kNoWord, entry_row = 0;
+        float entry_share = 0.0f;
+        const int32_t *list_word = nullptr, *list_row = nullptr;
+        const float *list_share = nullptr;
+        if constexpr (LISTS) {
+            const int64_t block = g * l.lists.blocks + (m0 + wm) / (TM / WM);
+            if (m0 + wm < M && n_wave < N) {
+                const int32_t *starts = l.lists.starts + block * (l.lists.windows + 1) + (lo >> l.lists.shift);
+                const int begin = starts[0];
+                entries = starts[1] - begin;
+                const int64_t at = block * (TM / WM) * w.top + begin;
+                list_word = l.lists.word + at;
+                list_row = l.lists.row + at;
+                list_share = l.lists.share + at;
+            }
+            if (lane < entries) {
+                entry_word = list_word[lane];
+                entry_row = list_row[lane];
+                if (BACKWARD) entry_share = list_share[lane];
+            }
+        }
+        // f(word, row and slot, share) for the words in columns j of rows i
+        const auto each_entry = [&](int i, int j, auto f) {
+            const auto mine = [&](int word, int row) { return word >= lo && word < hi && ((word - lo) >> 5) == j && (row >> 21) == i; };
+            if (mine(entry_word, entry_row)) f(entry_word, entry_row, entry_share);
+            for (int e = 64 + lane; e < entries; e += 64) {
+                const int word = list_word[e], row = list_row[e];
+                if (mine(word, row)) f(word, row, BACKWARD ? list_share[e] : 0.0f);
+            }
+        };
+        const auto put = [&](const v16f &rows) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<v4f *>(scratch + scratch_at(lane & 31, 8 * q + 4 * half)) = v4f{rows[4 * q], rows[4 * q + 1], rows[4 * q + 2], rows[4 * q + 3]};
+        };
+
+        if constexpr (SPLIT) {
+            int em[FM];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) em[i] = row_exponent(a.a_max[g * a.a_max_batch + min(m0 + wm + i * 32 + (lane & 31), M - 1)]);
+            const float *from = static_cast<const float *>(l.bias) + g * l.bias_batch;
+            const uint32_t *tops = a.b_max + g * a.b_max_batch;            // up to the end of the last tile, whatever lies behind N
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                v4f b[4];
+                v4u e[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n_wave + j * 32 + q * 8 + half * 4;
+                    b[q] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                    e[q] = *reinterpret_cast<const v4u_any *>(tops + n);
+                    const int rest = left - (j * 32 + q * 8);
+                    if (l.bias && rest >= 4) b[q] = read4<kF32>(from, n);
+                    else if (l.bias) {
+                        if (rest > 0) b[q][0] = from[n];
+                        if (rest > 1) b[q][1] = from[n + 1];
+                        if (rest > 2) b[q][2] = from[n + 2];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = ldexpf(acc[i][j][r], em[i] + row_exponent(e[r >> 2][r & 3])) + b[r >> 2][r & 3];
+            }
+        }
+        v4f total[BACKWARD ? FN : 1][2];
+        if constexpr (BACKWARD)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int row0 = m0 + wm + i * 32, m = row0 + (lane & 31);
+            if (!whole)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (j * 32 + (r >> 2) * 8 + (r & 3) >= left) acc[i][j][r] = -__builtin_inff();
+            int column = -1;                                // of the row's word
+            if constexpr (!LISTS) column = target[i] >= lo && target[i] < hi ? target[i] - lo : -1;
+            if constexpr (!BACKWARD) {
+                float most = acc[i][0][0];
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][j][r]);
+                // sums of 2^(z scale - from), from = most scale rounded; afterwards less most scale itself.  Rows far from 0 have a sum of their own: from an
+                // infinite logit nothing is taken away, it makes the sum infinite, or is nothing of it
+                const bool near = fabsf(most * scale) <= kPlain;
+                const float from = near ? most * scale : fabsf(most) < __builtin_inff() ? most : 0.0f;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (__all(near)) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sum[r & 3] += exp2_of(fmaf(acc[i][j][r], scale, -from));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sum[r & 3] += exp2_of(near ? fmaf(acc[i][j][r], scale, -from) : (acc[i][j][r] - from) * scale);
+                }
+                sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                if (near) sum[0] *= exp2_of(-fmaf(most, scale, -from));
+                stats[i] = join_stats(stats[i], float2{most, sum[0]}, scale);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    if constexpr (LISTS) {
+                        if (!__any(entry_word < hi && (entry_row >> 21) == i) && entries <= 64) continue;
+                        in_order();
+                        put(acc[i][j]);
+                        in_order();
+                        each_entry(i, j, [&](int word, int row, float) {
+                            const int r = (row >> 16) & 31;
+                            l.at[(g * w.rows + row0 + r) * w.top + (row & 0xffff)] = scratch[scratch_at(r, (word - lo) & 31)];
+                        });
+                    } else if (__any(column >> 5 == j)) {
+                        in_order();
+                        put(acc[i][j]);
+                        in_order();
+                        if (column >> 5 == j && half == 0) l.at[g * w.rows + m] = scratch[scratch_at(lane, column & 31)];
+                    }
+                }
+            } else {
+                if (__all(near[i])) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][j][r] = p_weight[i] * exp2_of(fmaf(acc[i][j][r], scale, -lse[i]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const float z = acc[i][j][r];
+                            acc[i][j][r] = p_weight[i] * exp2_of(near[i] ? fmaf(z, scale, -lse[i]) : fmaf(z, l.inv_tau, -lse[i]) * kLog2E);
+                        }
+                }
+                const float of_row = LISTS ? __shfl(weight[i], (entry_row >> 16) & 31) : weight[i];
+                // 32 rows of 32 columns at a time: 4 lanes a row
+                const int from = lane >> 2, eight = (lane & 3) * 8;
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    in_order();
+                    put(acc[i][j]);
+                    in_order();
+                    if constexpr (LISTS) {
+                        each_entry(i, j, [&](int word, int row, float part) {
+                            const int r = (row >> 16) & 31;
+                            const float of = row == entry_row ? of_row : row_weight(l, g, row0 + r, row_state(w, g, row0 + r)) * (l.sigma ? l.sigma[g] : 1.0f);
+                            scratch[scratch_at(r, (word - lo) & 31)] -= of * part;
+                        });
+                        in_order();
+                    } else if (__any(column >> 5 == j)) {
+                        if (column >> 5 == j && half == 0) scratch[scratch_at(lane, column & 31)] -= of_row;
+                        in_order();
+                    }
+                    const int n = n_wave + j * 32 + eight;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int r = k * 16 + from;
+                        const Eight z{{*reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight)), *reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight + 4))}};
+                        total[j][0] += z.v[0];
+                        total[j][1] += z.v[1];
+                        if (row0 + r < M && n < l.dz_ld) write8<SPLIT ? kF32 : T>(l.dz, g * l.dz_batch + (row0 + r) * l.dz_ld + n, z);
+                    }
+                }
+            }
+        }
+        if constexpr (BACKWARD) {
+            if (!l.col_sums) continue;
+            float *to = l.col_sums + ((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int n = n_wave + j * 32 + (lane & 3) * 8;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    float v = total[j][c >> 2][c & 3];
+#pragma unroll
+                    for (int d = 4; d < 64; d *= 2) v += __shfl_xor(v, d);
+                    if (lane < 4 && n + c < N) to[n + c] = v;
+                }
+            }
+        }
+    }
     if constexpr (!BACKWARD) {
+        // nothing of the stages is read any more
+        float2 *all = reinterpret_cast<float2 *>(&lds[0][0]);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const float2 other{__shfl_xor(stats[i].x, 32), __shfl_xor(stats[i].y, 32)};
+            const float2 s = join_stats(stats[i], other, scale);
+            if (half == 0) all[(wave / WM) * TM + wm + i * 32 + lane] = s;
+        }
         __syncthreads();
-        store_parts<TM, TN, WM, WN, 64 * WM * WN>(&lds[0][0], a.t, l, share.at);
+        for (int r = threadIdx.x; r < TM; r += THREADS) {
+            if (m0 + r >= M) continue;
+            float2 s = all[r];
+#pragma unroll
+            for (int v = 1; v < WN; ++v) s = join_stats(s, all[v * TM + r], scale);
+            l.parts[(g * l.part_tiles + l.first_tile + share.at.tn) * w.rows + m0 + r] = s;
+        }
     }
 }
 
@@ -32,14 +410,14 @@ int launch_vocab(const ProductArgs &a, const LossArgs &l, int32_t type, int tile
     LossArgs loss = l;
     void *argv[] = {&args, &loss};
     using Fn = void (*)(ProductArgs, LossArgs);
-    static constexpr Fn fns[3][2][2] = {
-        {{vocab_kernel<kF16, true, 128, 128, 2, 2, false>, vocab_kernel<kF16, true, 256, 256, 2, 4, false>},
-         {vocab_kernel<kF16, true, 128, 128, 2, 2, true>, vocab_kernel<kF16, true, 256, 256, 2, 4, true>}},
-        {{vocab_kernel<kBf16, false, 128, 128, 2, 2, false>, vocab_kernel<kBf16, false, 256, 256, 2, 4, false>},
-         {vocab_kernel<kBf16, false, 128, 128, 2, 2, true>, vocab_kernel<kBf16, false, 256, 256, 2, 4, true>}},
-        {{vocab_kernel<kF16, false, 128, 128, 2, 2, false>, vocab_kernel<kF16, false, 256, 256, 2, 4, false>},
-         {vocab_kernel<kF16, false, 128, 128, 2, 2, true>, vocab_kernel<kF16, false, 256, 256, 2, 4, true>}}};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][tile == 256 ? 1 : 0]),
+#define GBMUF_VOCAB(T, SPLIT, BACKWARD)                                                                                                       \
+    {{vocab_kernel<T, SPLIT, 128, 128, 2, 2, BACKWARD, false>, vocab_kernel<T, SPLIT, 128, 128, 2, 2, BACKWARD, true>},                        \
+     {vocab_kernel<T, SPLIT, 256, 256, 2, 4, BACKWARD, false>, vocab_kernel<T, SPLIT, 256, 256, 2, 4, BACKWARD, true>}}
+    static constexpr Fn fns[3][2][2][2] = {{GBMUF_VOCAB(kF16, true, false), GBMUF_VOCAB(kF16, true, true)},
+                                           {GBMUF_VOCAB(kBf16, false, false), GBMUF_VOCAB(kBf16, false, true)},
+                                           {GBMUF_VOCAB(kF16, false, false), GBMUF_VOCAB(kF16, false, true)}};
+#undef GBMUF_VOCAB
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][tile == 256 ? 1 : 0][l.lists.word ? 1 : 0]),
                                            dim3(static_cast<unsigned>(a.t.blocks())), dim3(tile == 256 ? 512 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(logits)", err, GBMUF_EDEVICE);
 }
