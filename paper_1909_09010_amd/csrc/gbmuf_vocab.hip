@@ -13,6 +13,16 @@ constexpr float kPlain = 65536.0f;       // up to here the rounding of what an e
 constexpr int kScratch = 32 * 32;
 __device__ __forceinline__ int scratch_at(int r, int c) { return r * 32 + (((c >> 2) ^ ((r >> 1) & 7)) << 2) + (c & 3); }
 
+// wait_and_meet, with the wait where the compiler sees it: what was read of LDS before is at hand then, and is not waited for once more together with what
+// is read next.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // Sends R rows of one step to LDS as Stage does.  Where the rows are is worked out for every step from one address a lane: Stage's addresses, kept over a
 // tile's steps, would go to memory and back (f32 by tiles of 256 8 x 700 x 10000 x 650: 436 us, where these take 3TODO).
 template <int R, int THREADS>
@@ -156,7 +166,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
     };
     if (!BACKWARD) load_bias(first);
 
-    wait_and_meet();
+    meet();
     send(lds[1]);
     constexpr int kReads = (SPLIT ? 2 : 1) * (FM + FN), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
     for (int tile = first; tile < last; ++tile) {
@@ -178,9 +188,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                 interleave<kReads, kMfmas>();
                 __builtin_amdgcn_sched_barrier(0);
             });
-            wait_and_meet();
+            meet();
             send(now);
-            if (s + 1 < steps) turn[0].template load<0>(next, wm, wn);
+            turn[0].template load<0>(next, wm, wn);         // of a tile's last step: not used
             turn[(kTurns - 1) & 1].multiply(acc);
             interleave<kReads, kMfmas>();
             __builtin_amdgcn_sched_barrier(0);
