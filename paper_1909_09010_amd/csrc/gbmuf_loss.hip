@@ -48,7 +48,10 @@ struct Pieces {
 Pieces pieces_of(int64_t G, int64_t V, int64_t bytes, int64_t most)
 {
     const int64_t worker = std::max<int64_t>(V * bytes, 1);
-    if (worker <= most) return Pieces{std::max<int64_t>(std::min(G, most / worker), 1), std::max<int64_t>(V, 1)};
+    if (worker <= most) {
+        const int64_t n = std::max<int64_t>(std::min(G, most / worker), 1), parts = (std::max<int64_t>(G, 1) + n - 1) / n;
+        return Pieces{(std::max<int64_t>(G, 1) + parts - 1) / parts, std::max<int64_t>(V, 1)};           // as many workers in each
+    }
     const int64_t n = (worker + most - 1) / most, words = ((V + n - 1) / n + 255) / 256 * 256;
     return Pieces{1, std::min(words, V)};
 }
@@ -181,6 +184,7 @@ Cut logits_shape(int64_t M, int64_t N, int64_t K, int64_t batch, bool split_type
     const int64_t steps = std::max<int64_t>(packed_words(K, split_type) / kStepWords, 1);
     Cut best;
     for (const int tile : {256, 128}) {
+        if (split_type && tile == 256) continue;
         const bool wide = tile == 256;
         const int64_t rows = (M + tile - 1) / tile * batch, words = (N + tile - 1) / tile, slots = wide ? 256 : 512;
         const double each = static_cast<double>(steps) * (wide ? 1.73 : 1.06) + (wide ? 4.0 : 2.5) * (backward ? 2.0 : 1.0);

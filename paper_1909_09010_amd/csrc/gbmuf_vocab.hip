@@ -15,13 +15,18 @@ __device__ __forceinline__ int scratch_at(int r, int c) { return r * 32 + (((c >
 
 // wait_and_meet, with the wait where the compiler sees it: what was read of LDS before is at hand then, and is not waited for once more together with what
 // is read next.
+template <bool MEMORY>
 __device__ __forceinline__ void meet()
 {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt(MEMORY ? 0x0070 : 0xc07f);  // vmcnt(0) lgkmcnt(0), or the latter alone
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+// Keeps what two branches end with from becoming one, with everything that either computes done for both.
+template <int N>
+__device__ __forceinline__ void apart() { asm volatile("; %0" ::"n"(N)); }
 
 // Sends R rows of one step to LDS as Stage does.  Where the rows are is worked out for every step from one address a lane: Stage's addresses, kept over a
 // tile's steps, would go to memory and back (f32 by tiles of 256 8 x 700 x 10000 x 650: 436 us, where these take 3TODO).
@@ -91,7 +96,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
     const Share share = share_of<TM, TN>(a.t, static_cast<int>(blockIdx.x), 0);
     const int64_t g = share.at.g;
     const int M = a.t.M, N = a.t.N, m0 = share.at.tm * TM, tiles = (N + TN - 1) / TN, first = share.at.tn * l.walk, last = min(first + l.walk, tiles);
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6, wm = (wave % WM) * (TM / WM), wn = (wave / WM) * kColumns;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave % WM) * (TM / WM), wn = (wave / WM) * kColumns;
     const Words &w = l.words;
     float *scratch = scratches[wave];
 
@@ -166,11 +171,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
     };
     if (!BACKWARD) load_bias(first);
 
-    meet();
+    meet<true>();
     send(lds[1]);
     constexpr int kReads = (SPLIT ? 2 : 1) * (FM + FN), kMfmas = (SPLIT ? 3 : 1) * FM * FN;
     for (int tile = first; tile < last; ++tile) {
         v16f acc[FM][FN];
+        int begin = 0, entries = 0;                         // of the list of the wave's rows and columns
+        if constexpr (LISTS)
+            if (m0 + wm < M && tile * TN + wn < N) {
+                const int32_t *starts = l.lists.starts + (g * l.lists.blocks + (m0 + wm) / (TM / WM)) * (l.lists.windows + 1) + ((l.first + tile * TN + wn) >> l.lists.shift);
+                begin = starts[0];
+                entries = starts[1] - begin;
+            }
         if (BACKWARD) load_bias(tile);                      // the registers that hold it while a tile is left are not to be had
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -188,7 +200,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                 interleave<kReads, kMfmas>();
                 __builtin_amdgcn_sched_barrier(0);
             });
-            meet();
+            // the stores of the tile before are not waited for here: what this step's waves read next arrived before they were sent
+            if (BACKWARD && s == 0 && tile > first) meet<false>();
+            else meet<true>();
             send(now);
             turn[0].template load<0>(next, wm, wn);         // of a tile's last step: not used
             turn[(kTurns - 1) & 1].multiply(acc);
@@ -205,21 +219,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
         const bool whole = n_wave + kColumns <= N;
         const int left = N - n_wave - half * 4;             // columns from the lane's first on
         // words of the wave's rows among its columns, 64 of them at hand
-        int entries = 0, entry_word = kNoWord, entry_row = 0;
+        int entry_word = kNoWord, entry_row = 0;
         float entry_share = 0.0f;
         const int32_t *list_word = nullptr, *list_row = nullptr;
         const float *list_share = nullptr;
         if constexpr (LISTS) {
-            const int64_t block = g * l.lists.blocks + (m0 + wm) / (TM / WM);
-            if (m0 + wm < M && n_wave < N) {
-                const int32_t *starts = l.lists.starts + block * (l.lists.windows + 1) + (lo >> l.lists.shift);
-                const int begin = starts[0];
-                entries = starts[1] - begin;
-                const int64_t at = block * (TM / WM) * w.top + begin;
-                list_word = l.lists.word + at;
-                list_row = l.lists.row + at;
-                list_share = l.lists.share + at;
-            }
+            const int64_t at = (g * l.lists.blocks + (m0 + wm) / (TM / WM)) * (TM / WM) * w.top + begin;
+            list_word = l.lists.word + at;
+            list_row = l.lists.row + at;
+            list_share = l.lists.share + at;
             if (lane < entries) {
                 entry_word = list_word[lane];
                 entry_row = list_row[lane];
@@ -270,10 +278,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                     for (int r = 0; r < 16; ++r) acc[i][j][r] = ldexpf(acc[i][j][r], em[i] + row_exponent(e[r >> 2][r & 3])) + b[r >> 2][r & 3];
             }
         }
+        static_assert(!BACKWARD || kColumns == 64, "a lane has a column of the sums");
         v4f total[BACKWARD ? FN : 1][2];
+        Eight z[2];                                         // of rows `from` and 16 on, columns eight .. of a fragment: 4 lanes a row
+        const int from = lane >> 2, eight = (lane & 3) * 8;
         if constexpr (BACKWARD)
 #pragma unroll
             for (int j = 0; j < FN; ++j) total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        const auto store = [&](int i, int j) {
+            const int n = n_wave + j * 32 + eight;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int row = m0 + wm + i * 32 + k * 16 + from;
+                total[j][0] += z[k].v[0];
+                total[j][1] += z[k].v[1];
+                if (row < M && n < l.dz_ld) write8<SPLIT ? kF32 : T>(l.dz, g * l.dz_batch + row * l.dz_ld + n, z[k]);
+            }
+        };
 
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
@@ -302,11 +323,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sum[r & 3] += exp2_of(fmaf(acc[i][j][r], scale, -from));
+                    apart<0>();
                 } else {
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) sum[r & 3] += exp2_of(near ? fmaf(acc[i][j][r], scale, -from) : (acc[i][j][r] - from) * scale);
+                    apart<1>();
                 }
                 sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 if (near) sum[0] *= exp2_of(-fmaf(most, scale, -from));
@@ -335,6 +358,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][j][r] = p_weight[i] * exp2_of(fmaf(acc[i][j][r], scale, -lse[i]));
+                    apart<0>();
                 } else {
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
@@ -343,10 +367,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                             const float z = acc[i][j][r];
                             acc[i][j][r] = p_weight[i] * exp2_of(near[i] ? fmaf(z, scale, -lse[i]) : fmaf(z, l.inv_tau, -lse[i]) * kLog2E);
                         }
+                    apart<1>();
                 }
                 const float of_row = LISTS ? __shfl(weight[i], (entry_row >> 16) & 31) : weight[i];
-                // 32 rows of 32 columns at a time: 4 lanes a row
-                const int from = lane >> 2, eight = (lane & 3) * 8;
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     in_order();
@@ -363,32 +386,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                         if (column >> 5 == j && half == 0) scratch[scratch_at(lane, column & 31)] -= of_row;
                         in_order();
                     }
-                    const int n = n_wave + j * 32 + eight;
+                    // what was read of the columns before leaves while these come back
+                    if (i + j == 0) __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): the next tile's first two steps are here
+                    else store(j == 0 ? i - 1 : i, j == 0 ? FN - 1 : j - 1);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int r = k * 16 + from;
-                        const Eight z{{*reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight)), *reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight + 4))}};
-                        total[j][0] += z.v[0];
-                        total[j][1] += z.v[1];
-                        if (row0 + r < M && n < l.dz_ld) write8<SPLIT ? kF32 : T>(l.dz, g * l.dz_batch + (row0 + r) * l.dz_ld + n, z);
+                        z[k] = Eight{{*reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight)), *reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight + 4))}};
                     }
                 }
             }
         }
         if constexpr (BACKWARD) {
+            store(FM - 1, FN - 1);
             if (!l.col_sums) continue;
-            float *to = l.col_sums + ((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N;
+            in_order();
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int n = n_wave + j * 32 + (lane & 3) * 8;
+            for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    float v = total[j][c >> 2][c & 3];
+                for (int c = 0; c < 2; ++c) *reinterpret_cast<v4f *>(scratch + from * kColumns + j * 32 + eight + c * 4) = total[j][c];
+            in_order();
+            float v = scratch[lane];
 #pragma unroll
-                    for (int d = 4; d < 64; d *= 2) v += __shfl_xor(v, d);
-                    if (lane < 4 && n + c < N) to[n + c] = v;
-                }
-            }
+            for (int k = 1; k < 16; ++k) v += scratch[k * kColumns + lane];
+            in_order();
+            if (n_wave + lane < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n_wave + lane] = v;
         }
     }
     if constexpr (!BACKWARD) {
@@ -420,12 +442,13 @@ int launch_vocab(const ProductArgs &a, const LossArgs &l, int32_t type, int tile
     LossArgs loss = l;
     void *argv[] = {&args, &loss};
     using Fn = void (*)(ProductArgs, LossArgs);
-#define GBMUF_VOCAB(T, SPLIT, BACKWARD)                                                                                                       \
-    {{vocab_kernel<T, SPLIT, 128, 128, 2, 2, BACKWARD, false>, vocab_kernel<T, SPLIT, 128, 128, 2, 2, BACKWARD, true>},                        \
-     {vocab_kernel<T, SPLIT, 256, 256, 2, 4, BACKWARD, false>, vocab_kernel<T, SPLIT, 256, 256, 2, 4, BACKWARD, true>}}
-    static constexpr Fn fns[3][2][2][2] = {{GBMUF_VOCAB(kF16, true, false), GBMUF_VOCAB(kF16, true, true)},
-                                           {GBMUF_VOCAB(kBf16, false, false), GBMUF_VOCAB(kBf16, false, true)},
-                                           {GBMUF_VOCAB(kF16, false, false), GBMUF_VOCAB(kF16, false, true)}};
+#define GBMUF_VOCAB(T, SPLIT, TILE, WN, BACKWARD) \
+    {vocab_kernel<T, SPLIT, TILE, TILE, 2, WN, BACKWARD, false>, vocab_kernel<T, SPLIT, TILE, TILE, 2, WN, BACKWARD, true>}
+    // [type][backward][tile][lists]
+    static constexpr Fn fns[3][2][2][2] = {
+        {{GBMUF_VOCAB(kF16, true, 128, 2, false), {}}, {GBMUF_VOCAB(kF16, true, 128, 2, true), {}}},
+        {{GBMUF_VOCAB(kBf16, false, 128, 2, false), GBMUF_VOCAB(kBf16, false, 256, 4, false)}, {GBMUF_VOCAB(kBf16, false, 128, 2, true), GBMUF_VOCAB(kBf16, false, 256, 4, true)}},
+        {{GBMUF_VOCAB(kF16, false, 128, 2, false), GBMUF_VOCAB(kF16, false, 256, 4, false)}, {GBMUF_VOCAB(kF16, false, 128, 2, true), GBMUF_VOCAB(kF16, false, 256, 4, true)}}};
 #undef GBMUF_VOCAB
     const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][tile == 256 ? 1 : 0][l.lists.word ? 1 : 0]),
                                            dim3(static_cast<unsigned>(a.t.blocks())), dim3(tile == 256 ? 512 : 256), argv, 0, stream);
