@@ -127,14 +127,15 @@ struct Words {
 };
 
 // The words of lists by where they meet a tile of logits: for every block of block_rows rows the words of each window of 64 << shift, one behind the
-// other, as (word, row of the block << 16 | place in the row's list, share); a word that a row has more than once is there once, with all its shares.
+// other, as codes: 15 bits of place in the window, 7 of row in the block, 10 of place in the row's list; a word that a row has more than once is there once.
 // starts: [g][block][windows + 1].
 struct WordLists {
-    int32_t *word, *row, *starts;
+    uint32_t *code;
+    int32_t *starts;
     float *share;            // nullptr: not wanted
     int32_t blocks, block_rows, windows, shift;          // shift: log2 of a window
 };
-constexpr int kMostWindows = 8192;
+constexpr int kMostWindows = 8192;         // of at most 2^15 words: 2^28, more than calls may have
 
 // What is done with logits z = s + bias of the words `first` .. of the vocabulary.
 struct LossArgs {
@@ -144,7 +145,7 @@ struct LossArgs {
     int32_t type;
     int32_t first;
     float inv_tau, tau;
-    WordLists lists;         // of tiles of many rows; word nullptr: rows have one word each
+    WordLists lists;         // of tiles of many rows; code nullptr: rows have one word each
     int32_t walk, reserved1; // tiles of logits that a workgroup takes one after the other
     // forward: parts[g][part][row], counted over the vocabulary from first_tile on, and z of the rows' words, at[g][row][top]
     float2 *parts;
@@ -169,7 +170,8 @@ struct TeacherArgs {
     int32_t *out_id, *out_state;
     float *out_share;
     int32_t rows, batch, top, vocab;
-    float inv_tau, reserved;
+    float inv_tau;
+    int32_t merge;           // a word that a row has more than once has all of its shares at the first place
 };
 
 // Losses from their parts.

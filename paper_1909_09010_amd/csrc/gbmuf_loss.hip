@@ -122,7 +122,7 @@ Words words_from(const Words &w, int64_t g)
     return p;
 }
 
-int order_words(const Loss &l, const Words &w, const Inputs &in, hipStream_t stream)
+int order_words(const Loss &l, const Words &w, const Inputs &in, bool merge, hipStream_t stream)
 {
     if (l.top == 0) return GBMUF_OK;
     TeacherArgs a{};
@@ -131,6 +131,7 @@ int order_words(const Loss &l, const Words &w, const Inputs &in, hipStream_t str
     a.out_id = const_cast<int32_t *>(w.id); a.out_share = const_cast<float *>(w.share); a.out_state = const_cast<int32_t *>(w.state);
     a.rows = w.rows; a.batch = l.linear.batch; a.top = w.top; a.vocab = w.vocab;
     a.inv_tau = 1.0f / l.tau;
+    a.merge = merge ? 1 : 0;
     return launch_teacher(a, stream);
 }
 
@@ -145,8 +146,7 @@ WordLists lists_of(const Loss &l, const Words &w, int tile, bool shares, Space &
     while ((static_cast<int64_t>(w.vocab) >> lists.shift) >= kMostWindows) ++lists.shift;
     lists.windows = (w.vocab >> lists.shift) + 1;
     const int64_t blocks = static_cast<int64_t>(l.linear.batch) * lists.blocks, n = blocks * lists.block_rows * w.top;
-    lists.word = space.take<int32_t>(n);
-    lists.row = space.take<int32_t>(n);
+    lists.code = space.take<uint32_t>(n);
     lists.share = space.take<float>(shares ? n : 0);
     if (!shares) lists.share = nullptr;
     lists.starts = space.take<int32_t>(blocks * (lists.windows + 1));
@@ -156,10 +156,9 @@ WordLists lists_of(const Loss &l, const Words &w, int tile, bool shares, Space &
 WordLists lists_from(const WordLists &lists, const Words &w, int64_t g)
 {
     WordLists p = lists;
-    if (!p.word) return p;
+    if (p.blocks == 0) return p;
     const int64_t n = g * p.blocks * p.block_rows * w.top;
-    p.word += n;
-    p.row += n;
+    p.code += n;
     if (p.share) p.share += n;
     p.starts += g * p.blocks * (p.windows + 1);
     return p;
@@ -291,7 +290,7 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
             LossArgs a = loss_args(l, at, words, Piece{0, G, 0, N});
             a.parts = parts; a.part_tiles = j.tiles;
             a.at = word_logits;
-            if ((rc = order_words(l, words, at, stream)) != GBMUF_OK) return rc;
+            if ((rc = order_words(l, words, at, false, stream)) != GBMUF_OK) return rc;
             rc = is_few ? launch_loss_few(f, a, type, stream) : launch_loss_direct(f, a, type, false, stream);
             return rc == GBMUF_OK ? launch_loss_join(j, stream) : rc;
         }
@@ -309,8 +308,8 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
     if (lay_w) w = packed(space, pieces.words, K, static_cast<int32_t>(pieces.workers), static_cast<int32_t>(pieces.workers), split,
                           space.take<uint32_t>(split ? pieces.workers * pieces.words + 256 : 0));
     if (!in) return GBMUF_OK;
-    if ((rc = order_words(l, words, at, stream)) != GBMUF_OK) return rc;
-    if (lists.word && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK) return rc;
+    if ((rc = order_words(l, words, at, false, stream)) != GBMUF_OK) return rc;
+    if (lists.blocks > 0 && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK) return rc;
     if (lay_x && (rc = lay_rows(lx, x, K, type, stream)) != GBMUF_OK) return rc;
     rc = each_piece(pieces, G, N, [&](const Piece &p) {
         Operand px = x, pw = w;
@@ -378,7 +377,7 @@ int backward_direct(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t 
     const Cut cx = chain_cut(M, dx ? K : 0, N, G, both);
     float *partial = space.take<float>(cx.partial);
     if (!io) return GBMUF_OK;
-    int rc = order_words(l, words, at, stream);
+    int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK) return rc;
     LossArgs a = grad_args(l, at, io, words, Piece{0, G, 0, N});
     a.dz = dz; a.dz_ld = ld; a.dz_batch = M * ld; a.dz_type = kF32;
@@ -450,8 +449,8 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     }
     if (!io) return GBMUF_OK;
 
-    int rc = order_words(l, words, at, stream);
-    if (rc != GBMUF_OK || (lists.word && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK)) return rc;
+    int rc = order_words(l, words, at, true, stream);
+    if (rc != GBMUF_OK || (lists.blocks > 0 && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK)) return rc;
     KeepArgs keep{};
     keep.words = words;
     keep.x = at.x.data; keep.ld = at.x.ld; keep.batch_stride = at.x.batch_stride;

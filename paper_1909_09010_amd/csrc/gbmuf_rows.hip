@@ -77,30 +77,110 @@ __global__ __launch_bounds__(256) void teacher_kernel(TeacherArgs a, int32_t pad
     for (int p = lane; p < a.top; p += 64) {
         const uint64_t k = key[p];
         const int32_t word = static_cast<int32_t>(k >> 32);
+        const auto share_of = [&](uint64_t x) { return expf((logit[static_cast<uint32_t>(x)] - from) * a.inv_tau) / total; };
+        float share = word == kNoWord ? 0.0f : share_of(k);
+        if (a.merge && word != kNoWord) {
+            if (p > 0 && static_cast<int32_t>(key[p - 1] >> 32) == word) share = 0.0f;
+            else
+                for (int q = p + 1; q < a.top && static_cast<int32_t>(key[q] >> 32) == word; ++q) share += share_of(key[q]);
+        }
         a.out_id[row * a.top + p] = word;
-        a.out_share[row * a.top + p] = word == kNoWord ? 0.0f : expf((logit[static_cast<uint32_t>(k)] - from) * a.inv_tau) / total;
+        a.out_share[row * a.top + p] = share;
     }
     if (lane == 0) a.out_state[row] = state;
+}
+
+// The value of the lane whose number differs in bit D: by the vector unit's own lane exchanges up to 8, which LDS's take four times as long for.
+template <int D>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v)
+{
+    const int x = static_cast<int>(v);
+    if constexpr (D == 1) return __builtin_amdgcn_update_dpp(x, x, 0xb1, 0xf, 0xf, false);             // quad_perm 1 0 3 2
+    if constexpr (D == 2) return __builtin_amdgcn_update_dpp(x, x, 0x4e, 0xf, 0xf, false);             // quad_perm 2 3 0 1
+    // row_shl 4 for the lanes without the bit, row_shr 4 for those with it
+    if constexpr (D == 4) return __builtin_amdgcn_update_dpp(__builtin_amdgcn_update_dpp(x, x, 0x104, 0xf, 0x5, false), x, 0x114, 0xf, 0xa, false);
+    if constexpr (D == 8) return __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false);            // row_ror 8
+    return __shfl_xor(x, D);
+}
+
+template <int SIZE, int D>
+__device__ __forceinline__ void sort_step(uint32_t &key, int lane)
+{
+    const uint32_t other = lane_xor<D>(key), less = min(key, other), more = max(key, other);
+    key = ((lane & D) == 0) == ((lane & SIZE) == 0) ? less : more;
+    if constexpr (D > 1) sort_step<SIZE, D / 2>(key, lane);
+}
+
+// The same for up to 64 words of a vocabulary below 2^25: a lane has one, and the key is the word and the lane, in 32 bits.
+constexpr int kShortTop = 64, kShortVocab = 1 << 25;
+__global__ __launch_bounds__(256) void short_teacher_kernel(TeacherArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= static_cast<int64_t>(a.rows) * a.batch) return;
+    const int64_t g = row / a.rows, i = row - g * a.rows;
+    const float inf = __builtin_inff();
+    int64_t v = -1;
+    float logit = -inf;
+    if (lane < a.top) {
+        v = a.id[g * a.id_batch + i * a.id_ld + lane];
+        logit = a.logit[g * a.logit_batch + i * a.logit_ld + lane];
+    }
+    const bool there = v >= 0 && logit != -inf;
+    const bool any = __any(there), bad = __any(there && v >= a.vocab);
+    uint32_t key = (!there ? 0xffffffc0u : static_cast<uint32_t>(v < a.vocab ? v : a.vocab) << 6) | static_cast<uint32_t>(lane);
+    const float most = max_of<64>(there ? logit : -inf), from = most == -inf ? 0.0f : most;
+    float share = there ? expf((logit - from) * a.inv_tau) : 0.0f;
+    share /= sum_of<64>(share);
+    if (!there) share = 0.0f;
+    sort_step<2, 1>(key, lane);
+    sort_step<4, 2>(key, lane);
+    sort_step<8, 4>(key, lane);
+    sort_step<16, 8>(key, lane);
+    sort_step<32, 16>(key, lane);
+    sort_step<64, 32>(key, lane);
+    share = __shfl(share, static_cast<int>(key & 63));
+    const int word = key >= 0xffffffc0u ? kNoWord : static_cast<int>(key >> 6);
+    if (a.merge) {
+        const int before = __shfl_up(word, 1);
+        const bool again = lane > 0 && word != kNoWord && before == word;
+        if (__any(again)) {
+            float all = share;
+            for (int d = 1; d < 64; ++d) {
+                const int w = __shfl_down(word, d);
+                const float s = __shfl_down(share, d);
+                if (lane + d < 64 && w == word) all += s;
+            }
+            share = again ? 0.0f : all;
+        }
+        if (word == kNoWord) share = 0.0f;
+    }
+    if (lane < a.top) {
+        a.out_id[row * a.top + lane] = word;
+        a.out_share[row * a.top + lane] = share;
+    }
+    if (lane == 0) a.out_state[row] = bad ? kBad : any ? kLive : kDead;
 }
 
 // ---------------------------------------------------------------------------------------
 // Lists of words by window: a workgroup takes the lists of a block of rows, counts the words of each window, and puts them there.  Within a window they lie in no
 // certain order, which no result depends on: no two are the same word of the same row.
 // ---------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void word_lists_kernel(Words w, WordLists l)
+constexpr int kListThreads = 1024;           // 8 x 5120 rows of 64 words: TODO us, 256 threads 46
+__global__ __launch_bounds__(kListThreads) void word_lists_kernel(Words w, WordLists l)
 {
     __shared__ int32_t count[kMostWindows];
-    __shared__ int32_t sums[4];
+    __shared__ int32_t sums[kListThreads / 64];
     const int64_t g = blockIdx.x / l.blocks;
     const int block = static_cast<int>(blockIdx.x % l.blocks), m0 = block * l.block_rows, rows = min(l.block_rows, w.rows - m0), n = rows * w.top;
     const int64_t first = (g * w.rows + m0) * w.top, out = static_cast<int64_t>(blockIdx.x) * l.block_rows * w.top;
     const int32_t *id = w.id + first;
     const float *share = w.share + first;
     int32_t *starts = l.starts + static_cast<int64_t>(blockIdx.x) * (l.windows + 1);
-    for (int i = threadIdx.x; i < l.windows; i += 256) count[i] = 0;
+    for (int i = threadIdx.x; i < l.windows; i += kListThreads) count[i] = 0;
     __syncthreads();
     const auto each = [&](auto f) {
-        for (int e = threadIdx.x; e < n; e += 256) {
+        for (int e = threadIdx.x; e < n; e += kListThreads) {
             const int word = id[e], p = e % w.top;
             if (word < w.vocab && (p == 0 || id[e - 1] != word)) f(word, e, p);
         }
@@ -108,7 +188,7 @@ __global__ __launch_bounds__(256) void word_lists_kernel(Words w, WordLists l)
     each([&](int word, int, int) { atomicAdd(&count[word >> l.shift], 1); });
     __syncthreads();
     // where each window begins: a thread's windows lie side by side
-    const int per = (l.windows + 255) / 256, from = threadIdx.x * per, to = min(from + per, l.windows);
+    const int per = (l.windows + kListThreads - 1) / kListThreads, from = threadIdx.x * per, to = min(from + per, l.windows);
     int mine = 0;
     for (int i = from; i < to; ++i) mine += count[i];
     int before = mine;
@@ -127,16 +207,12 @@ __global__ __launch_bounds__(256) void word_lists_kernel(Words w, WordLists l)
         count[i] = at;
         at += c;
     }
-    if (threadIdx.x == 255) starts[l.windows] = before;
+    if (threadIdx.x == kListThreads - 1) starts[l.windows] = before;
     __syncthreads();
     each([&](int word, int e, int p) {
         const int place = atomicAdd(&count[word >> l.shift], 1);
-        l.word[out + place] = word;
-        l.row[out + place] = ((e / w.top) << 16) | p;
-        if (!l.share) return;
-        float s = share[e];
-        for (int q = 1; p + q < w.top && id[e + q] == word; ++q) s += share[e + q];
-        l.share[out + place] = s;
+        l.code[out + place] = static_cast<uint32_t>(word & ((1 << l.shift) - 1)) << 17 | static_cast<uint32_t>(e / w.top) << 10 | static_cast<uint32_t>(p);
+        if (l.share) l.share[out + place] = share[e];
     });
 }
 
@@ -270,8 +346,8 @@ int launch_teacher(const TeacherArgs &a, hipStream_t stream)
     int32_t padded = 1;
     while (padded < a.top) padded *= 2;
     void *argv[] = {&args, &padded};
-    const auto fn = padded <= 128 ? teacher_kernel<128> : teacher_kernel<kMostTop>;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    const void *fn = a.top <= kShortTop && a.vocab < kShortVocab ? reinterpret_cast<const void *>(short_teacher_kernel) : reinterpret_cast<const void *>(padded <= 128 ? teacher_kernel<128> : teacher_kernel<kMostTop>);
+    const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(teacher)", err, GBMUF_EDEVICE);
 }
 
@@ -279,11 +355,11 @@ int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStre
 {
     const int64_t blocks = static_cast<int64_t>(l.blocks) * batch;
     if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
+    if (blocks > 0x7fffffffLL / kListThreads) return GBMUF_EUNSUPPORTED;
     Words words = w;
     WordLists lists = l;
     void *argv[] = {&words, &lists};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(word_lists_kernel), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(word_lists_kernel), dim3(static_cast<unsigned>(blocks)), dim3(kListThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(lists of words)", err, GBMUF_EDEVICE);
 }
 

@@ -219,28 +219,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
         const bool whole = n_wave + kColumns <= N;
         const int left = N - n_wave - half * 4;             // columns from the lane's first on
         // words of the wave's rows among its columns, 64 of them at hand
-        int entry_word = kNoWord, entry_row = 0;
+        // 64 codes at hand; a code's column among the wave's, its row among a fragment's
+        const bool holds = lane < entries;
+        uint32_t entry = 0;
         float entry_share = 0.0f;
-        const int32_t *list_word = nullptr, *list_row = nullptr;
-        const float *list_share = nullptr;
+        const uint32_t *codes = nullptr;
+        const float *shares = nullptr;
+        const int window = lo & ((1 << l.lists.shift) - 1);            // where the wave's columns begin in theirs
         if constexpr (LISTS) {
             const int64_t at = (g * l.lists.blocks + (m0 + wm) / (TM / WM)) * (TM / WM) * w.top + begin;
-            list_word = l.lists.word + at;
-            list_row = l.lists.row + at;
-            list_share = l.lists.share + at;
-            if (lane < entries) {
-                entry_word = list_word[lane];
-                entry_row = list_row[lane];
-                if (BACKWARD) entry_share = list_share[lane];
+            codes = l.lists.code + at;
+            shares = l.lists.share + at;
+            if (holds) {
+                entry = codes[lane];
+                if (BACKWARD) entry_share = shares[lane];
             }
         }
-        // f(word, row and slot, share) for the words in columns j of rows i
+        const auto column_of = [&](uint32_t code) { return static_cast<int>(code >> 17) - window; };
+        const auto row_in = [&](uint32_t code) { return static_cast<int>(code >> 10) & 31; };
+        const auto in_rows = [&](uint32_t code, int i) { return (static_cast<int>(code >> 15) & 3) == i; };
+        // f(code, share) for the words in columns j of rows i
         const auto each_entry = [&](int i, int j, auto f) {
-            const auto mine = [&](int word, int row) { return word >= lo && word < hi && ((word - lo) >> 5) == j && (row >> 21) == i; };
-            if (mine(entry_word, entry_row)) f(entry_word, entry_row, entry_share);
+            if (holds && in_rows(entry, i) && column_of(entry) >> 5 == j) f(entry, entry_share);
             for (int e = 64 + lane; e < entries; e += 64) {
-                const int word = list_word[e], row = list_row[e];
-                if (mine(word, row)) f(word, row, BACKWARD ? list_share[e] : 0.0f);
+                const uint32_t code = codes[e];
+                if (in_rows(code, i) && column_of(code) >> 5 == j) f(code, BACKWARD ? shares[e] : 0.0f);
             }
         };
         const auto put = [&](const v16f &rows) {
@@ -337,13 +340,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     if constexpr (LISTS) {
-                        if (!__any(entry_word < hi && (entry_row >> 21) == i) && entries <= 64) continue;
+                        if (!__any(holds && in_rows(entry, i) && column_of(entry) >> 5 == j) && entries <= 64) continue;
                         in_order();
                         put(acc[i][j]);
                         in_order();
-                        each_entry(i, j, [&](int word, int row, float) {
-                            const int r = (row >> 16) & 31;
-                            l.at[(g * w.rows + row0 + r) * w.top + (row & 0xffff)] = scratch[scratch_at(r, (word - lo) & 31)];
+                        each_entry(i, j, [&](uint32_t code, float) {
+                            l.at[(g * w.rows + row0 + row_in(code)) * w.top + (code & 1023)] = scratch[scratch_at(row_in(code), column_of(code) & 31)];
                         });
                     } else if (__any(column >> 5 == j)) {
                         in_order();
@@ -369,17 +371,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                         }
                     apart<1>();
                 }
-                const float of_row = LISTS ? __shfl(weight[i], (entry_row >> 16) & 31) : weight[i];
+                const float of_row = LISTS ? __shfl(weight[i], row_in(entry)) : weight[i];
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     in_order();
                     put(acc[i][j]);
                     in_order();
                     if constexpr (LISTS) {
-                        each_entry(i, j, [&](int word, int row, float part) {
-                            const int r = (row >> 16) & 31;
-                            const float of = row == entry_row ? of_row : row_weight(l, g, row0 + r, row_state(w, g, row0 + r)) * (l.sigma ? l.sigma[g] : 1.0f);
-                            scratch[scratch_at(r, (word - lo) & 31)] -= of * part;
+                        each_entry(i, j, [&](uint32_t code, float part) {
+                            const int row = row0 + row_in(code);
+                            const float of = holds && code == entry ? of_row : row_weight(l, g, row, row_state(w, g, row)) * (l.sigma ? l.sigma[g] : 1.0f);
+                            scratch[scratch_at(row_in(code), column_of(code) & 31)] -= of * part;
                         });
                         in_order();
                     } else if (__any(column >> 5 == j)) {
@@ -450,7 +452,7 @@ int launch_vocab(const ProductArgs &a, const LossArgs &l, int32_t type, int tile
         {{GBMUF_VOCAB(kBf16, false, 128, 2, false), GBMUF_VOCAB(kBf16, false, 256, 4, false)}, {GBMUF_VOCAB(kBf16, false, 128, 2, true), GBMUF_VOCAB(kBf16, false, 256, 4, true)}},
         {{GBMUF_VOCAB(kF16, false, 128, 2, false), GBMUF_VOCAB(kF16, false, 256, 4, false)}, {GBMUF_VOCAB(kF16, false, 128, 2, true), GBMUF_VOCAB(kF16, false, 256, 4, true)}}};
 #undef GBMUF_VOCAB
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][tile == 256 ? 1 : 0][l.lists.word ? 1 : 0]),
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][tile == 256 ? 1 : 0][l.lists.blocks > 0 ? 1 : 0]),
                                            dim3(static_cast<unsigned>(a.t.blocks())), dim3(tile == 256 ? 512 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(logits)", err, GBMUF_EDEVICE);
 }
