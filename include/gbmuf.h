@@ -456,7 +456,7 @@ int gbmuf_linear_backward(const gbmuf_linear_desc_t *desc, const gbmuf_linear_gr
  * Losses over a vocabulary, for each of `batch` workers g, from the rows x that go into its output matrix: with the logits
  *     z[g,i,v] = sum_k x[g,i,k] w[g,v,k] + bias[g,v]          i < rows, v < vocab, k < in_features
  * a row i is held to a word (cross entropy) or to what a teacher says of some words (distillation).  The logits are formed tile by
- * tile and never kept; a call's workspace does not grow with rows * vocab beyond half a gigabyte of their gradient.
+ * tile and never kept; a call's workspace does not grow with rows * vocab beyond 1.5 GB (16-bit types 0.75) of their gradient.
  * Any of the sizes may be 0.  Zero the struct, set struct_size, fill in what is needed.
  */
 #define GBMUF_MAX_TOP 1024

@@ -159,6 +159,7 @@ struct LossArgs {
     int64_t dz_ld, dz_batch;
     int32_t dz_type, reserved;
     float *col_sums;         // [g][parts of 64 or 128 rows][column], or nullptr
+    uint32_t *col_max;       // f32, [g][column]: bits of the largest magnitude, zero before; or nullptr
     int32_t *live;           // out: [g][row], or nullptr
 };
 
@@ -198,6 +199,7 @@ struct KeepArgs {
     float tau;
     int32_t reserved1;
     float *sigma;            // [batch], and behind them 1 / sigma; or nullptr
+    uint32_t *row_max;       // [batch][rows]: bits of what no value of the row's dz exceeds; or nullptr
 };
 
 struct CastArgs {            // out = from, [batch][rows][columns]

@@ -339,7 +339,9 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
 // ---------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------
-constexpr int64_t kGradBytes = 512 << 20;          // of dz, and what is laid out of it, at a time
+// Bytes of dz, and what is laid out of it, at a time.  Fewer, larger launches: us by 256 / 512 / 768 / 1024 MB, bf16 8 x 5120 x 8197 x 512 (672 MB) 1532 / 1556 / 1421 /
+// 1412, 2 x 5120 x 50000 x 1024 (1 GB) 3384 / 3180 / 3166 / 3312; f32 by 512 / 1024 / 1536 MB 8 x 700 x 10000 x 650 (720 MB) 1365 / 1260 / 1216.
+constexpr int64_t kGradBytes = 768 << 20, kSplitGradBytes = 1536 << 20;
 
 // dw's epilogue, for the words of a piece
 Epilogue weight_grad(const Loss &l, const gbmuf_matrix_t &m, int64_t values, int32_t type)
@@ -412,7 +414,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
 
     // of a word: its dz (f32: and both layouts of it), w's row along k (f32) and, taken apart, along the words
     const int64_t word_bytes = split ? M * 12 + 128 + packed_words(K, true) * 2 + K * 4 : M * 2;
-    const Pieces pieces = pieces_of(G, N, word_bytes, kGradBytes);
+    const Pieces pieces = pieces_of(G, N, word_bytes, split ? kSplitGradBytes : kGradBytes);
     const int64_t PG = pieces.workers, PN = pieces.words, ld = (PN + 63) / 64 * 64;
     const bool copy_w = !split && (!io || !as_it_lies(at.w, K));
     const int64_t kept = packed_words(K, false);                 // columns of a row of x that is kept
@@ -429,21 +431,21 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     char *dz = space.take<char>(PG * M * ld * static_cast<int64_t>(type_bytes(type)));
     const bool several = PN < N;
     float *dx_sums = space.take<float>(several && !split ? PG * M * K : 0);
-    const int64_t sum_rows = (M + kLayTile - 1) / kLayTile;
     float *sums = space.take<float>(db ? PG * 2 * ((M + 127) / 128) * PN : 0);         // of 64 rows, or of half a tile
 
     Operand x{reinterpret_cast<const uint16_t *>(kept_x), kept, M * kept, nullptr, 0, true, false}, w = operand_of(at.w), z, zt, wt, xt;
-    uint32_t *max = nullptr;
+    uint32_t *max = nullptr, *dz_rows = nullptr, *w_rows = nullptr;
     if (split) {
-        max = space.take<uint32_t>(PG * (M + PN + K));          // rows and columns of dz, columns of w
+        max = space.take<uint32_t>(PG * (2 * PN + K) + 256);    // of a piece: columns of dz, rows of w, up to the end of the last tile, and columns of w
+        dz_rows = space.take<uint32_t>(G * M);
         uint32_t *x_max = space.take<uint32_t>(G * K);          // columns of x
+        const int32_t workers = static_cast<int32_t>(PG);
         x = packed(space, M, K, G, G, true, space.take<uint32_t>(G * M));
         xt = packed(space, K, M, G, G, true, x_max);
-        const int32_t workers = static_cast<int32_t>(PG);
-        w = packed(space, PN, K, workers, workers, true, space.take<uint32_t>(PG * PN + 256));
-        wt = packed(space, K, PN, workers, workers, true, max + PG * (M + PN));
-        z = packed(space, M, PN, workers, workers, true, max);
-        zt = packed(space, PN, M, workers, workers, true, max + PG * M);
+        w = packed(space, PN, K, workers, workers, true, nullptr);
+        wt = packed(space, K, PN, workers, workers, true, nullptr);
+        z = packed(space, M, PN, workers, workers, true, dz_rows);
+        zt = packed(space, PN, M, workers, workers, true, nullptr);
     } else if (copy_w) {
         w = packed(space, PN, K, static_cast<int32_t>(PG), static_cast<int32_t>(PG), false, nullptr);
     }
@@ -459,6 +461,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     keep.dloss = static_cast<const float *>(out.dloss.data); keep.dloss_ld = out.dloss.ld; keep.dloss_batch = out.dloss.batch_stride;
     keep.tau = l.tau;
     keep.sigma = type == kF16 ? sigma : nullptr;
+    keep.row_max = dz_rows;
     if ((rc = launch_keep(keep, stream)) != GBMUF_OK) return rc;
     const gbmuf_matrix_t kept_m{kept_x, kept, M * kept};
     if (split) {
@@ -481,10 +484,30 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         px.p += p.g * x.batch;
         if (px.max) px.max += p.g * x.max_batch;
         int r = GBMUF_OK;
-        if (split || copy_w) {
+        Operand pwt = wt;
+        if (split) {
+            // w along k, for the logits, and along the words, for dx, from one reading after its maxima are known
+            LayArgs lw = source(wm, p.words, K, workers, type);
+            const bool shared = lw.batch < workers;
+            uint32_t *columns = max + p.workers * p.words;
+            w_rows = columns + p.workers * K;
+            pw.batch = shared ? 0 : p.words * w.ld;
+            pw.max = lw.row_max = w_rows; pw.max_batch = shared ? 0 : p.words;
+            lw.plain = const_cast<uint16_t *>(pw.p); lw.plain_ld = pw.ld; lw.plain_batch = pw.batch;
+            if (dx) {
+                pwt.ld = packed_words(p.words, true);
+                pwt.batch = shared ? 0 : K * pwt.ld;
+                pwt.max = lw.col_max = columns; pwt.max_batch = shared ? 0 : K;
+                lw.trans = const_cast<uint16_t *>(pwt.p); lw.trans_ld = pwt.ld; lw.trans_batch = pwt.batch;
+            }
+            LaySet set;
+            set.add(lw);
+            if ((r = launch_zero(max, p.workers * (2 * p.words + K), stream)) != GBMUF_OK || (r = launch_stats(set, stream)) != GBMUF_OK ||
+                (r = launch_lay(set, stream)) != GBMUF_OK)
+                return r;
+        } else if (copy_w) {
             const LayArgs lw = source(wm, p.words, K, workers, type);
             pw.batch = lw.batch < workers ? 0 : p.words * w.ld;
-            pw.max_batch = lw.batch < workers ? 0 : p.words;
             if ((r = lay_rows(lw, pw, K, type, stream)) != GBMUF_OK) return r;
         } else pw = operand_of(wm);
 
@@ -494,7 +517,8 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         a.walk = c.t.steps;
         a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld; a.dz_type = type;
         if (type == kF16) a.sigma = sigma + p.g;
-        if (db && !split) a.col_sums = sums;
+        if (db) a.col_sums = sums;
+        if (split && dw) a.col_max = max;
         if ((r = launch_vocab(logits_args(px, pw, K, type, c), a, type, c.tile, true, stream)) != GBMUF_OK) return r;
 
         const gbmuf_matrix_t dzm{dz, pld, M * pld}, pdx = part(out.dx, p.g, 0, type), pdw = part(out.dw, p.g, p.v, grad_type),
@@ -502,39 +526,29 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         const float *factor = type == kF16 ? sigma + G + p.g : nullptr;
         SumArgs s{};
         s.sums = sums; s.out = pdb.data; s.out_batch = pdb.batch_stride;
-        s.C = static_cast<int32_t>(p.words); s.tiles = static_cast<int32_t>(split ? sum_rows : 2 * c.t.tiles_m);
+        s.C = static_cast<int32_t>(p.words); s.tiles = 2 * c.t.tiles_m;
         s.batch = workers; s.type = grad_type; s.accumulate = l.accumulate;
         s.factor = factor;
 
         Operand oz{reinterpret_cast<const uint16_t *>(dz), pld, M * pld, nullptr, 0, false, false}, ozt = oz, ow = pw, ox = px;
         if (split) {
-            const int64_t n_max = p.workers * (M + p.words + K);
-            oz = z; ozt = zt; ow = wt; ox = xt;
-            oz.ld = packed_words(p.words, true); oz.batch = M * oz.ld; oz.max = max; oz.max_batch = M;
-            ozt.batch = p.words * ozt.ld; ozt.max = max + p.workers * M; ozt.max_batch = p.words;
-            const LayArgs lw0 = source(wm, p.words, K, workers, kF32);
-            ow.ld = packed_words(p.words, true); ow.batch = lw0.batch < workers ? 0 : K * ow.ld; ow.max = max + p.workers * (M + p.words);
-            ow.max_batch = lw0.batch < workers ? 0 : K;
+            oz = z; ozt = zt; ow = pwt; ox = xt;
+            oz.ld = packed_words(p.words, true); oz.batch = M * oz.ld; oz.max = dz_rows + p.g * M; oz.max_batch = M;
+            ozt.batch = p.words * ozt.ld; ozt.max = max; ozt.max_batch = p.words;
             ox.p += p.g * xt.batch; ox.max += p.g * xt.max_batch;
-            if ((r = launch_zero(max, n_max, stream)) != GBMUF_OK) return r;
-            LayArgs lz = source(dzm, M, p.words, workers, kF32), lw = lw0;
+            LayArgs lz = source(dzm, M, p.words, workers, kF32);
             lz.batch = workers;
             if (dx) {
                 lz.row_max = oz.max;
                 lz.plain = const_cast<uint16_t *>(oz.p); lz.plain_ld = oz.ld; lz.plain_batch = oz.batch;
-                lw.col_max = ow.max;
-                lw.trans = const_cast<uint16_t *>(ow.p); lw.trans_ld = ow.ld; lw.trans_batch = ow.batch;
             }
             if (dw) {
                 lz.col_max = ozt.max;
                 lz.trans = const_cast<uint16_t *>(ozt.p); lz.trans_ld = ozt.ld; lz.trans_batch = ozt.batch;
             }
-            lz.col_sums = db ? sums : nullptr;
-            LaySet stats, lay;
-            stats.add(lz);
+            LaySet lay;
             if (dx || dw) lay.add(lz);
-            if (dx) { stats.add(lw); lay.add(lw); }
-            if ((r = launch_stats(stats, stream)) != GBMUF_OK || (r = launch_lay(lay, stream)) != GBMUF_OK) return r;
+            if ((r = launch_lay(lay, stream)) != GBMUF_OK) return r;
         } else {
             ozt.across = ow.across = ox.across = true;
         }

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
     if (first < full) {
         sa.load(lds[0], first * kStep);
         sb.load(lds[0] + TM * kStep, first * kStep);
-        wait_and_meet();
+        meet<true>();
         if (first + 1 < full) {
             sa.load(lds[1], (first + 1) * kStep);
             sb.load(lds[1] + TM * kStep, (first + 1) * kStep);
@@ -51,12 +51,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
                 interleave<kReads, kMfmas>();
                 __builtin_amdgcn_sched_barrier(0);
             });
-            wait_and_meet();
+            meet<true>();
             if (s + 2 < full) {
                 sa.load(now, (s + 2) * kStep);
                 sb.load(now + TM * kStep, (s + 2) * kStep);
             }
-            if (s + 1 < full) turn[0].template load<0>(next, wm, wn);
+            turn[0].template load<0>(next, wm, wn);         // of the last step: not used
             turn[(kTurns - 1) & 1].multiply(acc);
             interleave<kReads, kMfmas>();
             __builtin_amdgcn_sched_barrier(0);

@@ -295,8 +295,13 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
         if (row >= static_cast<int64_t>(a.words.rows) * a.batch) return;
         const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
         const int64_t g = row / a.words.rows, from = g * a.batch_stride + (row - g * a.words.rows) * a.ld + c;
+        const int m = static_cast<int>(row - g * a.words.rows), state = row_state(a.words, g, m);
+        if (a.row_max && c == 0) {
+            const float d = fabsf(a.dloss[g * a.dloss_batch + m * a.dloss_ld] * a.tau);
+            a.row_max[row] = state != kDead && d < __builtin_inff() ? __float_as_uint(d) : 0u;
+        }
         Eight v{};
-        if (row_state(a.words, g, static_cast<int>(row - g * a.words.rows)) != kDead) {
+        if (state != kDead) {
             if (left >= 8) v = read8<T>(a.x, from);
             else
 #pragma unroll

@@ -233,9 +233,13 @@ __device__ __forceinline__ void repeat(F f)
     }
 }
 
-__device__ __forceinline__ void wait_and_meet()
+// The waves meet, everything that they read of LDS at hand and (MEMORY) everything on its way to LDS there.  The wait is one that the compiler sees: it does
+// not wait for what was read before once more, together with what is read next.
+template <bool MEMORY>
+__device__ __forceinline__ void meet()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(MEMORY ? 0x0070 : 0xc07f);  // vmcnt(0) lgkmcnt(0), or the latter alone
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }

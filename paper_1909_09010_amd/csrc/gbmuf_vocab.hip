@@ -13,17 +13,6 @@ constexpr float kPlain = 65536.0f;       // up to here the rounding of what an e
 constexpr int kScratch = 32 * 32;
 __device__ __forceinline__ int scratch_at(int r, int c) { return r * 32 + (((c >> 2) ^ ((r >> 1) & 7)) << 2) + (c & 3); }
 
-// wait_and_meet, with the wait where the compiler sees it: what was read of LDS before is at hand then, and is not waited for once more together with what
-// is read next.
-template <bool MEMORY>
-__device__ __forceinline__ void meet()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(MEMORY ? 0x0070 : 0xc07f);  // vmcnt(0) lgkmcnt(0), or the latter alone
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // Keeps what two branches end with from becoming one, with everything that either computes done for both.
 template <int N>
 __device__ __forceinline__ void apart() { asm volatile("; %0" ::"n"(N)); }
@@ -282,12 +271,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
             }
         }
         static_assert(!BACKWARD || kColumns == 64, "a lane has a column of the sums");
-        v4f total[BACKWARD ? FN : 1][2];
+        v4f total[BACKWARD ? FN : 1][2], top[BACKWARD && SPLIT ? FN : 1][2];
         Eight z[2];                                         // of rows `from` and 16 on, columns eight .. of a fragment: 4 lanes a row
         const int from = lane >> 2, eight = (lane & 3) * 8;
         if constexpr (BACKWARD)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < FN; ++j) {
+                total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                if (SPLIT) top[j][0] = top[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
         const auto store = [&](int i, int j) {
             const int n = n_wave + j * 32 + eight;
 #pragma unroll
@@ -295,6 +287,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                 const int row = m0 + wm + i * 32 + k * 16 + from;
                 total[j][0] += z[k].v[0];
                 total[j][1] += z[k].v[1];
+                if constexpr (SPLIT)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) top[j][c >> 2][c & 3] = fmaxf(top[j][c >> 2][c & 3], fabsf(z[k].v[c >> 2][c & 3]));
                 if (row < M && n < l.dz_ld) write8<SPLIT ? kF32 : T>(l.dz, g * l.dz_batch + row * l.dz_ld + n, z[k]);
             }
         };
@@ -401,18 +396,29 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
         }
         if constexpr (BACKWARD) {
             store(FM - 1, FN - 1);
-            if (!l.col_sums) continue;
-            in_order();
+            // a lane's column of what 16 groups of lanes have of all columns
+            const auto gather = [&](const v4f (&part)[FN][2], auto join) {
+                in_order();
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
+                for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) *reinterpret_cast<v4f *>(scratch + from * kColumns + j * 32 + eight + c * 4) = total[j][c];
-            in_order();
-            float v = scratch[lane];
+                    for (int c = 0; c < 2; ++c) *reinterpret_cast<v4f *>(scratch + from * kColumns + j * 32 + eight + c * 4) = part[j][c];
+                in_order();
+                float v = scratch[lane];
 #pragma unroll
-            for (int k = 1; k < 16; ++k) v += scratch[k * kColumns + lane];
-            in_order();
-            if (n_wave + lane < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n_wave + lane] = v;
+                for (int k = 1; k < 16; ++k) v = join(v, scratch[k * kColumns + lane]);
+                in_order();
+                return v;
+            };
+            if (l.col_sums) {
+                const float v = gather(total, [](float x, float y) { return x + y; });
+                if (n_wave + lane < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n_wave + lane] = v;
+            }
+            if constexpr (SPLIT)
+                if (l.col_max) {
+                    const uint32_t v = __float_as_uint(gather(top, [](float x, float y) { return fmaxf(x, y); }));
+                    if (n_wave + lane < N && v) atomicMax(l.col_max + g * N + n_wave + lane, v);
+                }
         }
     }
     if constexpr (!BACKWARD) {

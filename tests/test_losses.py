@@ -255,7 +255,7 @@ def test_large(size, dtype, top):
 
 
 # more of the gradient than is held at a time: parts of a vocabulary, and some of the workers
-PIECES = [(1, 2600, 110003, 40), (3, 1500, 60001, 24)]
+PIECES = [(1, 2600, 160003, 40), (3, 2000, 120001, 24)]
 
 
 @gpu
@@ -765,10 +765,10 @@ def test_workspaces_of_any_sizes():
 
 
 def test_workspaces_stay_bounded():
-    """Of 5120 rows against 267,735 words the logits' gradient alone would be 2.7 GB in 16 bits."""
+    """Of 16 times 5120 rows against 267,735 words the logits' gradient alone would be 44 GB in 16 bits."""
     for dtype in DTYPES:
-        assert B.CrossEntropy(5120, 267735, 512, 1, dtype).workspace_bytes(True) < 0.8e9
-        assert B.CrossEntropy(5120, 267735, 512, 16, dtype).workspace_bytes(True) < 1.2e9
+        assert B.CrossEntropy(5120, 267735, 512, 1, dtype).workspace_bytes(True) < 1.8e9
+        assert B.CrossEntropy(5120, 267735, 512, 16, dtype).workspace_bytes(True) < 2.5e9
         assert B.CrossEntropy(5120, 267735, 512, 1, dtype).workspace_bytes() < 0.4e9
 
 
