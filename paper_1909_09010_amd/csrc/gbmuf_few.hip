@@ -155,8 +155,11 @@ __global__ __launch_bounds__(64 * WAVES) void loss_few_kernel(DirectArgs a, Loss
         };
         const int end = min(n + 4, a.t.N);
         if (w.target) {
-            const int64_t word = w.target[g * w.batch + m * w.ld];
-            if (word >= n && word < end) l.at[row] = logit(word);
+            const int64_t *words = w.target + g * w.batch + m * w.ld;
+            for (int j = 0; j < w.top; ++j) {
+                const int64_t word = words[j];
+                if (word >= n && word < end) l.at[row * w.top + j] = logit(word);
+            }
         } else {
             const int32_t *list = w.id + row * w.top;
             int place = 0, step = 1;

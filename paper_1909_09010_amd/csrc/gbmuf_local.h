@@ -113,7 +113,7 @@ struct SumArgs {             // out[g][c] (+)= sum over t of sums[g][t][c]
 };
 
 // The words that rows are held to.  target: one of them each, negative where a row does not count.  Else lists of `top`: words in ascending order, kNoWord
-// behind the last, and the share of each.
+// behind the last, and the share of each; or, of few rows and up to kFewWords, as the teacher gives them: target and logit.
 enum : int32_t { kDead = 0, kLive = 1, kBad = 2 };         // what a row counts; kBad: it names a word that the vocabulary does not have
 constexpr int32_t kNoWord = 0x7fffffff;
 struct Words {
@@ -122,9 +122,12 @@ struct Words {
     const int32_t *id;       // [g][row][top], and share
     const float *share;
     const int32_t *state;    // [g][row]
-    int32_t top;             // 1 where target is
+    const float *logit;
+    int64_t logit_ld, logit_batch;
+    int32_t top;             // 1 where there is one word a row
     int32_t rows, vocab;     // of a worker, whole
 };
+constexpr int kFewWords = 16;
 
 // The words of lists by where they meet a tile of logits: for every block of block_rows rows the words of each window of 64 << shift, one behind the
 // other, as codes: 15 bits of place in the window, 7 of row in the block, 10 of place in the row's list; a word that a row has more than once is there once.

@@ -90,8 +90,10 @@ gbmuf_matrix_t vector_part(const gbmuf_matrix_t &m, int64_t g, int64_t n, int32_
 // ---------------------------------------------------------------------------------------
 // Words
 // ---------------------------------------------------------------------------------------
-Words words_of(const Loss &l, const gbmuf_matrix_t &target, Space &space)
+// as_given: few rows' lists of few words need no order.
+Words words_of(const Loss &l, const Inputs &in, bool as_given, Space &space)
 {
+    const gbmuf_matrix_t &target = in.target;
     const int64_t G = l.linear.batch, M = l.linear.rows;
     Words w{};
     w.top = 1;
@@ -103,6 +105,13 @@ Words words_of(const Loss &l, const gbmuf_matrix_t &target, Space &space)
         return w;
     }
     w.top = l.top;
+    if (as_given) {
+        w.target = static_cast<const int64_t *>(target.data);
+        w.ld = target.ld; w.batch = target.batch_stride;
+        w.logit = static_cast<const float *>(in.teacher.data);
+        w.logit_ld = in.teacher.ld; w.logit_batch = in.teacher.batch_stride;
+        return w;
+    }
     w.id = space.take<int32_t>(G * M * l.top);
     w.share = space.take<float>(G * M * l.top);
     w.state = space.take<int32_t>(G * M);
@@ -124,7 +133,7 @@ Words words_from(const Words &w, int64_t g)
 
 int order_words(const Loss &l, const Words &w, const Inputs &in, bool merge, hipStream_t stream)
 {
-    if (l.top == 0) return GBMUF_OK;
+    if (l.top == 0 || w.logit) return GBMUF_OK;
     TeacherArgs a{};
     a.id = static_cast<const int64_t *>(in.target.data); a.id_ld = in.target.ld; a.id_batch = in.target.batch_stride;
     a.logit = static_cast<const float *>(in.teacher.data); a.logit_ld = in.teacher.ld; a.logit_batch = in.teacher.batch_stride;
@@ -257,11 +266,11 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
     const bool split = type == kF32;
     const Inputs none{};
     const Inputs &at = in ? *in : none;
-    const Words words = words_of(l, at.target, space);
-    float *word_logits = space.take<float>(G * M * words.top);
     const Few few = few_of(d);
     const bool is_few = few == Few::kAlways || (few == Few::kUnlessAligned && (!in || !(lies_well(at.x) && lies_well(at.w))));
     const bool direct = takes_direct_forward(d) || few == Few::kDirect;
+    const Words words = words_of(l, at, in && is_few && l.top <= kFewWords, space);
+    float *word_logits = space.take<float>(G * M * words.top);
 
     LossJoin j{};
     j.words = words;
@@ -371,7 +380,7 @@ int backward_direct(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t 
     const gbmuf_loss_grad_io_t no_grads{};
     const gbmuf_loss_grad_io_t &out = io ? *io : no_grads;
     const bool dx = !io || out.dx.data, dw = !io || out.dw.data;
-    const Words words = words_of(l, at.target, space);
+    const Words words = words_of(l, at, false, space);
     const int64_t ld = (N + 63) / 64 * 64;
     float *dz = space.take<float>(G * M * ld);
     int32_t *live = space.take<int32_t>(G * M);
@@ -410,7 +419,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     const gbmuf_loss_grad_io_t no_grads{};
     const gbmuf_loss_grad_io_t &out = io ? *io : no_grads;
     const bool dx = !io || out.dx.data, dw = !io || out.dw.data, db = !io || out.dbias.data;
-    const Words words = words_of(l, at.target, space);
+    const Words words = words_of(l, at, false, space);
 
     // of a word: its dz (f32: and both layouts of it), w's row along k (f32) and, taken apart, along the words
     const int64_t word_bytes = split ? M * 12 + 128 + packed_words(K, true) * 2 + K * 4 : M * 2;

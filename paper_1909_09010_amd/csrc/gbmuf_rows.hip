@@ -223,37 +223,44 @@ template <int ROWS>
 __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
 {
     constexpr int kThreads = 256 / ROWS;
-    __shared__ float2 shared[kThreads][ROWS];
-    __shared__ float sums[ROWS];
+    __shared__ float2 shared[4][ROWS];
     const Words &w = a.words;
     const int blocks = (w.rows + ROWS - 1) / ROWS, m0 = static_cast<int>(blockIdx.x % blocks) * ROWS;
     const int64_t g = blockIdx.x / blocks;
     const float inf = __builtin_inff(), scale = a.inv_tau * kLog2E;
     {
-        const int r = threadIdx.x % ROWS, first = threadIdx.x / ROWS, m = min(m0 + r, w.rows - 1);
+        const int r = threadIdx.x % ROWS, m = min(m0 + r, w.rows - 1);
         const float2 *from = a.parts + g * a.tiles * w.rows + m;
         float2 s = {-inf, 0.0f};
 #pragma unroll 4
-        for (int t = first; t < a.tiles; t += kThreads) s = join_stats(s, from[static_cast<int64_t>(t) * w.rows], scale);
-        shared[first][r] = s;
-        __syncthreads();
-        for (int n = kThreads / 2; n; n /= 2) {
-            if (first < n) shared[first][r] = join_stats(shared[first][r], shared[first + n][r], scale);
-            __syncthreads();
-        }
-        if (first == 0) {
-            const float2 s = shared[0][r];
-            sums[r] = (fabsf(s.x) < inf ? s.x * a.inv_tau : 0.0f) + logf(s.y);
-        }
+        for (int t = threadIdx.x / ROWS; t < a.tiles; t += kThreads) s = join_stats(s, from[static_cast<int64_t>(t) * w.rows], scale);
+#pragma unroll
+        for (int d = ROWS; d < 64; d *= 2) s = join_stats(s, float2{__shfl_xor(s.x, d), __shfl_xor(s.y, d)}, scale);
+        if (static_cast<int>(threadIdx.x & 63) < ROWS) shared[threadIdx.x >> 6][r] = s;
         __syncthreads();
     }
     const int r = threadIdx.x / kThreads, first = threadIdx.x % kThreads, m = m0 + r;
     const bool inside = m < w.rows;
-    const int state = inside ? row_state(w, g, m) : kDead;
-    const float lse = sums[r];
+    float2 stats = shared[0][r];
+#pragma unroll
+    for (int v = 1; v < 4; ++v) stats = join_stats(stats, shared[v][r], scale);
+    const float lse = (fabsf(stats.x) < inf ? stats.x * a.inv_tau : 0.0f) + logf(stats.y);
     const int64_t row = g * w.rows + m;
+    int state = inside && !w.logit ? row_state(w, g, m) : kDead;
     float loss = 0.0f;
-    if (w.target) loss = state == kLive ? lse - a.at[row] : 0.0f;
+    if (w.logit) {
+        // a few words as the teacher gives them: the first threads of the row have one each
+        const int j = min(first, w.top - 1);
+        const int64_t i = min(m, w.rows - 1), word = w.target[g * w.batch + i * w.ld + j];
+        const float logit = w.logit[g * w.logit_batch + i * w.logit_ld + j];
+        const bool there = inside && first < w.top && word >= 0 && logit != -inf;
+        constexpr int kLanes = kThreads < 64 ? kThreads : 64;
+        const float most = max_of<kLanes>(there ? logit : -inf), e = there ? expf((logit - (most == -inf ? 0.0f : most)) * a.inv_tau) : 0.0f;
+        const float share = e / sum_of<kLanes>(e);
+        state = static_cast<int>(max_of<kLanes>(static_cast<float>(!there ? kDead : word < w.vocab ? kLive : kBad)));
+        if (there && word < w.vocab && share != 0.0f) loss = share * (logf(share) - fmaf(a.at[row * w.top + j], a.inv_tau, -lse));
+        loss = sum_of<kLanes>(loss) * (a.tau * a.tau);
+    } else if (w.target) loss = state == kLive ? lse - a.at[row] : 0.0f;
     else {
         if (state == kLive)
             for (int j = first; j < w.top; j += kThreads) {
@@ -372,7 +379,8 @@ int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStre
 int launch_loss_join(const LossJoin &a, hipStream_t stream)
 {
     if (a.words.rows <= 0 || a.batch <= 0) return GBMUF_OK;
-    const int rows = a.words.rows <= 2 ? 1 : static_cast<int64_t>(a.words.rows) * a.batch <= 4096 ? 4 : 32;
+    const int64_t all = static_cast<int64_t>(a.words.rows) * a.batch;
+    const int rows = a.words.rows <= 2 || all <= 256 ? 1 : all <= 4096 || a.words.logit ? 4 : 32;
     const int64_t blocks = static_cast<int64_t>((a.words.rows + rows - 1) / rows) * a.batch;
     if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
     LossJoin args = a;
