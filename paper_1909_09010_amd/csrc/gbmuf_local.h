@@ -205,6 +205,18 @@ struct KeepArgs {
     uint32_t *row_max;       // [batch][rows]: bits of what no value of the row's dz exceeds; or nullptr
 };
 
+// Gradients of few rows and features: small_grads_kernel.
+constexpr int kSmallRows = 64, kSmallColumns = 64, kSmallWords = 64;       // words of a piece of the vocabulary
+struct SmallGrads {
+    LossArgs l;              // words, bias, lse and dloss
+    const void *x, *w;
+    int64_t ldx, x_batch, ldw, w_batch;
+    void *dx, *dw, *dbias;   // any of them nullptr; of l.type, dw and dbias of grad_type
+    int64_t lddx, dx_batch, lddw, dw_batch, dbias_batch;
+    float *parts;            // [piece][worker][row][column] of dx, or nullptr
+    int32_t columns, batch, pieces, grad_type, accumulate, reserved;
+};
+
 struct CastArgs {            // out = from, [batch][rows][columns]
     const float *from;
     void *out;
@@ -231,6 +243,7 @@ int launch_loss_few(const DirectArgs &a, const LossArgs &l, int32_t type, hipStr
 int few_columns(const DirectArgs &a, int32_t type);        // of a tile of launch_loss_few
 int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, bool backward, hipStream_t stream);
 int launch_loss_grads(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream);   // dz in f32
+int launch_small_grads(const SmallGrads &a, hipStream_t stream);
 int launch_teacher(const TeacherArgs &a, hipStream_t stream);
 int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStream_t stream);
 int launch_loss_join(const LossJoin &a, hipStream_t stream);

@@ -19,6 +19,33 @@ __device__ __forceinline__ int row_state(const Words &w, int64_t g, int m)
     return t < 0 ? kDead : t < w.vocab ? kLive : kBad;
 }
 
+// The words of a row as the teacher gives them, by one lane: f(word, share) for those that are there, in their order.
+template <class F>
+__device__ __forceinline__ void each_given(const Words &w, int64_t g, int m, float inv_tau, F f)
+{
+    const int64_t *ids = w.target + g * w.batch + m * w.ld;
+    const float *logits = w.logit + g * w.logit_batch + m * w.logit_ld;
+    const float inf = __builtin_inff();
+    float most = -inf, total = 0.0f;
+    for (int j = 0; j < w.top; ++j)
+        if (ids[j] >= 0) most = fmaxf(most, logits[j]);
+    const float from = most == -inf ? 0.0f : most;
+    const auto term = [&](int j) { return ids[j] >= 0 && logits[j] != -inf ? expf((logits[j] - from) * inv_tau) : 0.0f; };
+    for (int j = 0; j < w.top; ++j) total += term(j);
+    for (int j = 0; j < w.top; ++j)
+        if (ids[j] >= 0 && logits[j] != -inf) f(ids[j], term(j) / total);
+}
+
+__device__ __forceinline__ int given_state(const Words &w, int64_t g, int m)
+{
+    const int64_t *ids = w.target + g * w.batch + m * w.ld;
+    const float *logits = w.logit + g * w.logit_batch + m * w.logit_ld;
+    int state = kDead;
+    for (int j = 0; j < w.top; ++j)
+        if (ids[j] >= 0 && logits[j] != -__builtin_inff()) state = max(state, static_cast<int>(ids[j] < w.vocab ? kLive : kBad));
+    return state;
+}
+
 // d loss / d logit of a row, up to what the row is held to: a row that does not count has none, whatever its dloss.
 __device__ __forceinline__ float row_weight(const LossArgs &a, int64_t g, int m, int state)
 {

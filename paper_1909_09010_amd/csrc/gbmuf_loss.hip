@@ -407,6 +407,40 @@ int backward_direct(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t 
     return rc != GBMUF_OK ? rc : launch_join(JoinArgs{px.t, 64, 0, e}, stream);
 }
 
+// Up to 64 rows and features: all of a piece of the vocabulary in one workgroup, dx's parts joined by a second launch.
+constexpr int64_t kSmallParts = 64 << 20;          // bytes of dx's parts
+int64_t small_pieces(const gbmuf_linear_desc_t &d) { return (d.out_features + kSmallWords - 1) / kSmallWords; }
+bool is_small(const gbmuf_linear_desc_t &d)
+{
+    return d.rows <= kSmallRows && d.rows > 0 && d.in_features <= kSmallColumns && d.out_features > 0 && small_pieces(d) <= 65535 &&
+           static_cast<double>(small_pieces(d)) * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.in_features) * 4.0 <= static_cast<double>(kSmallParts);
+}
+
+int backward_small(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io, Space &space, hipStream_t stream)
+{
+    const gbmuf_linear_desc_t &d = l.linear;
+    const int64_t M = d.rows, K = d.in_features, pieces = small_pieces(d);
+    const int32_t G = d.batch, type = d.dtype;
+    const Inputs none{};
+    const Inputs &at = in ? *in : none;
+    const Words words = words_of(l, at, in && l.top <= kFewWords, space);
+    float *parts = space.take<float>(pieces * G * M * K);
+    if (!io) return GBMUF_OK;
+    const int rc = order_words(l, words, at, true, stream);
+    if (rc != GBMUF_OK) return rc;
+    SmallGrads a{};
+    a.l = grad_args(l, at, io, words, Piece{0, G, 0, d.out_features});
+    a.x = at.x.data; a.ldx = at.x.ld; a.x_batch = at.x.batch_stride;
+    a.w = at.w.data; a.ldw = at.w.ld; a.w_batch = at.w.batch_stride;
+    a.dx = io->dx.data; a.lddx = io->dx.ld; a.dx_batch = io->dx.batch_stride;
+    a.dw = io->dw.data; a.lddw = io->dw.ld; a.dw_batch = io->dw.batch_stride;
+    a.dbias = io->dbias.data; a.dbias_batch = io->dbias.batch_stride;
+    a.parts = io->dx.data ? parts : nullptr;
+    a.columns = static_cast<int32_t>(K); a.batch = G; a.pieces = static_cast<int32_t>(pieces);
+    a.grad_type = l.weight_grad_f32 ? kF32 : type; a.accumulate = l.accumulate;
+    return launch_small_grads(a, stream);
+}
+
 // Everything else: dz a piece at a time, in 16 bits or taken apart, and the products of the piece on the 16-bit matrix instructions.
 int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io, Space &space, hipStream_t stream)
 {
@@ -595,6 +629,7 @@ int backward(const Loss &l, const Inputs &in, const gbmuf_loss_grad_io_t &io, Sp
     g.x = in.x; g.w = in.w; g.dx = io.dx; g.dw = io.dw; g.dbias = io.dbias;
     g.dy = gbmuf_matrix_t{nullptr, 64, 0};               // dz lies well
     const bool sums = !io.dbias.data || (io.dw.data && d.in_features > 0);
+    if (is_small(d)) return backward_small(l, &in, &io, space, stream);
     const bool direct = d.out_features == 0 || (may_be_direct(d) && sums && takes_direct_backward(d, g));
     return direct ? backward_direct(l, &in, &io, space, stream) : backward_laid(l, &in, &io, space, stream);
 }
@@ -605,6 +640,9 @@ int64_t workspace_bytes(const Loss &l, bool back)
     if (back) {
         (void)backward_laid(l, nullptr, nullptr, space, nullptr);
         if (may_be_direct(l.linear)) (void)backward_direct(l, nullptr, nullptr, direct, nullptr);
+        Space small{nullptr};
+        if (is_small(l.linear)) (void)backward_small(l, nullptr, nullptr, small, nullptr);
+        space.used = std::max(space.used, small.used);
     } else {
         (void)forward(l, nullptr, nullptr, space, nullptr);
     }
