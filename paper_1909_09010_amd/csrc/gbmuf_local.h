@@ -196,16 +196,18 @@ struct KeepArgs {
     int64_t ld, batch_stride;
     void *out;               // [batch][rows][out_ld]
     int64_t out_ld;
-    int32_t columns, batch, type, reserved;
+    int32_t columns, batch, type;
+    int32_t all;             // every row counts: words is not looked at but for its rows
     const float *dloss;
     int64_t dloss_ld, dloss_batch;
     float tau;
-    int32_t reserved1;
+    int32_t reserved;
     float *sigma;            // [batch], and behind them 1 / sigma; or nullptr
     uint32_t *row_max;       // [batch][rows]: bits of what no value of the row's dz exceeds; or nullptr
 };
 
-// Gradients of few rows and features: small_grads_kernel.
+// Gradients of few rows: small_grads_kernel, and few_grads_kernel for more columns.
+constexpr int kFewGradRows = 8, kFewGradColumns = 1024, kFewGradWords = 64;
 constexpr int kSmallRows = 64, kSmallColumns = 64, kSmallWords = 64;       // words of a piece of the vocabulary
 struct SmallGrads {
     LossArgs l;              // words, bias, lse and dloss
@@ -244,6 +246,9 @@ int few_columns(const DirectArgs &a, int32_t type);        // of a tile of launc
 int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, bool backward, hipStream_t stream);
 int launch_loss_grads(const DirectArgs &dx, const DirectArgs &dw, int32_t type, hipStream_t stream);   // dz in f32
 int launch_small_grads(const SmallGrads &a, hipStream_t stream);
+int launch_few_grads(const SmallGrads &a, int32_t workgroups, hipStream_t stream);
+int few_grads_lanes(int64_t K);
+int launch_join_parts(const SmallGrads &a, int32_t parts, hipStream_t stream);
 int launch_teacher(const TeacherArgs &a, hipStream_t stream);
 int launch_word_lists(const Words &w, const WordLists &l, int32_t batch, hipStream_t stream);
 int launch_loss_join(const LossJoin &a, hipStream_t stream);

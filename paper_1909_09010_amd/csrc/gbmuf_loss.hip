@@ -242,11 +242,19 @@ Operand operand_of(const gbmuf_matrix_t &m)
 // Lays out rows along their own axis: f32 taken apart with row maxima, 16-bit types copied.
 int lay_rows(LayArgs l, const Operand &o, int64_t K, int32_t type, hipStream_t stream)
 {
+    if (type != kF32) {
+        KeepArgs a{};
+        a.words.rows = l.R;
+        a.all = 1;
+        a.x = l.src; a.ld = l.ld; a.batch_stride = l.batch_stride;
+        a.out = const_cast<uint16_t *>(o.p); a.out_ld = o.ld;
+        a.columns = l.C; a.batch = l.batch; a.type = type;
+        return launch_keep(a, stream);
+    }
     l.plain = const_cast<uint16_t *>(o.p); l.plain_ld = o.ld; l.plain_batch = o.batch;
     l.row_max = o.max;
     LaySet set;
     set.add(l);
-    if (type != kF32) return launch_copy(set, stream);
     if (K > 0 && K <= kLongestRow) return launch_rows(set, stream);
     int rc = launch_zero(o.max, static_cast<int64_t>(l.R) * l.batch, stream);
     if (rc == GBMUF_OK) rc = launch_stats(set, stream);
@@ -416,17 +424,27 @@ bool is_small(const gbmuf_linear_desc_t &d)
            static_cast<double>(small_pieces(d)) * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.in_features) * 4.0 <= static_cast<double>(kSmallParts);
 }
 
-int backward_small(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io, Space &space, hipStream_t stream)
+// f32, up to 8 rows: w is read from memory once, by workgroups that each walk pieces of the vocabulary.
+bool is_few(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && d.rows <= kFewGradRows && d.rows > 0 && d.in_features <= kFewGradColumns && d.out_features > 0; }
+int64_t few_workgroups(const gbmuf_linear_desc_t &d)
+{
+    const int64_t pieces = (d.out_features + kFewGradWords - 1) / kFewGradWords;
+    return std::min<int64_t>(pieces, std::max<int64_t>(768 / std::max(d.batch, 1), 1));
+}
+
+int backward_few(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io, Space &space, hipStream_t stream)
 {
     const gbmuf_linear_desc_t &d = l.linear;
-    const int64_t M = d.rows, K = d.in_features, pieces = small_pieces(d);
+    const bool small = is_small(d);
+    const int64_t M = d.rows, K = d.in_features, pieces = small_pieces(d), groups = few_workgroups(d), parts = small ? pieces : groups * (256 / few_grads_lanes(K));
+    static_assert(kSmallWords == kFewGradWords, "pieces are the same");
     const int32_t G = d.batch, type = d.dtype;
     const Inputs none{};
     const Inputs &at = in ? *in : none;
-    const Words words = words_of(l, at, in && l.top <= kFewWords, space);
-    float *parts = space.take<float>(pieces * G * M * K);
+    const Words words = words_of(l, at, in && small && l.top <= kFewWords, space);
+    float *sums = space.take<float>(parts * G * M * K);
     if (!io) return GBMUF_OK;
-    const int rc = order_words(l, words, at, true, stream);
+    int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK) return rc;
     SmallGrads a{};
     a.l = grad_args(l, at, io, words, Piece{0, G, 0, d.out_features});
@@ -435,10 +453,12 @@ int backward_small(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *
     a.dx = io->dx.data; a.lddx = io->dx.ld; a.dx_batch = io->dx.batch_stride;
     a.dw = io->dw.data; a.lddw = io->dw.ld; a.dw_batch = io->dw.batch_stride;
     a.dbias = io->dbias.data; a.dbias_batch = io->dbias.batch_stride;
-    a.parts = io->dx.data ? parts : nullptr;
+    a.parts = io->dx.data ? sums : nullptr;
     a.columns = static_cast<int32_t>(K); a.batch = G; a.pieces = static_cast<int32_t>(pieces);
     a.grad_type = l.weight_grad_f32 ? kF32 : type; a.accumulate = l.accumulate;
-    return launch_small_grads(a, stream);
+    if (small) return launch_small_grads(a, stream);
+    rc = launch_few_grads(a, static_cast<int32_t>(groups), stream);
+    return rc == GBMUF_OK ? launch_join_parts(a, static_cast<int32_t>(parts), stream) : rc;
 }
 
 // Everything else: dz a piece at a time, in 16 bits or taken apart, and the products of the piece on the 16-bit matrix instructions.
@@ -629,7 +649,7 @@ int backward(const Loss &l, const Inputs &in, const gbmuf_loss_grad_io_t &io, Sp
     g.x = in.x; g.w = in.w; g.dx = io.dx; g.dw = io.dw; g.dbias = io.dbias;
     g.dy = gbmuf_matrix_t{nullptr, 64, 0};               // dz lies well
     const bool sums = !io.dbias.data || (io.dw.data && d.in_features > 0);
-    if (is_small(d)) return backward_small(l, &in, &io, space, stream);
+    if (is_small(d) || is_few(d)) return backward_few(l, &in, &io, space, stream);
     const bool direct = d.out_features == 0 || (may_be_direct(d) && sums && takes_direct_backward(d, g));
     return direct ? backward_direct(l, &in, &io, space, stream) : backward_laid(l, &in, &io, space, stream);
 }
@@ -641,7 +661,7 @@ int64_t workspace_bytes(const Loss &l, bool back)
         (void)backward_laid(l, nullptr, nullptr, space, nullptr);
         if (may_be_direct(l.linear)) (void)backward_direct(l, nullptr, nullptr, direct, nullptr);
         Space small{nullptr};
-        if (is_small(l.linear)) (void)backward_small(l, nullptr, nullptr, small, nullptr);
+        if (is_small(l.linear) || is_few(l.linear)) (void)backward_few(l, nullptr, nullptr, small, nullptr);
         space.used = std::max(space.used, small.used);
     } else {
         (void)forward(l, nullptr, nullptr, space, nullptr);

@@ -298,11 +298,21 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
 {
     const int64_t block = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
     if (block < copies) {
-        const int64_t id = block * 256 + threadIdx.x, per_row = a.out_ld / 8, row = id / per_row;
-        if (row >= static_cast<int64_t>(a.words.rows) * a.batch) return;
+        const int64_t id = block * 256 + threadIdx.x, all = static_cast<int64_t>(a.words.rows) * a.batch;
+        const uint32_t per_row = static_cast<uint32_t>(a.out_ld / 8), rows = static_cast<uint32_t>(a.words.rows);
+        int64_t row, g;
+        if (copies < 1 << 23) {                             // 32 bits hold every number: a division of 64 takes as long as the copy of 16 bytes
+            const uint32_t r = static_cast<uint32_t>(id) / per_row;
+            row = r;
+            g = r / rows;
+        } else {
+            row = id / per_row;
+            g = row / rows;
+        }
+        if (row >= all) return;
         const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
-        const int64_t g = row / a.words.rows, from = g * a.batch_stride + (row - g * a.words.rows) * a.ld + c;
-        const int m = static_cast<int>(row - g * a.words.rows), state = row_state(a.words, g, m);
+        const int64_t from = g * a.batch_stride + (row - g * a.words.rows) * a.ld + c;
+        const int m = static_cast<int>(row - g * a.words.rows), state = a.all ? kLive : row_state(a.words, g, m);
         if (a.row_max && c == 0) {
             const float d = fabsf(a.dloss[g * a.dloss_batch + m * a.dloss_ld] * a.tau);
             a.row_max[row] = state != kDead && d < __builtin_inff() ? __float_as_uint(d) : 0u;

@@ -208,12 +208,20 @@ int launch_small_grads(const SmallGrads &a, hipStream_t stream)
     void *argv[] = {&args};
     const int32_t type = a.l.type;
     const auto fn = type == kF32 ? small_grads_kernel<kF32> : type == kBf16 ? small_grads_kernel<kBf16> : small_grads_kernel<kF16>;
-    hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(a.pieces), static_cast<unsigned>(a.batch)), dim3(kThreads), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(a.pieces), static_cast<unsigned>(a.batch)), dim3(kThreads), argv, 0, stream);
     if (err != hipSuccess) return hip_failed("hipLaunchKernel(small gradients)", err, GBMUF_EDEVICE);
+    return launch_join_parts(a, a.pieces, stream);
+}
+
+int launch_join_parts(const SmallGrads &a, int32_t parts, hipStream_t stream)
+{
     const int64_t blocks = (static_cast<int64_t>(a.l.words.rows) * a.columns + 63) / 64;
-    if (!a.parts || blocks <= 0) return GBMUF_OK;
-    err = hipLaunchKernel(reinterpret_cast<const void *>(a.pieces > 32 ? small_join_kernel<16> : small_join_kernel<4>),
-                          dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.batch)), dim3(a.pieces > 32 ? 1024 : 256), argv, 0, stream);
+    if (!a.parts || blocks <= 0 || a.batch <= 0) return GBMUF_OK;
+    SmallGrads args = a;
+    args.pieces = parts;
+    void *argv[] = {&args};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(parts > 32 ? small_join_kernel<16> : small_join_kernel<4>),
+                                           dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.batch)), dim3(parts > 32 ? 1024 : 256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(parts of dx)", err, GBMUF_EDEVICE);
 }
 
