@@ -319,11 +319,16 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
         }
         Eight v{};
         if (state != kDead) {
-            if (left >= 8) v = read8<T>(a.x, from);
-            else
+            // a row's last values are read together with what follows in the matrix, where it does
+            if (m * a.ld + c + 8 <= (a.words.rows - 1) * a.ld + a.columns) {
+                v = read8<T>(a.x, from);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v.v[k >> 2][k & 3] = k < left ? v.v[k >> 2][k & 3] : 0.0f;
+            } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     if (k < left) v.v[k >> 2][k & 3] = load_one(a.x, from + k, T);
+            }
         }
         write8<T>(a.out, row * a.out_ld + c, v);
         return;

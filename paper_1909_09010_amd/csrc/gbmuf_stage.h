@@ -61,9 +61,15 @@ struct Stage {
         for (int i = 0; i < kPasses; ++i) {
             uint32_t v[4] = {0u, 0u, 0u, 0u};
             const int left = K - (k0 + chunk(i));
+            if (left >= 8) {                               // rows lie on 16 bytes
+                const v4u all = *reinterpret_cast<const v4u *>(row[i] + k0);
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                if (c < left) v[c >> 1] |= static_cast<uint32_t>(row[i][k0 + c]) << (16 * (c & 1));
+                for (int c = 0; c < 4; ++c) v[c] = all[c];
+            } else {
+#pragma unroll
+                for (int c = 0; c < 7; ++c)
+                    if (c < left) v[c >> 1] |= static_cast<uint32_t>(row[i][k0 + c]) << (16 * (c & 1));
+            }
             const int r = i * kPass + static_cast<int>(threadIdx.x >> 3);
             *reinterpret_cast<v4u *>(lds + r * kStep + (threadIdx.x & 7) * 8) = v4u{v[0], v[1], v[2], v[3]};
         }

@@ -63,9 +63,14 @@ struct Sender {
         for (int i = 0; i < kPasses; ++i) {
             uint32_t v[4] = {0u, 0u, 0u, 0u};
             const uint16_t *from = base + static_cast<int64_t>(min(first + r + i * kPass, count - 1)) * ld + k0 + chunk(t);
+            if (left >= 8) {                               // rows lie on 16 bytes
+                const v4u all = *reinterpret_cast<const v4u *>(from);
+                for (int c = 0; c < 4; ++c) v[c] = all[c];
+            } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                if (c < left) v[c >> 1] |= static_cast<uint32_t>(from[c]) << (16 * (c & 1));
+                for (int c = 0; c < 7; ++c)
+                    if (c < left) v[c >> 1] |= static_cast<uint32_t>(from[c]) << (16 * (c & 1));
+            }
             *reinterpret_cast<v4u *>(lds + (i * kPass + r) * kStep + (t & 7) * 8) = v4u{v[0], v[1], v[2], v[3]};
         }
     }
