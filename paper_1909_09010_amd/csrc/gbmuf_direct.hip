@@ -335,14 +335,15 @@ int launch_loss_direct(const DirectArgs &a, const LossArgs &l, int32_t type, boo
     const int32_t blocks = a.t.blocks();
     if (blocks <= 0) return GBMUF_OK;
     using Fn = void (*)(DirectArgs, LossArgs);
-    static constexpr Fn fns[3][2][2] = {
-        {{loss_direct_kernel<kF32, false, 1>, loss_direct_kernel<kF32, false, 4>}, {loss_direct_kernel<kF32, true, 1>, loss_direct_kernel<kF32, true, 4>}},
-        {{loss_direct_kernel<kBf16, false, 1>, loss_direct_kernel<kBf16, false, 4>}, {loss_direct_kernel<kBf16, true, 1>, loss_direct_kernel<kBf16, true, 4>}},
-        {{loss_direct_kernel<kF16, false, 1>, loss_direct_kernel<kF16, false, 4>}, {loss_direct_kernel<kF16, true, 1>, loss_direct_kernel<kF16, true, 4>}}};
+    static constexpr Fn forward[2] = {loss_direct_kernel<kF32, false, 1>, loss_direct_kernel<kF32, false, 4>};         // of f32 alone
+    static constexpr Fn grads[3][2] = {{loss_direct_kernel<kF32, true, 1>, loss_direct_kernel<kF32, true, 4>},
+                                       {loss_direct_kernel<kBf16, true, 1>, loss_direct_kernel<kBf16, true, 4>},
+                                       {loss_direct_kernel<kF16, true, 1>, loss_direct_kernel<kF16, true, 4>}};
+    const Fn fn = backward ? grads[type][grouped(blocks) ? 1 : 0] : forward[grouped(blocks) ? 1 : 0];
     DirectArgs args = a;
     LossArgs loss = l;
     void *argv[] = {&args, &loss};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fns[type][backward ? 1 : 0][grouped(blocks) ? 1 : 0]), dim3(static_cast<unsigned>(blocks)),
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)),
                                            dim3(grouped(blocks) ? 4 * kThreads : kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(direct logits)", err, GBMUF_EDEVICE);
 }

@@ -310,7 +310,8 @@ Few few_of(const gbmuf_linear_desc_t &d)
 // What a gradient of 16-bit types takes as it lies: matrices whose rows lie on 16 bytes and are whole pieces of that.
 bool as_it_lies(const gbmuf_matrix_t &m, int64_t cols) { return lies_well(m) && cols % 8 == 0; }
 
-bool takes_direct_backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t &io)
+// more: us that the other way takes beside that.
+bool takes_direct_backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad_io_t &io, double more = 0.0)
 {
     const bool split = d.dtype == GBMUF_F32;
     const double M = static_cast<double>(d.rows), N = static_cast<double>(d.out_features), K = static_cast<double>(d.in_features);
@@ -322,7 +323,7 @@ bool takes_direct_backward(const gbmuf_linear_desc_t &d, const gbmuf_linear_grad
     const double steps = (dx ? steps_us(d.rows, d.in_features, d.out_features, d.batch) : 0.0) +
                          (dw ? steps_us(d.out_features, d.in_features, d.rows, d.batch) : 0.0);
     const double laid = (split ? 38.0 : 28.0) + (split ? 3e-6 : 2e-6) * d.batch * values + ((dx ? 1 : 0) + (dw ? 1 : 0)) * products_us(d);
-    return 10.0 + 2.2 * steps <= laid;
+    return 10.0 + 2.2 * steps <= laid + more;
 }
 
 int check_workspace(const void *workspace, int64_t have, int64_t need, std::initializer_list<const Extent *> matrices)
