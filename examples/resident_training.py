@@ -6,6 +6,8 @@ The K replicas lie in rows of theta.  A mini-batch's forward and backward produc
 
     h = tanh(W1 [e(a), e(b)] + b1),  u = h + (W2 h + b2),  logits = W3 u + b3
 
+and its loss is the cross entropy of the logits' softmax, which no tensor keeps.
+
     python examples/resident_training.py [--steps 200] [--workers 4] [--layout rows|blocked]
 
 With ``--layout blocked`` the state keeps the library's recommended placement between mini-batches; the local step writes it
@@ -42,8 +44,8 @@ class Model:
         self.P = self.offsets[-1]
         self.l1 = B.Linear(tokens, hidden, 2 * embed, workers, torch.float32, B.ACT_TANH)
         self.l2 = B.Linear(tokens, hidden, hidden, workers, torch.float32, B.ACT_NONE, B.RESIDUAL_AFTER)
-        self.l3 = B.Linear(tokens, vocab, hidden, workers, torch.float32)
-        need = max(max(l.workspace_bytes(), l.workspace_bytes(True)) for l in (self.l1, self.l2, self.l3))
+        self.head = B.CrossEntropy(tokens, vocab, hidden, workers, torch.float32)
+        need = max(max(l.workspace_bytes(), l.workspace_bytes(True)) for l in (self.l1, self.l2, self.head))
         self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=DEV)
 
     def views(self, rows: torch.Tensor) -> dict:
@@ -52,26 +54,25 @@ class Model:
 
     def step(self, p: dict, g: dict, context: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
         """Mean loss of every worker for context [K, tokens, 2] and target [K, tokens]; gradients into g."""
-        K, T, E, H, V = self.K, self.tokens, self.embed, self.hidden, self.vocab
+        K, T, E, H = self.K, self.tokens, self.embed, self.hidden
         s, ws = torch.cuda.current_stream(), self.workspace
         worker = torch.arange(K, device=DEV)[:, None, None]
         x = p["embedding"][worker, context].reshape(K, T, 2 * E)
-        z1, h, u, logits = (torch.empty(K, T, n, device=DEV) for n in (H, H, H, V))
+        z1, h, u = (torch.empty(K, T, H, device=DEV) for _ in range(3))
+        losses, lse = (torch.empty(K, T, device=DEV) for _ in range(2))
         self.l1.forward(self.l1.forward_io(x, p["w1"], h, bias=p["b1"], pre=z1), ws, s)
         self.l2.forward(self.l2.forward_io(h, p["w2"], u, bias=p["b2"], residual=h), ws, s)
-        self.l3.forward(self.l3.forward_io(u, p["w3"], logits, bias=p["b3"]), ws, s)
-        logp = torch.log_softmax(logits, 2)
-        loss = -logp.gather(2, target[:, :, None]).mean((1, 2))
-        dlogits = (logp.exp() - torch.nn.functional.one_hot(target, V)) / T
+        self.head.forward(self.head.forward_io(u, p["w3"], target, losses, lse, bias=p["b3"]), ws, s)
+        each = torch.full((1, 1), 1 / T, device=DEV).expand(K, T)          # the mean's gradient
         du, dh, dx = (torch.empty(K, T, n, device=DEV) for n in (H, H, 2 * E))
-        self.l3.backward(self.l3.backward_io(dlogits, u, p["w3"], dx=du, dw=g["w3"], dbias=g["b3"]), ws, s)
+        self.head.backward(self.head.backward_io(u, p["w3"], target, lse, each, bias=p["b3"], dx=du, dw=g["w3"], dbias=g["b3"]), ws, s)
         self.l2.backward(self.l2.backward_io(du, h, p["w2"], dx=dh, dw=g["w2"], dbias=g["b2"]), ws, s)
         dh += du                                          # the residual's way around the product
         self.l1.backward(self.l1.backward_io(dh, x, p["w1"], pre=z1, dx=dx, dw=g["w1"], dbias=g["b1"]), ws, s)
         g["embedding"].zero_()
         at = (worker.expand(K, T, 2).reshape(-1), context.reshape(-1))
         g["embedding"].index_put_(at, dx.reshape(-1, E), accumulate=True)
-        return loss
+        return losses.mean(1)
 
 
 def text(workers: int, length: int, vocab: int, seed: int) -> torch.Tensor:

@@ -38,8 +38,10 @@ __device__ __forceinline__ void write_columns(float *p, int left, const float (&
 
 // A workgroup takes every gridDim.x-th piece of 64 words for all rows.  The logits of a piece come from matrix instructions as in few_sums; their gradient
 // stays in LDS, [word][row].  Then threads take C columns each of a word's row, which is in the L2 by now: dw's values are ROWS products with the thread's
-// columns of x, dx's sums go on in registers over all pieces: 2 ROWS C multiply-adds a word and thread, 0.21 us a word of 1024 columns and CU for 16 rows, where
-// its 4 KB (bf16) take 0.16 at 6.5 TB/s.  `lanes` threads have a word's columns, the others further words.  us, this / the routes of more rows: TODO
+// columns of x, dx's sums go on in registers over all pieces: 2 ROWS C multiply-adds a word and thread, 0.1 us a word of 1024 columns and CU for 8 rows, where
+// its 4 KB read and 4 KB written take 0.32 at 6.5 TB/s.  `lanes` threads have a word's columns, the others further words.  Bound by w's way from memory.  us, this /
+// the routes of more rows: 2 x 1 x 54538 x 241 78 / 142, 1 x 8 x 50000 x 1024 154 / 207, 9 x 6 x 5250 x 74 32 / 42, 1 x 1 x 2368 x 256 21 / 28, 1 x 3 x 300 x 700 as
+// long.  16-bit types were slower than laying w out, 16 rows short of registers: they take those routes.
 template <int ROWS, int C>
 __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, int32_t lanes)
 {

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void short_teacher_kernel(TeacherArgs a)
 // Lists of words by window: a workgroup takes the lists of a block of rows, counts the words of each window, and puts them there.  Within a window they lie in no
 // certain order, which no result depends on: no two are the same word of the same row.
 // ---------------------------------------------------------------------------------------
-constexpr int kListThreads = 1024;           // 8 x 5120 rows of 64 words: TODO us, 256 threads 46
+constexpr int kListThreads = 1024;           // 8 x 5120 rows of 64 words, without shares / with them: 18 / 33 us, 256 threads 46 / 67
 __global__ __launch_bounds__(kListThreads) void word_lists_kernel(Words w, WordLists l)
 {
     __shared__ int32_t count[kMostWindows];

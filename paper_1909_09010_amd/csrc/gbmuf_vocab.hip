@@ -17,8 +17,8 @@ __device__ __forceinline__ int scratch_at(int r, int c) { return r * 32 + (((c >
 template <int N>
 __device__ __forceinline__ void apart() { asm volatile("; %0" ::"n"(N)); }
 
-// Sends R rows of one step to LDS as Stage does.  Where the rows are is worked out for every step from one address a lane: Stage's addresses, kept over a
-// tile's steps, would go to memory and back (f32 by tiles of 256 8 x 700 x 10000 x 650: 436 us, where these take 3TODO).
+// Sends R rows of one step to LDS as Stage does.  Where the rows are is worked out for every step from one address a lane: Stage's addresses, kept over the
+// steps of all tiles beside statistics and sums, would go to memory and back.
 template <int R, int THREADS>
 struct Sender {
     static constexpr int kPass = THREADS / 8, kPasses = R / kPass;
@@ -79,7 +79,12 @@ struct Sender {
 // A workgroup takes one block of TM rows and walks `walk` tiles of TN words, as one stream of steps: while a tile is left the first two steps of the
 // next are on their way, so that only the arithmetic of leaving is paid.  Everything that a row needs is a lane's own (leave_loss): its statistics
 // stay in registers over all of the tiles, and lse and weight are loaded once.
-// Forward, per logit: a maximum, a multiply-add, an exponential and an addition.
+// Forward, per logit: a maximum, a multiply-add, an exponential and an addition.  Backward: a multiply-add, an exponential, a product, and its way through
+// LDS to where a row's 16 bytes leave together.
+// Bounds: the steps, and what leaving a tile takes between them, when the matrix cores wait: a tile of 256 x 256 bf16 has steps of 1.73 us and leaves in 3.5 us
+// forward, so that 512 features are 8 steps and a fifth of leaving.  A whole call, bf16 8 x 5120 x 8197 x 512: 362 us, 0.95 PFLOP/s where large products reach
+// 1.31.  Tiles of 128 have two workgroups on a CU, one's leaving beside the other's steps, but twice the LDS reads a product: the caller's rule compares rounds
+// of both.  f32, taken apart into two f16, has tiles of 128 only: those of 256 leave too few registers for the statistics (8 x 700 x 10000 x 650: 436 us, 333).
 template <int T, bool SPLIT, int TM, int TN, int WM, int WN, bool BACKWARD, bool LISTS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, LossArgs l)
 {
