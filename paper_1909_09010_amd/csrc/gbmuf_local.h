@@ -160,7 +160,7 @@ struct LossArgs {
     const float *sigma;      // [g]: a power of two that dz is multiplied with, or nullptr
     void *dz;
     int64_t dz_ld, dz_batch;
-    int32_t dz_type, reserved;
+    int32_t dz_type, streamed;      // streamed: dz is more than the caches hold
     float *col_sums;         // [g][parts of 64 or 128 rows][column], or nullptr
     uint32_t *col_max;       // f32, [g][column]: bits of the largest magnitude, zero before; or nullptr
     int32_t *live;           // out: [g][row], or nullptr

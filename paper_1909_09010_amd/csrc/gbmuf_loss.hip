@@ -579,6 +579,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         a.lists = lists_from(lists, words, p.g);
         a.walk = c.t.steps;
         a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld; a.dz_type = type;
+        a.streamed = p.workers * M * pld * static_cast<int64_t>(type_bytes(type)) > kCached ? 1 : 0;
         if (type == kF16) a.sigma = sigma + p.g;
         if (db) a.col_sums = sums;
         if (split && dw) a.col_max = max;

@@ -146,29 +146,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
         }
     }
 
-    // the logits' sums begin with the bias, loaded while the tile before is left
-    typedef typename Four<T>::type Raw;
-    Raw bias[SPLIT ? 1 : FN][SPLIT ? 1 : 4];
-    const auto load_bias = [&](int tile) {
-        if constexpr (!SPLIT) {
-            const int n_wave = tile * TN + wn;
-            const typename Num<T>::type *from = static_cast<const typename Num<T>::type *>(l.bias) + g * l.bias_batch;
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = n_wave + j * 32 + q * 8 + half * 4;
-                    bias[j][q] = Raw{};
-                    if (!l.bias || tile >= last) continue;
-                    if (n_wave + kColumns <= N) bias[j][q] = *reinterpret_cast<const Raw *>(from + n);
-                    else
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            if (n + c < N) bias[j][q][c] = from[n + c];
-                }
-        }
+    // the logits' sums begin with the bias: a lane has one column's, loaded before anything of the tile before is stored -- a load is waited for together with
+    // the stores before it
+    static_assert(kColumns == 64, "a lane has a column");
+    float bias = 0.0f;
+    const auto load_bias = [&](int tile, int lane) {
+        const int n = tile * TN + wn + lane;
+        if constexpr (!SPLIT) bias = l.bias && n < N ? load_one(l.bias, g * l.bias_batch + n, T) : 0.0f;
     };
-    if (!BACKWARD) load_bias(first);
+    load_bias(first, lane);
 
     meet<true>();
     send(lds[1]);
@@ -182,13 +168,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                 begin = starts[0];
                 entries = starts[1] - begin;
             }
-        if (BACKWARD) load_bias(tile);                      // the registers that hold it while a tile is left are not to be had
+        if constexpr (!SPLIT) {
+            in_order();
+            scratch[threadIdx.x & 63] = bias;
+            in_order();
+        }
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
+            for (int q = 0; q < 4; ++q) {
+                const v4f from = SPLIT ? v4f{0.0f, 0.0f, 0.0f, 0.0f} : *reinterpret_cast<const v4f *>(scratch + j * 32 + q * 8 + half * 4);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = SPLIT ? 0.0f : static_cast<float>(bias[j][r >> 2][r & 3]);
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[i][j][4 * q + c] = from[c];
+            }
         Turn<T, SPLIT, TM, TN, FM, FN, 0> turn[2];
         if (steps > 0) turn[0].template load<0>(lds[t & 1], wm, wn);
         for (int s = 0; s < steps; ++s, ++t) {
@@ -208,43 +202,38 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
             interleave<kReads, kMfmas>();
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (!BACKWARD) load_bias(tile + 1);
 
         // what leaving derives from the lane is derived anew for every tile: kept over the steps, it would take the registers of the sums
         int lane = threadIdx.x & 63;
         asm volatile("" : "+v"(lane));
         const int half = lane >> 5;
+        if (tile + 1 < last) load_bias(tile + 1, lane);
         const int n_wave = tile * TN + wn, lo = l.first + n_wave, hi = l.first + min(n_wave + kColumns, N);
         const bool whole = n_wave + kColumns <= N;
         const int left = N - n_wave - half * 4;             // columns from the lane's first on
-        // words of the wave's rows among its columns, 64 of them at hand
-        // 64 codes at hand; a code's column among the wave's, its row among a fragment's
-        const bool holds = lane < entries;
-        uint32_t entry = 0;
-        float entry_share = 0.0f;
+        // words of the wave's rows among its columns, kHeld lanes' of them at hand; a code's column among the wave's, its row among a fragment's
+        constexpr int kHeld = 2;
+        uint32_t entry[kHeld] = {};
+        float entry_share[kHeld] = {};
         const uint32_t *codes = nullptr;
         const float *shares = nullptr;
         const int window = lo & ((1 << l.lists.shift) - 1);            // where the wave's columns begin in theirs
+        const uint32_t none = static_cast<uint32_t>(window + kColumns) << 17;         // no column of the wave's, past 2^15 too
         if constexpr (LISTS) {
             const int64_t at = (g * l.lists.blocks + (m0 + wm) / (TM / WM)) * (TM / WM) * w.top + begin;
             codes = l.lists.code + at;
             shares = l.lists.share + at;
-            if (holds) {
-                entry = codes[lane];
-                if (BACKWARD) entry_share = shares[lane];
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                entry[k] = none;
+                if (k * 64 + lane >= entries) continue;
+                entry[k] = codes[k * 64 + lane];
+                if (BACKWARD) entry_share[k] = shares[k * 64 + lane];
             }
         }
         const auto column_of = [&](uint32_t code) { return static_cast<int>(code >> 17) - window; };
         const auto row_in = [&](uint32_t code) { return static_cast<int>(code >> 10) & 31; };
-        const auto in_rows = [&](uint32_t code, int i) { return (static_cast<int>(code >> 15) & 3) == i; };
-        // f(code, share) for the words in columns j of rows i
-        const auto each_entry = [&](int i, int j, auto f) {
-            if (holds && in_rows(entry, i) && column_of(entry) >> 5 == j) f(entry, entry_share);
-            for (int e = 64 + lane; e < entries; e += 64) {
-                const uint32_t code = codes[e];
-                if (in_rows(code, i) && column_of(code) >> 5 == j) f(code, BACKWARD ? shares[e] : 0.0f);
-            }
-        };
+        const auto in_fragment = [&](uint32_t code, int i, int j) { return (static_cast<int>(code >> 15) & 3) == i && column_of(code) >> 5 == j; };
         const auto put = [&](const v16f &rows) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -280,42 +269,22 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                     for (int r = 0; r < 16; ++r) acc[i][j][r] = ldexpf(acc[i][j][r], em[i] + row_exponent(e[r >> 2][r & 3])) + b[r >> 2][r & 3];
             }
         }
-        static_assert(!BACKWARD || kColumns == 64, "a lane has a column of the sums");
-        v4f total[BACKWARD ? FN : 1][2], top[BACKWARD && SPLIT ? FN : 1][2];
-        Eight z[2];                                         // of rows `from` and 16 on, columns eight .. of a fragment: 4 lanes a row
-        const int from = lane >> 2, eight = (lane & 3) * 8;
-        if constexpr (BACKWARD)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-                if (SPLIT) top[j][0] = top[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-        const auto store = [&](int i, int j) {
-            const int n = n_wave + j * 32 + eight;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int row = m0 + wm + i * 32 + k * 16 + from;
-                total[j][0] += z[k].v[0];
-                total[j][1] += z[k].v[1];
-                if constexpr (SPLIT)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) top[j][c >> 2][c & 3] = fmaxf(top[j][c >> 2][c & 3], fabsf(z[k].v[c >> 2][c & 3]));
-                if (row < M && n < l.dz_ld) write8<SPLIT ? kF32 : T>(l.dz, g * l.dz_batch + row * l.dz_ld + n, z[k]);
-            }
-        };
-
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int row0 = m0 + wm + i * 32, m = row0 + (lane & 31);
+        const auto cut = [&](int i, int j) {               // words behind the last
             if (!whole)
 #pragma unroll
-                for (int j = 0; j < FN; ++j)
+                for (int r = 0; r < 16; ++r)
+                    if (j * 32 + (r >> 2) * 8 + (r & 3) >= left) acc[i][j][r] = -__builtin_inff();
+        };
+        const auto word_of = [&](int i) {                  // a row's word among the wave's columns
+            if constexpr (LISTS) return -1;
+            else return target[i] >= lo && target[i] < hi ? target[i] - lo : -1;
+        };
+        if constexpr (!BACKWARD) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (j * 32 + (r >> 2) * 8 + (r & 3) >= left) acc[i][j][r] = -__builtin_inff();
-            int column = -1;                                // of the row's word
-            if constexpr (!LISTS) column = target[i] >= lo && target[i] < hi ? target[i] - lo : -1;
-            if constexpr (!BACKWARD) {
+            for (int i = 0; i < FM; ++i) {
+                const int row0 = m0 + wm + i * 32, m = row0 + (lane & 31), column = word_of(i);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) cut(i, j);
                 float most = acc[i][0][0];
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
@@ -345,13 +314,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     if constexpr (LISTS) {
-                        if (!__any(holds && in_rows(entry, i) && column_of(entry) >> 5 == j) && entries <= 64) continue;
+                        if (!__any(in_fragment(entry[0], i, j) || in_fragment(entry[1], i, j)) && entries <= 64 * kHeld) continue;
                         in_order();
                         put(acc[i][j]);
                         in_order();
-                        each_entry(i, j, [&](uint32_t code, float) {
-                            l.at[(g * w.rows + row0 + row_in(code)) * w.top + (code & 1023)] = scratch[scratch_at(row_in(code), column_of(code) & 31)];
-                        });
+                        const auto leave = [&](uint32_t code) {
+                            if (in_fragment(code, i, j))
+                                l.at[(g * w.rows + row0 + row_in(code)) * w.top + (code & 1023)] = scratch[scratch_at(row_in(code), column_of(code) & 31)];
+                        };
+#pragma unroll
+                        for (int k = 0; k < kHeld; ++k) leave(entry[k]);
+                        for (int e = 64 * kHeld + lane; e < entries; e += 64) {
+                            leave(codes[e]);
+                            __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0), as below
+                        }
                     } else if (__any(column >> 5 == j)) {
                         in_order();
                         put(acc[i][j]);
@@ -359,76 +335,100 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                         if (column >> 5 == j && half == 0) l.at[g * w.rows + m] = scratch[scratch_at(lane, column & 31)];
                     }
                 }
-            } else {
-                if (__all(near[i])) {
+            }
+        } else {
+            // columns outside, so that only 32 columns' sums are held; no load between the stores, which it would wait for
+            const int from = lane >> 2, eight = (lane & 3) * 8;             // what a lane stores: rows `from` and 16 on, 8 columns; 4 lanes a row
 #pragma unroll
-                    for (int j = 0; j < FN; ++j)
+            for (int j = 0; j < FN; ++j) {
+                v4f total[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}}, top[2] = {total[0], total[0]};
+                Eight z[2];
+                const auto store = [&](int i) {
+                    const int n = n_wave + j * 32 + eight;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int row = m0 + wm + i * 32 + k * 16 + from;
+                        total[0] += z[k].v[0];
+                        total[1] += z[k].v[1];
+                        if constexpr (SPLIT)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) top[c >> 2][c & 3] = fmaxf(top[c >> 2][c & 3], fabsf(z[k].v[c >> 2][c & 3]));
+                        if (row >= M || n >= l.dz_ld) continue;
+                        const int64_t at = g * l.dz_batch + row * l.dz_ld + n;
+                        if (l.streamed) write8<SPLIT ? kF32 : T, true>(l.dz, at, z[k]);
+                        else write8<SPLIT ? kF32 : T>(l.dz, at, z[k]);
+                    }
+                };
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    const int row0 = m0 + wm + i * 32, column = word_of(i);
+                    cut(i, j);
+                    if (__all(near[i])) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][j][r] = p_weight[i] * exp2_of(fmaf(acc[i][j][r], scale, -lse[i]));
-                    apart<0>();
-                } else {
-#pragma unroll
-                    for (int j = 0; j < FN; ++j)
+                        apart<0>();
+                    } else {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const float z = acc[i][j][r];
                             acc[i][j][r] = p_weight[i] * exp2_of(near[i] ? fmaf(z, scale, -lse[i]) : fmaf(z, l.inv_tau, -lse[i]) * kLog2E);
                         }
-                    apart<1>();
-                }
-                const float of_row = LISTS ? __shfl(weight[i], row_in(entry)) : weight[i];
-#pragma unroll
-                for (int j = 0; j < FN; ++j) {
+                        apart<1>();
+                    }
                     in_order();
                     put(acc[i][j]);
                     in_order();
                     if constexpr (LISTS) {
-                        each_entry(i, j, [&](uint32_t code, float part) {
-                            const int row = row0 + row_in(code);
-                            const float of = holds && code == entry ? of_row : row_weight(l, g, row, row_state(w, g, row)) * (l.sigma ? l.sigma[g] : 1.0f);
-                            scratch[scratch_at(row_in(code), column_of(code) & 31)] -= of * part;
-                        });
+                        const auto take = [&](uint32_t code, float part, float of) {
+                            if (in_fragment(code, i, j)) scratch[scratch_at(row_in(code), column_of(code) & 31)] -= of * part;
+                        };
+#pragma unroll
+                        for (int k = 0; k < kHeld; ++k)
+                            if (__any(in_fragment(entry[k], i, j))) take(entry[k], entry_share[k], __shfl(weight[i], row_in(entry[k])));
+                        for (int e = 64 * kHeld; e < entries; e += 64) {           // all lanes: a row's weight is another lane's
+                            const uint32_t code = e + lane < entries ? codes[e + lane] : none;
+                            take(code, code == none ? 0.0f : shares[e + lane], __shfl(weight[i], row_in(code)));
+                            // vmcnt(0): else it would be waited for, with the stores, wherever its registers are used next, also when nothing was loaded
+                            __builtin_amdgcn_s_waitcnt(0x0f70);
+                        }
                         in_order();
                     } else if (__any(column >> 5 == j)) {
-                        if (column >> 5 == j && half == 0) scratch[scratch_at(lane, column & 31)] -= of_row;
+                        if (column >> 5 == j && half == 0) scratch[scratch_at(lane, column & 31)] -= weight[i];
                         in_order();
                     }
-                    // what was read of the columns before leaves while these come back
+                    // what was read of the rows before leaves while these come back
                     if (i + j == 0) __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): the next tile's first two steps are here
-                    else store(j == 0 ? i - 1 : i, j == 0 ? FN - 1 : j - 1);
+                    if (i > 0) store(i - 1);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int r = k * 16 + from;
                         z[k] = Eight{{*reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight)), *reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight + 4))}};
                     }
                 }
-            }
-        }
-        if constexpr (BACKWARD) {
-            store(FM - 1, FN - 1);
-            // a lane's column of what 16 groups of lanes have of all columns
-            const auto gather = [&](const v4f (&part)[FN][2], auto join) {
-                in_order();
+                store(FM - 1);
+                // a lane's column of what 16 groups of lanes have of all columns
+                const int n = n_wave + j * 32 + lane;
+                const auto gather = [&](const v4f (&part)[2], auto join) {
+                    in_order();
+                    *reinterpret_cast<v4f *>(scratch + from * 32 + eight) = part[0];
+                    *reinterpret_cast<v4f *>(scratch + from * 32 + eight + 4) = part[1];
+                    in_order();
+                    float v = scratch[half * 8 * 32 + (lane & 31)];
 #pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) *reinterpret_cast<v4f *>(scratch + from * kColumns + j * 32 + eight + c * 4) = part[j][c];
-                in_order();
-                float v = scratch[lane];
-#pragma unroll
-                for (int k = 1; k < 16; ++k) v = join(v, scratch[k * kColumns + lane]);
-                in_order();
-                return v;
-            };
-            if (l.col_sums) {
-                const float v = gather(total, [](float x, float y) { return x + y; });
-                if (n_wave + lane < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n_wave + lane] = v;
-            }
-            if constexpr (SPLIT)
-                if (l.col_max) {
-                    const uint32_t v = __float_as_uint(gather(top, [](float x, float y) { return fmaxf(x, y); }));
-                    if (n_wave + lane < N && v) atomicMax(l.col_max + g * N + n_wave + lane, v);
+                    for (int k = 1; k < 8; ++k) v = join(v, scratch[(half * 8 + k) * 32 + (lane & 31)]);
+                    in_order();
+                    return join(v, __shfl_xor(v, 32));
+                };
+                if (l.col_sums) {
+                    const float v = gather(total, [](float x, float y) { return x + y; });
+                    if (half == 0 && n < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n] = v;
                 }
+                if constexpr (SPLIT)
+                    if (l.col_max) {
+                        const uint32_t v = __float_as_uint(gather(top, [](float x, float y) { return fmaxf(x, y); }));
+                        if (half == 0 && n < N && v) atomicMax(l.col_max + g * N + n, v);
+                    }
+            }
         }
     }
     if constexpr (!BACKWARD) {
