@@ -4,22 +4,22 @@
 namespace gbmuf {
 namespace {
 
-constexpr int kRows = kSmallRows, kWords = kSmallWords, kSlab = kSmallColumns, kThreads = 256, kPitch = kWords + 1;     // + 1: rows of dz are read down their columns too
+constexpr int kWords = kSmallWords, kSlab = kSmallColumns, kThreads = 256, kPitch = kWords + 1;     // + 1: rows of dz are read down their columns too
 
 // 64 rows of kSlab values as f32, the 16-byte chunk c of row r at place c ^ (r % 16): 16 rows lie in all banks at any chunk.
 __device__ __forceinline__ int slab_at(int r, int k) { return r * kSlab + (((k >> 2) ^ (r & 15)) << 2) + (k & 3); }
 
-// A thread's share of a slab on its way to LDS: 4 values of every 16th row.
-template <int T>
+// A thread's share of a slab of R rows on its way to LDS: 4 values of every 16th row.
+template <int T, int R>
 struct Slab {
-    v4f v[4];
+    v4f v[R / 16];
 
     // rows behind the last are read as the last one, and what lies behind the columns as zeros
     __device__ __forceinline__ void load(const void *p, int64_t ld, int rows, int K)
     {
         const int k = static_cast<int>(threadIdx.x & 15) * 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R / 16; ++i) {
             const int64_t at = min(i * 16 + static_cast<int>(threadIdx.x >> 4), rows - 1) * ld + k;
             v[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
             if (k + 4 <= K) v[i] = read4<T>(p, at);
@@ -34,7 +34,7 @@ struct Slab {
     __device__ __forceinline__ void put(float *lds, const int32_t *keep) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R / 16; ++i) {
             const int r = i * 16 + static_cast<int>(threadIdx.x >> 4);
             const bool is = !keep || keep[r] != kDead;
             *reinterpret_cast<v4f *>(lds + slab_at(r, static_cast<int>(threadIdx.x & 15) * 4)) =
@@ -52,25 +52,28 @@ __device__ __forceinline__ v16f zeros()
 }
 
 // A workgroup takes 64 words for all rows: z = x w' first, then dz in LDS, and from it dw = dz' x, which is whole, and its part of dx = dz w, which
-// another launch adds up.  Everything is f32, every operand is read once.  Bound by its chain of loads and 96 matrix instructions a wave.  us, with that launch /
-// by the three launches of larger sizes (dz, both products, joining), workers x rows x vocabulary x features: f16 4 x 40 x 1000 x 64 16.6 / 22.1, f32 1 x 8 x 1000 x 64 15
-// / 20.6, 4 x 64 x 200 x 64 17 / 18, 1 x 64 x 10000 x 64 17 / 26, 1 x 16 x 100,000 x 64 60 / 76; in turns of 64 features, with x and w read twice, 128 of them gained
-// nothing (f32 2 x 48 x 3000 x 128 23.6 / 25.4, f16 26.4 / 26.0), 256 lost (f32 1 x 64 x 10000 x 256 42 / 34).
-template <int T>
+// another launch adds up.  Bound by its chain of loads, barriers and 96 matrix instructions a wave (up to 32 rows 32 fewer, on two waves), which 3 workgroups
+// of 49 KB on a CU, of up to 32 rows 4 of 33 KB, do beside each other.  us, with that launch / by the launches of larger sizes (dz, both products, joining),
+// workers x rows x vocabulary x features: f16 4 x 40 x 1000 x 64 16.6 / 24, bf16 8 x 40 x 20000 x 64 72 / 76, 8 x 7 x 20000 x 64 46 / 67, 8 x 24 x 20000 x 50 57 / 79, 8 x 7 x
+// 63165 x 37 134 / 202, f32 1 x 8 x 1000 x 64 15 / 20.6, 4 x 64 x 200 x 64 17 / 18, 1 x 64 x 10000 x 64 17 / 26, 1 x 16 x 100,000 x 64 39 / 76; in turns of 64 features, with x and w read
+// twice, 128 of them gained nothing (f32 2 x 48 x 3000 x 128 23.6 / 25.4, f16 26.4 / 26.0), 256 lost (f32 1 x 64 x 10000 x 256 42 / 34).
+template <int T, int ROWS>
 __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
 {
-    __shared__ __align__(16) float xs[kRows * kSlab], ws[kWords * kSlab];
-    __shared__ float dz[kRows * kPitch];
-    __shared__ int32_t states[kRows];
-    __shared__ float weights[kRows];
+    __shared__ __align__(16) float xs[ROWS * kSlab], ws[kWords * kSlab];
+    __shared__ float dz[ROWS * kPitch];
+    __shared__ int32_t states[ROWS];
+    __shared__ float weights[ROWS];
     const LossArgs &l = a.l;
     const Words &w = l.words;
     const int64_t g = blockIdx.y;
     const int n0 = static_cast<int>(blockIdx.x) * kWords, words = min(kWords, w.vocab - n0), M = w.rows, K = a.columns;
-    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6, wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
+    const int rows = (M + 7) / 8 * 8;                       // sums over rows end here; a wave of rows that are not there has nothing to do with them
     const typename Num<T>::type *x = static_cast<const typename Num<T>::type *>(a.x) + g * a.x_batch,
                                 *wp = static_cast<const typename Num<T>::type *>(a.w) + g * a.w_batch + static_cast<int64_t>(n0) * a.ldw;
-    Slab<T> sx, sw;
+    Slab<T, ROWS> sx;
+    Slab<T, kWords> sw;
     if (K > 0) {
         sx.load(x, a.ldx, M, K);
         sw.load(wp, a.ldw, words, K);
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
             for (int c = 0; c < 3; ++c)
                 if (n + c < words) bias[q][c] = load_one(l.bias, g * l.bias_batch + n0 + n + c, T);
     }
-    if (threadIdx.x < kRows) {
+    if (threadIdx.x < ROWS) {
         const int m = threadIdx.x;
         states[m] = m >= M ? kDead : w.logit ? given_state(w, g, m) : row_state(w, g, m);
     }
@@ -99,6 +102,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
         sx.put(xs, states);
         sw.put(ws, nullptr);
         __syncthreads();
+        if (wm < M)
 #pragma unroll
         for (int t = 0; t < kSlab / 8; ++t) {
             const v4f p = *reinterpret_cast<const v4f *>(xs + slab_at(wm + (lane & 31), (2 * t + half) * 4)),
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
             for (int c = 0; c < 4; ++c) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(q[c], p[c], acc, 0, 0, 0);
         }
     }
-    {
+    if (wm < M) {
         const int state = states[m_lane];
         const float weight = state == kDead ? 0.0f : state == kLive ? dloss * l.tau : __builtin_nanf("");
         if (wn == 0 && half == 0) weights[m_lane] = weight;
@@ -120,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
     }
     __syncthreads();
     // the words that a row is held to, in their order, by one lane
-    if (threadIdx.x < kRows && states[threadIdx.x] != kDead) {
+    if (threadIdx.x < ROWS && states[threadIdx.x] != kDead) {
         const int m = threadIdx.x;
         const float weight = weights[m];
         float *row = dz + m * kPitch;
@@ -144,7 +148,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
     if (a.dbias && threadIdx.x < static_cast<unsigned>(words)) {
         float v = 0.0f;
 #pragma unroll 8
-        for (int m = 0; m < kRows; ++m) v += dz[m * kPitch + threadIdx.x];
+        for (int m = 0; m < rows; ++m) v += dz[m * kPitch + threadIdx.x];
         const int64_t at = g * a.dbias_batch + n0 + threadIdx.x;
         if (a.accumulate) v += load_one(a.dbias, at, a.grad_type);
         store_one(a.dbias, at, a.grad_type, v);
@@ -154,8 +158,8 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
     const int k = wn + (lane & 31);
     if (a.dw) {
         v16f out = zeros();
-#pragma unroll 8
-        for (int m = 0; m < kRows; m += 2)
+#pragma unroll 4
+        for (int m = 0; m < rows; m += 2)
             out = __builtin_amdgcn_mfma_f32_32x32x2f32(dz[(m + half) * kPitch + wm + (lane & 31)], xs[slab_at(m + half, k)], out, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -165,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
             store_one(a.dw, at, a.grad_type, a.accumulate ? out[r] + load_one(a.dw, at, a.grad_type) : out[r]);
         }
     }
-    if (a.parts) {
+    if (a.parts && wm < M) {
         v16f out = zeros();
 #pragma unroll 8
         for (int n = 0; n < kWords; n += 2)
@@ -206,8 +210,11 @@ int launch_small_grads(const SmallGrads &a, hipStream_t stream)
     if (a.pieces <= 0 || a.batch <= 0) return GBMUF_OK;
     SmallGrads args = a;
     void *argv[] = {&args};
-    const int32_t type = a.l.type;
-    const auto fn = type == kF32 ? small_grads_kernel<kF32> : type == kBf16 ? small_grads_kernel<kBf16> : small_grads_kernel<kF16>;
+    using Fn = void (*)(SmallGrads);
+    static constexpr Fn fns[3][2] = {{small_grads_kernel<kF32, kSmallRows>, small_grads_kernel<kF32, kSmallRows / 2>},
+                                     {small_grads_kernel<kBf16, kSmallRows>, small_grads_kernel<kBf16, kSmallRows / 2>},
+                                     {small_grads_kernel<kF16, kSmallRows>, small_grads_kernel<kF16, kSmallRows / 2>}};
+    const Fn fn = fns[a.l.type][2 * a.l.words.rows <= kSmallRows ? 1 : 0];
     const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(a.pieces), static_cast<unsigned>(a.batch)), dim3(kThreads), argv, 0, stream);
     if (err != hipSuccess) return hip_failed("hipLaunchKernel(small gradients)", err, GBMUF_EDEVICE);
     return launch_join_parts(a, a.pieces, stream);
