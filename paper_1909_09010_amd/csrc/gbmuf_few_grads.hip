@@ -1,4 +1,4 @@
-// gbmuf_few_grads.hip -- f32 gradients of losses of up to 8 rows against any vocabulary: w is read from memory once, and dw written once.
+// gbmuf_few_grads.hip -- gradients of losses of up to 8 rows against any vocabulary: w is read from memory once, and dw written once.
 #include "gbmuf_few.h"
 
 namespace gbmuf {
@@ -6,33 +6,37 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kWords = kFewGradWords, kTilesN = kWords / 16, kPitch = kWords + 4;
 
-template <int C>
-__device__ __forceinline__ void read_columns(const float *p, int left, float (&v)[C])
+template <int T, int C>
+__device__ __forceinline__ void read_columns(const void *p, int64_t i, int left, float (&v)[C])
 {
-    typedef float Piece __attribute__((ext_vector_type(C), aligned(4)));
+    using N = typename Num<T>::type;
+    typedef N Piece __attribute__((ext_vector_type(C), aligned(sizeof(N))));
+    const N *from = static_cast<const N *>(p) + i;
     if (left >= C) {
-        const Piece r = *reinterpret_cast<const Piece *>(p);
+        const Piece r = *reinterpret_cast<const Piece *>(from);
 #pragma unroll
-        for (int c = 0; c < C; ++c) v[c] = r[c];
+        for (int c = 0; c < C; ++c) v[c] = static_cast<float>(r[c]);
     } else {
 #pragma unroll
-        for (int c = 0; c < C; ++c) v[c] = c < left ? p[c] : 0.0f;
+        for (int c = 0; c < C; ++c) v[c] = c < left ? static_cast<float>(from[c]) : 0.0f;
     }
 }
 
-template <int C>
-__device__ __forceinline__ void write_columns(float *p, int left, const float (&v)[C])
+template <int T, int C>
+__device__ __forceinline__ void write_columns(void *p, int64_t i, int left, const float (&v)[C])
 {
-    typedef float Piece __attribute__((ext_vector_type(C), aligned(4)));
+    using N = typename Num<T>::type;
+    typedef N Piece __attribute__((ext_vector_type(C), aligned(sizeof(N))));
+    N *to = static_cast<N *>(p) + i;
     if (left >= C) {
         Piece r;
 #pragma unroll
-        for (int c = 0; c < C; ++c) r[c] = v[c];
-        *reinterpret_cast<Piece *>(p) = r;
+        for (int c = 0; c < C; ++c) r[c] = static_cast<N>(v[c]);
+        *reinterpret_cast<Piece *>(to) = r;
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (c < left) p[c] = v[c];
+            if (c < left) to[c] = static_cast<N>(v[c]);
     }
 }
 
@@ -41,20 +45,19 @@ __device__ __forceinline__ void write_columns(float *p, int left, const float (&
 // columns of x, dx's sums go on in registers over all pieces: 2 ROWS C multiply-adds a word and thread, 0.1 us a word of 1024 columns and CU for 8 rows, where
 // its 4 KB read and 4 KB written take 0.32 at 6.5 TB/s.  `lanes` threads have a word's columns, the others further words.  Bound by w's way from memory.  us, this /
 // the routes of more rows: 2 x 1 x 54538 x 241 78 / 142, 1 x 8 x 50000 x 1024 154 / 207, 9 x 6 x 5250 x 74 32 / 42, 1 x 1 x 2368 x 256 21 / 28, 1 x 3 x 300 x 700 as
-// long.  16-bit types were slower than laying w out, 16 rows short of registers: they take those routes.
-template <int ROWS, int C>
+// long.  16 rows are short of registers.  Values of w and dw are of type T and D.
+template <int T, int D, int ROWS, int C>
 __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, int32_t lanes)
 {
-    constexpr int T = kF32, kStep = 16, kUnroll = 2, kAhead = 4;
-    constexpr size_t kBytes = sizeof(float);
+    constexpr int kStep = T == kF32 ? 16 : 32, kUnroll = 2, kAhead = 4;
+    constexpr size_t kBytes = sizeof(typename Num<T>::type);
     __shared__ __align__(16) float part[kWaves][16 * kPitch];
     __shared__ __align__(16) float dz[kWords][ROWS];
     const LossArgs &l = a.l;
     const Words &w = l.words;
     const int64_t g = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, M = w.rows, K = a.columns, V = w.vocab;
-    const float *xp = static_cast<const float *>(a.x) + g * a.x_batch, *wp = static_cast<const float *>(a.w) + g * a.w_batch;
-    float *dw = static_cast<float *>(a.dw) + g * a.dw_batch;
+    const char *wp = static_cast<const char *>(a.w) + g * a.w_batch * kBytes;
 
     // a thread's columns of the rows that count
     const int groups = kThreads / lanes, group = static_cast<int>(threadIdx.x) / lanes, k_mine = static_cast<int>(threadIdx.x) % lanes * C, left = K - k_mine;
@@ -64,7 +67,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
         const bool is = m < M && left > 0 && row_state(w, g, m) != kDead;
 #pragma unroll
         for (int c = 0; c < C; ++c) x[m][c] = dx[m][c] = 0.0f;
-        if (is) read_columns<C>(xp + m * a.ldx + k_mine, left, x[m]);
+        if (is) read_columns<T, C>(a.x, g * a.x_batch + m * a.ldx + k_mine, left, x[m]);
     }
     // what the row of the logits that a thread finishes brings along
     const int m_z = static_cast<int>(threadIdx.x) / (kWords / 4), mc = min(m_z, M - 1), state = m_z < M ? row_state(w, g, mc) : kDead;
@@ -78,7 +81,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
         v4f acc[kTilesN];
 #pragma unroll
         for (int j = 0; j < kTilesN; ++j) {
-            ws[j] = reinterpret_cast<const char *>(wp) + static_cast<int64_t>(min(n0 + j * 16 + (lane & 15), V - 1)) * a.ldw * kBytes;
+            ws[j] = wp + static_cast<int64_t>(min(n0 + j * 16 + (lane & 15), V - 1)) * a.ldw * kBytes;
             acc[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         }
         for (int k0 = wave * kStep * kUnroll; k0 < K; k0 += kWaves * kStep * kUnroll) {
@@ -146,8 +149,8 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
 #pragma unroll
             for (int m = 0; m < ROWS; ++m) v += dz[threadIdx.x][m];
             const int64_t at = g * a.dbias_batch + n0 + threadIdx.x;
-            if (a.accumulate) v += load_one(a.dbias, at, T);
-            store_one(a.dbias, at, T, v);
+            if (a.accumulate) v += load_one(a.dbias, at, D);
+            store_one(a.dbias, at, D, v);
         }
         if (left > 0)
             for (int n = group; n < words; n += kAhead * groups) {
@@ -156,8 +159,8 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
                     const int64_t row = n0 + min(n + u * groups, words - 1);
-                    if (a.parts) read_columns<C>(wp + row * a.ldw + k_mine, left, v[u]);
-                    if (a.dw && a.accumulate) read_columns<C>(dw + row * a.lddw + k_mine, left, was[u]);
+                    if (a.parts) read_columns<T, C>(wp, row * a.ldw + k_mine, left, v[u]);
+                    if (a.dw && a.accumulate) read_columns<D, C>(a.dw, g * a.dw_batch + row * a.lddw + k_mine, left, was[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
                         if (a.accumulate)
 #pragma unroll
                             for (int c = 0; c < C; ++c) out[c] += was[u][c];
-                        write_columns<C>(dw + static_cast<int64_t>(n0 + word) * a.lddw + k_mine, left, out);
+                        write_columns<D, C>(a.dw, g * a.dw_batch + static_cast<int64_t>(n0 + word) * a.lddw + k_mine, left, out);
                     }
                 }
             }
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, in
     float *to = a.parts + ((static_cast<int64_t>(blockIdx.x) * groups + group) * gridDim.y + g) * M * K;
 #pragma unroll
     for (int m = 0; m < ROWS; ++m)
-        if (m < M) write_columns<C>(to + static_cast<int64_t>(m) * K + k_mine, left, dx[m]);
+        if (m < M) write_columns<kF32, C>(to, static_cast<int64_t>(m) * K + k_mine, left, dx[m]);
 }
 
 }  // namespace
@@ -208,7 +211,12 @@ int launch_few_grads(const SmallGrads &a, int32_t workgroups, hipStream_t stream
     SmallGrads args = a;
     int32_t lanes = few_grads_lanes(a.columns);
     void *argv[] = {&args, &lanes};
-    const void *fn = reinterpret_cast<const void *>(a.l.words.rows <= 4 ? few_grads_kernel<4, 4> : few_grads_kernel<8, 4>);
+    using Fn = void (*)(SmallGrads, int32_t);
+    // [type][gradients in f32][more than 4 rows]
+    static constexpr Fn fns[3][2][2] = {{{}, {few_grads_kernel<kF32, kF32, 4, 4>, few_grads_kernel<kF32, kF32, 8, 4>}},
+                                        {{few_grads_kernel<kBf16, kBf16, 4, 4>, few_grads_kernel<kBf16, kBf16, 8, 4>}, {few_grads_kernel<kBf16, kF32, 4, 4>, few_grads_kernel<kBf16, kF32, 8, 4>}},
+                                        {{few_grads_kernel<kF16, kF16, 4, 4>, few_grads_kernel<kF16, kF16, 8, 4>}, {few_grads_kernel<kF16, kF32, 4, 4>, few_grads_kernel<kF16, kF32, 8, 4>}}};
+    const void *fn = reinterpret_cast<const void *>(fns[a.l.type][a.grad_type == kF32 ? 1 : 0][a.l.words.rows > 4 ? 1 : 0]);
     const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(workgroups), static_cast<unsigned>(a.batch)), dim3(kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(few rows' gradients)", err, GBMUF_EDEVICE);
 }

@@ -424,8 +424,15 @@ bool is_small(const gbmuf_linear_desc_t &d)
            static_cast<double>(small_pieces(d)) * d.batch * static_cast<double>(d.rows) * static_cast<double>(d.in_features) * 4.0 <= static_cast<double>(kSmallParts);
 }
 
-// f32, up to 8 rows: w is read from memory once, by workgroups that each walk pieces of the vocabulary.
-bool is_few(const gbmuf_linear_desc_t &d) { return d.dtype == GBMUF_F32 && d.rows <= kFewGradRows && d.rows > 0 && d.in_features <= kFewGradColumns && d.out_features > 0; }
+// Up to 8 rows: w is read from memory once, by workgroups that each walk pieces of the vocabulary; of 16-bit types while w is not more than 64 MB.  us, this / laid
+// out: bf16 1 x 2 x 1000 x 256 18 / 25, 4 x 8 x 5000 x 512 41 / 48, 2 x 8 x 20000 x 304 61 / 56, f16 8 x 6 x 3000 x 301 42 / 59, bf16 1 x 8 x 30000 x 1024 82 / 91, 4 x 5 x 12800 x
+// 832 156 / 99, 8 x 4 x 10000 x 640 164 / 110; f32 1 x 8 x 50000 x 1024 154 / 207.
+constexpr double kFewGradValues = 1 << 25;
+bool is_few(const gbmuf_linear_desc_t &d)
+{
+    const double values = static_cast<double>(d.batch) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
+    return d.rows <= kFewGradRows && d.rows > 0 && d.in_features <= kFewGradColumns && d.out_features > 0 && (d.dtype == GBMUF_F32 || values <= kFewGradValues);
+}
 int64_t few_workgroups(const gbmuf_linear_desc_t &d)
 {
     const int64_t pieces = (d.out_features + kFewGradWords - 1) / kFewGradWords;
