@@ -544,6 +544,54 @@ def test_infinities_and_nan(size, dtype):
     assert (b[0] == -INF).all() and torch.isnan(a[0]).all()
 
 
+# up to 8 rows of more than 64 features, and 33 rows, which are more than half of what a workgroup has
+FEW = [(2, 5, 300, 72), (1, 8, 1067, 200), (3, 1, 130, 129), (2, 33, 300, 50)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", FEW)
+@pytest.mark.parametrize("top", [0, 4])
+def test_few_rows(size, dtype, top):
+    for f32_grads, accumulate in ((False, False), (True, False), (False, True), (True, True)):
+        run_case(Case(*size, dtype, top=top, tau=1.0 if top == 0 else 1.5, seed=4, ignored=0.1), f32_grads=f32_grads, accumulate=accumulate)
+    for want in (("dx",), ("dw",), ("dbias",), ("dw", "dbias")):
+        run_case(Case(*size, dtype, top=top, seed=5), want=want)
+    test_no_row_counts(size, dtype, top)
+    test_forbidden_words(size, dtype, top, "-inf")
+    if size[1] < 4:                                         # the others write into rows 0 to 3
+        return
+    test_words_beyond_the_vocabulary(size, dtype, top)
+    test_infinities_and_nan(size, dtype)
+    if top:
+        test_teachers_words_in_any_order_absent_and_twice(size, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(2, 5, 300, 72), (1, 8, 1067, 200), (2, 32, 300, 50)])
+@pytest.mark.parametrize("top", [0, 4])
+def test_few_rows_that_do_not_count(size, dtype, top):
+    test_rows_that_do_not_count_may_hold_anything(size, dtype, top)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("top", [5, 90])
+def test_windows_of_more_than_a_tile(dtype, top):
+    """So large a vocabulary that a window of the lists holds the columns of two waves."""
+    run_case(Case(1, 70, 600001, 16, dtype, top=top, tau=2.0, seed=6))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_all_rows_are_held_to_the_same_words(dtype):
+    """Lists that lie in one window each: more words of a wave's rows and columns than are held at hand."""
+    c = Case(1, 300, 700, 40, dtype, top=9, seed=7)
+    c.words = torch.where(c.words < 0, c.words, 130 + torch.arange(9, device=DEV) * 2)
+    run_case(c)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("size", [(1, 40, 500, 64), (1, 700, 1500, 200)])
