@@ -513,12 +513,12 @@ typedef struct gbmuf_loss_grad_io {
  * Sums of products and everything that comes of them are held in f32; operands of type f32 are taken apart as in gbmuf_linear.
  * Backward: dz[v] = dloss tau (exp(z[v] / tau - lse) - sum of the q_j with t_j = v)   (cross entropy: q = 1 for the word, tau = 1)
  *     dx = dz w,   dw = dz' x,   dbias[v] = sum_i dz[i,v]
- *   for each worker by itself.  With bf16 and f16 large sizes round dz to dtype once before the products of dx and dw (f16: times a power of two, the same
- *   for all rows of a worker, that takes its largest below 2^15; values below 2^-39 of the largest |dloss tau| are lost), small ones do not; dbias sums what was
+ *   for each worker by itself.  With bf16 and f16 large sizes round dz to dtype once before the products of dx and dw, times a factor of the worker
+ *   that takes its largest |dloss tau| to 1 (f16: 2^14; values below 2^-39 of it are lost) and is taken out again afterwards; small ones do not; dbias sums what was
  *   not rounded.  No gradient is formed of the teacher's logits.
  * Equal calls give equal bits.
  * Workspace and errors as for gbmuf_linear; EINVAL also for a top or temperature that the loss does not take (top 0 asks gbmuf_loss_workspace for
- * cross entropy's bytes), EUNSUPPORTED for top above GBMUF_MAX_TOP, temperatures beyond 2^-40 .. 2^40 and batch * rows above 2^29.
+ * cross entropy's bytes), EUNSUPPORTED for top above GBMUF_MAX_TOP, temperatures beyond 2^-40 .. 2^40 and batch * rows above 2^28 (distillation: 2^25).
  */
 int gbmuf_loss_workspace(const gbmuf_loss_desc_t *desc, int32_t backward, int64_t *bytes);
 int gbmuf_cross_entropy(const gbmuf_loss_desc_t *desc, const gbmuf_loss_io_t *io, void *workspace, int64_t workspace_bytes, void *stream);

@@ -149,7 +149,7 @@ struct LossArgs {
     int32_t first;
     float inv_tau, tau;
     WordLists lists;         // of tiles of many rows; code nullptr: rows have one word each
-    int32_t walk, reserved1; // tiles of logits that a workgroup takes one after the other
+    int32_t walk, most_parts; // walk: tiles of logits that a workgroup takes one after the other
     // forward: parts[g][part][row], counted over the vocabulary from first_tile on, and z of the rows' words, at[g][row][top]
     float2 *parts;
     float *at;
@@ -157,7 +157,8 @@ struct LossArgs {
     // backward: dz[g][row][column], rows dz_ld apart, whole pieces of 8 up to there
     const float *lse, *dloss;
     int64_t lse_ld, lse_batch, dloss_ld, dloss_batch;
-    const float *sigma;      // [g]: a power of two that dz is multiplied with, or nullptr
+    const float *most;       // 16-bit types, [g][kMostParts]: largest weights of most_parts parts of a worker's rows, or nullptr
+    float *factor;           // out, [g]: 1 / what dz is multiplied with for that
     void *dz;
     int64_t dz_ld, dz_batch;
     int32_t dz_type, streamed;      // streamed: dz is more than the caches hold
@@ -189,7 +190,8 @@ struct LossJoin {
     float inv_tau, tau;
 };
 
-// Rows of x that count, at aligned places with zeros behind them, zeros in place of the others; and for f16 the power of two that a worker's dz takes.
+// Rows of x that count, at aligned places with zeros behind them, zeros in place of the others; and for 16-bit types the largest weight of parts of a worker's rows.
+constexpr int kMostParts = 64;
 struct KeepArgs {
     Words words;
     const void *x;
@@ -201,8 +203,8 @@ struct KeepArgs {
     const float *dloss;
     int64_t dloss_ld, dloss_batch;
     float tau;
-    int32_t reserved;
-    float *sigma;            // [batch], and behind them 1 / sigma; or nullptr
+    int32_t most_parts;
+    float *most;             // [batch][kMostParts], or nullptr
     uint32_t *row_max;       // [batch][rows]: bits of what no value of the row's dz exceeds; or nullptr
 };
 

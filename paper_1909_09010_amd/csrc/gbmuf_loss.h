@@ -53,6 +53,27 @@ __device__ __forceinline__ float row_weight(const LossArgs &a, int64_t g, int m,
     return state == kDead ? 0.0f : state == kLive ? d : __builtin_nanf("");
 }
 
+// Maximum of WIDTH neighbouring lanes.
+template <int WIDTH>
+__device__ __forceinline__ float max_of(float v)
+{
+#pragma unroll
+    for (int d = 1; d < WIDTH; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+// What 16-bit dz, no value of which exceeds the worker's largest weight, is multiplied with, and 1 / that: f16's range is filled from above, so that what a row has
+// below 2^-39 of that weight is nothing; and -weight, which every row's own word has nearly, is a number of the type.  As it is, equal weights (1 / rows) would all be
+// rounded the same way, by up to half a unit, and so would be the gradients: by 0.3 % for 895 rows in bf16.
+template <int T>
+__device__ __forceinline__ float2 dz_scale(float most)
+{
+    if (!(most > 0.0f)) return float2{1.0f, 1.0f};
+    const int e = ilogbf(most), s = max(-112, min(126, (T == kF16 ? 14 : 0) - e));
+    const float part = ldexpf(most, -e);                   // 1 .. 2
+    return float2{ldexpf(1.0f / part, s), ldexpf(part, -s)};
+}
+
 // Two parts of a softmax's sum: (largest logit, sum of exp of the logits less that, or of themselves where that is infinite).
 __device__ __forceinline__ float2 join_stats(float2 a, float2 b, float scale)
 {
@@ -157,7 +178,6 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
     };
 
     const float scale = a.inv_tau * kLog2E;
-    const float sigma = BACKWARD && a.sigma ? a.sigma[g] : 1.0f;
     Eight total{};
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
@@ -203,7 +223,7 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
         } else {
             constexpr int kLanes = kColumns / 8, kTogether = 64 / kLanes, kTurns = 32 / kTogether;
             const float lse = a.lse[g * a.lse_batch + mc * a.lse_ld];
-            const float weight = row_weight(a, g, mc, state[i]) * sigma;
+            const float weight = row_weight(a, g, mc, state[i]);
             if (a.live && tile.tn == 0 && wave / WM == 0 && half == 0 && m < M) a.live[g * w.rows + m] = state[i];
 #pragma unroll
             for (int j = 0; j < FN; ++j)

@@ -24,7 +24,7 @@ int check_desc(const gbmuf_loss_desc_t *d, bool distill, Loss &l)
     if (d->batch > 65535 || d->rows > kLargest / 2 - 64 || d->vocab > kLargest / 2 - 64 || d->in_features > kLargest / 2 - 64) return GBMUF_EUNSUPPORTED;
     const int64_t M = d->rows, N = d->vocab, K = d->in_features, G = d->batch;
     if (too_many_tiles(M, N, G) || too_many_tiles(M, K, G) || too_many_tiles(N, K, G) || d->top > kMostTop) return GBMUF_EUNSUPPORTED;
-    if (static_cast<double>(M) * static_cast<double>(G) > 0x1p29) return GBMUF_EUNSUPPORTED;
+    if (static_cast<double>(M) * static_cast<double>(G) > (distill ? 0x1p25 : 0x1p28)) return GBMUF_EUNSUPPORTED;          // what launches over rows may have
     // 1 / tau, tau^2 and what they are multiplied with stay in f32's range
     if (distill && !(d->temperature >= 0x1p-40f && d->temperature <= 0x1p40f)) return GBMUF_EUNSUPPORTED;
     l = Loss{};
@@ -497,7 +497,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
             if (workers > 0 && n > 0) parts = std::max({parts, shape_of(M, K, n, workers, split).partial, shape_of(n, K, M, workers, split).partial});
     float *partial = space.take<float>(parts);
     char *kept_x = space.take<char>(G * M * kept * static_cast<int64_t>(type_bytes(type)));
-    float *sigma = space.take<float>(type == kF16 ? 2 * G : 0);
+    float *most = space.take<float>(split ? 0 : G * (kMostParts + 1)), *factors = split ? nullptr : most + G * kMostParts;
     char *dz = space.take<char>(PG * M * ld * static_cast<int64_t>(type_bytes(type)));
     const bool several = PN < N;
     float *dx_sums = space.take<float>(several && !split ? PG * M * K : 0);
@@ -530,7 +530,8 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
     keep.columns = static_cast<int32_t>(K); keep.batch = G; keep.type = type;
     keep.dloss = static_cast<const float *>(out.dloss.data); keep.dloss_ld = out.dloss.ld; keep.dloss_batch = out.dloss.batch_stride;
     keep.tau = l.tau;
-    keep.sigma = type == kF16 ? sigma : nullptr;
+    keep.most_parts = static_cast<int32_t>(std::min<int64_t>((M + 2047) / 2048, kMostParts));
+    keep.most = split || M == 0 ? nullptr : most;
     keep.row_max = dz_rows;
     if ((rc = launch_keep(keep, stream)) != GBMUF_OK) return rc;
     const gbmuf_matrix_t kept_m{kept_x, kept, M * kept};
@@ -587,14 +588,17 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         a.walk = c.t.steps;
         a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld; a.dz_type = type;
         a.streamed = p.workers * M * pld * static_cast<int64_t>(type_bytes(type)) > kCached ? 1 : 0;
-        if (type == kF16) a.sigma = sigma + p.g;
+        if (!split) {
+            a.most = most + p.g * kMostParts; a.most_parts = keep.most_parts;
+            a.factor = factors + p.g;
+        }
         if (db) a.col_sums = sums;
         if (split && dw) a.col_max = max;
         if ((r = launch_vocab(logits_args(px, pw, K, type, c), a, type, c.tile, true, stream)) != GBMUF_OK) return r;
 
         const gbmuf_matrix_t dzm{dz, pld, M * pld}, pdx = part(out.dx, p.g, 0, type), pdw = part(out.dw, p.g, p.v, grad_type),
                              pdb = vector_part(out.dbias, p.g, p.v, grad_type);
-        const float *factor = type == kF16 ? sigma + G + p.g : nullptr;
+        const float *factor = split || M == 0 ? nullptr : factors + p.g;         // M: else nobody writes it
         SumArgs s{};
         s.sums = sums; s.out = pdb.data; s.out_batch = pdb.batch_stride;
         s.C = static_cast<int32_t>(p.words); s.tiles = 2 * c.t.tiles_m;

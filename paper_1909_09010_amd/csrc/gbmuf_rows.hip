@@ -4,20 +4,12 @@
 namespace gbmuf {
 namespace {
 
-// Sums and maxima of WIDTH neighbouring lanes.
+// Sum of WIDTH neighbouring lanes.
 template <int WIDTH>
 __device__ __forceinline__ float sum_of(float v)
 {
 #pragma unroll
     for (int d = 1; d < WIDTH; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
-template <int WIDTH>
-__device__ __forceinline__ float max_of(float v)
-{
-#pragma unroll
-    for (int d = 1; d < WIDTH; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
     return v;
 }
 
@@ -289,9 +281,8 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
 }
 
 // ---------------------------------------------------------------------------------------
-// Rows of x: zeros where a row does not count, whatever it holds, since 0 times that is not always 0.  8 columns a thread.  The last `batch` workgroups, where
-// sigma is wanted, find the power of two that takes the largest finite weight of a worker's rows below 2^15: with it dz, whose values are
-// at most that, fills f16's range from above, and what a row has below 2^-39 of the largest weight is nothing.
+// Rows of x: zeros where a row does not count, whatever it holds, since 0 times that is not always 0.  8 columns a thread.  The last workgroups, where
+// `most` is wanted, `most_parts` for each worker, find the largest finite weight of rows that count.
 // ---------------------------------------------------------------------------------------
 template <int T>
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
@@ -333,28 +324,28 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
         write8<T>(a.out, row * a.out_ld + c, v);
         return;
     }
-    const int64_t g = block - copies;
-    if (g >= a.batch || !a.sigma) return;
+    if (!a.most) return;
+    const int64_t of = block - copies, g = of / a.most_parts;
+    if (g >= a.batch) return;
+    const int part = static_cast<int>(of - g * a.most_parts), rows = a.words.rows;
     __shared__ float waves[4];
     float most = 0.0f;
-    for (int m = threadIdx.x; m < a.words.rows; m += 256) {
-        const float d = fabsf(a.dloss[g * a.dloss_batch + m * a.dloss_ld] * a.tau);
-        if (d < __builtin_inff() && row_state(a.words, g, m) == kLive) most = fmaxf(most, d);
-    }
+    for (int64_t first = part * 256; first < rows; first += a.most_parts * 256 * 8)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                       // rows behind the last are read as the last one
+            const int m = static_cast<int>(min(first + k * a.most_parts * 256 + static_cast<int>(threadIdx.x), static_cast<int64_t>(rows - 1)));
+            const float d = fabsf(a.dloss[g * a.dloss_batch + m * a.dloss_ld] * a.tau);
+            if (row_state(a.words, g, m) == kLive && d < __builtin_inff()) most = fmaxf(most, d);
+        }
     most = max_of<64>(most);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    most = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
-    const int e = most > 0.0f ? 14 - ilogbf(most) : 0;
-    const int s = e > 126 ? 126 : e < -112 ? -112 : e;
-    a.sigma[g] = ldexpf(1.0f, s);
-    a.sigma[a.batch + g] = ldexpf(1.0f, -s);
+    if (threadIdx.x == 0) a.most[g * kMostParts + part] = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
 }
 
 __global__ __launch_bounds__(256) void cast_kernel(CastArgs a)
 {
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, per_row = (a.columns + 7) / 8, row = id / per_row;
+    const int64_t id = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 256 + threadIdx.x, per_row = (a.columns + 7) / 8, row = id / per_row;
     if (row >= static_cast<int64_t>(a.rows) * a.batch) return;
     const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
     const int64_t g = row / a.rows, to = g * a.batch_stride + (row - g * a.rows) * a.ld + c, from = row * a.columns + c;
@@ -408,7 +399,7 @@ int launch_loss_join(const LossJoin &a, hipStream_t stream)
 int launch_keep(const KeepArgs &a, hipStream_t stream)
 {
     int64_t copies = (static_cast<int64_t>(a.words.rows) * a.batch * (a.out_ld / 8) + 255) / 256;
-    const int64_t blocks = copies + (a.sigma ? a.batch : 0);
+    const int64_t blocks = copies + (a.most ? static_cast<int64_t>(a.batch) * a.most_parts : 0);
     if (blocks <= 0) return GBMUF_OK;
     KeepArgs args = a;
     void *argv[] = {&args, &copies};
@@ -423,10 +414,11 @@ int launch_cast(const CastArgs &a, hipStream_t stream)
 {
     const int64_t blocks = (static_cast<int64_t>(a.rows) * a.batch * ((a.columns + 7) / 8) + 255) / 256;
     if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
     CastArgs args = a;
     void *argv[] = {&args};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(cast_kernel), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    const int64_t across = blocks < (1 << 22) ? blocks : 1 << 22;
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(cast_kernel), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
+                                           dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(cast)", err, GBMUF_EDEVICE);
 }
 

@@ -122,6 +122,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
 
     // what a row brings along
     const float scale = l.inv_tau * kLog2E;
+    float2 sigma{1.0f, 1.0f};
+    if constexpr (BACKWARD && !SPLIT) {
+        sigma = dz_scale<T>(max_of<64>(lane < l.most_parts ? l.most[g * kMostParts + lane] : 0.0f));
+        if (share.at.tm == 0 && share.at.tn == 0 && threadIdx.x == 0) l.factor[g] = sigma.y;
+    }
     float2 stats[FM];                                     // forward: as join_stats has them, of the lane's own columns
     float weight[FM], p_weight[FM], lse[FM];              // backward
     int32_t target[LISTS ? 1 : FM];
@@ -136,8 +141,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
         }
         if constexpr (BACKWARD) {
             const int state = m < M ? row_state(w, g, mc) : kDead;
-            const float sigma = l.sigma ? l.sigma[g] : 1.0f;
-            weight[i] = row_weight(l, g, mc, state) * sigma;
+            weight[i] = row_weight(l, g, mc, state) * sigma.x;
             // a row that does not count: exp of something far below, times 0
             const float n = state == kDead ? 1e30f : l.lse[g * l.lse_batch + mc * l.lse_ld];
             near[i] = state == kDead || fabsf(n) <= kPlain;

@@ -584,6 +584,19 @@ def test_windows_of_more_than_a_tile(dtype, top):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", DTYPES[1:])
+def test_equal_weights_are_not_rounded_one_way(dtype):
+    """The mean's weights are one number, of which each row's own word has -(1 - p): rounded as it is, all rows' errors would be the same.  A rounding of half a unit h is off
+    by 0.43 h of a value in the root mean square (ulp^2 / 12 over the value's square, averaged over a binade's logarithm); two of them, of dz and of the result, by 0.6 of the
+    most that one can be; 2 / 3 leaves a tenth for how values lie."""
+    c = Case(1, 895, 6000, 200, dtype, weighted=False, ignored=0.0, seed=12)
+    dz, _ = c.solve()
+    out = gradients(c, c.lse32)
+    for got, want in ((out["dx"], mm(dz, c.w.transpose(1, 2))), (out["dw"], mm(dz.transpose(1, 2), c.x.transpose(1, 2)))):
+        assert (got.double() - want).norm() <= 2 / 3 * HALF[dtype] * want.norm()
+
+
+@gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_all_rows_are_held_to_the_same_words(dtype):
     """Lists that lie in one window each: more words of a wave's rows and columns than are held at hand."""
@@ -798,6 +811,13 @@ def test_descriptions():
     for k in (dict(top=0), dict(top=2, temperature=0.0), dict(top=2000)):
         with pytest.raises(B.GbmufError):
             B.Distill(4, 6, 8, **k)
+
+
+def test_more_rows_than_launches_have():
+    assert workspace_status(desc(rows=2 ** 20, vocab=8, batch=2 ** 7, in_features=8))[0] == B.GBMUF_OK
+    assert workspace_status(desc(rows=2 ** 18 + 1, vocab=0, batch=2 ** 10)) == (B.GBMUF_EUNSUPPORTED, 0)
+    assert workspace_status(desc(rows=2 ** 20, vocab=8, batch=2 ** 5, in_features=8, top=2, temperature=1.0))[0] == B.GBMUF_OK
+    assert workspace_status(desc(rows=2 ** 20 + 1, vocab=8, batch=2 ** 5, in_features=8, top=2, temperature=1.0)) == (B.GBMUF_EUNSUPPORTED, 0)
 
 
 def test_workspaces_of_any_sizes():
