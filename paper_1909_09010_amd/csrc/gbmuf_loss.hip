@@ -655,6 +655,8 @@ bool may_be_direct(const gbmuf_linear_desc_t &d) { return d.batch * d.rows * (d.
 
 // f32 laid out takes the logits' product as well, 40 us or so more.  Directly / laid out, us: f32 1 x 1000 x 1000 x 1000 83 / 123, 6 x 130 x 18188 x 294 430 / 475, 8 x
 // 128 x 2600 x 650 145 / 189; bf16 4 x 100 x 1000 x 256 30 / 42, 4 x 200 x 1024 x 512 52 / 43, 1 x 327 x 16183 x 190 124 / 66.
+// dw's sums over the rows are not cut there: f32 1 x 2000 x 300 x 1000 109 / 113, 1 x 5000 x 300 x 200 181 / 98, 6 x 4835 x 219 x 142 383 / 165.
+constexpr int64_t kDirectRows = 2500;
 // The column sums go along with dw: what is asked for without it takes the other way.
 int backward(const Loss &l, const Inputs &in, const gbmuf_loss_grad_io_t &io, Space &space, hipStream_t stream)
 {
@@ -664,7 +666,7 @@ int backward(const Loss &l, const Inputs &in, const gbmuf_loss_grad_io_t &io, Sp
     g.dy = gbmuf_matrix_t{nullptr, 64, 0};               // dz lies well
     const bool sums = !io.dbias.data || (io.dw.data && d.in_features > 0);
     if (is_small(d) || is_few(d)) return backward_few(l, &in, &io, space, stream);
-    const bool direct = d.out_features == 0 || (may_be_direct(d) && sums && takes_direct_backward(d, g, d.dtype == GBMUF_F32 ? 40.0 : 0.0));
+    const bool direct = d.out_features == 0 || (may_be_direct(d) && sums && d.rows <= kDirectRows && takes_direct_backward(d, g, d.dtype == GBMUF_F32 ? 40.0 : 0.0));
     return direct ? backward_direct(l, &in, &io, space, stream) : backward_laid(l, &in, &io, space, stream);
 }
 
