@@ -85,6 +85,8 @@ struct Sender {
 // forward, so that 512 features are 8 steps and a fifth of leaving.  A whole call, bf16 8 x 5120 x 8197 x 512: 362 us, 0.95 PFLOP/s where large products reach
 // 1.31.  Tiles of 128 have two workgroups on a CU, one's leaving beside the other's steps, but twice the LDS reads a product: the caller's rule compares rounds
 // of both.  f32, taken apart into two f16, has tiles of 128 only: those of 256 leave too few registers for the statistics (8 x 700 x 10000 x 650: 436 us, 333).
+// Backward the stores share the way to memory with the steps' operands: dz of 8 x 5120 x 8197 x 512 bf16 takes 555 to 585 us, without them 460.  Registers read back from memory
+// behind the stores, or a load among them, cost 40; one half of all rows' 128 bytes before the other 30 to 50, with a third more written to memory.
 template <int T, bool SPLIT, int TM, int TN, int WM, int WN, bool BACKWARD, bool LISTS>
 __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, LossArgs l)
 {
@@ -341,31 +343,36 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                 }
             }
         } else {
-            // columns outside, so that only 32 columns' sums are held; no load between the stores, which it would wait for
+            // both halves of a row's 128 bytes one after the other; no load between the stores, which it would wait for
             const int from = lane >> 2, eight = (lane & 3) * 8;             // what a lane stores: rows `from` and 16 on, 8 columns; 4 lanes a row
+            v4f total[FN][2], top[SPLIT ? FN : 1][2];
+            Eight z[2];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                v4f total[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}}, top[2] = {total[0], total[0]};
-                Eight z[2];
-                const auto store = [&](int i) {
-                    const int n = n_wave + j * 32 + eight;
+                total[j][0] = total[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                if (SPLIT) top[j][0] = top[j][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            const auto store = [&](int i, int j) {
+                const int n = n_wave + j * 32 + eight;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int row = m0 + wm + i * 32 + k * 16 + from;
-                        total[0] += z[k].v[0];
-                        total[1] += z[k].v[1];
-                        if constexpr (SPLIT)
+                for (int k = 0; k < 2; ++k) {
+                    const int row = m0 + wm + i * 32 + k * 16 + from;
+                    total[j][0] += z[k].v[0];
+                    total[j][1] += z[k].v[1];
+                    if constexpr (SPLIT)
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) top[c >> 2][c & 3] = fmaxf(top[c >> 2][c & 3], fabsf(z[k].v[c >> 2][c & 3]));
-                        if (row >= M || n >= l.dz_ld) continue;
-                        const int64_t at = g * l.dz_batch + row * l.dz_ld + n;
-                        if (l.streamed) write8<SPLIT ? kF32 : T, true>(l.dz, at, z[k]);
-                        else write8<SPLIT ? kF32 : T>(l.dz, at, z[k]);
-                    }
-                };
+                        for (int c = 0; c < 8; ++c) top[j][c >> 2][c & 3] = fmaxf(top[j][c >> 2][c & 3], fabsf(z[k].v[c >> 2][c & 3]));
+                    if (row >= M || n >= l.dz_ld) continue;
+                    const int64_t at = g * l.dz_batch + row * l.dz_ld + n;
+                    if (l.streamed) write8<SPLIT ? kF32 : T, true>(l.dz, at, z[k]);
+                    else write8<SPLIT ? kF32 : T>(l.dz, at, z[k]);
+                }
+            };
 #pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    const int row0 = m0 + wm + i * 32, column = word_of(i);
+            for (int i = 0; i < FM; ++i) {
+                const int row0 = m0 + wm + i * 32, column = word_of(i);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
                     cut(i, j);
                     if (__all(near[i])) {
 #pragma unroll
@@ -400,16 +407,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                         if (column >> 5 == j && half == 0) scratch[scratch_at(lane, column & 31)] -= weight[i];
                         in_order();
                     }
-                    // what was read of the rows before leaves while these come back
+                    // what was read of the columns before leaves while these come back
                     if (i + j == 0) __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): the next tile's first two steps are here
-                    if (i > 0) store(i - 1);
+                    else store(j == 0 ? i - 1 : i, j == 0 ? FN - 1 : j - 1);
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const int r = k * 16 + from;
                         z[k] = Eight{{*reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight)), *reinterpret_cast<const v4f *>(scratch + scratch_at(r, eight + 4))}};
                     }
                 }
-                store(FM - 1);
+            }
+            store(FM - 1, FN - 1);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
                 // a lane's column of what 16 groups of lanes have of all columns
                 const int n = n_wave + j * 32 + lane;
                 const auto gather = [&](const v4f (&part)[2], auto join) {
@@ -424,12 +434,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
                     return join(v, __shfl_xor(v, 32));
                 };
                 if (l.col_sums) {
-                    const float v = gather(total, [](float x, float y) { return x + y; });
+                    const float v = gather(total[j], [](float x, float y) { return x + y; });
                     if (half == 0 && n < N) l.col_sums[((g * a.t.tiles_m + share.at.tm) * WM + wave % WM) * N + n] = v;
                 }
                 if constexpr (SPLIT)
                     if (l.col_max) {
-                        const uint32_t v = __float_as_uint(gather(top, [](float x, float y) { return fmaxf(x, y); }));
+                        const uint32_t v = __float_as_uint(gather(top[j], [](float x, float y) { return fmaxf(x, y); }));
                         if (half == 0 && n < N && v) atomicMax(l.col_max + g * N + n, v);
                     }
             }
