@@ -147,8 +147,9 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
     __syncthreads();
     if (a.dbias && threadIdx.x < static_cast<unsigned>(words)) {
         float v = 0.0f;
-#pragma unroll 8
-        for (int m = 0; m < rows; ++m) v += dz[m * kPitch + threadIdx.x];
+        for (int m0 = 0; m0 < rows; m0 += 8)
+#pragma unroll
+            for (int m = m0; m < m0 + 8; ++m) v += dz[m * kPitch + threadIdx.x];
         const int64_t at = g * a.dbias_batch + n0 + threadIdx.x;
         if (a.accumulate) v += load_one(a.dbias, at, a.grad_type);
         store_one(a.dbias, at, a.grad_type, v);
@@ -158,9 +159,10 @@ __global__ __launch_bounds__(kThreads) void small_grads_kernel(SmallGrads a)
     const int k = wn + (lane & 31);
     if (a.dw) {
         v16f out = zeros();
-#pragma unroll 4
-        for (int m = 0; m < rows; m += 2)
-            out = __builtin_amdgcn_mfma_f32_32x32x2f32(dz[(m + half) * kPitch + wm + (lane & 31)], xs[slab_at(m + half, k)], out, 0, 0, 0);
+        for (int m0 = 0; m0 < rows; m0 += 8)
+#pragma unroll
+            for (int m = m0; m < m0 + 8; m += 2)
+                out = __builtin_amdgcn_mfma_f32_32x32x2f32(dz[(m + half) * kPitch + wm + (lane & 31)], xs[slab_at(m + half, k)], out, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int n = wm + (r >> 2) * 8 + half * 4 + (r & 3);

@@ -370,7 +370,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void vocab_kernel(ProductArgs a, L
             };
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const int row0 = m0 + wm + i * 32, column = word_of(i);
+                const int column = word_of(i);
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     cut(i, j);
