@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void short_teacher_kernel(TeacherArgs a)
 // Lists of words by window: a workgroup takes the lists of a block of rows, counts the words of each window, and puts them there.  Within a window they lie in no
 // certain order, which no result depends on: no two are the same word of the same row.
 // ---------------------------------------------------------------------------------------
-constexpr int kListThreads = 1024;           // 8 x 5120 rows of 64 words, without shares / with them: 18 / 33 us, 256 threads 46 / 67
+constexpr int kListThreads = 1024;           // 8 x 5120 rows of 64 words, without shares / with them: 18 / 30 us; 256 threads, an entry at a time, 46 / 67
 __global__ __launch_bounds__(kListThreads) void word_lists_kernel(Words w, WordLists l)
 {
     __shared__ int32_t count[kMostWindows];
@@ -171,13 +171,33 @@ __global__ __launch_bounds__(kListThreads) void word_lists_kernel(Words w, WordL
     int32_t *starts = l.starts + static_cast<int64_t>(blockIdx.x) * (l.windows + 1);
     for (int i = threadIdx.x; i < l.windows; i += kListThreads) count[i] = 0;
     __syncthreads();
-    const auto each = [&](auto f) {
-        for (int e = threadIdx.x; e < n; e += kListThreads) {
-            const int word = id[e], p = e % w.top;
-            if (word < w.vocab && (p == 0 || id[e - 1] != word)) f(word, e, p);
+    // kBatch entries of a thread at a time, all sent for before the first is looked at: f(word or kNoWord, share, e, p of each)
+    constexpr int kBatch = 4;
+    const auto each = [&](auto with_shares, auto f) {
+        for (int first_e = threadIdx.x; first_e < n; first_e += kBatch * kListThreads) {
+            int word[kBatch], before[kBatch], place[kBatch];
+            float part[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {              // entries behind the last are read as the last one
+                const int e = min(first_e + u * kListThreads, n - 1);
+                word[u] = id[e];
+                before[u] = id[max(e - 1, 0)];
+                if (with_shares) part[u] = share[e];
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int e = first_e + u * kListThreads;
+                place[u] = e % w.top;
+                if (e >= n || word[u] >= w.vocab || (place[u] != 0 && before[u] == word[u])) word[u] = kNoWord;
+            }
+            f(word, part, place, first_e);
         }
     };
-    each([&](int word, int, int) { atomicAdd(&count[word >> l.shift], 1); });
+    each(std::false_type{}, [&](const int (&word)[kBatch], const float (&)[kBatch], const int (&)[kBatch], int) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (word[u] != kNoWord) atomicAdd(&count[word[u] >> l.shift], 1);
+    });
     __syncthreads();
     // where each window begins: a thread's windows lie side by side
     const int per = (l.windows + kListThreads - 1) / kListThreads, from = threadIdx.x * per, to = min(from + per, l.windows);
@@ -201,11 +221,20 @@ __global__ __launch_bounds__(kListThreads) void word_lists_kernel(Words w, WordL
     }
     if (threadIdx.x == kListThreads - 1) starts[l.windows] = before;
     __syncthreads();
-    each([&](int word, int e, int p) {
-        const int place = atomicAdd(&count[word >> l.shift], 1);
-        l.code[out + place] = static_cast<uint32_t>(word & ((1 << l.shift) - 1)) << 17 | static_cast<uint32_t>(e / w.top) << 10 | static_cast<uint32_t>(p);
-        if (l.share) l.share[out + place] = share[e];
-    });
+    const auto put = [&](const int (&word)[kBatch], const float (&part)[kBatch], const int (&p)[kBatch], int first_e) {
+        int to_place[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) to_place[u] = word[u] != kNoWord ? atomicAdd(&count[word[u] >> l.shift], 1) : 0;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (word[u] == kNoWord) continue;
+            const uint32_t row = static_cast<uint32_t>((first_e + u * kListThreads) / w.top);
+            l.code[out + to_place[u]] = static_cast<uint32_t>(word[u] & ((1 << l.shift) - 1)) << 17 | row << 10 | static_cast<uint32_t>(p[u]);
+            if (l.share) l.share[out + to_place[u]] = part[u];
+        }
+    };
+    if (l.share) each(std::true_type{}, put);
+    else each(std::false_type{}, put);
 }
 
 // ---------------------------------------------------------------------------------------
