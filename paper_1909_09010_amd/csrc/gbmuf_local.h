@@ -209,7 +209,7 @@ struct KeepArgs {
 };
 
 // Gradients of few rows: small_grads_kernel, and few_grads_kernel for more columns.
-constexpr int kFewGradRows = 8, kFewGradColumns = 1024, kFewGradWords = 64;
+constexpr int kFewGradRows = 8, kFewGradColumns = 1024;
 constexpr int kSmallRows = 64, kSmallColumns = 64, kSmallWords = 64;       // words of a piece of the vocabulary
 struct SmallGrads {
     LossArgs l;              // words, bias, lse and dloss
@@ -218,7 +218,8 @@ struct SmallGrads {
     void *dx, *dw, *dbias;   // any of them nullptr; of l.type, dw and dbias of grad_type
     int64_t lddx, dx_batch, lddw, dw_batch, dbias_batch;
     float *parts;            // [piece][worker][row][column] of dx, or nullptr
-    int32_t columns, batch, pieces, grad_type, accumulate, reserved;
+    int32_t columns, batch, pieces, grad_type, accumulate;
+    int32_t words;           // of a piece, few_grads_kernel: 64 or 32
 };
 
 struct CastArgs {            // out = from, [batch][rows][columns]

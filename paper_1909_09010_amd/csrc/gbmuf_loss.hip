@@ -433,18 +433,17 @@ bool is_few(const gbmuf_linear_desc_t &d)
     const double values = static_cast<double>(d.batch) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
     return d.rows <= kFewGradRows && d.rows > 0 && d.in_features <= kFewGradColumns && d.out_features > 0 && (d.dtype == GBMUF_F32 || values <= kFewGradValues);
 }
-int64_t few_workgroups(const gbmuf_linear_desc_t &d)
-{
-    const int64_t pieces = (d.out_features + kFewGradWords - 1) / kFewGradWords;
-    return std::min<int64_t>(pieces, std::max<int64_t>(768 / std::max(d.batch, 1), 1));
-}
+// Words of a piece: of few pieces, up to one workgroup a CU, half.  us, 32 / 64: f32 1 x 3 x 300 x 700 20 / 32, 1 x 1 x 2368 x 256 12.5 / 16, bf16 1 x 2 x 1000 x 256 11 / 16, 4 x 8 x 5000 x
+// 512 42 / 39, f16 8 x 6 x 3000 x 301 47 / 41.
+int64_t few_words(const gbmuf_linear_desc_t &d) { return (d.out_features + 63) / 64 * d.batch <= 256 ? 32 : 64; }
+int64_t few_pieces(const gbmuf_linear_desc_t &d) { return (d.out_features + few_words(d) - 1) / few_words(d); }
+int64_t few_workgroups(const gbmuf_linear_desc_t &d) { return std::min<int64_t>(few_pieces(d), std::max<int64_t>(768 / std::max(d.batch, 1), 1)); }
 
 int backward_few(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io, Space &space, hipStream_t stream)
 {
     const gbmuf_linear_desc_t &d = l.linear;
     const bool small = is_small(d);
-    const int64_t M = d.rows, K = d.in_features, pieces = small_pieces(d), groups = few_workgroups(d), parts = small ? pieces : groups * (256 / few_grads_lanes(K));
-    static_assert(kSmallWords == kFewGradWords, "pieces are the same");
+    const int64_t M = d.rows, K = d.in_features, pieces = small ? small_pieces(d) : few_pieces(d), groups = few_workgroups(d), parts = small ? pieces : groups * (256 / few_grads_lanes(K));
     const int32_t G = d.batch, type = d.dtype;
     const Inputs none{};
     const Inputs &at = in ? *in : none;
@@ -464,6 +463,7 @@ int backward_few(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io
     a.columns = static_cast<int32_t>(K); a.batch = G; a.pieces = static_cast<int32_t>(pieces);
     a.grad_type = l.weight_grad_f32 ? kF32 : type; a.accumulate = l.accumulate;
     if (small) return launch_small_grads(a, stream);
+    a.words = static_cast<int32_t>(few_words(d));
     rc = launch_few_grads(a, static_cast<int32_t>(groups), stream);
     return rc == GBMUF_OK ? launch_join_parts(a, static_cast<int32_t>(parts), stream) : rc;
 }
