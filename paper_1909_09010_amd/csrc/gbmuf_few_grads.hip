@@ -40,11 +40,11 @@ __device__ __forceinline__ void write_columns(void *p, int64_t i, int left, cons
     }
 }
 
-// A workgroup takes every gridDim.x-th piece of 64 or 32 words for all rows.  The logits of a piece come from matrix instructions as in few_sums; their gradient
+// A workgroup takes every gridDim.x-th piece of 64, 32 or 16 words for all rows.  The logits of a piece come from matrix instructions as in few_sums; their gradient
 // stays in LDS, [word][row].  Then threads take C columns each of a word's row, which is in the L2 by now: dw's values are ROWS products with the thread's
 // columns of x, dx's sums go on in registers over all pieces: 2 ROWS C multiply-adds a word and thread, 0.1 us a word of 1024 columns and CU for 8 rows, where
 // its 4 KB read and 4 KB written take 0.32 at 6.5 TB/s.  `lanes` threads have a word's columns, the others further words.  Bound by w's way from memory.  us, this /
-// the routes of more rows: 2 x 1 x 54538 x 241 78 / 142, 1 x 8 x 50000 x 1024 154 / 207, 9 x 6 x 5250 x 74 32 / 42, 1 x 1 x 2368 x 256 12.5 / 28, 1 x 3 x 300 x 700 20
+// the routes of more rows: 2 x 1 x 54538 x 241 78 / 142, 1 x 8 x 50000 x 1024 154 / 207, 9 x 6 x 5250 x 74 32 / 42, 1 x 1 x 2368 x 256 12.5 / 28, 1 x 3 x 300 x 700 16
 // / 32.  16 rows are short of registers.  Values of w and dw are of type T and D.
 template <int T, int D, int ROWS, int kWords>
 __global__ __launch_bounds__(kThreads, 2) void few_grads_kernel(SmallGrads a, int32_t lanes)
@@ -213,12 +213,13 @@ int launch_few_grads(const SmallGrads &a, int32_t workgroups, hipStream_t stream
     int32_t lanes = few_grads_lanes(a.columns);
     void *argv[] = {&args, &lanes};
     using Fn = void (*)(SmallGrads, int32_t);
-    // [type][gradients in f32][more than 4 rows][pieces of 32 words]
+    // [type][gradients in f32][more than 4 rows][pieces of 64, 32, 16 words]
 #define GBMUF_FEW(T, D) \
-    {{few_grads_kernel<T, D, 4, 64>, few_grads_kernel<T, D, 4, 32>}, {few_grads_kernel<T, D, 8, 64>, few_grads_kernel<T, D, 8, 32>}}
-    static constexpr Fn fns[3][2][2][2] = {{{}, GBMUF_FEW(kF32, kF32)}, {GBMUF_FEW(kBf16, kBf16), GBMUF_FEW(kBf16, kF32)}, {GBMUF_FEW(kF16, kF16), GBMUF_FEW(kF16, kF32)}};
+    {{few_grads_kernel<T, D, 4, 64>, few_grads_kernel<T, D, 4, 32>, few_grads_kernel<T, D, 4, 16>}, \
+     {few_grads_kernel<T, D, 8, 64>, few_grads_kernel<T, D, 8, 32>, few_grads_kernel<T, D, 8, 16>}}
+    static constexpr Fn fns[3][2][2][3] = {{{}, GBMUF_FEW(kF32, kF32)}, {GBMUF_FEW(kBf16, kBf16), GBMUF_FEW(kBf16, kF32)}, {GBMUF_FEW(kF16, kF16), GBMUF_FEW(kF16, kF32)}};
 #undef GBMUF_FEW
-    const void *fn = reinterpret_cast<const void *>(fns[a.l.type][a.grad_type == kF32 ? 1 : 0][a.l.words.rows > 4 ? 1 : 0][a.words == 32 ? 1 : 0]);
+    const void *fn = reinterpret_cast<const void *>(fns[a.l.type][a.grad_type == kF32 ? 1 : 0][a.l.words.rows > 4 ? 1 : 0][a.words == 64 ? 0 : a.words == 32 ? 1 : 2]);
     const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(workgroups), static_cast<unsigned>(a.batch)), dim3(kThreads), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(few rows' gradients)", err, GBMUF_EDEVICE);
 }

@@ -219,7 +219,7 @@ struct SmallGrads {
     int64_t lddx, dx_batch, lddw, dw_batch, dbias_batch;
     float *parts;            // [piece][worker][row][column] of dx, or nullptr
     int32_t columns, batch, pieces, grad_type, accumulate;
-    int32_t words;           // of a piece, few_grads_kernel: 64 or 32
+    int32_t words;           // of a piece, few_grads_kernel: 64, 32 or 16
 };
 
 struct CastArgs {            // out = from, [batch][rows][columns]

@@ -433,9 +433,13 @@ bool is_few(const gbmuf_linear_desc_t &d)
     const double values = static_cast<double>(d.batch) * static_cast<double>(d.out_features) * static_cast<double>(d.in_features);
     return d.rows <= kFewGradRows && d.rows > 0 && d.in_features <= kFewGradColumns && d.out_features > 0 && (d.dtype == GBMUF_F32 || values <= kFewGradValues);
 }
-// Words of a piece: of few pieces, up to one workgroup a CU, half.  us, 32 / 64: f32 1 x 3 x 300 x 700 20 / 32, 1 x 1 x 2368 x 256 12.5 / 16, bf16 1 x 2 x 1000 x 256 11 / 16, 4 x 8 x 5000 x
-// 512 42 / 39, f16 8 x 6 x 3000 x 301 47 / 41.
-int64_t few_words(const gbmuf_linear_desc_t &d) { return (d.out_features + 63) / 64 * d.batch <= 256 ? 32 : 64; }
+// Words of a piece: fewer where that makes work for more CUs.  us, 16 / 32 / 64: f32 1 x 3 x 300 x 700 16 / 21 / 32, bf16 2 x 5 x 1216 x 448 16 / 20 / 27, 1 x 8 x 5000 x 1024 27 / 31 /
+// -, f32 9 x 6 x 1250 x 74 27 / 17.5 / -, bf16 1 x 8 x 10000 x 1024 43 / 40 / 57, 4 x 8 x 5000 x 512 - / 42 / 39, f16 8 x 6 x 3000 x 301 - / 47 / 41.
+int64_t few_words(const gbmuf_linear_desc_t &d)
+{
+    const int64_t pieces = (d.out_features + 63) / 64 * d.batch;
+    return pieces <= 80 ? 16 : pieces <= 256 ? 32 : 64;
+}
 int64_t few_pieces(const gbmuf_linear_desc_t &d) { return (d.out_features + few_words(d) - 1) / few_words(d); }
 int64_t few_workgroups(const gbmuf_linear_desc_t &d) { return std::min<int64_t>(few_pieces(d), std::max<int64_t>(768 / std::max(d.batch, 1), 1)); }
 
