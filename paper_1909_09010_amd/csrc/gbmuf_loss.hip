@@ -262,22 +262,20 @@ int lay_rows(LayArgs l, const Operand &o, int64_t K, int32_t type, hipStream_t s
 }
 
 // ---------------------------------------------------------------------------------------
-// Forward.  in nullptr: only count the workspace, for matrices that lie as badly as can be.
+// Forward.  io nullptr: only count the workspace, for matrices that lie as those of `at` do.
 // ---------------------------------------------------------------------------------------
 constexpr int64_t kLaidBytes = 256 << 20;          // of w, at a time
 
-int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &space, hipStream_t stream)
+int forward(const Loss &l, const Inputs &at, const gbmuf_loss_io_t *io, Space &space, hipStream_t stream)
 {
     const gbmuf_linear_desc_t &d = l.linear;
     const int64_t M = d.rows, N = d.out_features, K = d.in_features;
     const int32_t G = d.batch, type = d.dtype;
     const bool split = type == kF32;
-    const Inputs none{};
-    const Inputs &at = in ? *in : none;
     const Few few = few_of(d);
-    const bool is_few = few == Few::kAlways || (few == Few::kUnlessAligned && (!in || !(lies_well(at.x) && lies_well(at.w))));
+    const bool is_few = few == Few::kAlways || (few == Few::kUnlessAligned && !(lies_well(at.x) && lies_well(at.w)));
     const bool direct = takes_direct_forward(d) || few == Few::kDirect;
-    const Words words = words_of(l, at, in && is_few && l.top <= kFewWords, space);
+    const Words words = words_of(l, at, is_few && l.top <= kFewWords, space);
     float *word_logits = space.take<float>(G * M * words.top);
 
     LossJoin j{};
@@ -285,7 +283,7 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
     j.at = word_logits;
     j.batch = G;
     j.inv_tau = 1.0f / l.tau; j.tau = l.tau;
-    if (in) {
+    if (io) {
         j.loss = static_cast<float *>(io->loss.data); j.loss_ld = io->loss.ld; j.loss_batch = io->loss.batch_stride;
         j.lse = static_cast<float *>(io->lse.data); j.lse_ld = io->lse.ld; j.lse_batch = io->lse.batch_stride;
     }
@@ -301,19 +299,17 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
         const DirectArgs f = direct_args(source_of(at.x), source_of(at.w), K, c, Epilogue{});
         const int columns = is_few ? few_columns(f, type) : 64;
         float2 *parts = parts_of((N + columns - 1) / columns);
-        if (!in) {
-            if (!is_few || few == Few::kAlways) return GBMUF_OK;
-        } else {
-            LossArgs a = loss_args(l, at, words, Piece{0, G, 0, N});
-            a.parts = parts; a.part_tiles = j.tiles;
-            a.at = word_logits;
-            if ((rc = order_words(l, words, at, false, stream)) != GBMUF_OK) return rc;
-            rc = is_few ? launch_loss_few(f, a, type, stream) : launch_loss_direct(f, a, type, false, stream);
-            return rc == GBMUF_OK ? launch_loss_join(j, stream) : rc;
-        }
+        if (!io) return GBMUF_OK;
+        if (!space.fits()) return GBMUF_EINVAL;
+        LossArgs a = loss_args(l, at, words, Piece{0, G, 0, N});
+        a.parts = parts; a.part_tiles = j.tiles;
+        a.at = word_logits;
+        if ((rc = order_words(l, words, at, false, stream)) != GBMUF_OK) return rc;
+        rc = is_few ? launch_loss_few(f, a, type, stream) : launch_loss_direct(f, a, type, false, stream);
+        return rc == GBMUF_OK ? launch_loss_join(j, stream) : rc;
     }
     // w is laid out a piece at a time, x once
-    const bool may_lay = few == Few::kNo, lay_x = split || (may_lay && (!in || !lies_well(at.x))), lay_w = split || (may_lay && (!in || !lies_well(at.w)));
+    const bool may_lay = few == Few::kNo, lay_x = split || (may_lay && !lies_well(at.x)), lay_w = split || (may_lay && !lies_well(at.w));
     const Pieces pieces = lay_w ? pieces_of(G, N, packed_words(K, split) * 2, kLaidBytes) : Pieces{std::max(G, 1), std::max<int64_t>(N, 1)};
     const Cut shape = logits_shape(M, pieces.words, K, pieces.workers, split, false);
     const int64_t whole_pieces = N / pieces.words;
@@ -321,10 +317,11 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
     const WordLists lists = lists_of(l, words, shape.tile, false, space);
     const LayArgs lx = source(at.x, M, K, G, type);
     Operand x = operand_of(at.x), w = operand_of(at.w);
-    if (lay_x) x = packed(space, M, K, G, in ? lx.batch : G, split, space.take<uint32_t>(split ? G * M : 0));
+    if (lay_x) x = packed(space, M, K, G, lx.batch, split, space.take<uint32_t>(split ? G * M : 0));
     if (lay_w) w = packed(space, pieces.words, K, static_cast<int32_t>(pieces.workers), static_cast<int32_t>(pieces.workers), split,
                           space.take<uint32_t>(split ? pieces.workers * pieces.words + 256 : 0));
-    if (!in) return GBMUF_OK;
+    if (!io) return GBMUF_OK;
+    if (!space.fits()) return GBMUF_EINVAL;
     if ((rc = order_words(l, words, at, false, stream)) != GBMUF_OK) return rc;
     if (lists.blocks > 0 && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK) return rc;
     if (lay_x && (rc = lay_rows(lx, x, K, type, stream)) != GBMUF_OK) return rc;
@@ -351,6 +348,23 @@ int forward(const Loss &l, const Inputs *in, const gbmuf_loss_io_t *io, Space &s
         return launch_vocab(logits_args(px, pw, K, type, c), a, type, shape.tile, false, stream);
     });
     return rc == GBMUF_OK ? launch_loss_join(j, stream) : rc;
+}
+
+// What any placement takes.  A w that lies well is taken whole, and one that does not in pieces, whose tiles go to workgroups otherwise: neither's parts are always the more.
+int64_t forward_bytes(const Loss &l)
+{
+    const gbmuf_matrix_t well{}, badly{nullptr, 1, 0};
+    const auto bytes = [&](const gbmuf_matrix_t &x, const gbmuf_matrix_t &w) {
+        Space space{nullptr};
+        (void)forward(l, Inputs{x, w, {}, {}, {}}, nullptr, space, nullptr);
+        return space.used;
+    };
+    const int64_t most = bytes(badly, badly);
+    switch (few_of(l.linear)) {
+        case Few::kNo: return l.linear.dtype == kF32 ? most : std::max(most, bytes(badly, well));           // f32: however they lie
+        case Few::kUnlessAligned: return std::max(most, bytes(well, well));
+        default: return most;
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -396,6 +410,7 @@ int backward_direct(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t 
     const Cut cx = chain_cut(M, dx ? K : 0, N, G, both);
     float *partial = space.take<float>(cx.partial);
     if (!io) return GBMUF_OK;
+    if (!space.fits()) return GBMUF_EINVAL;
     int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK) return rc;
     LossArgs a = grad_args(l, at, io, words, Piece{0, G, 0, N});
@@ -454,6 +469,7 @@ int backward_few(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *io
     const Words words = words_of(l, at, in && small && l.top <= kFewWords, space);
     float *sums = space.take<float>(parts * G * M * K);
     if (!io) return GBMUF_OK;
+    if (!space.fits()) return GBMUF_EINVAL;
     int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK) return rc;
     SmallGrads a{};
@@ -524,6 +540,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         w = packed(space, PN, K, static_cast<int32_t>(PG), static_cast<int32_t>(PG), false, nullptr);
     }
     if (!io) return GBMUF_OK;
+    if (!space.fits()) return GBMUF_EINVAL;
 
     int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK || (lists.blocks > 0 && (rc = launch_word_lists(words, lists, G, stream)) != GBMUF_OK)) return rc;
@@ -676,17 +693,12 @@ int backward(const Loss &l, const Inputs &in, const gbmuf_loss_grad_io_t &io, Sp
 
 int64_t workspace_bytes(const Loss &l, bool back)
 {
-    Space space{nullptr}, direct{nullptr};
-    if (back) {
-        (void)backward_laid(l, nullptr, nullptr, space, nullptr);
-        if (may_be_direct(l.linear)) (void)backward_direct(l, nullptr, nullptr, direct, nullptr);
-        Space small{nullptr};
-        if (is_small(l.linear) || is_few(l.linear)) (void)backward_few(l, nullptr, nullptr, small, nullptr);
-        space.used = std::max(space.used, small.used);
-    } else {
-        (void)forward(l, nullptr, nullptr, space, nullptr);
-    }
-    return std::max(space.used, direct.used);
+    if (!back) return forward_bytes(l);
+    Space laid{nullptr}, direct{nullptr}, small{nullptr};
+    (void)backward_laid(l, nullptr, nullptr, laid, nullptr);
+    if (may_be_direct(l.linear)) (void)backward_direct(l, nullptr, nullptr, direct, nullptr);
+    if (is_small(l.linear) || is_few(l.linear)) (void)backward_few(l, nullptr, nullptr, small, nullptr);
+    return std::max({laid.used, direct.used, small.used});
 }
 
 // ---------------------------------------------------------------------------------------
@@ -729,8 +741,8 @@ int run_forward(const gbmuf_loss_desc_t *desc, const gbmuf_loss_io_t *io, void *
     if (M == 0 || G == 0) return GBMUF_OK;
     if ((rc = check_workspace(workspace, workspace_bytes_, workspace_bytes(l, false), {&e.x, &e.w, &e.bias, &e.target, &e.teacher, &loss, &lse})) != GBMUF_OK) return rc;
     if ((rc = check_device()) != GBMUF_OK) return rc;
-    Space space{static_cast<char *>(workspace)};
-    return forward(l, &in, io, space, static_cast<hipStream_t>(stream));
+    Space space{static_cast<char *>(workspace), workspace_bytes_};
+    return forward(l, in, io, space, static_cast<hipStream_t>(stream));
 }
 
 int run_backward(const gbmuf_loss_desc_t *desc, const gbmuf_loss_grad_io_t *io, void *workspace, int64_t workspace_bytes_, void *stream, bool distill)
@@ -760,7 +772,7 @@ int run_backward(const gbmuf_loss_desc_t *desc, const gbmuf_loss_grad_io_t *io, 
     if ((rc = check_workspace(workspace, workspace_bytes_, need, {&e.x, &e.w, &e.bias, &e.target, &e.teacher, &lse, &dloss, &dx, &dw, &db})) != GBMUF_OK) return rc;
     if ((rc = check_device()) != GBMUF_OK) return rc;
     if (!io->dx.data && !io->dw.data && !io->dbias.data) return GBMUF_OK;
-    Space space{static_cast<char *>(workspace)};
+    Space space{static_cast<char *>(workspace), workspace_bytes_};
     return backward(l, in, *io, space, static_cast<hipStream_t>(stream));
 }
 

@@ -100,7 +100,9 @@ int check_device()
 // ---------------------------------------------------------------------------------------
 struct Space {
     char *base;
+    int64_t have = 0;            // what the caller gave
     int64_t used = 0;
+    bool fits() const { return used <= have; }           // before anything is launched
     template <class T>
     T *take(int64_t n)
     {
