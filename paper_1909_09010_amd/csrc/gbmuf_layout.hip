@@ -256,9 +256,9 @@ __global__ __launch_bounds__(256) void lay_kernel(LaySet set)
 __global__ __launch_bounds__(256) void column_sums_kernel(SumArgs a)
 {
     __shared__ float part[4][64];
-    const int blocks = (a.C + 63) / 64, wave = threadIdx.x >> 6, c = static_cast<int>(blockIdx.x) % blocks * 64 + static_cast<int>(threadIdx.x & 63);
-    const int64_t g = blockIdx.x / blocks;
-    const float *from = a.sums + g * a.tiles * a.C + min(c, a.C - 1);
+    const int blocks = (a.C + 63) / 64, wave = threadIdx.x >> 6, g = block_number() / blocks, c = (block_number() - g * blocks) * 64 + static_cast<int>(threadIdx.x & 63);
+    if (g >= a.batch) return;
+    const float *from = a.sums + static_cast<int64_t>(g) * a.tiles * a.C + min(c, a.C - 1);
     float s = 0.0f;
 #pragma unroll 8
     for (int t = wave; t < a.tiles; t += 4) s += from[static_cast<int64_t>(t) * a.C];
@@ -278,15 +278,10 @@ __global__ __launch_bounds__(256) void zero_kernel(uint32_t *p, int64_t words)
     if (i < words) p[i] = 0u;
 }
 
-template <class Args>
-int launch_256(void (*fn)(Args), const Args &a, int64_t blocks, const char *what, hipStream_t stream)
+dim3 grid_of(int64_t blocks)
 {
-    if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
-    Args args = a;
-    void *argv[] = {&args};
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
-    return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
+    const int64_t across = blocks < kGridRow ? blocks : kGridRow;
+    return dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across));
 }
 
 int64_t tiles_over(int64_t rows, int64_t columns, int64_t wide, int64_t batch) { return (columns + wide - 1) / wide * ((rows + kT - 1) / kT) * batch; }
@@ -308,9 +303,7 @@ int launch_set(void (*fn)(LaySet), const LaySet &set, BlocksOf blocks_of, const 
     if (blocks > 0x7fffffffLL - kGridRow) return GBMUF_EUNSUPPORTED;
     s.first[s.n] = static_cast<int32_t>(blocks);
     void *argv[] = {&s};
-    const int64_t across = blocks < kGridRow ? blocks : kGridRow;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
-                                           dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), grid_of(blocks), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed(what, err, GBMUF_EDEVICE);
 }
 
@@ -343,7 +336,13 @@ int launch_copy(const LaySet &set, hipStream_t stream)
 
 int launch_column_sums(const SumArgs &a, hipStream_t stream)
 {
-    return launch_256(column_sums_kernel, a, static_cast<int64_t>((a.C + 63) / 64) * a.batch, "hipLaunchKernel(column sums)", stream);
+    const int64_t blocks = static_cast<int64_t>((a.C + 63) / 64) * a.batch;
+    if (blocks <= 0) return GBMUF_OK;
+    if (blocks > 0x7fffffffLL - kGridRow) return GBMUF_EUNSUPPORTED;
+    SumArgs args = a;
+    void *argv[] = {&args};
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(column_sums_kernel), grid_of(blocks), dim3(256), argv, 0, stream);
+    return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(column sums)", err, GBMUF_EDEVICE);
 }
 
 int launch_zero(uint32_t *p, int64_t words, hipStream_t stream)

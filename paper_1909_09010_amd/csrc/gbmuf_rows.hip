@@ -4,6 +4,15 @@
 namespace gbmuf {
 namespace {
 
+// More workgroups than a grid's first dimension holds lie in two; the last row's surplus has nothing to do.
+constexpr int64_t kGridRow = 1 << 22;
+__device__ __forceinline__ int64_t block_number() { return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x; }
+dim3 grid_of(int64_t blocks)
+{
+    const int64_t across = blocks < kGridRow ? blocks : kGridRow;
+    return dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across));
+}
+
 // Sum of WIDTH neighbouring lanes.
 template <int WIDTH>
 __device__ __forceinline__ float sum_of(float v)
@@ -23,7 +32,7 @@ __global__ __launch_bounds__(256) void teacher_kernel(TeacherArgs a, int32_t pad
 {
     __shared__ uint64_t keys[4][MOST];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t all = static_cast<int64_t>(a.rows) * a.batch, at = static_cast<int64_t>(blockIdx.x) * 4 + wave, row = at < all ? at : all - 1;
+    const int64_t all = static_cast<int64_t>(a.rows) * a.batch, at = block_number() * 4 + wave, row = at < all ? at : all - 1;
     const int64_t g = row / a.rows, i = row - g * a.rows;
     const int64_t *id = a.id + g * a.id_batch + i * a.id_ld;
     const float *logit = a.logit + g * a.logit_batch + i * a.logit_ld;
@@ -108,7 +117,7 @@ constexpr int kShortTop = 64, kShortVocab = 1 << 25;
 __global__ __launch_bounds__(256) void short_teacher_kernel(TeacherArgs a)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t row = block_number() * 4 + (threadIdx.x >> 6);
     if (row >= static_cast<int64_t>(a.rows) * a.batch) return;
     const int64_t g = row / a.rows, i = row - g * a.rows;
     const float inf = __builtin_inff();
@@ -246,8 +255,10 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
     constexpr int kThreads = 256 / ROWS;
     __shared__ float2 shared[4][ROWS];
     const Words &w = a.words;
-    const int blocks = (w.rows + ROWS - 1) / ROWS, m0 = static_cast<int>(blockIdx.x % blocks) * ROWS;
-    const int64_t g = blockIdx.x / blocks;
+    const uint32_t block = static_cast<uint32_t>(block_number()), blocks = static_cast<uint32_t>(w.rows + ROWS - 1) / ROWS;
+    const int64_t g = block / blocks;
+    if (g >= a.batch) return;
+    const int m0 = static_cast<int>(block % blocks) * ROWS;
     const float inf = __builtin_inff(), scale = a.inv_tau * kLog2E;
     {
         const int r = threadIdx.x % ROWS, m = min(m0 + r, w.rows - 1);
@@ -316,7 +327,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
 template <int T>
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
 {
-    const int64_t block = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+    const int64_t block = block_number();
     if (block < copies) {
         const int64_t id = block * 256 + threadIdx.x, all = static_cast<int64_t>(a.words.rows) * a.batch;
         const uint32_t per_row = static_cast<uint32_t>(a.out_ld / 8), rows = static_cast<uint32_t>(a.words.rows);
@@ -374,7 +385,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a, int64_t copies)
 
 __global__ __launch_bounds__(256) void cast_kernel(CastArgs a)
 {
-    const int64_t id = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * 256 + threadIdx.x, per_row = (a.columns + 7) / 8, row = id / per_row;
+    const int64_t id = block_number() * 256 + threadIdx.x, per_row = (a.columns + 7) / 8, row = id / per_row;
     if (row >= static_cast<int64_t>(a.rows) * a.batch) return;
     const int c = static_cast<int>(id - row * per_row) * 8, left = a.columns - c;
     const int64_t g = row / a.rows, to = g * a.batch_stride + (row - g * a.rows) * a.ld + c, from = row * a.columns + c;
@@ -388,13 +399,12 @@ int launch_teacher(const TeacherArgs &a, hipStream_t stream)
 {
     const int64_t blocks = (static_cast<int64_t>(a.rows) * a.batch + 3) / 4;
     if (blocks <= 0) return GBMUF_OK;
-    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
     TeacherArgs args = a;
     int32_t padded = 1;
     while (padded < a.top) padded *= 2;
     void *argv[] = {&args, &padded};
     const void *fn = a.top <= kShortTop && a.vocab < kShortVocab ? reinterpret_cast<const void *>(short_teacher_kernel) : reinterpret_cast<const void *>(padded <= 128 ? teacher_kernel<128> : teacher_kernel<kMostTop>);
-    const hipError_t err = hipLaunchKernel(fn, dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(fn, grid_of(blocks), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(teacher)", err, GBMUF_EDEVICE);
 }
 
@@ -417,11 +427,10 @@ int launch_loss_join(const LossJoin &a, hipStream_t stream)
     const int64_t all = static_cast<int64_t>(a.words.rows) * a.batch;
     const int rows = a.words.rows <= 2 || all <= 256 ? 1 : all <= 4096 || a.words.logit ? 4 : 32;
     const int64_t blocks = static_cast<int64_t>((a.words.rows + rows - 1) / rows) * a.batch;
-    if (blocks > 0x7fffffffLL / 256) return GBMUF_EUNSUPPORTED;
     LossJoin args = a;
     void *argv[] = {&args};
     const auto fn = rows == 1 ? loss_join_kernel<1> : rows == 4 ? loss_join_kernel<4> : loss_join_kernel<32>;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(blocks)), dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), grid_of(blocks), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(losses)", err, GBMUF_EDEVICE);
 }
 
@@ -432,10 +441,8 @@ int launch_keep(const KeepArgs &a, hipStream_t stream)
     if (blocks <= 0) return GBMUF_OK;
     KeepArgs args = a;
     void *argv[] = {&args, &copies};
-    const int64_t across = blocks < (1 << 22) ? blocks : 1 << 22;
     const auto fn = a.type == kF32 ? keep_kernel<kF32> : a.type == kBf16 ? keep_kernel<kBf16> : keep_kernel<kF16>;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
-                                           dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(fn), grid_of(blocks), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(rows of x)", err, GBMUF_EDEVICE);
 }
 
@@ -445,9 +452,7 @@ int launch_cast(const CastArgs &a, hipStream_t stream)
     if (blocks <= 0) return GBMUF_OK;
     CastArgs args = a;
     void *argv[] = {&args};
-    const int64_t across = blocks < (1 << 22) ? blocks : 1 << 22;
-    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(cast_kernel), dim3(static_cast<unsigned>(across), static_cast<unsigned>((blocks + across - 1) / across)),
-                                           dim3(256), argv, 0, stream);
+    const hipError_t err = hipLaunchKernel(reinterpret_cast<const void *>(cast_kernel), grid_of(blocks), dim3(256), argv, 0, stream);
     return err == hipSuccess ? GBMUF_OK : hip_failed("hipLaunchKernel(cast)", err, GBMUF_EDEVICE);
 }
 

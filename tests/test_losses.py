@@ -930,3 +930,71 @@ def test_the_binding_refuses(top):
     if top:
         with pytest.raises(B.GbmufError):
             op.forward_io(t["x"], t["w"], t["target"], t["teacher"].half(), t["loss"], t["lse"])
+
+
+# -- as many rows, and as many words, as descriptions may have -------------------------------------------
+@gpu
+@pytest.mark.parametrize("size", [(2 ** 20, 2 ** 5), (2 ** 17 - 1, 2 ** 8)])
+def test_as_many_rows_of_a_teacher_as_there_may_be(size):
+    """2^25, and some fewer: one word of a teacher has the whole share, so the loss is cross entropy's."""
+    M, G = size
+    V, K = 8, 8
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(G, M, K, generator=g, device=DEV).bfloat16()
+    w = torch.randn(G, V, K, generator=g, device=DEV).bfloat16()
+    words = torch.randint(-1, V, (G, M, 1), generator=g, device=DEV)
+    teacher = torch.randn(G, M, 1, generator=g, device=DEV)
+    op = B.Distill(M, V, K, 1, 1.0, G, torch.bfloat16)
+    loss, lse = torch.full((G, M), 7.0, device=DEV), torch.full((G, M), 7.0, device=DEV)
+    dx, dw, dloss = torch.empty_like(x), torch.empty_like(w), torch.ones(1, 1, device=DEV).expand(G, M)
+    ws = torch.empty(max(op.workspace_bytes(), op.workspace_bytes(True)), dtype=torch.uint8, device=DEV)
+    op.forward(op.forward_io(x, w, words, teacher, loss, lse), ws)
+    op.backward(op.backward_io(x, w, words, teacher, lse, dloss, dx=dx, dw=dw), ws)
+    torch.cuda.synchronize()
+    for i in (0, G // 2, G - 1):
+        xs, ws_ = x[i].double(), w[i].double()
+        z, S = xs @ ws_.T.contiguous(), xs.abs() @ ws_.abs().T.contiguous()
+        live, word = words[i, :, 0] >= 0, words[i].clamp(min=0)
+        n = torch.logsumexp(z, 1, keepdim=True)
+        p, d = torch.exp(z - n), (z - n).abs()
+        # as derived above: a logit, lse (every logit's, and adding up), and p with lse rounded to f32
+        bz = (2 * K + 32) * U * S
+        e_lse = bz.amax(1) + U * ((p * (4 * d + 8)).sum(1) + 400 + 8 * n[:, 0].abs())
+        want = torch.where(live, n[:, 0] - z.gather(1, word)[:, 0], 0.0)
+        assert ((loss[i] - want).abs() <= e_lse + bz.gather(1, word)[:, 0] + 8 * U * (n[:, 0].abs() + z.abs().amax(1) + 1)).all()
+        share = torch.zeros_like(z).scatter_(1, word, 1.0)
+        dz = torch.where(live[:, None], p - share, 0.0)
+        edz = p * (bz + e_lse[:, None] + U * (4 * d + 16)) + 8 * U * share
+        want, size = dz @ ws_, dz.abs() @ ws_.abs()
+        bound = (edz + 2.0 ** -8 * (dz.abs() + edz)) @ ws_.abs() + (2 * V + 32) * U * size               # dz is rounded once
+        worst = ((dx[i].double() - want).abs() - (bound + 2.0 ** -8 * (want.abs() + bound))).amax().item()
+        assert worst <= 0, worst
+        assert torch.isfinite(dw[i]).all()
+
+
+@gpu
+def test_as_many_rows_as_there_may_be():
+    """2^28 of a vocabulary of none: half of them do not count, the others name words that there are not."""
+    M, G = 2 ** 21, 2 ** 7
+    x, w = torch.empty(G, M, 0, device=DEV), torch.empty(G, 0, 0, device=DEV)
+    target = (torch.arange(M, device=DEV) % 2 - 1).expand(G, M)
+    loss, lse = torch.full((G, M), 7.0, device=DEV), torch.full((G, M), 7.0, device=DEV)
+    op = B.CrossEntropy(M, 0, 0, G)
+    op.forward(op.forward_io(x, w, target, loss, lse), torch.empty(max(op.workspace_bytes(), 256), dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    for t in (loss, lse):
+        assert (t[:, ::2] == 0).all() and torch.isnan(t[:, 1::2]).all()
+
+
+@gpu
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_as_many_words_as_there_may_be(accumulate):
+    """Sums over no rows, of 2^29 words: more workgroups of 64 than a grid's first dimension holds."""
+    V = 2 ** 29 + 70
+    op = B.CrossEntropy(0, V, 0, 1, torch.bfloat16, accumulate=accumulate)
+    db = torch.full((1, V), 3.0, dtype=torch.bfloat16, device=DEV)
+    none = lambda *s, t=torch.float32: torch.empty(s, dtype=t, device=DEV)
+    op.backward(op.backward_io(none(1, 0, 0, t=torch.bfloat16), none(1, V, 0, t=torch.bfloat16), none(1, 0, t=torch.int64), none(1, 0), none(1, 0), dbias=db),
+                torch.empty(max(op.workspace_bytes(True), 256), dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert (db == (3.0 if accumulate else 0.0)).all()
