@@ -998,3 +998,28 @@ def test_as_many_words_as_there_may_be(accumulate):
                 torch.empty(max(op.workspace_bytes(True), 256), dtype=torch.uint8, device=DEV))
     torch.cuda.synchronize()
     assert (db == (3.0 if accumulate else 0.0)).all()
+
+
+# -- rows that do not count, whatever the logits are -----------------------------------------------------
+# few rows, up to 64 features, small sizes, many rows; f32 of more rows than small sizes have
+ROUTES = [*ROWS, (2, 6, 300, 200), (1, 2600, 300, 72), (1, 900, 3000, 64)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", ROUTES)
+@pytest.mark.parametrize("top", [0, 4])
+@pytest.mark.parametrize("bad", [float("nan"), INF, "most"])
+def test_rows_that_do_not_count_have_no_gradient_whatever_the_logits_are(size, dtype, top, bad):
+    """A bias that is no number, infinite or the type's largest value; the last worker has no row that counts."""
+    c = Case(*size, dtype, top=top, seed=8, ignored=0.5)
+    c.words[-1] = -1
+    c.bias = c.bias.clone()
+    c.bias[:, [1, size[2] - 1]] = torch.finfo(dtype).max if bad == "most" else bad
+    loss, lse = run_forward(c)
+    dead = (c.words < 0).all(2) if top else c.words < 0
+    assert dead.any()
+    assert (loss[dead] == 0).all() and (lse[dead] == 0).all()
+    got = gradients(c, lse)
+    assert (got["dx"][dead] == 0).all()
+    assert (got["dw"][-1] == 0).all() and (got["dbias"][-1] == 0).all()
