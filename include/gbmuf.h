@@ -468,7 +468,7 @@ typedef struct gbmuf_loss_desc {
     int32_t top;             /* distillation: words of the teacher in a row, 1 .. GBMUF_MAX_TOP; else 0           */
     int32_t weight_grad_f32; /* backward: 1 = dw and dbias are f32 whatever dtype is                              */
     int32_t accumulate;      /* backward: 1 = dw and dbias are added to what is there                             */
-    float temperature;       /* distillation: tau, 2^-40 .. 2^40; else unused                                     */
+    float temperature;       /* distillation: tau, 2^-10 .. 2^10; else unused                                     */
     int32_t reserved0;
     int64_t rows;            /* tokens per worker                                                                 */
     int64_t vocab;
@@ -510,7 +510,8 @@ typedef struct gbmuf_loss_grad_io {
  * Rows: one whose word is negative, or that has no words there, does not count: its loss, lse and gradients are 0, whatever its x, dloss and lse
  * hold, NaN among it.  One that names a word of `vocab` or above gets NaN for its loss and lse, and its gradients are NaN.
  * Logits of -infinity (a word that a bias forbids) have the probability 0; a row of nothing else, and NaN anywhere, follow IEEE arithmetic.
- * Sums of products and everything that comes of them are held in f32; operands of type f32 are taken apart as in gbmuf_linear.
+ * Sums of products and everything that comes of them are held in f32; operands of type f32 are taken apart as in gbmuf_linear.  So is lse: what the backward
+ * forms of it, exp(z / tau - lse), is off by |lse| 2^-24 of itself, 2^-8 where z / tau reaches 2^16; and the distillation's loss is off by tau^2 2^-22 |lse|.
  * Backward: dz[v] = dloss tau (exp(z[v] / tau - lse) - sum of the q_j with t_j = v)   (cross entropy: q = 1 for the word, tau = 1)
  *     dx = dz w,   dw = dz' x,   dbias[v] = sum_i dz[i,v]
  *   for each worker by itself.  With bf16 and f16 large sizes round dz to dtype once before the products of dx and dw, times a factor of the worker
@@ -518,7 +519,7 @@ typedef struct gbmuf_loss_grad_io {
  *   not rounded.  No gradient is formed of the teacher's logits.
  * Equal calls give equal bits.
  * Workspace and errors as for gbmuf_linear; EINVAL also for a top or temperature that the loss does not take (top 0 asks gbmuf_loss_workspace for
- * cross entropy's bytes), EUNSUPPORTED for top above GBMUF_MAX_TOP, temperatures beyond 2^-40 .. 2^40 and batch * rows above 2^28 (distillation: 2^25).
+ * cross entropy's bytes), EUNSUPPORTED for top above GBMUF_MAX_TOP, temperatures beyond 2^-10 .. 2^10 and batch * rows above 2^28 (distillation: 2^25).
  */
 int gbmuf_loss_workspace(const gbmuf_loss_desc_t *desc, int32_t backward, int64_t *bytes);
 int gbmuf_cross_entropy(const gbmuf_loss_desc_t *desc, const gbmuf_loss_io_t *io, void *workspace, int64_t workspace_bytes, void *stream);

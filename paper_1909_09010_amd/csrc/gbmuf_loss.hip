@@ -25,8 +25,9 @@ int check_desc(const gbmuf_loss_desc_t *d, bool distill, Loss &l)
     const int64_t M = d->rows, N = d->vocab, K = d->in_features, G = d->batch;
     if (too_many_tiles(M, N, G) || too_many_tiles(M, K, G) || too_many_tiles(N, K, G) || d->top > kMostTop) return GBMUF_EUNSUPPORTED;
     if (static_cast<double>(M) * static_cast<double>(G) > (distill ? 0x1p25 : 0x1p28)) return GBMUF_EUNSUPPORTED;          // what launches over rows may have
-    // 1 / tau, tau^2 and what they are multiplied with stay in f32's range
-    if (distill && !(d->temperature >= 0x1p-40f && d->temperature <= 0x1p40f)) return GBMUF_EUNSUPPORTED;
+    // lse is handed over in one f32, so that a probability is off by |lse| 2^-24: at 2^-10 logits of 64 leave it 8 bits.  The gradient is tau times a difference of two
+    // probabilities, the loss tau^2 times one of logarithms, which cancel where student and teacher agree: at 2^10 they keep 14 and 4 bits.
+    if (distill && !(d->temperature >= 0x1p-10f && d->temperature <= 0x1p10f)) return GBMUF_EUNSUPPORTED;
     l = Loss{};
     l.linear.struct_size = sizeof(l.linear);
     l.linear.dtype = d->dtype; l.linear.batch = d->batch;

@@ -1023,3 +1023,89 @@ def test_rows_that_do_not_count_have_no_gradient_whatever_the_logits_are(size, d
     got = gradients(c, lse)
     assert (got["dx"][dead] == 0).all()
     assert (got["dw"][-1] == 0).all() and (got["dbias"][-1] == 0).all()
+
+
+# -- temperatures, and logits far from 0 -----------------------------------------------------------------
+def test_temperatures():
+    """What one f32 of lse can carry: beyond, exp(z / tau - lse) would keep fewer than 8 bits for logits of 64."""
+    for t in (2.0 ** -10, 0.01, 1.0, 2.0 ** 10):
+        assert workspace_status(desc(top=2, temperature=t))[0] == B.GBMUF_OK, t
+    for t in (2.0 ** -11, 2.0 ** -20, 2.0 ** -40, 2.0 ** 11, 2.0 ** 20, 2.0 ** 40):
+        assert workspace_status(desc(top=2, temperature=t)) == (B.GBMUF_EUNSUPPORTED, 0), t
+
+
+class Exact(Case):
+    """Logits that every type holds exactly: products of eighths, few enough for 24 bits; `far` is added to those of every second row."""
+
+    def __init__(self, G, M, V, K, dtype, far=0.0, **k):
+        super().__init__(G, M, V, K, dtype, **k)
+        eighths = lambda t, most: ((t.float() * 8).round().clamp(-8 * most, 8 * most) / 8).to(dtype)
+        self.x, self.w, self.bias = eighths(self.x, 2), eighths(self.w, 2), eighths(self.bias, 2)
+        self.w[:, :, 0] = 1.0
+        self.x[:, ::2, 0] = far
+        self.x[:, 1::2, 0] = 0.0
+
+    def compare(self):
+        """Loss and gradients, those from the forward's own lse, against 64 bits."""
+        G, M, V, K = self.size
+        tau = self.tau
+        z = (mm(self.x, self.w) + self.bias.double()[:, None]) / tau
+        words = (self.words if self.top else self.words[:, :, None]).clamp(min=0)
+        there = self.words >= 0 if self.top else (self.words >= 0)[:, :, None]
+        if self.top:
+            s = self.teacher.double().masked_fill(~there, -INF) / tau
+            q = torch.softmax(s, 2).masked_fill(~there, 0.0)
+            off = (s - s.amax(2, keepdim=True)).abs().masked_fill(~there, 0.0)
+            eq = q * (8 * off + self.top + 16) * U
+        else:
+            q, eq = there.double(), torch.zeros_like(there, dtype=torch.float64)
+        live = there.any(2)
+        n = torch.logsumexp(z, 2)
+        p, d = torch.exp(z - n[:, :, None]), (z - n[:, :, None]).abs()
+        # as at the head of this file, of logits that are exact
+        e_lse = U * ((p * (4 * d + 8)).sum(2) + 400 + 8 * n.abs())
+        loss, lse = run_forward(self)
+        out = gradients(self, lse)
+        assert (loss[~live] == 0).all() and (lse[~live] == 0).all()
+        assert ((lse.double() - n).abs() <= e_lse)[live].all()
+        logq = torch.where(q > 0, torch.log(q.clamp(min=1e-300)), torch.zeros_like(q))
+        at = z.gather(2, words)
+        term = torch.where(q > 0, logq - at + n[:, :, None], torch.zeros_like(q))
+        want = tau ** 2 * (q * term).sum(2)
+        size = logq.abs() + at.abs() + n.abs()[:, :, None] + 1
+        e_loss = tau ** 2 * (q * (e_lse[:, :, None] + 8 * U * size) + 2 * eq * (term.abs() + 1) + U * (self.top + 8) * q * term.abs()).sum(2)
+        assert ((loss.double() - want).abs() <= e_loss)[live].all()
+        weight = torch.where(live, tau * self.dloss.double(), 0.0)[:, :, None]
+        share, more = (torch.zeros_like(z).scatter_add_(2, words, v) for v in (q, eq))
+        dz = weight * (p - share)
+        edz = weight * (p * torch.expm1(e_lse[:, :, None] + U * (4 * d + 16 + 4 * n.abs()[:, :, None])) + more + (self.top + 4) * U * share)
+        h = HALF[self.dtype]
+        if self.dtype != torch.float32:                     # rounded once, where sizes are large
+            edz = edz + h * (dz.abs() + edz) + 2.0 ** -39 * (tau * self.dloss.double().abs()).amax(1)[:, None, None]
+        x = torch.where(live[:, :, None], self.x.double(), 0.0)
+        for got, a, e, b in ((out["dx"], dz, edz, self.w.double().transpose(1, 2)), (out["dw"], dz.transpose(1, 2), edz.transpose(1, 2), x.transpose(1, 2))):
+            want = mm(a, b)
+            bound = mm(e, b.abs()) + sum_bound(a, b, self.dtype)[0]
+            bound = bound + h * (want.abs() + bound) + 2.0 ** -25
+            worst = ((got.double() - want).abs() - bound).amax().item()
+            assert worst <= 0, worst
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", ROUTES)
+@pytest.mark.parametrize("tau", [2.0 ** -10, 2.0 ** -3, 2.0 ** 10])
+def test_temperatures_at_their_ends(size, dtype, tau):
+    Exact(*size, dtype, top=5, tau=tau, seed=17).compare()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", ROUTES)
+def test_logits_far_from_0(size, dtype):
+    """100 / tau is more than what exponents are formed of in one multiply-add, for every second row."""
+    Exact(*size, dtype, top=5, tau=2.0 ** -10, far=100.0, seed=18).compare()
+    Exact(*size, dtype, top=5, tau=2.0 ** -10, far=-100.0, seed=19).compare()
+    if dtype != torch.float16:
+        Exact(*size, dtype, far=2.0 ** 17, seed=20).compare()
+        Exact(*size, dtype, far=-(2.0 ** 17), seed=21).compare()
