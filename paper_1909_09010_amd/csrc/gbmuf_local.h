@@ -154,17 +154,18 @@ struct LossArgs {
     float2 *parts;
     float *at;
     int32_t part_tiles, first_tile;
-    // backward: dz[g][row][column], rows dz_ld apart, whole pieces of 8 up to there
+    // backward: dz[g][row][column], f32 or of 16-bit types (launch_vocab), rows dz_ld apart, whole pieces of 8 up to there
     const float *lse, *dloss;
     int64_t lse_ld, lse_batch, dloss_ld, dloss_batch;
     const float *most;       // 16-bit types, [g][kMostParts]: largest weights of most_parts parts of a worker's rows, or nullptr
     float *factor;           // out, [g]: 1 / what dz is multiplied with for that
     void *dz;
     int64_t dz_ld, dz_batch;
-    int32_t dz_type, streamed;      // streamed: dz is more than the caches hold
-    float *col_sums;         // [g][parts of 64 or 128 rows][column], or nullptr
-    uint32_t *col_max;       // f32, [g][column]: bits of the largest magnitude, zero before; or nullptr
-    int32_t *live;           // out: [g][row], or nullptr
+    int32_t streamed;        // dz is more than the caches hold
+    int32_t reserved;
+    float *col_sums;         // launch_vocab, [g][parts of 64 or 128 rows][column], or nullptr
+    uint32_t *col_max;       // the same, f32, [g][column]: bits of the largest magnitude, zero before; or nullptr
+    int32_t *live;           // launch_loss_direct, out: [g][row], or nullptr
 };
 
 // A teacher's words of every row, as it gives them, made lists of Words.

@@ -98,7 +98,7 @@ __device__ __forceinline__ void in_order()
 // halves of the wave.  Words whose logits or shares are wanted are few (64 of 8197 words: 1 in 2 lanes and tile): their rows go through LDS, where a lane
 // finds any column, only where the wave has one.
 // Forward: (largest logit, sum of exp of the others less that) of every row of the tile, and the logits of the row's words.
-// Backward: dz = weight (exp(z / tau - lse) - share), through LDS so that stores follow rows, and its column sums before it is rounded.
+// Backward: dz = weight (exp(z / tau - lse) - share) in f32, through LDS so that stores follow rows; its column sums go along with dw.
 template <int TM, int TN, int WM, int WN, bool BACKWARD>
 __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 32], void *lds, const Tiles &t, const LossArgs &a, const TileAt &tile)
 {
@@ -178,7 +178,6 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
     };
 
     const float scale = a.inv_tau * kLog2E;
-    Eight total{};
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int m = row_of(i), mc = min(m, M - 1);
@@ -250,22 +249,9 @@ __device__ __forceinline__ void leave_loss(v16f (&acc)[TM / WM / 32][TN / WN / 3
                 const float *from = out + (first + k * kTogether) * kPitch + column;
                 const Eight z{{*reinterpret_cast<const v4f *>(from), *reinterpret_cast<const v4f *>(from + 4)}};
                 const int row = m_wave + i * 32 + first + k * kTogether;
-                total.v[0] += z.v[0];
-                total.v[1] += z.v[1];
-                if (row < M && n < a.dz_ld) store_eight(a.dz, g * a.dz_batch + row * a.dz_ld + n, a.dz_type, z);
+                if (row < M && n < a.dz_ld) write8<kF32>(a.dz, g * a.dz_batch + row * a.dz_ld + n, z);
             }
             in_order();
-            if (i + 1 == FM && a.col_sums) {
-#pragma unroll
-                for (int d = kLanes; d < 64; d *= 2)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) total.v[c >> 2][c & 3] += __shfl_xor(total.v[c >> 2][c & 3], d);
-                float *to = a.col_sums + ((g * t.tiles_m + tile.tm) * WM + wave % WM) * N + n;
-                if (first == 0)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        if (n + c < N) to[c] = total.v[c >> 2][c & 3];
-            }
         }
     }
 }

@@ -415,7 +415,7 @@ int backward_direct(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t 
     int rc = order_words(l, words, at, true, stream);
     if (rc != GBMUF_OK) return rc;
     LossArgs a = grad_args(l, at, io, words, Piece{0, G, 0, N});
-    a.dz = dz; a.dz_ld = ld; a.dz_batch = M * ld; a.dz_type = kF32;
+    a.dz = dz; a.dz_ld = ld; a.dz_batch = M * ld;
     a.live = live;
     if ((rc = launch_loss_direct(direct_args(source_of(at.x), source_of(at.w), K, cz, Epilogue{}), a, type, true, stream)) != GBMUF_OK) return rc;
     Source z{};
@@ -608,7 +608,7 @@ int backward_laid(const Loss &l, const Inputs *in, const gbmuf_loss_grad_io_t *i
         LossArgs a = grad_args(l, at, io, words, p);
         a.lists = lists_from(lists, words, p.g);
         a.walk = c.t.steps;
-        a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld; a.dz_type = type;
+        a.dz = dz; a.dz_ld = pld; a.dz_batch = M * pld;
         a.streamed = p.workers * M * pld * static_cast<int64_t>(type_bytes(type)) > kCached ? 1 : 0;
         if (!split) {
             a.most = most + p.g * kMostParts; a.most_parts = keep.most_parts;

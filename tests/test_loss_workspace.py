@@ -136,7 +136,7 @@ int launch_vocab(const ProductArgs &a, const LossArgs &l, int32_t type, int tile
         if (l.first_tile + t.tiles_n > l.part_tiles) reached = INT64_MAX, worst = "a part that no row has";
         uses(l.at, t.batch * static_cast<int64_t>(l.words.rows) * l.words.top * 4, "words' logits");
     } else {
-        matrix(l.dz, t.batch, l.dz_batch, t.M, l.dz_ld, l.dz_ld, type_bytes(l.dz_type), "dz");
+        matrix(l.dz, t.batch, l.dz_batch, t.M, l.dz_ld, l.dz_ld, type_bytes(type), "dz");
         uses(l.col_sums, static_cast<int64_t>(t.batch) * t.tiles_m * 2 * t.N * 4, "sums of columns");
         uses(l.col_max, static_cast<int64_t>(t.batch) * t.N * 4, "columns' largest");
         uses(l.factor, t.batch * 4, "factors");
