@@ -1109,3 +1109,43 @@ def test_logits_far_from_0(size, dtype):
     if dtype != torch.float16:
         Exact(*size, dtype, far=2.0 ** 17, seed=20).compare()
         Exact(*size, dtype, far=-(2.0 ** 17), seed=21).compare()
+
+
+# -- wide rows -------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(1, 300, 2100, 2050), (2, 140, 1000, 4100), (1, 1100, 700, 1536)])
+@pytest.mark.parametrize("top", [0, 20])
+def test_wide_rows(size, dtype, top):
+    """More than 16 steps a tile."""
+    run_case(Case(*size, dtype, top=top, tau=1.5 if top else 1.0, seed=22), accumulate=size[0] == 2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(1, 300, 70000, 2050), (3, 80, 30000, 2050)])
+def test_pieces_of_wide_words(size, dtype):
+    """w lies on no 16 bytes and is more than is laid out at a time: parts of the vocabulary, and some of the workers."""
+    G, M, V, K = size
+    crooked = {"w": in_rows(5, V * K + 11)}
+    run_case(Case(*size, dtype, top=0 if G == 1 else 6, tau=1.0 if G == 1 else 2.0, seed=23, place=crooked))
+    c = Case(*size, dtype, seed=24, place={**crooked, "x": in_rows(3, M * K + 5)})
+    loss, lse = run_forward(c)
+    c.x, c.w = columns_of(K + 6, 0)(c.x), columns_of(K + 6, 0)(c.w)
+    assert all(t.data_ptr() % 16 == 0 and t.stride(1) % 8 == 0 and t.stride(0) % 8 == 0 for t in (c.x, c.w))
+    a, b = run_forward(c)                                   # 16-bit types take them as they lie: other tiles, the same sums
+    c.solve()
+    assert ((a - loss).abs().double() <= 2 * c.e_loss)[c.live].all() and ((b - lse).abs().double() <= 2 * c.e_lse)[c.live].all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M", [3, 200])
+def test_words_of_no_vocabulary(M, dtype):
+    """A row that names one gets NaN; its dx is a sum of nothing."""
+    c = Case(2, M, 0, 8, dtype, ignored=2.0)
+    c.words[:, 1] = 0
+    loss, lse = run_forward(c)
+    assert torch.isnan(loss[:, 1]).all() and torch.isnan(lse[:, 1]).all()
+    assert (loss[:, 0] == 0).all() and (lse[:, 0] == 0).all()
+    assert (gradients(c, lse)["dx"] == 0).all()
